@@ -273,6 +273,36 @@ fg_status fg_contract_plan(int32_t nA, const int32_t *modesA, const int64_t *str
                            int32_t n_modes, const int32_t *mode_labels, const int64_t *mode_extents,
                            char *buf, int32_t buf_len);
 
+/* ---- operators on the rows of a matrix: the ends of a language model --------------------------------------
+ * Hidden states, embedding tables and vocabulary matrices are row-major fg_matrix descriptors (layout FG_ROW, `im` NULL) with a leading
+ * dimension of any size from the row's length on and element-aligned pointers, of FG_F16, FG_BF16 or (where it is said) FG_F32
+ * elements.  All arithmetic is FP32 or wider; every result is rounded to nearest even once, when it is stored.  Results do not
+ * depend on scheduling: the same call gives the same bits.  Calls that need scratch memory take a workspace from the caller, of at
+ * least the bytes that the query beside it gives; it holds nothing from one call to the next, needs no clearing and may be
+ * reused by the next call on the same stream.  These calls allocate nothing and only enqueue kernels: they may be recorded into a HIP graph.
+ * Sizes of zero are accepted.
+ */
+
+/*
+ * Layer norm of each row: Y = (X - mean) * rstd * gamma + beta, with mean = sum X / cols, rstd = 1 / sqrt(sum (X - mean)^2 / cols + eps).
+ *   X, Y        : rows x cols, the same element type (FG_F32 too); Y may alias X exactly.
+ *   gamma, beta : `cols` values of type param_dtype (FG_F32 or the type of X); NULL: ones, zeros.
+ *   mean, rstd  : `rows` FP32 values, written for fg_layernorm_grad; NULL: not wanted.
+ */
+fg_status fg_layernorm(int64_t rows, int64_t cols, const fg_matrix *X, const void *gamma, const void *beta, int32_t param_dtype, float eps,
+                       const fg_matrix *Y, float *mean, float *rstd, void *hip_stream);
+
+/*
+ * Its gradient: with xh = (X - mean) * rstd and g = dY * gamma, dX = rstd * (g - sum g / cols - xh * sum(g * xh) / cols); dgamma = sum over rows of
+ * dY * xh, dbeta = sum over rows of dY (zero without rows).  mean and rstd are those of the forward call.  dgamma and dbeta (type
+ * param_dtype) may be NULL; with both NULL no workspace is needed.  dX may alias dY or X exactly.
+ * dY may have ld 0: the same row for all.
+ */
+fg_status fg_layernorm_grad(int64_t rows, int64_t cols, const fg_matrix *dY, const fg_matrix *X, const void *gamma, int32_t param_dtype,
+                            const float *mean, const float *rstd, const fg_matrix *dX, void *dgamma, void *dbeta,
+                            void *workspace, int64_t workspace_bytes, void *hip_stream);
+int64_t fg_layernorm_grad_workspace(int64_t rows, int64_t cols, int32_t dtype);
+
 /* Message for the most recent failing call on this thread ("" if none).  The pointer refers to
  * thread-local static storage: valid until the next library call on the same thread. */
 const char *fg_last_error(void);

@@ -28,7 +28,8 @@ FG_COL, FG_ROW, FG_DIAG, FG_ZERO = 0, 1, 2, 3
 FG_ACT_NONE, FG_ACT_RELU = 0, 1
 
 EXPORTS = ("fg_init", "fg_gemm", "fg_gemm_ex", "fg_gemm_noalloc", "fg_gemm_dual", "fg_contract", "fg_contract_plan", "fg_last_error", "fg_version",
-           "fg_reload_tuning", "fg_gemm_plan", "fg_probe_mfma", "fg_probe_mfma_k32", "fg_probe_kloop_mix")
+           "fg_reload_tuning", "fg_gemm_plan", "fg_probe_mfma", "fg_probe_mfma_k32", "fg_probe_kloop_mix",
+           "fg_layernorm", "fg_layernorm_grad", "fg_layernorm_grad_workspace")
 FG_PLAN_REAL, FG_PLAN_COMPLEX, FG_PLAN_DUAL, FG_PLAN_REAL_BF16, FG_PLAN_COMPLEX_INTERLEAVED, FG_PLAN_REAL_F16_CD = 0, 1, 2, 3, 4, 5
 FG_PLAN_REAL_AB_ADD = 6
 
@@ -98,6 +99,13 @@ def load_library() -> C.CDLL:
         lib.fg_probe_mfma_k32.argtypes = [vp, i64, i32, C.POINTER(C.c_int64), vp]
         lib.fg_probe_kloop_mix.restype = C.c_int
         lib.fg_probe_kloop_mix.argtypes = [vp, i64, i32, C.POINTER(C.c_int64), vp]
+        mp = C.POINTER(fg_matrix)
+        lib.fg_layernorm.restype = C.c_int
+        lib.fg_layernorm.argtypes = [i64, i64, mp, vp, vp, i32, f32, mp, vp, vp, vp]
+        lib.fg_layernorm_grad.restype = C.c_int
+        lib.fg_layernorm_grad.argtypes = [i64, i64, mp, mp, vp, i32, vp, vp, mp, vp, vp, vp, i64, vp]
+        lib.fg_layernorm_grad_workspace.restype = i64
+        lib.fg_layernorm_grad_workspace.argtypes = [i64, i64, i32]
         _load_fastcall(lib)
         _lib = lib
     return _lib
@@ -332,3 +340,84 @@ def fg_probe_mfma(fp16_operands: torch.Tensor, iters: int, stream=None, k32: boo
     st = fn(fp16_operands.data_ptr(), fp16_operands.numel() * fp16_operands.element_size(), iters, C.byref(flops), _stream_handle(stream))
     _check(st, True)
     return int(flops.value)
+
+
+# ---- operators on the rows of a matrix ------------------------------------------------------------
+# These take device tensors and read sizes, strides and types off them; see include/flexgemm.h for what they compute.  The library sees
+# pointers only, so what it cannot know is checked here: device, extents, and that a row is contiguous.
+
+def _rows(t: torch.Tensor, name: str, shape=None, dev: Optional[int] = None) -> fg_matrix:
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
+        raise ValueError("%s: expected a matrix%s, got shape %s" % (name, "" if shape is None else " of shape %s" % (tuple(shape),), tuple(t.shape)))
+    if not t.is_cuda or (dev is not None and t.get_device() != dev):
+        raise ValueError("%s: a tensor on the current GPU is needed, got one on %s" % (name, t.device))
+    rows, cols = t.shape
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError("%s: rows must be contiguous, the stride along a row is %d" % (name, inner))
+    return fg_matrix(t.data_ptr(), None, _DTYPES.get(t.dtype, -1), FG_ROW, ld if rows > 1 else max(ld, cols))
+
+
+def _vector(t: Optional[torch.Tensor], n: int, name: str, dtype, dev: int) -> Optional[int]:
+    """The address of n contiguous values of type dtype."""
+    if t is None:
+        return None
+    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError("%s: expected %d contiguous values, got shape %s, strides %s" % (name, n, tuple(t.shape), t.stride()))
+    if t.dtype != dtype:
+        raise ValueError("%s: expected %s, got %s" % (name, dtype, t.dtype))
+    if t.get_device() != dev:
+        raise ValueError("%s: a tensor on the current GPU is needed, got one on %s" % (name, t.device))
+    return t.data_ptr()
+
+
+def _workspace(given: Optional[torch.Tensor], need: int, stream, dev: int):
+    """(address, bytes, what keeps it alive) of the caller's workspace, or of one from torch's allocator for the stream of the call."""
+    if given is not None:
+        if not given.is_cuda or given.get_device() != dev or not given.is_contiguous():
+            raise ValueError("workspace: a contiguous tensor on the current GPU is needed")
+        return given.data_ptr(), given.numel() * given.element_size(), given
+    if need <= 0:
+        return None, 0, None
+    t = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", dev))
+    if stream is not None:          # torch takes it for memory of the current stream
+        t.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream_handle(stream)))
+    return t.data_ptr(), need, t
+
+
+def fg_layernorm(X: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float, Y: torch.Tensor,
+                 mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, stream=None, raise_on_error: bool = True) -> int:
+    """Y = layer norm of the rows of X; mean and rstd of the rows are kept for fg_layernorm_grad."""
+    lib = _lib or load_library()
+    dev = _current_device()
+    x = _rows(X, "X", None, dev)
+    y = _rows(Y, "Y", X.shape, dev)
+    rows, cols = X.shape
+    ptype = gamma.dtype if gamma is not None else beta.dtype if beta is not None else X.dtype
+    st = lib.fg_layernorm(rows, cols, C.byref(x), _vector(gamma, cols, "gamma", ptype, dev), _vector(beta, cols, "beta", ptype, dev),
+                          _DTYPES.get(ptype, -1), eps, C.byref(y), _vector(mean, rows, "mean", torch.float32, dev),
+                          _vector(rstd, rows, "rstd", torch.float32, dev), _stream_handle(stream))
+    return _check(st, raise_on_error)
+
+
+def fg_layernorm_grad_workspace(rows: int, cols: int, dtype: torch.dtype) -> int:
+    return int(load_library().fg_layernorm_grad_workspace(rows, cols, _DTYPES.get(dtype, -1)))
+
+
+def fg_layernorm_grad(dY: torch.Tensor, X: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor, dX: torch.Tensor,
+                      dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                      stream=None, raise_on_error: bool = True) -> int:
+    """Gradients of fg_layernorm with respect to X, gamma and beta."""
+    lib = _lib or load_library()
+    dev = _current_device()
+    x = _rows(X, "X", None, dev)
+    dy = _rows(dY, "dY", X.shape, dev)
+    dx = _rows(dX, "dX", X.shape, dev)
+    rows, cols = X.shape
+    ptype = next((t.dtype for t in (gamma, dgamma, dbeta) if t is not None), X.dtype)
+    need = lib.fg_layernorm_grad_workspace(rows, cols, x.dtype) if dgamma is not None or dbeta is not None else 0
+    ws, ws_bytes, _keep = _workspace(workspace, need, stream, dev)
+    st = lib.fg_layernorm_grad(rows, cols, C.byref(dy), C.byref(x), _vector(gamma, cols, "gamma", ptype, dev), _DTYPES.get(ptype, -1),
+                               _vector(mean, rows, "mean", torch.float32, dev), _vector(rstd, rows, "rstd", torch.float32, dev), C.byref(dx),
+                               _vector(dgamma, cols, "dgamma", ptype, dev), _vector(dbeta, cols, "dbeta", ptype, dev), ws, ws_bytes, _stream_handle(stream))
+    return _check(st, raise_on_error)

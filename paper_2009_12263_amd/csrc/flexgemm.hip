@@ -16,12 +16,13 @@
 #include "cache_policy.hpp"
 #include "general_kernel.hpp"
 #include "kernel_table.hpp"
+#include "status.hpp"
 
 namespace {
-
 thread_local char g_err[512] = "";
+}
 
-fg_status fail(fg_status st, const char *fmt, ...) {
+fg_status fg::fail(fg_status st, const char *fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
     vsnprintf(g_err, sizeof g_err, fmt, ap);
@@ -29,8 +30,11 @@ fg_status fail(fg_status st, const char *fmt, ...) {
     return st;
 }
 
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool aligned_to(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+namespace {
+
+using fg::aligned_to;
+using fg::fail;
+bool aligned16(const void *p) { return aligned_to(p, 16); }
 
 // Requirements of the tiled kernels that the general kernel does not have (16-byte aligned bases,
 // leading dimensions in whole 16-byte chunks, K a multiple of 8).  A call that misses one of them

@@ -1,0 +1,391 @@
+// Layer norm of the rows of a matrix, and its gradient.
+//
+//   mean = sum x / n,  var = sum (x - mean)^2 / n,  rstd = 1 / sqrt(var + eps),  xh = (x - mean) rstd,  y = xh gamma + beta
+//   g = dy gamma,  dx = rstd (g - sum g / n - xh sum (g xh) / n),  dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy
+//
+// Bound by memory: x is read and y written once; x and dy are read and dx written once.  A row is held in the registers of W
+// waves (up to kPieces pieces of 16 bytes per lane), so nothing is read twice and the variance is summed from the
+// differences to the mean, without the cancellation of a mean of squares.  A lane keeps the same columns in every row that
+// its workgroup takes: gamma and beta stay in registers, and so do the sums of dgamma and dbeta over those rows; each wave group
+// writes its sums once, and a second pass adds them in a fixed order, so that results do not depend on scheduling.  All
+// arithmetic is FP32; each result is rounded once, when it is stored.
+#include "row_ops.hpp"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace fg {
+namespace {
+
+constexpr int kPieces = 4;                  // of 16 bytes per lane and row
+constexpr int kMaxWaves = 16;
+
+struct LayerNormArgs {
+    const void *x, *dy;
+    void *out;                              // y, or dx
+    const void *gamma, *beta;
+    float *mean, *rstd;
+    float *partial;                         // per wave group: dgamma's sums over its rows, then dbeta's (cols each)
+    int64_t ldx, lddy, ldo, rows;
+    int32_t cols;
+    float eps, width;                       // width: cols, to divide by
+};
+
+// Workgroups of one wave a row hold four rows.
+template <int W> constexpr int kRowsPerGroup = W == 1 ? 4 : 1;
+
+template <class T, class P, int W>
+struct RowLane {
+    static constexpr int N = Piece<T>::N, NT = 64 * W, R = kRowsPerGroup<W>;
+    int lane, cols, pieces;
+    int64_t group;                          // of W waves, among all of the launch
+    __device__ RowLane(int n) : lane(W == 1 ? threadIdx.x & 63 : threadIdx.x), cols(n), pieces((n + N - 1) / N),
+                                group((int64_t)blockIdx.x * R + (W == 1 ? threadIdx.x >> 6 : 0)) {}
+    // f(c, piece) for the pieces of this lane
+    template <class F> __device__ __forceinline__ void each(F &&f) const {
+#pragma unroll
+        for (int c = 0; c < kPieces; ++c)
+            if (lane + c * NT < pieces) f(c, lane + c * NT);
+    }
+    __device__ __forceinline__ void params(const void *p, float (&out)[kPieces][N], float otherwise) const {
+        each([&](int c, int piece) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int col = piece * N + i;
+                out[c][i] = p && col < cols ? (float)((const P *)p)[col] : otherwise;
+            }
+        });
+    }
+};
+
+template <class T, class P, int W>
+__global__ __launch_bounds__(64 * W * kRowsPerGroup<W>) void layernorm(const LayerNormArgs a) {
+    using Lane = RowLane<T, P, W>;
+    constexpr int N = Lane::N;
+    __shared__ float slots[2][W];
+    const Lane l(a.cols);
+    float gamma[kPieces][N], beta[kPieces][N];
+    l.params(a.gamma, gamma, 1.f);
+    l.params(a.beta, beta, 0.f);
+    for (int64_t row = l.group; row < a.rows; row += (int64_t)gridDim.x * Lane::R) {
+        const T *x = (const T *)a.x + row * a.ldx;
+        T *y = (T *)a.out + row * a.ldo;
+        float v[kPieces][N], sum = 0.f, square = 0.f;
+        l.each([&](int c, int p) {
+            load_piece(x, p, a.cols, v[c]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum += v[c][i];
+        });
+        const float mean = group_sum<W>(sum, slots[0]) / a.width;
+        l.each([&](int c, int p) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                v[c][i] -= mean;
+                square += p * N + i < a.cols ? v[c][i] * v[c][i] : 0.f;
+            }
+        });
+        const float rstd = 1.f / __builtin_sqrtf(group_sum<W>(square, slots[1]) / a.width + a.eps);
+        l.each([&](int c, int p) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[c][i] = v[c][i] * rstd * gamma[c][i] + beta[c][i];
+            store_piece(y, p, a.cols, v[c]);
+        });
+        if (l.lane == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+    }
+}
+
+template <class T, class P, int W, bool SUMS>
+__global__ __launch_bounds__(64 * W * kRowsPerGroup<W>) void layernorm_grad(const LayerNormArgs a) {
+    using Lane = RowLane<T, P, W>;
+    constexpr int N = Lane::N;
+    __shared__ float slots[4][W];
+    const Lane l(a.cols);
+    float gamma[kPieces][N], sum_gamma[SUMS ? kPieces : 1][N] = {}, sum_beta[SUMS ? kPieces : 1][N] = {};
+    l.params(a.gamma, gamma, 1.f);
+    int turn = 0;
+    for (int64_t row = l.group; row < a.rows; row += (int64_t)gridDim.x * Lane::R) {
+        const T *x = (const T *)a.x + row * a.ldx, *dy = (const T *)a.dy + row * a.lddy;
+        T *dx = (T *)a.out + row * a.ldo;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float xh[kPieces][N], g[kPieces][N], s1 = 0.f, s2 = 0.f;
+        l.each([&](int c, int p) {
+            load_piece(x, p, a.cols, xh[c], mean);          // past the end: xh = 0, dy = 0
+            load_piece(dy, p, a.cols, g[c]);
+        });
+        l.each([&](int c, int p) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                xh[c][i] = (xh[c][i] - mean) * rstd;
+                if constexpr (SUMS) {
+                    sum_gamma[c][i] += g[c][i] * xh[c][i];
+                    sum_beta[c][i] += g[c][i];
+                }
+                g[c][i] *= gamma[c][i];
+                s1 += g[c][i];
+                s2 += g[c][i] * xh[c][i];
+            }
+        });
+        const float c1 = group_sum<W>(s1, slots[turn]) / a.width, c2 = group_sum<W>(s2, slots[turn + 1]) / a.width;
+        turn ^= 2;
+        l.each([&](int c, int p) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) g[c][i] = rstd * (g[c][i] - c1 - xh[c][i] * c2);
+            store_piece(dx, p, a.cols, g[c]);
+        });
+    }
+    if constexpr (SUMS) {
+        float *to = a.partial + l.group * 2 * a.cols;
+        l.each([&](int c, int p) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (p * N + i < a.cols) {
+                    to[p * N + i] = sum_gamma[c][i];
+                    to[a.cols + p * N + i] = sum_beta[c][i];
+                }
+        });
+    }
+}
+
+// ---- rows that the registers do not hold --------------------------------------------------------
+// One workgroup a row, which is read again for each sum (from the L2).
+template <class T, class P>
+__global__ __launch_bounds__(1024) void layernorm_wide(const LayerNormArgs a) {
+    constexpr int N = Piece<T>::N;
+    __shared__ float slots[2][16];
+    const int n = a.cols, pieces = (n + N - 1) / N;
+    const int64_t row = blockIdx.x;
+    const T *x = (const T *)a.x + row * a.ldx;
+    T *y = (T *)a.out + row * a.ldo;
+    float v[N], sum = 0.f, square = 0.f;
+    for (int p = threadIdx.x; p < pieces; p += 1024) {
+        load_piece(x, p, n, v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum += v[i];
+    }
+    const float mean = group_sum<16>(sum, slots[0]) / a.width;
+    for (int p = threadIdx.x; p < pieces; p += 1024) {
+        load_piece(x, p, n, v, mean);
+#pragma unroll
+        for (int i = 0; i < N; ++i) square += (v[i] - mean) * (v[i] - mean);
+    }
+    const float rstd = 1.f / __builtin_sqrtf(group_sum<16>(square, slots[1]) / a.width + a.eps);
+    const P *gamma = (const P *)a.gamma, *beta = (const P *)a.beta;
+    for (int p = threadIdx.x; p < pieces; p += 1024) {
+        load_piece(x, p, n, v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int col = p * N + i < n ? p * N + i : n - 1;
+            v[i] = (v[i] - mean) * rstd * (gamma ? (float)gamma[col] : 1.f) + (beta ? (float)beta[col] : 0.f);
+        }
+        store_piece(y, p, n, v);
+    }
+    if (threadIdx.x == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+}
+
+template <class T, class P>
+__global__ __launch_bounds__(1024) void layernorm_grad_wide(const LayerNormArgs a) {
+    constexpr int N = Piece<T>::N;
+    __shared__ float slots[2][16];
+    const int n = a.cols, pieces = (n + N - 1) / N;
+    const int64_t row = blockIdx.x;
+    const T *x = (const T *)a.x + row * a.ldx, *dy = (const T *)a.dy + row * a.lddy;
+    T *dx = (T *)a.out + row * a.ldo;
+    const P *gamma = (const P *)a.gamma;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float xh[N], g[N], s1 = 0.f, s2 = 0.f;
+    auto load = [&](int p) {
+        load_piece(x, p, n, xh, mean);
+        load_piece(dy, p, n, g);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            xh[i] = (xh[i] - mean) * rstd;
+            if (gamma) g[i] *= (float)gamma[p * N + i < n ? p * N + i : n - 1];
+        }
+    };
+    for (int p = threadIdx.x; p < pieces; p += 1024) {
+        load(p);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            s1 += g[i];
+            s2 += g[i] * xh[i];
+        }
+    }
+    const float c1 = group_sum<16>(s1, slots[0]) / a.width, c2 = group_sum<16>(s2, slots[1]) / a.width;
+    for (int p = threadIdx.x; p < pieces; p += 1024) {
+        load(p);
+#pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = rstd * (g[i] - c1 - xh[i] * c2);
+        store_piece(dx, p, n, g);
+    }
+}
+
+// The columns' sums over every gridDim.y-th row, for such rows (before dx is written, which may be in place).
+template <class T>
+__global__ __launch_bounds__(256) void layernorm_column_sums(const LayerNormArgs a) {
+    const int col = blockIdx.x * 256 + threadIdx.x;
+    if (col >= a.cols) return;
+    float sum_gamma = 0.f, sum_beta = 0.f;
+    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        const float d = (float)((const T *)a.dy)[row * a.lddy + col];
+        sum_gamma += d * (((float)((const T *)a.x)[row * a.ldx + col] - a.mean[row]) * a.rstd[row]);
+        sum_beta += d;
+    }
+    float *to = a.partial + (int64_t)blockIdx.y * 2 * a.cols;
+    to[col] = sum_gamma;
+    to[a.cols + col] = sum_beta;
+}
+
+// ---- second pass of the columns' sums ---------------------------------------------------------------
+// A workgroup adds the `groups` sums of 32 of the 2 cols columns: 32 lanes along the columns, 32 runs of groups side by
+// side, which are then added in order.
+template <class P>
+__global__ __launch_bounds__(1024) void layernorm_sums(const float *partial, int groups, int cols, P *dgamma, P *dbeta) {
+    __shared__ float part[32][33];
+    const int at = threadIdx.x & 31, run = threadIdx.x >> 5, col = blockIdx.x * 32 + at;
+    const int each = (groups + 31) / 32, first = run * each, last = min(first + each, groups);
+    float sum = 0.f;
+    if (col < 2 * cols) {
+#pragma unroll 4
+        for (int g = first; g < last; ++g) sum += partial[(int64_t)g * 2 * cols + col];
+    }
+    part[run][at] = sum;
+    __syncthreads();
+    if (run == 0 && col < 2 * cols) {
+        for (int r = 1; r < 32; ++r) sum += part[r][at];
+        if (col < cols) { if (dgamma) dgamma[col] = (P)sum; }
+        else if (dbeta) dbeta[col - cols] = (P)sum;
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+constexpr int kNumCU = 256;
+
+// How many waves hold a row: as few as its pieces need; 0: too wide.
+int waves_for(int64_t cols, int elem) {
+    const int64_t pieces = (cols * elem + 15) / 16;
+    for (int w = 1; w <= kMaxWaves; w *= 2)
+        if (pieces <= (int64_t)64 * w * kPieces) return w;
+    return 0;
+}
+// How many wave groups share the rows of a gradient: enough to fill the GPU, and no more sums than that for the second pass.
+int64_t grad_groups(int64_t rows, int64_t cols, int elem) {
+    const int w = waves_for(cols, elem);
+    if (w == 0) return std::min<int64_t>(rows, 64);
+    const int64_t groups = std::min<int64_t>(rows, kNumCU * 8 / w);
+    return w == 1 ? (groups + 3) / 4 * 4 : groups;
+}
+
+template <class F> fg_status with_type(int dtype, F &&f) {
+    switch (dtype) {
+        case FG_F16: return f(f16_t{});
+        case FG_BF16: return f(bf16_t{});
+        default: return f(float{});
+    }
+}
+// f(element, parameter): the parameters are FP32 or of the elements' type
+template <class F> fg_status with_types(int dtype, int param_dtype, F &&f) {
+    return with_type(dtype, [&](auto t) { return param_dtype == FG_F32 ? f(t, float{}) : f(t, t); });
+}
+template <class F> void with_waves(int w, F &&f) {
+    switch (w) {
+        case 1: f(std::integral_constant<int, 1>{}); break;
+        case 2: f(std::integral_constant<int, 2>{}); break;
+        case 4: f(std::integral_constant<int, 4>{}); break;
+        case 8: f(std::integral_constant<int, 8>{}); break;
+        default: f(std::integral_constant<int, 16>{});
+    }
+}
+
+fg_status check_layernorm(int64_t rows, int64_t cols, const fg_matrix *X, const char *name, const fg_matrix *Y, const void *gamma, int32_t param_dtype) {
+    if (rows < 0 || cols < 0) return fail(FG_ERR_SHAPE, "negative size: %lld rows of %lld", (long long)rows, (long long)cols);
+    if (rows > (1 << 30) || cols > (1 << 30)) return fail(FG_ERR_UNSUPPORTED, "sizes above 2^30 are not supported");
+    if (fg_status st = check_rows("X", X, rows, cols)) return st;
+    if (fg_status st = check_rows(name, Y, rows, cols)) return st;
+    if (X->dtype != Y->dtype) return fail(FG_ERR_UNSUPPORTED, "X and %s must have the same element type", name);
+    if (param_dtype != FG_F32 && param_dtype != X->dtype) return fail(FG_ERR_LAYOUT, "gamma and beta must be FG_F32 or of the type of X");
+    if (!aligned_to(gamma, element_bytes(param_dtype))) return fail(FG_ERR_ALIGN, "gamma must be aligned to an element");
+    return FG_OK;
+}
+
+}  // namespace
+}  // namespace fg
+
+using namespace fg;
+
+extern "C" {
+
+fg_status fg_layernorm(int64_t rows, int64_t cols, const fg_matrix *X, const void *gamma, const void *beta, int32_t param_dtype, float eps,
+                       const fg_matrix *Y, float *mean, float *rstd, void *hip_stream) {
+    if (fg_status st = check_layernorm(rows, cols, X, "Y", Y, gamma, param_dtype)) return st;
+    if (!(eps >= 0.f)) return fail(FG_ERR_SHAPE, "eps must not be negative");
+    if (!aligned_to(beta, element_bytes(param_dtype)) || !aligned_to(mean, 4) || !aligned_to(rstd, 4))
+        return fail(FG_ERR_ALIGN, "beta, mean and rstd must be aligned to an element");
+    if (rows == 0 || cols == 0) return FG_OK;
+    LayerNormArgs a = {X->re, nullptr, Y->re, gamma, beta, mean, rstd, nullptr, X->ld, 0, Y->ld, rows, (int32_t)cols, eps, (float)cols};
+    hipStream_t stream = (hipStream_t)hip_stream;
+    const int w = waves_for(cols, element_bytes(X->dtype));
+    return with_types(X->dtype, param_dtype, [&](auto t, auto p) {
+        using T = decltype(t);
+        using P = decltype(p);
+        if (w == 0) hipLaunchKernelGGL((layernorm_wide<T, P>), dim3((unsigned)rows), dim3(1024), 0, stream, a);
+        else with_waves(w, [&](auto tag) {
+            constexpr int W = tag, R = kRowsPerGroup<W>;
+            const unsigned grid = (unsigned)std::min<int64_t>((rows + R - 1) / R, kNumCU * 32 / (W * R));
+            hipLaunchKernelGGL((layernorm<T, P, W>), dim3(grid), dim3(64 * W * R), 0, stream, a);
+        });
+        return check_launch("layernorm");
+    });
+}
+
+int64_t fg_layernorm_grad_workspace(int64_t rows, int64_t cols, int32_t dtype) {
+    if (rows <= 0 || cols <= 0 || !element_bytes(dtype)) return 0;
+    return grad_groups(rows, cols, element_bytes(dtype)) * 2 * cols * 4;
+}
+
+fg_status fg_layernorm_grad(int64_t rows, int64_t cols, const fg_matrix *dY, const fg_matrix *X, const void *gamma, int32_t param_dtype,
+                            const float *mean, const float *rstd, const fg_matrix *dX, void *dgamma, void *dbeta,
+                            void *workspace, int64_t workspace_bytes, void *hip_stream) {
+    if (fg_status st = check_layernorm(rows, cols, X, "dX", dX, gamma, param_dtype)) return st;
+    if (fg_status st = check_rows("dY", dY, rows, cols, true)) return st;
+    if (dY->dtype != X->dtype) return fail(FG_ERR_UNSUPPORTED, "X and dY must have the same element type");
+    const unsigned es = element_bytes(param_dtype);
+    if (!aligned_to(dgamma, es) || !aligned_to(dbeta, es) || !aligned_to(mean, 4) || !aligned_to(rstd, 4) || !aligned_to(workspace, 4))
+        return fail(FG_ERR_ALIGN, "mean, rstd, dgamma, dbeta and the workspace must be aligned to an element");
+    if (cols == 0) return FG_OK;
+    const bool sums = dgamma || dbeta;
+    if (rows > 0 && (!mean || !rstd)) return fail(FG_ERR_NULL, "mean and rstd of the forward pass are NULL");
+    const int64_t need = sums ? fg_layernorm_grad_workspace(rows, cols, X->dtype) : 0;
+    if (need > 0 && !workspace) return fail(FG_ERR_NULL, "the workspace is NULL");
+    if (workspace_bytes < need) return fail(FG_ERR_SHAPE, "the workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)need);
+    LayerNormArgs a = {X->re, dY->re, dX->re, gamma, nullptr, const_cast<float *>(mean), const_cast<float *>(rstd), (float *)workspace,
+                       X->ld, dY->ld, dX->ld, rows, (int32_t)cols, 0.f, (float)cols};
+    hipStream_t stream = (hipStream_t)hip_stream;
+    const int w = waves_for(cols, element_bytes(X->dtype));
+    const int64_t groups = rows > 0 ? grad_groups(rows, cols, element_bytes(X->dtype)) : 0;      // no row: the sums are zero
+    return with_types(X->dtype, param_dtype, [&](auto t, auto p) {
+        using T = decltype(t);
+        using P = decltype(p);
+        if (rows > 0 && w == 0) {
+            if (sums) hipLaunchKernelGGL((layernorm_column_sums<T>), dim3((unsigned)((cols + 255) / 256), (unsigned)groups), dim3(256), 0, stream, a);
+            hipLaunchKernelGGL((layernorm_grad_wide<T, P>), dim3((unsigned)rows), dim3(1024), 0, stream, a);
+        } else if (rows > 0) with_waves(w, [&](auto tag) {
+            constexpr int W = tag, R = kRowsPerGroup<W>;
+            const dim3 grid((unsigned)((groups + R - 1) / R)), block(64 * W * R);
+            if (sums) hipLaunchKernelGGL((layernorm_grad<T, P, W, true>), grid, block, 0, stream, a);
+            else hipLaunchKernelGGL((layernorm_grad<T, P, W, false>), grid, block, 0, stream, a);
+        });
+        if (fg_status st = check_launch("layernorm_grad")) return st;
+        if (!sums) return FG_OK;
+        hipLaunchKernelGGL((layernorm_sums<P>), dim3((unsigned)((2 * cols + 31) / 32)), dim3(1024), 0, stream, (const float *)workspace, (int)groups, (int)cols,
+                           (P *)dgamma, (P *)dbeta);
+        return check_launch("layernorm_sums");
+    });
+}
+
+}  // extern "C"

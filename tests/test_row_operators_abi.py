@@ -1,0 +1,74 @@
+"""CPU tests: what the operators on rows refuse, and with which status, before anything is launched."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2009_12263_amd import binding as fg
+
+PTR = 0x10000
+
+
+def row(dtype=fg.FG_BF16, ld=64, re=PTR, layout=fg.FG_ROW, im=None):
+    return C.byref(fg.fg_matrix(re, im, dtype, layout, ld))
+
+
+def layernorm(rows=4, cols=64, X=None, gamma=PTR, beta=PTR, pt=fg.FG_F32, eps=1e-5, Y=None, mean=PTR, rstd=PTR):
+    X = row() if X is None else X
+    Y = row() if Y is None else Y
+    return fg.load_library().fg_layernorm(rows, cols, X, gamma, beta, pt, eps, Y, mean, rstd, None)
+
+
+def layernorm_grad(rows=4, cols=64, dY=None, X=None, gamma=PTR, pt=fg.FG_F32, mean=PTR, rstd=PTR, dX=None, dgamma=PTR, dbeta=PTR, ws=PTR, size=1 << 30):
+    dY, X, dX = (row() if m is None else m for m in (dY, X, dX))
+    return fg.load_library().fg_layernorm_grad(rows, cols, dY, X, gamma, pt, mean, rstd, dX, dgamma, dbeta, ws, size, None)
+
+
+NULL = C.POINTER(fg.fg_matrix)()
+
+
+@pytest.mark.parametrize("call,args,status,word", [
+    (layernorm, dict(rows=-1), fg.FG_ERR_SHAPE, "negative"),
+    (layernorm, dict(X=NULL), fg.FG_ERR_NULL, "X is NULL"),
+    (layernorm, dict(Y=NULL), fg.FG_ERR_NULL, "Y is NULL"),
+    (layernorm, dict(X=row(re=None)), fg.FG_ERR_NULL, "X->re"),
+    (layernorm, dict(X=row(layout=fg.FG_COL)), fg.FG_ERR_LAYOUT, "row-major"),
+    (layernorm, dict(X=row(dtype=fg.FG_CF16)), fg.FG_ERR_LAYOUT, "FG_F16, FG_BF16 or FG_F32"),
+    (layernorm, dict(X=row(im=PTR)), fg.FG_ERR_LAYOUT, "real"),
+    (layernorm, dict(X=row(ld=63)), fg.FG_ERR_SHAPE, "ld=63"),
+    (layernorm, dict(X=row(ld=0)), fg.FG_ERR_SHAPE, "ld=0"),
+    (layernorm, dict(X=row(re=PTR + 1)), fg.FG_ERR_ALIGN, "aligned"),
+    (layernorm, dict(Y=row(dtype=fg.FG_F16)), fg.FG_ERR_UNSUPPORTED, "same element type"),
+    (layernorm, dict(pt=fg.FG_F16), fg.FG_ERR_LAYOUT, "gamma"),
+    (layernorm, dict(gamma=PTR + 2), fg.FG_ERR_ALIGN, "gamma"),
+    (layernorm, dict(mean=PTR + 2), fg.FG_ERR_ALIGN, "mean"),
+    (layernorm, dict(eps=-1.0), fg.FG_ERR_SHAPE, "eps"),
+    (layernorm, dict(eps=float("nan")), fg.FG_ERR_SHAPE, "eps"),
+    (layernorm, dict(rows=2 << 30), fg.FG_ERR_UNSUPPORTED, "2^30"),
+    (layernorm_grad, dict(dY=NULL), fg.FG_ERR_NULL, "dY is NULL"),
+    (layernorm_grad, dict(dX=row(ld=3)), fg.FG_ERR_SHAPE, "dX"),
+    (layernorm_grad, dict(dY=row(dtype=fg.FG_F32)), fg.FG_ERR_UNSUPPORTED, "dY"),
+    (layernorm_grad, dict(mean=None), fg.FG_ERR_NULL, "mean"),
+    (layernorm_grad, dict(ws=None), fg.FG_ERR_NULL, "workspace"),
+    (layernorm_grad, dict(size=100), fg.FG_ERR_SHAPE, "workspace"),
+    (layernorm_grad, dict(dgamma=PTR + 1), fg.FG_ERR_ALIGN, "dgamma"),
+])
+def test_refusals(call, args, status, word):
+    assert call(**args) == status
+    assert word in fg.fg_last_error()
+
+
+def test_sizes_of_zero_launch_nothing():
+    assert layernorm(rows=0) == fg.FG_OK and layernorm(cols=0) == fg.FG_OK and layernorm_grad(cols=0) == fg.FG_OK
+
+
+def test_workspace_queries():
+    lib = fg.load_library()
+    assert lib.fg_layernorm_grad_workspace(0, 64, fg.FG_F32) == 0 and lib.fg_layernorm_grad_workspace(4, 64, 77) == 0
+    assert lib.fg_layernorm_grad_workspace(4, 64, fg.FG_F32) >= 2 * 64 * 4
+
+
+def test_binding_wants_tensors_on_the_gpu():
+    x = torch.zeros(4, 64)
+    with pytest.raises((ValueError, RuntimeError)):
+        fg.fg_layernorm(x, None, None, 1e-5, x)
