@@ -95,7 +95,8 @@ typedef enum {
     FG_F16 = 0, FG_BF16 = 1,   /* A, B: IEEE binary16 / bfloat16 (FG_F16 also for C, D: see fg_gemm) */
     FG_F32 = 2,                /* C, D                                                           */
     FG_CF16 = 3,               /* A, B: interleaved complex, element = (re, im) as two binary16  */
-    FG_CF32 = 4                /* C, D: interleaved complex, element = (re, im) as two binary32  */
+    FG_CF32 = 4,               /* C, D: interleaved complex, element = (re, im) as two binary32  */
+    FG_I32 = 5, FG_I64 = 6     /* token ids and targets                                          */
 } fg_dtype;
 
 typedef enum {
@@ -277,8 +278,8 @@ fg_status fg_contract_plan(int32_t nA, const int32_t *modesA, const int64_t *str
  * Hidden states, embedding tables and vocabulary matrices are row-major fg_matrix descriptors (layout FG_ROW, `im` NULL) with a leading
  * dimension of any size from the row's length on and element-aligned pointers, of FG_F16, FG_BF16 or (where it is said) FG_F32
  * elements.  All arithmetic is FP32 or wider; every result is rounded to nearest even once, when it is stored.  Results do not
- * depend on scheduling: the same call gives the same bits.  Calls that need scratch memory take a workspace from the caller, of at
- * least the bytes that the query beside it gives; it holds nothing from one call to the next, needs no clearing and may be
+ * depend on scheduling: the same call gives the same bits.  Calls that need scratch memory take a 16-byte aligned workspace from the
+ * caller, of at least the bytes that the query beside it gives; it holds nothing from one call to the next, needs no clearing and may be
  * reused by the next call on the same stream.  These calls allocate nothing and only enqueue kernels: they may be recorded into a HIP graph.
  * Sizes of zero are accepted.
  */
@@ -302,6 +303,25 @@ fg_status fg_layernorm_grad(int64_t rows, int64_t cols, const fg_matrix *dY, con
                             const float *mean, const float *rstd, const fg_matrix *dX, void *dgamma, void *dbeta,
                             void *workspace, int64_t workspace_bytes, void *hip_stream);
 int64_t fg_layernorm_grad_workspace(int64_t rows, int64_t cols, int32_t dtype);
+
+/*
+ * Embedding lookup: Y[t] = scale * table[ids[t]], and zeros where ids[t] is not in [0, vocab) (padding).
+ *   table : vocab x dim (FG_F32 too); Y : tokens x dim, of the same type; ids : `tokens` indices of type index_dtype (FG_I32, FG_I64).
+ */
+fg_status fg_embedding(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *table, const void *ids, int32_t index_dtype, float scale,
+                       const fg_matrix *Y, void *hip_stream);
+
+/*
+ * Its gradient: dtable[v] = scale * sum of dY[t] over the t with ids[t] == v, + Cin[v].  The tokens are sorted by id on the device and each
+ * sum is formed in the order of the tokens, in FP32, without atomics on values.
+ *   dY     : tokens x dim (FG_F32 too; ld 0: the same row for all).
+ *   Cin    : vocab x dim, of the type of dtable, or NULL: nothing is added.  Cin may be dtable itself: then only the rows that
+ *            have tokens are read and written (an embedding that shares its weights with the output layer).
+ *   dtable : vocab x dim, of the type of dY or FG_F32.
+ */
+fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *dY, const void *ids, int32_t index_dtype, float scale,
+                            const fg_matrix *Cin, const fg_matrix *dtable, void *workspace, int64_t workspace_bytes, void *hip_stream);
+int64_t fg_embedding_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim);
 
 /* Message for the most recent failing call on this thread ("" if none).  The pointer refers to
  * thread-local static storage: valid until the next library call on the same thread. */

@@ -23,13 +23,13 @@ FASTCALL_PATH = os.path.join(_PKG, "_fastcall.%s.torch-%s.so" % (sysconfig.get_c
 
 FG_OK = 0
 FG_ERR_NULL, FG_ERR_SHAPE, FG_ERR_LAYOUT, FG_ERR_ALIGN, FG_ERR_UNSUPPORTED, FG_ERR_MODES, FG_ERR_LAUNCH = range(1, 8)
-FG_F16, FG_BF16, FG_F32, FG_CF16, FG_CF32 = 0, 1, 2, 3, 4
+FG_F16, FG_BF16, FG_F32, FG_CF16, FG_CF32, FG_I32, FG_I64 = 0, 1, 2, 3, 4, 5, 6
 FG_COL, FG_ROW, FG_DIAG, FG_ZERO = 0, 1, 2, 3
 FG_ACT_NONE, FG_ACT_RELU = 0, 1
 
 EXPORTS = ("fg_init", "fg_gemm", "fg_gemm_ex", "fg_gemm_noalloc", "fg_gemm_dual", "fg_contract", "fg_contract_plan", "fg_last_error", "fg_version",
            "fg_reload_tuning", "fg_gemm_plan", "fg_probe_mfma", "fg_probe_mfma_k32", "fg_probe_kloop_mix",
-           "fg_layernorm", "fg_layernorm_grad", "fg_layernorm_grad_workspace")
+           "fg_layernorm", "fg_layernorm_grad", "fg_layernorm_grad_workspace", "fg_embedding", "fg_embedding_grad", "fg_embedding_grad_workspace")
 FG_PLAN_REAL, FG_PLAN_COMPLEX, FG_PLAN_DUAL, FG_PLAN_REAL_BF16, FG_PLAN_COMPLEX_INTERLEAVED, FG_PLAN_REAL_F16_CD = 0, 1, 2, 3, 4, 5
 FG_PLAN_REAL_AB_ADD = 6
 
@@ -106,6 +106,12 @@ def load_library() -> C.CDLL:
         lib.fg_layernorm_grad.argtypes = [i64, i64, mp, mp, vp, i32, vp, vp, mp, vp, vp, vp, i64, vp]
         lib.fg_layernorm_grad_workspace.restype = i64
         lib.fg_layernorm_grad_workspace.argtypes = [i64, i64, i32]
+        lib.fg_embedding.restype = C.c_int
+        lib.fg_embedding.argtypes = [i64, i64, i64, mp, vp, i32, f32, mp, vp]
+        lib.fg_embedding_grad.restype = C.c_int
+        lib.fg_embedding_grad.argtypes = [i64, i64, i64, mp, vp, i32, f32, mp, mp, vp, i64, vp]
+        lib.fg_embedding_grad_workspace.restype = i64
+        lib.fg_embedding_grad_workspace.argtypes = [i64, i64, i64]
         _load_fastcall(lib)
         _lib = lib
     return _lib
@@ -134,7 +140,8 @@ def _load_fastcall(lib: C.CDLL) -> None:
     _fast = fast
 
 
-_DTYPES = {torch.float16: FG_F16, torch.bfloat16: FG_BF16, torch.float32: FG_F32, torch.complex32: FG_CF16, torch.complex64: FG_CF32}
+_DTYPES = {torch.float16: FG_F16, torch.bfloat16: FG_BF16, torch.float32: FG_F32, torch.complex32: FG_CF16, torch.complex64: FG_CF32,
+           torch.int32: FG_I32, torch.int64: FG_I64}
 
 
 @dataclass
@@ -420,4 +427,42 @@ def fg_layernorm_grad(dY: torch.Tensor, X: torch.Tensor, gamma: Optional[torch.T
     st = lib.fg_layernorm_grad(rows, cols, C.byref(dy), C.byref(x), _vector(gamma, cols, "gamma", ptype, dev), _DTYPES.get(ptype, -1),
                                _vector(mean, rows, "mean", torch.float32, dev), _vector(rstd, rows, "rstd", torch.float32, dev), C.byref(dx),
                                _vector(dgamma, cols, "dgamma", ptype, dev), _vector(dbeta, cols, "dbeta", ptype, dev), ws, ws_bytes, _stream_handle(stream))
+    return _check(st, raise_on_error)
+
+
+def _indices(t: torch.Tensor, n: int, name: str, dev: int):
+    if t.dtype not in (torch.int32, torch.int64):
+        raise ValueError("%s: expected int32 or int64, got %s" % (name, t.dtype))
+    return _vector(t, n, name, t.dtype, dev), _DTYPES[t.dtype]
+
+
+def fg_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float, Y: torch.Tensor, stream=None, raise_on_error: bool = True) -> int:
+    """Y[t] = scale * table[ids[t]]; zeros where ids[t] names no row."""
+    lib = _lib or load_library()
+    dev = _current_device()
+    m = _rows(table, "table", None, dev)
+    vocab, dim = table.shape
+    tokens = ids.shape[0]
+    y = _rows(Y, "Y", (tokens, dim), dev)
+    at, kind = _indices(ids, tokens, "ids", dev)
+    return _check(lib.fg_embedding(tokens, vocab, dim, C.byref(m), at, kind, scale, C.byref(y), _stream_handle(stream)), raise_on_error)
+
+
+def fg_embedding_grad_workspace(tokens: int, vocab: int, dim: int) -> int:
+    return int(load_library().fg_embedding_grad_workspace(tokens, vocab, dim))
+
+
+def fg_embedding_grad(dY: torch.Tensor, ids: torch.Tensor, scale: float, Cin: Optional[torch.Tensor], dtable: torch.Tensor,
+                      workspace: Optional[torch.Tensor] = None, stream=None, raise_on_error: bool = True) -> int:
+    """dtable[v] = scale * sum of dY[t] over the t with ids[t] == v, + Cin[v] (None: nothing; dtable itself: only rows with tokens are touched)."""
+    lib = _lib or load_library()
+    dev = _current_device()
+    d = _rows(dtable, "dtable", None, dev)
+    vocab, dim = dtable.shape
+    tokens = ids.shape[0]
+    dy = _rows(dY, "dY", (tokens, dim), dev)
+    c = _rows(Cin, "Cin", (vocab, dim), dev) if Cin is not None else None
+    at, kind = _indices(ids, tokens, "ids", dev)
+    ws, ws_bytes, _keep = _workspace(workspace, lib.fg_embedding_grad_workspace(tokens, vocab, dim), stream, dev)
+    st = lib.fg_embedding_grad(tokens, vocab, dim, C.byref(dy), at, kind, scale, _ref(c), C.byref(d), ws, ws_bytes, _stream_handle(stream))
     return _check(st, raise_on_error)

@@ -1,0 +1,385 @@
+// Embedding lookup with scaling, and its gradient by sorted tokens.
+//
+//   y[t] = scale table[ids[t]]            dtable[v] = scale sum over ids[t] = v of dy[t] + c[v]
+//
+// Both are bound by memory.  The gradient's sums must not depend on scheduling, so no value is added with an atomic: the tokens are
+// sorted by id, stably, and the sorted list is cut into tiles of kTile tokens.  A wave takes a tile and 64 pieces of its columns
+// and walks the tokens in order; the sum of an id whose tokens all lie in the tile is a row of the result, and the sums of an
+// id that reaches over the tile's edges are kept and joined in the order of the tiles by a last pass.  So an
+// id that half of the tokens have costs as little as a rare one.  Rows without tokens are filled by other waves of the same launch.
+//
+// Sorting: runs of kRun tokens are sorted in LDS, one workgroup each, and merged in one step: a token's place in the whole list is
+// the number of tokens in front of it in every run, found by bisection.
+#include "row_ops.hpp"
+
+#include <algorithm>
+
+namespace fg {
+namespace {
+
+constexpr int kTile = 16;                   // sorted tokens per tile
+constexpr int kRunThreads = 1024, kRunWaves = kRunThreads / 64;
+constexpr int kDigit = 6;                   // bits that one pass of the sort takes
+
+// ---- lookup -----------------------------------------------------------------------------------------
+// A wave takes rows << shift lanes: 64 >> shift rows at a time, 2^shift lanes each.
+template <class T>
+__global__ __launch_bounds__(256) void embedding(const T *table, int64_t ld, const void *ids, bool wide, float scale, T *y, int64_t ldy, int64_t tokens,
+                                                 int vocab, int dim, int shift) {
+    constexpr int N = Piece<T>::N, AHEAD = 4;
+    const int lane = threadIdx.x & 63, at = lane & ((1 << shift) - 1), rows = 64 >> shift, pieces = (dim + N - 1) / N;
+    const int chunks = (pieces + (AHEAD << shift) - 1) / (AHEAD << shift);
+    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t t = wave / chunks * rows + (lane >> shift);
+    const int first = (int)(wave % chunks) * (AHEAD << shift) + at;
+    if (t >= tokens) return;
+    const int id = load_index(ids, wide, t, vocab);
+    const T *row = table + (int64_t)(id < 0 ? 0 : id) * ld;
+    float v[AHEAD][N];
+#pragma unroll
+    for (int c = 0; c < AHEAD; ++c)
+        if (first + (c << shift) < pieces) {
+            if (id >= 0) load_piece(row, first + (c << shift), dim, v[c]);
+            else
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[c][i] = 0.f;
+        }
+#pragma unroll
+    for (int c = 0; c < AHEAD; ++c)
+        if (first + (c << shift) < pieces) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[c][i] = id >= 0 ? v[c][i] * scale : 0.f;
+            store_piece(y + t * ldy, first + (c << shift), dim, v[c]);
+        }
+}
+
+// ---- sorting ----------------------------------------------------------------------------------------
+// Sorts run blockIdx.x of ITEMS * 1024 tokens by id, stably; ids that name no row count as `vocab` and come last.  Also clears the
+// bits of the rows that have tokens.
+template <int ITEMS>
+__global__ __launch_bounds__(kRunThreads) void embedding_sort(const void *ids, bool wide, int tokens, int vocab, int passes, uint32_t *keys, uint32_t *order, uint32_t *present) {
+    constexpr int RUN = ITEMS * kRunThreads;
+    __shared__ uint32_t key[RUN];
+    __shared__ uint16_t pos[RUN];
+    __shared__ uint32_t count[kRunWaves][1 << kDigit], total[kRunWaves];
+    static_assert(kRunWaves << kDigit == kRunThreads, "one thread per counter");
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.x * RUN, n = min(tokens - first, RUN);
+    for (int64_t w = (int64_t)blockIdx.x * kRunThreads + threadIdx.x; w < (vocab + 31) / 32; w += (int64_t)gridDim.x * kRunThreads) present[w] = 0;
+#pragma unroll
+    for (int r = 0; r < ITEMS; ++r) {
+        const int i = (wave * ITEMS + r) * 64 + lane;
+        const int id = i < n ? load_index(ids, wide, first + i, vocab) : -1;
+        key[i] = i >= n ? (uint32_t)vocab + 1 : id < 0 ? (uint32_t)vocab : (uint32_t)id;
+        pos[i] = (uint16_t)i;
+    }
+    for (int pass = 0; pass < passes; ++pass) {
+        count[wave][lane] = 0;              // (a wave's own counters: LDS operations of a wave take place in order)
+        __syncthreads();
+        uint32_t k[ITEMS], at[ITEMS];
+        int place[ITEMS];
+        volatile uint32_t *mine = count[wave];
+#pragma unroll
+        for (int r = 0; r < ITEMS; ++r) {
+            const int i = (wave * ITEMS + r) * 64 + lane;
+            k[r] = key[i];
+            at[r] = pos[i];
+            const uint32_t digit = (k[r] >> (pass * kDigit)) & ((1 << kDigit) - 1);
+            uint64_t same = ~0ull;          // lanes with the same digit
+#pragma unroll
+            for (int b = 0; b < kDigit; ++b) {
+                const uint64_t set = __ballot((digit >> b) & 1);
+                same &= (digit >> b) & 1 ? set : ~set;
+            }
+            const uint32_t before = (uint32_t)__popcll(same & ((1ull << lane) - 1)), base = mine[digit];
+            __builtin_amdgcn_wave_barrier();
+            if (before == 0) mine[digit] = base + (uint32_t)__popcll(same);
+            __builtin_amdgcn_wave_barrier();
+            place[r] = (int)(base + before);
+        }
+        __syncthreads();
+        // where the tokens of (digit, wave) begin: the sum of all counters in front of it, digits first
+        const int d = threadIdx.x / kRunWaves, w = threadIdx.x % kRunWaves;
+        const uint32_t own = count[w][d];
+        uint32_t sum = own;
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2) {
+            const uint32_t other = __shfl_up(sum, s);
+            if (lane >= s) sum += other;
+        }
+        if (lane == 63) total[wave] = sum;
+        __syncthreads();
+        for (int o = 0; o < wave; ++o) sum += total[o];
+        count[w][d] = sum - own;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < ITEMS; ++r) {
+            const uint32_t to = count[wave][(k[r] >> (pass * kDigit)) & ((1 << kDigit) - 1)] + place[r];
+            key[to] = k[r];
+            pos[to] = (uint16_t)at[r];
+        }
+        __syncthreads();
+    }
+    for (int i = threadIdx.x; i < n; i += kRunThreads) {
+        keys[first + i] = key[i];
+        order[first + i] = first + pos[i];
+    }
+}
+
+// How many of the n sorted keys are below k (or equal to it, with `equal`).
+__device__ __forceinline__ int keys_before(const uint32_t *keys, int n, uint32_t k, bool equal) {
+    int lo = 0;
+    for (int left = n; left > 0;) {
+        const int half = left >> 1;
+        const uint32_t at = keys[lo + half];
+        if (at < k || (equal && at == k)) { lo += half + 1; left -= half + 1; }
+        else left = half;
+    }
+    return lo;
+}
+// Token i of the sorted runs goes to its place in the whole list: behind all smaller ids, and behind equal ones of earlier runs.
+__global__ __launch_bounds__(256) void embedding_merge(const uint32_t *keys, const uint32_t *order, int tokens, int run, uint32_t *all_keys, uint32_t *all_order,
+                                                       int vocab, uint32_t *present) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= tokens) return;
+    const int own = i / run, runs = (tokens + run - 1) / run;
+    const uint32_t k = keys[i];
+    int place = i - own * run;
+    for (int r = 0; r < runs; ++r)
+        if (r != own) place += keys_before(keys + (int64_t)r * run, min(run, tokens - r * run), k, r < own);
+    all_keys[place] = k;
+    all_order[place] = order[i];
+    if (k < (uint32_t)vocab && (i == own * run || keys[i - 1] != k)) atomicOr(&present[k >> 5], 1u << (k & 31));      // (bits: in any order)
+}
+
+// ---- sums -------------------------------------------------------------------------------------------
+struct EmbeddingGradArgs {
+    const void *dy;
+    const void *c;
+    void *out;
+    const uint32_t *keys, *order, *present;
+    float *open;                            // tile t: the sum of the id that comes in over its front at 2 t dim, of the one that goes out at (2 t + 1) dim
+    int64_t lddy, ldc, ldo;
+    int tokens, vocab, dim, tiles, chunks;  // chunks: of 64 pieces, that cover the columns
+    int sum_groups;                         // workgroups of sums in front of those that fill rows
+    int shift;                              // lanes of a row to fill
+    float scale;
+};
+
+// A row's sum becomes the result: scaled, what is there added, rounded once.
+template <class D, int N>
+__device__ __forceinline__ void embedding_finish(const EmbeddingGradArgs &a, uint32_t id, int p, float (&sum)[N]) {
+    float c[N];
+    if (a.c) load_piece((const D *)a.c + (int64_t)id * a.ldc, p, a.dim, c);
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] = a.c ? sum[i] * a.scale + c[i] : sum[i] * a.scale;
+    store_piece((D *)a.out + (int64_t)id * a.ldo, p, a.dim, sum);
+}
+
+template <class T, class D>
+__global__ __launch_bounds__(256) void embedding_grad(const EmbeddingGradArgs a) {
+    constexpr int N = Piece<T>::N;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pieces = (a.dim + N - 1) / N;
+    if ((int)blockIdx.x >= a.sum_groups) {
+        // rows without tokens: zeros, or what is there
+        constexpr int AHEAD = 4;
+        const int at = lane & ((1 << a.shift) - 1), rows = 64 >> a.shift, chunks = (pieces + (AHEAD << a.shift) - 1) / (AHEAD << a.shift);
+        const int64_t item = (int64_t)(blockIdx.x - a.sum_groups) * 4 + wave;
+        const int64_t row = item / chunks * rows + (lane >> a.shift);
+        const int first = (int)(item % chunks) * (AHEAD << a.shift) + at;
+        if (row >= a.vocab || (a.present[row >> 5] >> (row & 31) & 1)) return;
+        float v[AHEAD][N] = {};
+        if (a.c) {
+#pragma unroll
+            for (int c = 0; c < AHEAD; ++c)
+                if (first + (c << a.shift) < pieces) load_piece((const D *)a.c + row * a.ldc, first + (c << a.shift), a.dim, v[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < AHEAD; ++c)
+            if (first + (c << a.shift) < pieces) store_piece((D *)a.out + row * a.ldo, first + (c << a.shift), a.dim, v[c]);
+        return;
+    }
+    const int item = blockIdx.x * 4 + wave, tile = item / a.chunks, p = item % a.chunks * 64 + lane;
+    if (tile >= a.tiles) return;
+    const int i0 = tile * kTile, n = min(kTile, a.tokens - i0);
+    const bool on = p < pieces;             // (lanes without columns hold tokens all the same)
+    // the tokens of the tile, one per lane; and whether the ids at its edges reach beyond it
+    const uint32_t key_of_lane = a.keys[i0 + min(lane, n - 1)], token_of_lane = a.order[i0 + min(lane, n - 1)];
+    const bool comes_in = i0 > 0 && a.keys[i0 - 1] == a.keys[i0], goes_out = i0 + n < a.tokens && a.keys[i0 + n] == a.keys[i0 + n - 1];
+    float sum[N] = {}, v[kTile][N];
+#pragma unroll
+    for (int e = 0; e < kTile; ++e)
+        if (e < n && on) load_piece((const T *)a.dy + (int64_t)(uint32_t)__builtin_amdgcn_readlane(token_of_lane, e) * a.lddy, p, a.dim, v[e]);
+    bool in = comes_in;                     // the current id began in an earlier tile
+#pragma unroll
+    for (int e = 0; e < kTile; ++e) {
+        const uint32_t id = __builtin_amdgcn_readlane(key_of_lane, e);
+        if (e < n && id < (uint32_t)a.vocab) {                          // (ids that name no row are the last)
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum[i] += v[e][i];
+            const bool last = e + 1 == n;
+            if (last || (uint32_t)__builtin_amdgcn_readlane(key_of_lane, (e + 1) % kTile) != id) {
+                if (on) {
+                    if (in || (last && goes_out)) store_piece(a.open + ((int64_t)tile * 2 + (in ? 0 : 1)) * a.dim, p, a.dim, sum);
+                    else embedding_finish<D>(a, id, p, sum);
+                }
+                in = false;
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[i] = 0.f;
+            }
+        }
+    }
+}
+
+// Joins the sums of an id that goes out of a tile it began in: that tile's, then one of each tile that it comes into.
+template <class T, class D>
+__global__ __launch_bounds__(256) void embedding_join(const EmbeddingGradArgs a) {
+    constexpr int N = Piece<T>::N, AHEAD = 8;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pieces = (a.dim + N - 1) / N;
+    const int item = blockIdx.x * 4 + wave, tile = item / a.chunks, p = item % a.chunks * 64 + lane;
+    if (tile + 1 >= a.tiles) return;
+    const int i0 = tile * kTile, next = i0 + kTile;
+    const uint32_t id = a.keys[next - 1];
+    if (id >= (uint32_t)a.vocab || a.keys[next] != id || (a.keys[i0] == id && i0 > 0 && a.keys[i0 - 1] == id)) return;
+    // tiles that it comes into
+    int into = 0;
+    for (;;) {
+        const int t = tile + 1 + into + lane;
+        const uint64_t same = __ballot(t < a.tiles && a.keys[(int64_t)t * kTile] == id);
+        const int more = same == ~0ull ? 64 : __builtin_ctzll(~same);
+        into += more;
+        if (more < 64) break;
+    }
+    if (p >= pieces) return;
+    float sum[N];
+    load_piece(a.open + ((int64_t)tile * 2 + 1) * a.dim, p, a.dim, sum);
+    for (int t0 = 0; t0 < into; t0 += AHEAD) {
+        float v[AHEAD][N];
+#pragma unroll
+        for (int t = 0; t < AHEAD; ++t)
+            if (t0 + t < into) load_piece(a.open + (int64_t)(tile + 1 + t0 + t) * 2 * a.dim, p, a.dim, v[t]);
+#pragma unroll
+        for (int t = 0; t < AHEAD; ++t)
+            if (t0 + t < into)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[i] += v[t][i];
+    }
+    embedding_finish<D>(a, id, p, sum);
+}
+
+// ---- host ----------------------------------------------------------------------------------------------
+// Lanes of a row: as many as have a piece each, at most a wave (as a power of two).
+int lanes_shift(int pieces) {
+    int s = 0;
+    while (s < 6 && (1 << s) < pieces) ++s;
+    return s;
+}
+int run_items(int64_t tokens) { return tokens <= 65536 ? 4 : 8; }
+
+// The workspace: sorted runs, the whole list, the rows that have tokens, open sums.
+struct EmbeddingSpace {
+    int64_t keys, order, all_keys, all_order, present, open, bytes;
+    EmbeddingSpace(int64_t tokens, int64_t vocab, int64_t dim) {
+        auto up = [](int64_t b) { return (b + 255) / 256 * 256; };
+        keys = 0;
+        order = keys + up(4 * tokens);
+        all_keys = order + up(4 * tokens);
+        all_order = all_keys + up(4 * tokens);
+        present = all_order + up(4 * tokens);
+        open = present + up((vocab + 31) / 32 * 4);
+        bytes = open + (tokens + kTile - 1) / kTile * 2 * dim * 4;
+    }
+};
+
+template <class F> void with_element(int dtype, F &&f) {
+    switch (dtype) {
+        case FG_F16: f(f16_t{}); break;
+        case FG_BF16: f(bf16_t{}); break;
+        default: f(float{});
+    }
+}
+
+fg_status check_embedding(int64_t tokens, int64_t vocab, int64_t dim, const void *ids, int32_t index_dtype) {
+    if (tokens < 0 || vocab < 0 || dim < 0) return fail(FG_ERR_SHAPE, "negative size: %lld tokens, %lld rows of %lld", (long long)tokens, (long long)vocab, (long long)dim);
+    if (tokens > (1 << 30) || vocab > (1 << 30) || dim > (1 << 30)) return fail(FG_ERR_UNSUPPORTED, "sizes above 2^30 are not supported");
+    return check_indices("ids", ids, index_dtype, tokens);
+}
+
+}  // namespace
+}  // namespace fg
+
+using namespace fg;
+
+extern "C" {
+
+fg_status fg_embedding(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *table, const void *ids, int32_t index_dtype, float scale,
+                       const fg_matrix *Y, void *hip_stream) {
+    if (fg_status st = check_embedding(tokens, vocab, dim, ids, index_dtype)) return st;
+    if (fg_status st = check_rows("table", table, vocab, dim)) return st;
+    if (fg_status st = check_rows("Y", Y, tokens, dim)) return st;
+    if (table->dtype != Y->dtype) return fail(FG_ERR_UNSUPPORTED, "the table and Y must have the same element type");
+    if (tokens == 0 || dim == 0) return FG_OK;
+    with_element(Y->dtype, [&](auto t) {
+        using T = decltype(t);
+        const int pieces = (int)((dim + Piece<T>::N - 1) / Piece<T>::N), shift = lanes_shift((pieces + 3) / 4);
+        const int64_t waves = (tokens + (64 >> shift) - 1) / (64 >> shift) * ((pieces + (4 << shift) - 1) / (4 << shift));
+        hipLaunchKernelGGL((embedding<T>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, (hipStream_t)hip_stream, (const T *)table->re, table->ld, ids,
+                           index_dtype == FG_I64, scale, (T *)Y->re, Y->ld, tokens, (int)vocab, (int)dim, shift);
+    });
+    return check_launch("embedding");
+}
+
+int64_t fg_embedding_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim) {
+    if (tokens < 0 || vocab <= 0 || dim <= 0) return 0;
+    return EmbeddingSpace(tokens, vocab, dim).bytes;
+}
+
+fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *dY, const void *ids, int32_t index_dtype, float scale,
+                            const fg_matrix *Cin, const fg_matrix *dtable, void *workspace, int64_t workspace_bytes, void *hip_stream) {
+    if (fg_status st = check_embedding(tokens, vocab, dim, ids, index_dtype)) return st;
+    if (fg_status st = check_rows("dY", dY, tokens, dim, true)) return st;
+    if (fg_status st = check_rows("dtable", dtable, vocab, dim)) return st;
+    if (dtable->dtype != dY->dtype && dtable->dtype != FG_F32) return fail(FG_ERR_UNSUPPORTED, "dtable must be FG_F32 or of the type of dY");
+    if (Cin) {
+        if (fg_status st = check_rows("Cin", Cin, vocab, dim)) return st;
+        if (Cin->dtype != dtable->dtype) return fail(FG_ERR_UNSUPPORTED, "Cin and dtable must have the same element type");
+        if (Cin->re == dtable->re && Cin->ld != dtable->ld) return fail(FG_ERR_LAYOUT, "Cin in the place of dtable must have its leading dimension");
+    }
+    if (vocab == 0 || dim == 0) return FG_OK;
+    const EmbeddingSpace at(tokens, vocab, dim);
+    if (fg_status st = check_workspace(workspace, workspace_bytes, at.bytes)) return st;
+    char *w = (char *)workspace;
+    uint32_t *keys = (uint32_t *)(w + at.keys), *order = (uint32_t *)(w + at.order), *present = (uint32_t *)(w + at.present);
+    uint32_t *all_keys = (uint32_t *)(w + at.all_keys), *all_order = (uint32_t *)(w + at.all_order);
+    hipStream_t stream = (hipStream_t)hip_stream;
+    int passes = 1;
+    while (((vocab + 1) >> (passes * kDigit)) != 0) ++passes;             // the largest key is vocab + 1
+    const bool wide = index_dtype == FG_I64;
+    const int items = run_items(tokens), run = items * kRunThreads;
+    const unsigned runs = (unsigned)std::max<int64_t>(1, (tokens + run - 1) / run);
+    if (items == 4) hipLaunchKernelGGL((embedding_sort<4>), dim3(runs), dim3(kRunThreads), 0, stream, ids, wide, (int)tokens, (int)vocab, passes, keys, order, present);
+    else hipLaunchKernelGGL((embedding_sort<8>), dim3(runs), dim3(kRunThreads), 0, stream, ids, wide, (int)tokens, (int)vocab, passes, keys, order, present);
+    if (tokens > 0)
+        hipLaunchKernelGGL(embedding_merge, dim3((unsigned)((tokens + 255) / 256)), dim3(256), 0, stream, keys, order, (int)tokens, run, all_keys, all_order, (int)vocab, present);
+    if (fg_status st = check_launch("embedding_sort")) return st;
+    const bool in_place = Cin && Cin->re == dtable->re;
+    auto launch = [&](auto t, auto d) {
+        using T = decltype(t);
+        using D = decltype(d);
+        const int64_t pieces = (dim + Piece<T>::N - 1) / Piece<T>::N, tiles = (tokens + kTile - 1) / kTile, chunks = (pieces + 63) / 64;
+        const int shift = lanes_shift((int)((pieces + 3) / 4));
+        const int64_t fills = in_place ? 0 : (vocab + (64 >> shift) - 1) / (64 >> shift) * ((pieces + (4 << shift) - 1) / (4 << shift));
+        const int64_t sum_groups = (tiles * chunks + 3) / 4;
+        EmbeddingGradArgs a = {dY->re, Cin ? Cin->re : nullptr, dtable->re, all_keys, all_order, present, (float *)(w + at.open), dY->ld, Cin ? Cin->ld : 0,
+                               dtable->ld, (int)tokens, (int)vocab, (int)dim, (int)tiles, (int)chunks, (int)sum_groups, shift, scale};
+        const int64_t groups = sum_groups + (fills + 3) / 4;
+        if (groups > 0) hipLaunchKernelGGL((embedding_grad<T, D>), dim3((unsigned)groups), dim3(256), 0, stream, a);
+        if (tiles > 1) hipLaunchKernelGGL((embedding_join<T, D>), dim3((unsigned)sum_groups), dim3(256), 0, stream, a);
+    };
+    with_element(dY->dtype, [&](auto t) {
+        if (dtable->dtype == FG_F32) launch(t, float{});
+        else launch(t, t);
+    });
+    return check_launch("embedding_grad");
+}
+
+}  // extern "C"

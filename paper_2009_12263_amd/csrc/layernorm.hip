@@ -355,14 +355,13 @@ fg_status fg_layernorm_grad(int64_t rows, int64_t cols, const fg_matrix *dY, con
     if (fg_status st = check_rows("dY", dY, rows, cols, true)) return st;
     if (dY->dtype != X->dtype) return fail(FG_ERR_UNSUPPORTED, "X and dY must have the same element type");
     const unsigned es = element_bytes(param_dtype);
-    if (!aligned_to(dgamma, es) || !aligned_to(dbeta, es) || !aligned_to(mean, 4) || !aligned_to(rstd, 4) || !aligned_to(workspace, 4))
-        return fail(FG_ERR_ALIGN, "mean, rstd, dgamma, dbeta and the workspace must be aligned to an element");
+    if (!aligned_to(dgamma, es) || !aligned_to(dbeta, es) || !aligned_to(mean, 4) || !aligned_to(rstd, 4))
+        return fail(FG_ERR_ALIGN, "mean, rstd, dgamma and dbeta must be aligned to an element");
     if (cols == 0) return FG_OK;
     const bool sums = dgamma || dbeta;
     if (rows > 0 && (!mean || !rstd)) return fail(FG_ERR_NULL, "mean and rstd of the forward pass are NULL");
     const int64_t need = sums ? fg_layernorm_grad_workspace(rows, cols, X->dtype) : 0;
-    if (need > 0 && !workspace) return fail(FG_ERR_NULL, "the workspace is NULL");
-    if (workspace_bytes < need) return fail(FG_ERR_SHAPE, "the workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)need);
+    if (fg_status st = check_workspace(workspace, workspace_bytes, need)) return st;
     LayerNormArgs a = {X->re, dY->re, dX->re, gamma, nullptr, const_cast<float *>(mean), const_cast<float *>(rstd), (float *)workspace,
                        X->ld, dY->ld, dX->ld, rows, (int32_t)cols, 0.f, (float)cols};
     hipStream_t stream = (hipStream_t)hip_stream;

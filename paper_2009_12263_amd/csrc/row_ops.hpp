@@ -11,20 +11,19 @@ namespace fg {
 typedef _Float16 f16_t;
 typedef __bf16 bf16_t;
 
-// Sixteen bytes of T.  The type is aligned to an element only: a row of odd length begins anywhere, and the memory system takes
-// an access of 16 bytes at any element.
-template <class T> struct Piece {
-    static constexpr int N = 16 / sizeof(T);
-    typedef T vec __attribute__((ext_vector_type(N)));
+// N elements of T, sixteen bytes unless it is said otherwise.  The type is aligned to an element only: a row of odd length begins
+// anywhere, and the memory system takes an access of 16 bytes at any element.
+template <class T, int N_ = 16 / (int)sizeof(T)> struct Piece {
+    static constexpr int N = N_;
+    typedef T vec __attribute__((ext_vector_type(N_)));
     typedef vec unaligned __attribute__((aligned(sizeof(T))));
 };
 
-// Piece p of a row of n elements as FP32; past the end: `fill`.
-template <class T>
-__device__ __forceinline__ void load_piece(const T *row, int p, int n, float (&out)[Piece<T>::N], float fill = 0.f) {
-    constexpr int N = Piece<T>::N;
+// Piece p (of N elements) of a row of n elements as FP32; past the end: `fill`.
+template <class T, int N>
+__device__ __forceinline__ void load_piece(const T *row, int p, int n, float (&out)[N], float fill = 0.f) {
     if ((p + 1) * N <= n) {
-        const typename Piece<T>::vec v = *(const typename Piece<T>::unaligned *)(row + p * N);
+        const typename Piece<T, N>::vec v = *(const typename Piece<T, N>::unaligned *)(row + p * N);
 #pragma unroll
         for (int e = 0; e < N; ++e) out[e] = (float)v[e];
     } else {
@@ -33,14 +32,13 @@ __device__ __forceinline__ void load_piece(const T *row, int p, int n, float (&o
     }
 }
 // Rounded to nearest even once.
-template <class T>
-__device__ __forceinline__ void store_piece(T *row, int p, int n, const float (&in)[Piece<T>::N]) {
-    constexpr int N = Piece<T>::N;
+template <class T, int N>
+__device__ __forceinline__ void store_piece(T *row, int p, int n, const float (&in)[N]) {
     if ((p + 1) * N <= n) {
-        typename Piece<T>::vec v;
+        typename Piece<T, N>::vec v;
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = (T)in[e];
-        *(typename Piece<T>::unaligned *)(row + p * N) = v;
+        *(typename Piece<T, N>::unaligned *)(row + p * N) = v;
     } else {
 #pragma unroll
         for (int e = 0; e < N; ++e)
@@ -85,6 +83,12 @@ __device__ __forceinline__ float group_sum(float v, float *slot) {
     return v;
 }
 
+// Row index `at` of a list of ids; -1 where it names none of the n rows.
+__device__ __forceinline__ int load_index(const void *ids, bool wide, int64_t at, int n) {
+    const int64_t id = wide ? ((const int64_t *)ids)[at] : (int64_t)((const int32_t *)ids)[at];
+    return id >= 0 && id < n ? (int)id : -1;
+}
+
 // ---- host ---------------------------------------------------------------------------------------
 inline int element_bytes(int dtype) { return dtype == FG_F32 ? 4 : dtype == FG_F16 || dtype == FG_BF16 ? 2 : 0; }
 
@@ -99,6 +103,19 @@ inline fg_status check_rows(const char *name, const fg_matrix *m, int64_t rows, 
         if (!aligned_to(m->re, element_bytes(m->dtype))) return fail(FG_ERR_ALIGN, "%s: element pointers must be aligned to an element", name);
         if (m->ld < cols && !(broadcast && m->ld == 0)) return fail(FG_ERR_SHAPE, "%s: ld=%lld is smaller than %lld", name, (long long)m->ld, (long long)cols);
     }
+    return FG_OK;
+}
+// Token ids and targets: FG_I32 or FG_I64.
+inline fg_status check_indices(const char *name, const void *p, int dtype, int64_t n) {
+    if (dtype != FG_I32 && dtype != FG_I64) return fail(FG_ERR_LAYOUT, "%s must be FG_I32 or FG_I64", name);
+    if (n > 0 && !p) return fail(FG_ERR_NULL, "%s is NULL", name);
+    if (!aligned_to(p, dtype == FG_I64 ? 8 : 4)) return fail(FG_ERR_ALIGN, "%s must be aligned to an element", name);
+    return FG_OK;
+}
+inline fg_status check_workspace(const void *workspace, int64_t bytes, int64_t need) {
+    if (need > 0 && !workspace) return fail(FG_ERR_NULL, "the workspace is NULL");
+    if (!aligned_to(workspace, 16)) return fail(FG_ERR_ALIGN, "the workspace must be 16-byte aligned");
+    if (bytes < need) return fail(FG_ERR_SHAPE, "the workspace has %lld bytes, %lld are needed", (long long)bytes, (long long)need);
     return FG_OK;
 }
 inline fg_status check_launch(const char *what) {

@@ -24,6 +24,16 @@ def layernorm_grad(rows=4, cols=64, dY=None, X=None, gamma=PTR, pt=fg.FG_F32, me
     return fg.load_library().fg_layernorm_grad(rows, cols, dY, X, gamma, pt, mean, rstd, dX, dgamma, dbeta, ws, size, None)
 
 
+def embedding(tokens=4, vocab=100, dim=64, table=None, ids=PTR, kind=fg.FG_I64, Y=None):
+    table, Y = (row() if m is None else m for m in (table, Y))
+    return fg.load_library().fg_embedding(tokens, vocab, dim, table, ids, kind, 1.0, Y, None)
+
+
+def embedding_grad(tokens=4, vocab=100, dim=64, dY=None, ids=PTR, kind=fg.FG_I64, Cin=None, dtable=None, ws=PTR, size=1 << 30):
+    dY, dtable = (row() if m is None else m for m in (dY, dtable))
+    return fg.load_library().fg_embedding_grad(tokens, vocab, dim, dY, ids, kind, 1.0, Cin, dtable, ws, size, None)
+
+
 NULL = C.POINTER(fg.fg_matrix)()
 
 
@@ -52,6 +62,20 @@ NULL = C.POINTER(fg.fg_matrix)()
     (layernorm_grad, dict(ws=None), fg.FG_ERR_NULL, "workspace"),
     (layernorm_grad, dict(size=100), fg.FG_ERR_SHAPE, "workspace"),
     (layernorm_grad, dict(dgamma=PTR + 1), fg.FG_ERR_ALIGN, "dgamma"),
+    (layernorm_grad, dict(ws=PTR + 4), fg.FG_ERR_ALIGN, "workspace"),
+    (embedding, dict(tokens=-1), fg.FG_ERR_SHAPE, "negative"),
+    (embedding, dict(vocab=2 << 30), fg.FG_ERR_UNSUPPORTED, "2^30"),
+    (embedding, dict(ids=None), fg.FG_ERR_NULL, "ids"),
+    (embedding, dict(ids=PTR + 4), fg.FG_ERR_ALIGN, "ids"),
+    (embedding, dict(kind=fg.FG_F32), fg.FG_ERR_LAYOUT, "FG_I32"),
+    (embedding, dict(table=row(ld=63)), fg.FG_ERR_SHAPE, "table"),
+    (embedding, dict(Y=row(dtype=fg.FG_F32)), fg.FG_ERR_UNSUPPORTED, "same element type"),
+    (embedding_grad, dict(dY=NULL), fg.FG_ERR_NULL, "dY"),
+    (embedding_grad, dict(dtable=row(dtype=fg.FG_F16)), fg.FG_ERR_UNSUPPORTED, "dtable"),
+    (embedding_grad, dict(Cin=row(dtype=fg.FG_F32, re=2 * PTR)), fg.FG_ERR_UNSUPPORTED, "Cin"),
+    (embedding_grad, dict(Cin=row(ld=128)), fg.FG_ERR_LAYOUT, "Cin"),
+    (embedding_grad, dict(ws=None), fg.FG_ERR_NULL, "workspace"),
+    (embedding_grad, dict(size=64), fg.FG_ERR_SHAPE, "workspace"),
 ])
 def test_refusals(call, args, status, word):
     assert call(**args) == status
@@ -60,6 +84,8 @@ def test_refusals(call, args, status, word):
 
 def test_sizes_of_zero_launch_nothing():
     assert layernorm(rows=0) == fg.FG_OK and layernorm(cols=0) == fg.FG_OK and layernorm_grad(cols=0) == fg.FG_OK
+    assert embedding(tokens=0, ids=None) == fg.FG_OK and embedding(dim=0) == fg.FG_OK
+    assert embedding_grad(vocab=0) == fg.FG_OK and embedding_grad(dim=0) == fg.FG_OK
 
 
 def test_workspace_queries():
