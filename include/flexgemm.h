@@ -323,6 +323,35 @@ fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg
                             const fg_matrix *Cin, const fg_matrix *dtable, void *workspace, int64_t workspace_bytes, void *hip_stream);
 int64_t fg_embedding_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim);
 
+/*
+ * Softmax cross entropy of a linear layer over a vocabulary, without the logits in memory: with z[t][v] = scale * sum over k of X[t][k] * W[v][k],
+ *   lse[t] = log of the sum over v of exp(z[t][v]),   loss[t] = lse[t] - z[t][targets[t]].
+ * A token whose target is not in [0, vocab) is left out: its loss is 0, and it has no part in a gradient (its lse is
+ * that of its logits all the same).  No logits are kept: the vocabulary is walked in pieces, of which the statistics remain.
+ *   X : tokens x dim, W : vocab x dim, both FG_F16 or both FG_BF16 (multiplied exactly, summed in FP32); targets : `tokens` indices of type
+ *   index_dtype (FG_I32, FG_I64); loss, lse : `tokens` FP32 values each; vocab >= 1.
+ * Infinite logits give a NaN.  16-byte aligned pointers and leading dimensions and a dim of multiples of 8 are served by kernels that form the statistics
+ * of a tile of logits in its registers, with a bounded leading dimension as in fg_gemm; anything else by general ones, which pass pieces of the logits
+ * through the workspace.  Splits of K use the workspace of fg_gemm (fg_init before a graph capture).
+ */
+fg_status fg_linear_xent(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *X, const fg_matrix *W, const void *targets, int32_t index_dtype,
+                         float scale, float *loss, float *lse, void *workspace, int64_t workspace_bytes, void *hip_stream);
+int64_t fg_linear_xent_workspace(int64_t tokens, int64_t vocab, int64_t dim);
+
+/*
+ * Its gradient, from the lse of the forward call: with dz[t][v] = (exp(z[t][v] - lse[t]) - (v == targets[t])) * dloss[t] (0 for tokens that
+ * are left out),   dX[t] = scale * sum over v of dz[t][v] * W[v],   dW[v] = scale * sum over t of dz[t][v] * X[t].
+ * The logits are formed again, a piece of the vocabulary at a time; dz is rounded to the type of X (binary16: relative to the
+ * largest dloss, so that it neither overflows nor vanishes where dX and dW do not) and multiplied by W and X into FP32.
+ *   dloss  : FP32, one value per token, or with dloss_inc 0 a single one for all (1 otherwise).
+ *   dX, dW : of the type of X, the shapes of X and W.
+ * A larger workspace than the query's is used for larger pieces.
+ */
+fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *X, const fg_matrix *W, const void *targets, int32_t index_dtype,
+                              float scale, const float *lse, const float *dloss, int64_t dloss_inc, const fg_matrix *dX, const fg_matrix *dW,
+                              void *workspace, int64_t workspace_bytes, void *hip_stream);
+int64_t fg_linear_xent_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim);
+
 /* Message for the most recent failing call on this thread ("" if none).  The pointer refers to
  * thread-local static storage: valid until the next library call on the same thread. */
 const char *fg_last_error(void);

@@ -29,7 +29,8 @@ FG_ACT_NONE, FG_ACT_RELU = 0, 1
 
 EXPORTS = ("fg_init", "fg_gemm", "fg_gemm_ex", "fg_gemm_noalloc", "fg_gemm_dual", "fg_contract", "fg_contract_plan", "fg_last_error", "fg_version",
            "fg_reload_tuning", "fg_gemm_plan", "fg_probe_mfma", "fg_probe_mfma_k32", "fg_probe_kloop_mix",
-           "fg_layernorm", "fg_layernorm_grad", "fg_layernorm_grad_workspace", "fg_embedding", "fg_embedding_grad", "fg_embedding_grad_workspace")
+           "fg_layernorm", "fg_layernorm_grad", "fg_layernorm_grad_workspace", "fg_embedding", "fg_embedding_grad", "fg_embedding_grad_workspace",
+           "fg_linear_xent", "fg_linear_xent_workspace", "fg_linear_xent_grad", "fg_linear_xent_grad_workspace")
 FG_PLAN_REAL, FG_PLAN_COMPLEX, FG_PLAN_DUAL, FG_PLAN_REAL_BF16, FG_PLAN_COMPLEX_INTERLEAVED, FG_PLAN_REAL_F16_CD = 0, 1, 2, 3, 4, 5
 FG_PLAN_REAL_AB_ADD = 6
 
@@ -112,6 +113,12 @@ def load_library() -> C.CDLL:
         lib.fg_embedding_grad.argtypes = [i64, i64, i64, mp, vp, i32, f32, mp, mp, vp, i64, vp]
         lib.fg_embedding_grad_workspace.restype = i64
         lib.fg_embedding_grad_workspace.argtypes = [i64, i64, i64]
+        lib.fg_linear_xent.restype = C.c_int
+        lib.fg_linear_xent.argtypes = [i64, i64, i64, mp, mp, vp, i32, f32, vp, vp, vp, i64, vp]
+        lib.fg_linear_xent_grad.restype = C.c_int
+        lib.fg_linear_xent_grad.argtypes = [i64, i64, i64, mp, mp, vp, i32, f32, vp, vp, i64, mp, mp, vp, i64, vp]
+        lib.fg_linear_xent_workspace.restype = lib.fg_linear_xent_grad_workspace.restype = i64
+        lib.fg_linear_xent_workspace.argtypes = lib.fg_linear_xent_grad_workspace.argtypes = [i64, i64, i64]
         _load_fastcall(lib)
         _lib = lib
     return _lib
@@ -465,4 +472,49 @@ def fg_embedding_grad(dY: torch.Tensor, ids: torch.Tensor, scale: float, Cin: Op
     at, kind = _indices(ids, tokens, "ids", dev)
     ws, ws_bytes, _keep = _workspace(workspace, lib.fg_embedding_grad_workspace(tokens, vocab, dim), stream, dev)
     st = lib.fg_embedding_grad(tokens, vocab, dim, C.byref(dy), at, kind, scale, _ref(c), C.byref(d), ws, ws_bytes, _stream_handle(stream))
+    return _check(st, raise_on_error)
+
+
+def fg_linear_xent_workspace(tokens: int, vocab: int, dim: int) -> int:
+    return int(load_library().fg_linear_xent_workspace(tokens, vocab, dim))
+
+
+def fg_linear_xent(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, scale: float, loss: torch.Tensor, lse: torch.Tensor,
+                   workspace: Optional[torch.Tensor] = None, stream=None, raise_on_error: bool = True) -> int:
+    """loss[t] = lse[t] - z[t][targets[t]] with z = scale * X W^T, lse its log-sum-exp over the words; 0 where the target names no word."""
+    lib = _lib or load_library()
+    dev = _current_device()
+    x, w = _rows(X, "X", None, dev), _rows(W, "W", None, dev)
+    (tokens, dim), vocab = X.shape, W.shape[0]
+    if W.shape[1] != dim:
+        raise ValueError("X and W: rows of %d and %d values" % (dim, W.shape[1]))
+    at, kind = _indices(targets, tokens, "targets", dev)
+    ws, ws_bytes, _keep = _workspace(workspace, lib.fg_linear_xent_workspace(tokens, vocab, dim), stream, dev)
+    st = lib.fg_linear_xent(tokens, vocab, dim, C.byref(x), C.byref(w), at, kind, scale, _vector(loss, tokens, "loss", torch.float32, dev),
+                            _vector(lse, tokens, "lse", torch.float32, dev), ws, ws_bytes, _stream_handle(stream))
+    return _check(st, raise_on_error)
+
+
+def fg_linear_xent_grad_workspace(tokens: int, vocab: int, dim: int) -> int:
+    return int(load_library().fg_linear_xent_grad_workspace(tokens, vocab, dim))
+
+
+def fg_linear_xent_grad(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, scale: float, lse: torch.Tensor, dloss: torch.Tensor,
+                        dX: torch.Tensor, dW: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None, raise_on_error: bool = True) -> int:
+    """Gradients of the losses of fg_linear_xent, weighted with dloss (one value per token, which may be a single one expanded)."""
+    lib = _lib or load_library()
+    dev = _current_device()
+    x, w = _rows(X, "X", None, dev), _rows(W, "W", None, dev)
+    (tokens, dim), vocab = X.shape, W.shape[0]
+    if W.shape[1] != dim:
+        raise ValueError("X and W: rows of %d and %d values" % (dim, W.shape[1]))
+    dx, dw = _rows(dX, "dX", X.shape, dev), _rows(dW, "dW", W.shape, dev)
+    at, kind = _indices(targets, tokens, "targets", dev)
+    inc = 1
+    if dloss.dim() == 1 and dloss.shape[0] == tokens and tokens > 1 and dloss.stride(0) == 0:
+        dloss, inc = dloss[:1], 0
+    g = _vector(dloss, tokens if inc else 1, "dloss", torch.float32, dev)
+    ws, ws_bytes, _keep = _workspace(workspace, lib.fg_linear_xent_grad_workspace(tokens, vocab, dim), stream, dev)
+    st = lib.fg_linear_xent_grad(tokens, vocab, dim, C.byref(x), C.byref(w), at, kind, scale, _vector(lse, tokens, "lse", torch.float32, dev), g, inc,
+                                 C.byref(dx), C.byref(dw), ws, ws_bytes, _stream_handle(stream))
     return _check(st, raise_on_error)

@@ -1324,9 +1324,10 @@ fg_status fg_init(void) {
 // static_only: the allocation-free entry point.  Same plan as the ordinary call; partial products
 // of a K split go to the static scratch array (FG_ERR_UNSUPPORTED if they do not fit), and nothing
 // on this path allocates, frees or creates anything.
+// k_rows (0: K): an operand that is not K-contiguous stores its first k_rows k's only, and the others count as zero.
 static fg_status gemm_impl(int64_t M, int64_t N, int64_t K, float alpha, const fg_matrix *A, const fg_matrix *B,
                            float beta, const fg_matrix *C, const fg_matrix *D, const fg_epilogue *ep, bool dual,
-                           const fg_load_transforms *lt, void *hip_stream, bool static_only = false) {
+                           const fg_load_transforms *lt, void *hip_stream, bool static_only = false, int64_t k_rows = 0) {
     Problem q;
     if (fg_status st = normalise(M, N, K, alpha, A, B, beta, C, D, ep, dual, lt, q)) return st;
     if (q.M == 0 || q.N == 0) return FG_OK;
@@ -1346,8 +1347,8 @@ static fg_status gemm_impl(int64_t M, int64_t N, int64_t K, float alpha, const f
     p.b_rs = q.b_kc ? q.ldb : 1; p.b_ks = q.b_kc ? 1 : q.ldb;
     // stored span of each operand, rounded up to whole 16-byte chunks (see TileLoader::begin)
     auto span8 = [](bool kc, int64_t rows, int64_t k, int64_t ld) { int64_t s = kc ? (rows - 1) * ld + k : (k - 1) * ld + rows; return (s + 7) / 8 * 8; };
-    p.a_span = q.K > 0 ? span8(q.a_kc, q.M, q.K, q.lda) : 0;
-    p.b_span = q.K > 0 ? span8(q.b_kc, q.N, q.K, q.ldb) : 0;
+    p.a_span = q.K > 0 ? span8(q.a_kc, q.M, q.a_kc || !k_rows ? q.K : k_rows, q.lda) : 0;
+    p.b_span = q.K > 0 ? span8(q.b_kc, q.N, q.b_kc || !k_rows ? q.K : k_rows, q.ldb) : 0;
     // A and B may be of any size; what must fit 32 bits is the byte offset a lane forms inside one
     // block panel at one K step (up to 256 rows by 64 k) and the advance from one K step to the next.
     const int64_t ab_elem_bytes = q.ilv ? 4 : 2;
@@ -1411,6 +1412,15 @@ static fg_status gemm_impl(int64_t M, int64_t N, int64_t K, float alpha, const f
     if (e != hipSuccess) return fail(FG_ERR_LAUNCH, "launch of the split-K reduction failed: %s", hipGetErrorString(e));
     return scratch.release(stream);
 }
+
+}  // extern "C"
+
+fg_status fg::gemm_stored(int64_t M, int64_t N, int64_t K, int64_t k_rows, float alpha, const fg_matrix *A, const fg_matrix *B, float beta,
+                          const fg_matrix *C, const fg_matrix *D, void *hip_stream) {
+    return gemm_impl(M, N, K, alpha, A, B, beta, C, D, nullptr, false, nullptr, hip_stream, false, k_rows);
+}
+
+extern "C" {
 
 fg_status fg_gemm(int64_t M, int64_t N, int64_t K, float alpha, const fg_matrix *A, const fg_matrix *B,
                   float beta, const fg_matrix *C, const fg_matrix *D, const fg_epilogue *ep, void *hip_stream) {

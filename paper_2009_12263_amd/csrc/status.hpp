@@ -9,6 +9,11 @@ namespace fg {
 // Notes the message that fg_last_error() returns and gives the status back.
 fg_status fail(fg_status st, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 
+// fg_gemm where an operand that is not K-contiguous stores its first k_rows k's only (0: all of them); the others count as zero, and K can be
+// rounded up to what the tiled kernels take.  For operands that meet their alignment (aligned16 pointers, leading dimensions of 8).
+fg_status gemm_stored(int64_t M, int64_t N, int64_t K, int64_t k_rows, float alpha, const fg_matrix *A, const fg_matrix *B, float beta,
+                      const fg_matrix *C, const fg_matrix *D, void *hip_stream);
+
 inline bool aligned_to(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 }  // namespace fg

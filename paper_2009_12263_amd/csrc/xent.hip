@@ -1,0 +1,296 @@
+// Softmax cross entropy of a linear layer over a vocabulary, and its gradient.
+//
+//   z[t][v] = scale x[t].w[v],   lse[t] = log sum over v of exp z[t][v],   loss[t] = lse[t] - z[t][target[t]]
+//   dz[t][v] = (exp(z[t][v] - lse[t]) - [v = target[t]]) dloss[t],   dx[t] = scale dz[t].w,   dw[v] = scale sum over t of dz[t][v] x[t]
+//
+// The logits are as large as tokens x vocabulary and nobody wants them.  The vocabulary is walked in pieces: of a piece's logits, each token
+// keeps the maximum and the sum of exponentials relative to it, and the logit of its target; the pairs (m, s) of all pieces are
+// joined as sum s exp(m - max m).  The gradient forms a piece's logits again and turns them into dz, in 16 bits, which two products
+// read: dw's rows of the piece, and the piece's part of dx, added up in FP32.
+#include "row_ops.hpp"
+
+#include <algorithm>
+
+namespace fg {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+struct Stat { float m, s; };                // maximum, and sum of exp(z - m)
+
+// exp(z - m) of a maximum that is no number (no logit, or none above minus infinity): relative to 0
+__device__ __forceinline__ float base_of(float m) { return m == -__builtin_inff() ? 0.f : m; }
+
+template <int W>
+__device__ __forceinline__ float group_max(float v, float *slot) {
+    v = wave_max(v);
+    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = slot[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) v = __builtin_fmaxf(v, slot[w]);
+    return v;
+}
+
+// ---- pieces of the logits in memory ---------------------------------------------------------------------
+// Statistics of token blockIdx.x over the n logits of a piece that begins at word v0.
+__global__ __launch_bounds__(256) void xent_row_stats(const float *z, int64_t ld, int n, int v0, const void *targets, bool wide, int vocab, Stat *stats, float *z_target) {
+    __shared__ float slots[2][4];
+    const int64_t t = blockIdx.x;
+    const float *row = z + t * ld;
+    const int pieces = (n + 3) / 4;
+    float m = -__builtin_inff(), s = 0.f, v[4];
+    for (int p = threadIdx.x; p < pieces; p += 256) {
+        load_piece(row, p, n, v, -__builtin_inff());
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = __builtin_fmaxf(m, v[i]);
+    }
+    m = group_max<4>(m, slots[0]);
+    const float base = base_of(m);
+    for (int p = threadIdx.x; p < pieces; p += 256) {
+        load_piece(row, p, n, v, -__builtin_inff());
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s += __builtin_amdgcn_exp2f((v[i] - base) * kLog2e);
+    }
+    s = group_sum<4>(s, slots[1]);
+    if (threadIdx.x == 0) {
+        stats[t] = {m, s};
+        const int target = load_index(targets, wide, t, vocab) - v0;
+        if (target >= 0 && target < n) z_target[t] = row[target];
+    }
+}
+
+// dz of token blockIdx.x over a piece, ld columns of it: those from n on are zero.
+template <class T>
+__global__ __launch_bounds__(256) void xent_row_grad(const float *z, int64_t ldz, int n, int v0, const void *targets, bool wide, int vocab, const float *lse,
+                                                     const float *dloss, int64_t dloss_inc, const float *factor, T *dz, int64_t ld) {
+    const int64_t t = blockIdx.x;
+    const float *row = z + t * ldz;
+    const int target = load_index(targets, wide, t, vocab);
+    const float g = target < 0 ? 0.f : dloss[t * dloss_inc] * factor[0], base = lse[t];
+    for (int p = threadIdx.x; p < ld / 8; p += 256) {
+        float v[8];
+        load_piece(row, p, n, v, -__builtin_inff());
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int col = p * 8 + i;
+            const float d = __builtin_amdgcn_exp2f((v[i] - base) * kLog2e) - (v0 + col == target ? 1.f : 0.f);
+            v[i] = target < 0 || col >= n ? 0.f : d * g;
+        }
+        store_piece(dz + t * ld, p, (int)ld, v);
+    }
+}
+
+// ---- joining ----------------------------------------------------------------------------------------------
+// A workgroup joins the statistics of 1024 / G tokens, G threads a token, in a fixed order.  stats: `parts` runs of `stride` tokens.
+template <int G>
+__global__ __launch_bounds__(1024) void xent_join(const Stat *stats, int parts, int64_t stride, int64_t tokens, const void *targets, bool wide, int vocab,
+                                                  const float *z_target, float *loss, float *lse) {
+    constexpr int TOKENS = 1024 / G;
+    __shared__ Stat part[G][TOKENS + 1];
+    const int at = threadIdx.x % TOKENS, g = threadIdx.x / TOKENS;
+    const int64_t t = (int64_t)blockIdx.x * TOKENS + at;
+    float m = -__builtin_inff(), s = 0.f;
+    auto add = [&](Stat o) {
+        const float top = __builtin_fmaxf(m, o.m), base = base_of(top);
+        // (a part without anything has m = -inf and s = 0: exp of minus infinity, or of 0, times 0)
+        s = s * __builtin_amdgcn_exp2f((m - base) * kLog2e) + o.s * __builtin_amdgcn_exp2f((o.m - base) * kLog2e);
+        m = top;
+    };
+    if (t < tokens) {
+#pragma unroll 4
+        for (int p = g; p < parts; p += G) add(stats[p * stride + t]);
+    }
+    part[g][at] = {m, s};
+    __syncthreads();
+    if (g != 0 || t >= tokens) return;
+    for (int o = 1; o < G; ++o) add(part[o][at]);
+    const float total = base_of(m) + __builtin_logf(s);
+    lse[t] = total;
+    loss[t] = load_index(targets, wide, t, vocab) < 0 ? 0.f : total - z_target[t];
+}
+
+// ---- scaling of dz ------------------------------------------------------------------------------------------
+// dz is kept as c dz, c = 2^k / max |dloss|.  With one dloss for all tokens (the mean of the losses) what is rounded is then exp(z - lse) - 1 or exp(z -
+// lse) itself: relative to dloss, the same rounding of nearly -1 in every token would shift all of dx and dw one way (8192 tokens,
+// bfloat16: error against 64 bits 2.6e-3 so, half of which is the rounding of the results).  Binary16: k = 14, so that |c dz|
+// is at most 2^14 and what is 2^-38 of the largest is still a number.  factor[0] = c, factor[1] = scale / c.
+__global__ __launch_bounds__(1024) void xent_factor(const float *dloss, int64_t dloss_inc, const void *targets, bool wide, int vocab, int64_t tokens, bool half,
+                                                    float scale, float *factor) {
+    __shared__ float slots[16];
+    float top = 0.f;
+    for (int64_t t = threadIdx.x; t < tokens; t += 1024)
+        if (load_index(targets, wide, t, vocab) >= 0) top = __builtin_fmaxf(top, __builtin_fabsf(dloss[t * dloss_inc]));
+    top = group_max<16>(top, slots);
+    if (threadIdx.x == 0) {
+        const bool usable = top > 0.f && top < __builtin_inff();
+        const float range = half ? 16384.f : 1.f, unit = usable ? __builtin_fmaxf(top, 1e-30f) : 1.f;
+        factor[0] = usable ? range / unit : 1.f;
+        factor[1] = usable ? scale * (unit / range) : scale;
+    }
+}
+
+// rows x cols FP32 values times *factor, rounded into `out`
+template <class T>
+__global__ __launch_bounds__(256) void xent_round(const float *in, int64_t ld, const float *factor, T *out, int64_t ldo, int64_t rows, int cols) {
+    const int pieces = (cols + 7) / 8;
+    const float f = *factor;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / pieces;
+        const int p = (int)(i - row * pieces);
+        float v[8];
+        load_piece(in + row * ld, p, cols, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= f;
+        store_piece(out + row * ldo, p, cols, v);
+    }
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------
+constexpr int64_t kPieceBytes = 256ll << 20;        // of logits (FP32) or dz
+
+int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// Words of a piece of which each costs `bytes` per token.
+int64_t piece_words(int64_t tokens, int64_t vocab, int64_t bytes) {
+    const int64_t words = std::max<int64_t>(2048, kPieceBytes / (bytes * std::max<int64_t>(tokens, 1)) / 256 * 256);
+    return std::min({words, up(vocab, 8), (int64_t)1 << 20});            // (a row of logits is a leading dimension of fg_gemm's D)
+}
+
+struct XentSpace {          // of the forward call
+    int64_t words, parts, z, stats, z_target, bytes;
+    XentSpace(int64_t tokens, int64_t vocab) {
+        words = piece_words(tokens, vocab, 4);
+        parts = (vocab + words - 1) / words;
+        z = 0;
+        stats = z + up(tokens * words * 4, 256);
+        z_target = stats + up(parts * tokens * (int64_t)sizeof(Stat), 256);
+        bytes = z_target + up(tokens * 4, 256);
+    }
+};
+struct XentGradSpace {      // of the gradient: a piece of logits, dz, dw, and the sums of dx
+    int64_t words, ld_dx, ld_dw, z, dz, dw, dx, factor, bytes;
+    XentGradSpace(int64_t tokens, int64_t vocab, int64_t dim) {
+        words = piece_words(tokens, vocab, 4);
+        ld_dx = ld_dw = up(dim, 4);
+        z = 0;
+        dz = z + up(tokens * words * 4, 256);
+        dw = dz + up(tokens * words * 2, 256);
+        dx = dw + up(words * ld_dw * 4, 256);
+        factor = dx + up(tokens * ld_dx * 4, 256);
+        bytes = factor + 256;
+    }
+};
+
+fg_status check_xent(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *X, const fg_matrix *W, const void *targets, int32_t index_dtype) {
+    if (tokens < 0 || vocab < 0 || dim < 0) return fail(FG_ERR_SHAPE, "negative size: %lld tokens, %lld words, %lld values", (long long)tokens, (long long)vocab, (long long)dim);
+    if (vocab == 0) return fail(FG_ERR_SHAPE, "the vocabulary is empty");
+    if (tokens > (1 << 30) || vocab > (1 << 30) || dim > (1 << 30)) return fail(FG_ERR_UNSUPPORTED, "sizes above 2^30 are not supported");
+    if (fg_status st = check_rows("X", X, tokens, dim)) return st;
+    if (fg_status st = check_rows("W", W, vocab, dim)) return st;
+    if (X->dtype == FG_F32 || X->dtype != W->dtype) return fail(FG_ERR_UNSUPPORTED, "X and W must both be FG_F16 or both FG_BF16");
+    return check_indices("targets", targets, index_dtype, tokens);
+}
+
+fg_matrix rows_of(const void *p, int32_t dtype, int64_t ld, int32_t layout = FG_ROW) { return {const_cast<void *>(p), nullptr, dtype, layout, ld}; }
+const void *row_at(const fg_matrix *m, int64_t row) { return (const char *)m->re + row * m->ld * element_bytes(m->dtype); }
+
+template <class F> void with_half(int dtype, F &&f) {
+    if (dtype == FG_F16) f(f16_t{});
+    else f(bf16_t{});
+}
+
+// logits of words v0 .. v0 + n - 1
+fg_status piece_logits(int64_t tokens, int64_t dim, const fg_matrix *X, const fg_matrix *W, float scale, int64_t v0, int64_t n, float *z, int64_t ldz, void *stream) {
+    const fg_matrix b = rows_of(row_at(W, v0), W->dtype, W->ld, FG_COL), d = rows_of(z, FG_F32, ldz);
+    return fg_gemm(tokens, n, dim, scale, X, &b, 0.f, nullptr, &d, nullptr, stream);
+}
+
+}  // namespace
+}  // namespace fg
+
+using namespace fg;
+
+extern "C" {
+
+int64_t fg_linear_xent_workspace(int64_t tokens, int64_t vocab, int64_t dim) {
+    if (tokens <= 0 || vocab <= 0 || dim < 0) return 0;
+    return XentSpace(tokens, vocab).bytes;
+}
+
+fg_status fg_linear_xent(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *X, const fg_matrix *W, const void *targets, int32_t index_dtype,
+                         float scale, float *loss, float *lse, void *workspace, int64_t workspace_bytes, void *hip_stream) {
+    if (fg_status st = check_xent(tokens, vocab, dim, X, W, targets, index_dtype)) return st;
+    if (tokens == 0) return FG_OK;
+    if (!loss || !lse) return fail(FG_ERR_NULL, "loss or lse is NULL");
+    if (!aligned_to(loss, 4) || !aligned_to(lse, 4)) return fail(FG_ERR_ALIGN, "loss and lse must be aligned to an element");
+    const XentSpace at(tokens, vocab);
+    if (fg_status st = check_workspace(workspace, workspace_bytes, at.bytes)) return st;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    char *w = (char *)workspace;
+    float *z = (float *)(w + at.z), *z_target = (float *)(w + at.z_target);
+    Stat *stats = (Stat *)(w + at.stats);
+    const bool wide = index_dtype == FG_I64;
+    for (int64_t part = 0; part < at.parts; ++part) {
+        const int64_t v0 = part * at.words, n = std::min(at.words, vocab - v0);
+        if (fg_status st = piece_logits(tokens, dim, X, W, scale, v0, n, z, at.words, stream)) return st;
+        hipLaunchKernelGGL(xent_row_stats, dim3((unsigned)tokens), dim3(256), 0, stream, z, at.words, (int)n, (int)v0, targets, wide, (int)vocab, stats + part * tokens, z_target);
+    }
+    hipLaunchKernelGGL((xent_join<16>), dim3((unsigned)((tokens + 63) / 64)), dim3(1024), 0, stream, stats, (int)at.parts, tokens, tokens, targets, wide, (int)vocab, z_target, loss, lse);
+    return check_launch("xent");
+}
+
+int64_t fg_linear_xent_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim) {
+    if (tokens < 0 || vocab <= 0 || dim <= 0) return 0;
+    return XentGradSpace(tokens, vocab, dim).bytes;
+}
+
+fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *X, const fg_matrix *W, const void *targets, int32_t index_dtype,
+                              float scale, const float *lse, const float *dloss, int64_t dloss_inc, const fg_matrix *dX, const fg_matrix *dW,
+                              void *workspace, int64_t workspace_bytes, void *hip_stream) {
+    if (fg_status st = check_xent(tokens, vocab, dim, X, W, targets, index_dtype)) return st;
+    if (fg_status st = check_rows("dX", dX, tokens, dim)) return st;
+    if (fg_status st = check_rows("dW", dW, vocab, dim)) return st;
+    if (dX->dtype != X->dtype || dW->dtype != X->dtype) return fail(FG_ERR_UNSUPPORTED, "dX and dW must have the element type of X");
+    if (dloss_inc != 0 && dloss_inc != 1) return fail(FG_ERR_SHAPE, "dloss_inc must be 0 or 1");
+    if (dim == 0) return FG_OK;
+    if (tokens > 0 && (!lse || !dloss)) return fail(FG_ERR_NULL, "lse or dloss is NULL");
+    if (!aligned_to(lse, 4) || !aligned_to(dloss, 4)) return fail(FG_ERR_ALIGN, "lse and dloss must be aligned to an element");
+    const XentGradSpace at(tokens, vocab, dim);
+    if (fg_status st = check_workspace(workspace, workspace_bytes, at.bytes)) return st;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    char *w = (char *)workspace;
+    float *z = (float *)(w + at.z), *dw = (float *)(w + at.dw), *dx = (float *)(w + at.dx), *factor = (float *)(w + at.factor);
+    void *dz = w + at.dz;
+    const bool wide = index_dtype == FG_I64;
+    hipLaunchKernelGGL(xent_factor, dim3(1), dim3(1024), 0, stream, dloss, dloss_inc, targets, wide, (int)vocab, tokens, X->dtype == FG_F16, scale, factor);
+    const fg_matrix sum_dx = rows_of(dx, FG_F32, at.ld_dx), part_dw = rows_of(dw, FG_F32, at.ld_dw);
+    auto round = [&](const float *in, int64_t ld, const fg_matrix *out, int64_t row0, int64_t rows) {
+        if (rows == 0) return;
+        const unsigned groups = (unsigned)std::min<int64_t>((rows * ((dim + 7) / 8) + 255) / 256, 8192);
+        with_half(X->dtype, [&](auto t) {
+            using T = decltype(t);
+            hipLaunchKernelGGL((xent_round<T>), dim3(groups), dim3(256), 0, stream, in, ld, factor + 1, (T *)row_at(out, row0), out->ld, rows, (int)dim);
+        });
+    };
+    for (int64_t v0 = 0; v0 < vocab; v0 += at.words) {
+        const int64_t n = std::min(at.words, vocab - v0);
+        if (tokens > 0) {
+            if (fg_status st = piece_logits(tokens, dim, X, W, scale, v0, n, z, at.words, stream)) return st;
+            with_half(X->dtype, [&](auto t) {
+                using T = decltype(t);
+                hipLaunchKernelGGL((xent_row_grad<T>), dim3((unsigned)tokens), dim3(256), 0, stream, z, at.words, (int)n, (int)v0, targets, wide, (int)vocab, lse,
+                                   dloss, dloss_inc, factor, (T *)dz, at.words);
+            });
+        }
+        const fg_matrix dz_t = rows_of(dz, X->dtype, at.words, FG_COL), dz_r = rows_of(dz, X->dtype, at.words), w_piece = rows_of(row_at(W, v0), W->dtype, W->ld);
+        if (fg_status st = fg_gemm(n, dim, tokens, 1.f, &dz_t, X, 0.f, nullptr, &part_dw, nullptr, stream)) return st;
+        round(dw, at.ld_dw, dW, v0, n);
+        if (tokens > 0)
+            if (fg_status st = fg_gemm(tokens, dim, n, 1.f, &dz_r, &w_piece, v0 == 0 ? 0.f : 1.f, &sum_dx, &sum_dx, nullptr, stream)) return st;
+    }
+    round(dx, at.ld_dx, dX, 0, tokens);
+    return check_launch("xent_grad");
+}
+
+}  // extern "C"

@@ -34,6 +34,16 @@ def embedding_grad(tokens=4, vocab=100, dim=64, dY=None, ids=PTR, kind=fg.FG_I64
     return fg.load_library().fg_embedding_grad(tokens, vocab, dim, dY, ids, kind, 1.0, Cin, dtable, ws, size, None)
 
 
+def xent(tokens=4, vocab=100, dim=64, X=None, W=None, targets=PTR, kind=fg.FG_I64, loss=PTR, lse=PTR, ws=PTR, size=1 << 40):
+    X, W = (row() if m is None else m for m in (X, W))
+    return fg.load_library().fg_linear_xent(tokens, vocab, dim, X, W, targets, kind, 1.0, loss, lse, ws, size, None)
+
+
+def xent_grad(tokens=4, vocab=100, dim=64, X=None, W=None, targets=PTR, kind=fg.FG_I64, lse=PTR, dloss=PTR, inc=1, dX=None, dW=None, ws=PTR, size=1 << 40):
+    X, W, dX, dW = (row() if m is None else m for m in (X, W, dX, dW))
+    return fg.load_library().fg_linear_xent_grad(tokens, vocab, dim, X, W, targets, kind, 1.0, lse, dloss, inc, dX, dW, ws, size, None)
+
+
 NULL = C.POINTER(fg.fg_matrix)()
 
 
@@ -76,6 +86,23 @@ NULL = C.POINTER(fg.fg_matrix)()
     (embedding_grad, dict(Cin=row(ld=128)), fg.FG_ERR_LAYOUT, "Cin"),
     (embedding_grad, dict(ws=None), fg.FG_ERR_NULL, "workspace"),
     (embedding_grad, dict(size=64), fg.FG_ERR_SHAPE, "workspace"),
+    (xent, dict(dim=-8), fg.FG_ERR_SHAPE, "negative"),
+    (xent, dict(vocab=0), fg.FG_ERR_SHAPE, "empty"),
+    (xent, dict(vocab=2 << 30), fg.FG_ERR_UNSUPPORTED, "2^30"),
+    (xent, dict(X=row(dtype=fg.FG_F32), W=row(dtype=fg.FG_F32)), fg.FG_ERR_UNSUPPORTED, "FG_F16"),
+    (xent, dict(X=row(dtype=fg.FG_F16)), fg.FG_ERR_UNSUPPORTED, "both"),
+    (xent, dict(W=row(layout=fg.FG_COL)), fg.FG_ERR_LAYOUT, "row-major"),
+    (xent, dict(targets=None), fg.FG_ERR_NULL, "targets"),
+    (xent, dict(loss=None), fg.FG_ERR_NULL, "loss"),
+    (xent, dict(lse=PTR + 2), fg.FG_ERR_ALIGN, "lse"),
+    (xent, dict(ws=None), fg.FG_ERR_NULL, "workspace"),
+    (xent, dict(size=16), fg.FG_ERR_SHAPE, "workspace"),
+    (xent_grad, dict(dX=row(dtype=fg.FG_F32)), fg.FG_ERR_UNSUPPORTED, "dX"),
+    (xent_grad, dict(dW=row(ld=8)), fg.FG_ERR_SHAPE, "dW"),
+    (xent_grad, dict(inc=2), fg.FG_ERR_SHAPE, "dloss_inc"),
+    (xent_grad, dict(lse=None), fg.FG_ERR_NULL, "lse"),
+    (xent_grad, dict(dloss=None), fg.FG_ERR_NULL, "dloss"),
+    (xent_grad, dict(size=16), fg.FG_ERR_SHAPE, "workspace"),
 ])
 def test_refusals(call, args, status, word):
     assert call(**args) == status
@@ -85,6 +112,7 @@ def test_refusals(call, args, status, word):
 def test_sizes_of_zero_launch_nothing():
     assert layernorm(rows=0) == fg.FG_OK and layernorm(cols=0) == fg.FG_OK and layernorm_grad(cols=0) == fg.FG_OK
     assert embedding(tokens=0, ids=None) == fg.FG_OK and embedding(dim=0) == fg.FG_OK
+    assert xent(tokens=0) == fg.FG_OK and xent_grad(dim=0) == fg.FG_OK
     assert embedding_grad(vocab=0) == fg.FG_OK and embedding_grad(dim=0) == fg.FG_OK
 
 
