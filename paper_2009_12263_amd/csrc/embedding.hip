@@ -26,7 +26,7 @@ constexpr int kDigit = 6;                   // bits that one pass of the sort ta
 template <class T>
 __global__ __launch_bounds__(256) void embedding(const T *table, int64_t ld, const void *ids, bool wide, float scale, T *y, int64_t ldy, int64_t tokens,
                                                  int vocab, int dim, int shift) {
-    constexpr int N = Piece<T>::N, AHEAD = 4;
+    constexpr int N = RowPiece<T>::N, AHEAD = 4;
     const int lane = threadIdx.x & 63, at = lane & ((1 << shift) - 1), rows = 64 >> shift, pieces = (dim + N - 1) / N;
     const int chunks = (pieces + (AHEAD << shift) - 1) / (AHEAD << shift);
     const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -177,7 +177,7 @@ __device__ __forceinline__ void embedding_finish(const EmbeddingGradArgs &a, uin
 
 template <class T, class D>
 __global__ __launch_bounds__(256) void embedding_grad(const EmbeddingGradArgs a) {
-    constexpr int N = Piece<T>::N;
+    constexpr int N = RowPiece<T>::N;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pieces = (a.dim + N - 1) / N;
     if ((int)blockIdx.x >= a.sum_groups) {
         // rows without tokens: zeros, or what is there
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(256) void embedding_grad(const EmbeddingGradArgs a)
 // Joins the sums of an id that goes out of a tile it began in: that tile's, then one of each tile that it comes into.
 template <class T, class D>
 __global__ __launch_bounds__(256) void embedding_join(const EmbeddingGradArgs a) {
-    constexpr int N = Piece<T>::N, AHEAD = 8;
+    constexpr int N = RowPiece<T>::N, AHEAD = 8;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pieces = (a.dim + N - 1) / N;
     const int item = blockIdx.x * 4 + wave, tile = item / a.chunks, p = item % a.chunks * 64 + lane;
     if (tile + 1 >= a.tiles) return;
@@ -320,7 +320,7 @@ fg_status fg_embedding(int64_t tokens, int64_t vocab, int64_t dim, const fg_matr
     if (tokens == 0 || dim == 0) return FG_OK;
     with_element(Y->dtype, [&](auto t) {
         using T = decltype(t);
-        const int pieces = (int)((dim + Piece<T>::N - 1) / Piece<T>::N), shift = lanes_shift((pieces + 3) / 4);
+        const int pieces = (int)((dim + RowPiece<T>::N - 1) / RowPiece<T>::N), shift = lanes_shift((pieces + 3) / 4);
         const int64_t waves = (tokens + (64 >> shift) - 1) / (64 >> shift) * ((pieces + (4 << shift) - 1) / (4 << shift));
         hipLaunchKernelGGL((embedding<T>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, (hipStream_t)hip_stream, (const T *)table->re, table->ld, ids,
                            index_dtype == FG_I64, scale, (T *)Y->re, Y->ld, tokens, (int)vocab, (int)dim, shift);
@@ -365,7 +365,7 @@ fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg
     auto launch = [&](auto t, auto d) {
         using T = decltype(t);
         using D = decltype(d);
-        const int64_t pieces = (dim + Piece<T>::N - 1) / Piece<T>::N, tiles = (tokens + kTile - 1) / kTile, chunks = (pieces + 63) / 64;
+        const int64_t pieces = (dim + RowPiece<T>::N - 1) / RowPiece<T>::N, tiles = (tokens + kTile - 1) / kTile, chunks = (pieces + 63) / 64;
         const int shift = lanes_shift((int)((pieces + 3) / 4));
         const int64_t fills = in_place ? 0 : (vocab + (64 >> shift) - 1) / (64 >> shift) * ((pieces + (4 << shift) - 1) / (4 << shift));
         const int64_t sum_groups = (tiles * chunks + 3) / 4;

@@ -17,6 +17,7 @@
 #include "general_kernel.hpp"
 #include "kernel_table.hpp"
 #include "status.hpp"
+#include "xent_kernel.hpp"
 
 namespace {
 thread_local char g_err[512] = "";
@@ -1308,6 +1309,12 @@ fg_status fg_init(void) {
         {fg::kernel_table_cplx(), fg::CTILE_COUNT * 4}, {fg::kernel_table_dual(), fg::CTILE_COUNT * 4},
         {fg::kernel_table_cplx_il(), fg::CTILE_COUNT * 4},
     };
+    for (int kind : {fg::XENT_STATS, fg::XENT_DZ, fg::XENT_ROUND})
+        for (bool bf16 : {false, true})
+            for (int i = 0; i < fg::XENT_TILES; ++i) {
+                int per_cu = 0;
+                if (fg_status st = prepare(fg::kernel_table_xent(kind, bf16)[i], dev, per_cu)) return st;
+            }
     for (auto &tb : tables)
         for (int i = 0; i < tb.n; ++i) {
             int per_cu = 0;
@@ -1414,6 +1421,14 @@ static fg_status gemm_impl(int64_t M, int64_t N, int64_t K, float alpha, const f
 }
 
 }  // extern "C"
+
+int fg::plan_tile(int64_t M, int64_t N, int64_t K) { return plan_product(M, N, K, false, 2, 0, K <= 512 ? kPricesShort : kPrices).tile; }
+fg_status fg::launch_product(const KernelEntry &k, GemmParams &p, hipStream_t stream) {
+    p.tile_begin = 0;
+    p.tile_count = p.tiles_m * p.tiles_n;
+    p.splits = 1;
+    return launch(k, p, stream);
+}
 
 fg_status fg::gemm_stored(int64_t M, int64_t N, int64_t K, int64_t k_rows, float alpha, const fg_matrix *A, const fg_matrix *B, float beta,
                           const fg_matrix *C, const fg_matrix *D, void *hip_stream) {

@@ -158,6 +158,9 @@ struct TileCfg {
     static constexpr int acc_col(int r) { return M16_ ? 16 * (r >> 3) + 4 * ((r >> 2) & 1) + (r & 3) : 8 * (r >> 2) + (r & 3); }
     static constexpr bool A_KC = A_KC_, B_KC = B_KC_, STRIDED = STRIDED_;
     using Params = typename std::conditional<STRIDED_, ContractParams, GemmParams>::type;   // what the kernel takes
+    // OWN_STORE: results do not become D = act(alpha A.B + beta C + bias); what becomes of them is said by a configuration derived
+    // from this one, in store(parameters, blocks, m_base, n_base, lane): blocks(i, j), with compile-time indices, is a 32x32 block.
+    static constexpr bool OWN_STORE = false;
     // 0: real; 1: complex (i^2 = -1), 2: dual (eps^2 = 0) numbers in planar-split storage
     static constexpr int CPLX = CPLX_;
     static constexpr bool SPLITK_KERNEL = !STRIDED_ && DIAG_ == 0 && CPLX_ == 0;
@@ -1713,7 +1716,11 @@ __global__ __launch_bounds__(Cfg::NTHREADS, Cfg::WAVES) void gemm_kernel(const t
             }
             // the matrix kernels that stream C and D have a second copy of the epilogue without the hint
             constexpr bool TWO_POLICIES = !Cfg::STRIDED && Cfg::DIAG == 0;
-            if constexpr (Cfg::WIDE) {
+            if constexpr (Cfg::OWN_STORE && Cfg::WIDE) {
+                Cfg::store(ep, [](auto i, auto j) { return gather_wide<Cfg, decltype(i)::value, decltype(j)::value>(); }, mb, nb, lane);
+            } else if constexpr (Cfg::OWN_STORE) {
+                Cfg::store(ep, [&](auto i, auto j) -> floatx16 { return acc[0][decltype(i)::value][decltype(j)::value]; }, mb, nb, lane);
+            } else if constexpr (Cfg::WIDE) {
                 if (ep.cd_cached) {
                     if (ep.has_c) epilogue_wide<Cfg, true, true>(ep, mb, nb, lane);
                     else epilogue_wide<Cfg, false, true>(ep, mb, nb, lane);

@@ -2,6 +2,7 @@
 // (tile shape, A K-contiguous?, B K-contiguous?, strided tensor addressing?, operator).
 #pragma once
 #include "gemm_kernel.hpp"
+#include "status.hpp"
 
 namespace fg {
 
@@ -84,6 +85,11 @@ const KernelEntry *kernel_table_cplx_il();
 // Planar dual numbers (eps^2 = 0): same indexing as the complex table.
 const KernelEntry *kernel_table_dual();
 enum { CTILE_64x64 = 2, CTILE_64x64_KG2 = 3, CTILE_COUNT = 4 };
+
+// The block tile (TileId) that the planner picks for a product of M x N x K that is not split, and the launch of a kernel on all tiles of p (the other
+// parameters of which are set); both for products whose results a kernel does not store as a matrix.
+int plan_tile(int64_t M, int64_t N, int64_t K);
+fg_status launch_product(const KernelEntry &k, GemmParams &p, hipStream_t stream);
 
 // Second pass of a split-K product (splitk_reduce.hip).
 hipError_t launch_splitk_reduce(const float *W, int splits, int tile_begin, int tile_count, int bm, int bn, int tiles_m,

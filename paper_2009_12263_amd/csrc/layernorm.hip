@@ -36,7 +36,7 @@ template <int W> constexpr int kRowsPerGroup = W == 1 ? 4 : 1;
 
 template <class T, class P, int W>
 struct RowLane {
-    static constexpr int N = Piece<T>::N, NT = 64 * W, R = kRowsPerGroup<W>;
+    static constexpr int N = RowPiece<T>::N, NT = 64 * W, R = kRowsPerGroup<W>;
     int lane, cols, pieces;
     int64_t group;                          // of W waves, among all of the launch
     __device__ RowLane(int n) : lane(W == 1 ? threadIdx.x & 63 : threadIdx.x), cols(n), pieces((n + N - 1) / N),
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(64 * W * kRowsPerGroup<W>) void layernorm_grad(cons
 // One workgroup a row, which is read again for each sum (from the L2).
 template <class T, class P>
 __global__ __launch_bounds__(1024) void layernorm_wide(const LayerNormArgs a) {
-    constexpr int N = Piece<T>::N;
+    constexpr int N = RowPiece<T>::N;
     __shared__ float slots[2][16];
     const int n = a.cols, pieces = (n + N - 1) / N;
     const int64_t row = blockIdx.x;
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(1024) void layernorm_wide(const LayerNormArgs a) {
 
 template <class T, class P>
 __global__ __launch_bounds__(1024) void layernorm_grad_wide(const LayerNormArgs a) {
-    constexpr int N = Piece<T>::N;
+    constexpr int N = RowPiece<T>::N;
     __shared__ float slots[2][16];
     const int n = a.cols, pieces = (n + N - 1) / N;
     const int64_t row = blockIdx.x;

@@ -13,7 +13,7 @@ typedef __bf16 bf16_t;
 
 // N elements of T, sixteen bytes unless it is said otherwise.  The type is aligned to an element only: a row of odd length begins
 // anywhere, and the memory system takes an access of 16 bytes at any element.
-template <class T, int N_ = 16 / (int)sizeof(T)> struct Piece {
+template <class T, int N_ = 16 / (int)sizeof(T)> struct RowPiece {
     static constexpr int N = N_;
     typedef T vec __attribute__((ext_vector_type(N_)));
     typedef vec unaligned __attribute__((aligned(sizeof(T))));
@@ -23,7 +23,7 @@ template <class T, int N_ = 16 / (int)sizeof(T)> struct Piece {
 template <class T, int N>
 __device__ __forceinline__ void load_piece(const T *row, int p, int n, float (&out)[N], float fill = 0.f) {
     if ((p + 1) * N <= n) {
-        const typename Piece<T, N>::vec v = *(const typename Piece<T, N>::unaligned *)(row + p * N);
+        const typename RowPiece<T, N>::vec v = *(const typename RowPiece<T, N>::unaligned *)(row + p * N);
 #pragma unroll
         for (int e = 0; e < N; ++e) out[e] = (float)v[e];
     } else {
@@ -35,10 +35,10 @@ __device__ __forceinline__ void load_piece(const T *row, int p, int n, float (&o
 template <class T, int N>
 __device__ __forceinline__ void store_piece(T *row, int p, int n, const float (&in)[N]) {
     if ((p + 1) * N <= n) {
-        typename Piece<T, N>::vec v;
+        typename RowPiece<T, N>::vec v;
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = (T)in[e];
-        *(typename Piece<T, N>::unaligned *)(row + p * N) = v;
+        *(typename RowPiece<T, N>::unaligned *)(row + p * N) = v;
     } else {
 #pragma unroll
         for (int e = 0; e < N; ++e)
