@@ -17,8 +17,9 @@
 namespace fg {
 namespace {
 
-constexpr int kPieces = 4;                  // of 16 bytes per lane and row
+constexpr int kPieces = 2;                  // of 16 bytes per lane and row
 constexpr int kMaxWaves = 16;
+constexpr int kGradWaves = 4;               // waves per SIMD that the registers of the gradient's kernels leave room for
 
 struct LayerNormArgs {
     const void *x, *dy;
@@ -37,6 +38,8 @@ template <int W> constexpr int kRowsPerGroup = W == 1 ? 4 : 1;
 template <class T, class P, int W>
 struct RowLane {
     static constexpr int N = RowPiece<T>::N, NT = 64 * W, R = kRowsPerGroup<W>;
+    using Raw = typename RowPiece<T>::vec;
+    using Param = typename RowPiece<P, N>::vec;
     int lane, cols, pieces;
     int64_t group;                          // of W waves, among all of the launch
     __device__ RowLane(int n) : lane(W == 1 ? threadIdx.x & 63 : threadIdx.x), cols(n), pieces((n + N - 1) / N),
@@ -47,47 +50,56 @@ struct RowLane {
         for (int c = 0; c < kPieces; ++c)
             if (lane + c * NT < pieces) f(c, lane + c * NT);
     }
-    __device__ __forceinline__ void params(const void *p, float (&out)[kPieces][N], float otherwise) const {
-        each([&](int c, int piece) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int col = piece * N + i;
-                out[c][i] = p && col < cols ? (float)((const P *)p)[col] : otherwise;
-            }
-        });
+    __device__ __forceinline__ void load(const T *row, Raw (&out)[kPieces]) const {      // zeros past the end
+        each([&](int c, int p) { out[c] = load_raw<T, N>(row, p, cols); });
+    }
+    __device__ __forceinline__ void params(const void *p, Param (&out)[kPieces], float otherwise) const {
+        each([&](int c, int piece) { out[c] = p ? load_raw<P, N>((const P *)p, piece, cols) : (Param)(P)otherwise; });
     }
 };
 
+// A workgroup requests its next row before it works on the one that it has: rows are on their way all the time.  (One row at a time: 16384x4096
+// bfloat16 97 us.)
 template <class T, class P, int W>
 __global__ __launch_bounds__(64 * W * kRowsPerGroup<W>) void layernorm(const LayerNormArgs a) {
     using Lane = RowLane<T, P, W>;
     constexpr int N = Lane::N;
     __shared__ float slots[2][W];
     const Lane l(a.cols);
-    float gamma[kPieces][N], beta[kPieces][N];
+    const int64_t step = (int64_t)gridDim.x * Lane::R;
+    typename Lane::Param gamma[kPieces], beta[kPieces];
+    typename Lane::Raw ahead[kPieces];
+    if (l.group < a.rows) l.load((const T *)a.x + l.group * a.ldx, ahead);
     l.params(a.gamma, gamma, 1.f);
     l.params(a.beta, beta, 0.f);
-    for (int64_t row = l.group; row < a.rows; row += (int64_t)gridDim.x * Lane::R) {
-        const T *x = (const T *)a.x + row * a.ldx;
+    for (int64_t row = l.group; row < a.rows; row += step) {
         T *y = (T *)a.out + row * a.ldo;
         float v[kPieces][N], sum = 0.f, square = 0.f;
-        l.each([&](int c, int p) {
-            load_piece(x, p, a.cols, v[c]);
+        l.each([&](int c, int) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[c][i] = (float)ahead[c][i];
+        });
+        if (row + step < a.rows) l.load((const T *)a.x + (row + step) * a.ldx, ahead);
+        l.each([&](int c, int) {
 #pragma unroll
             for (int i = 0; i < N; ++i) sum += v[c][i];
         });
         const float mean = group_sum<W>(sum, slots[0]) / a.width;
         l.each([&](int c, int p) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                v[c][i] -= mean;
-                square += p * N + i < a.cols ? v[c][i] * v[c][i] : 0.f;
+            for (int i = 0; i < N; ++i) v[c][i] -= mean;
+            if ((p + 1) * N <= a.cols) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) square += v[c][i] * v[c][i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) square += p * N + i < a.cols ? v[c][i] * v[c][i] : 0.f;
             }
         });
         const float rstd = 1.f / __builtin_sqrtf(group_sum<W>(square, slots[1]) / a.width + a.eps);
         l.each([&](int c, int p) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) v[c][i] = v[c][i] * rstd * gamma[c][i] + beta[c][i];
+            for (int i = 0; i < N; ++i) v[c][i] = v[c][i] * rstd * (float)gamma[c][i] + (float)beta[c][i];
             store_piece(y, p, a.cols, v[c]);
         });
         if (l.lane == 0) {
@@ -98,53 +110,61 @@ __global__ __launch_bounds__(64 * W * kRowsPerGroup<W>) void layernorm(const Lay
 }
 
 template <class T, class P, int W, bool SUMS>
-__global__ __launch_bounds__(64 * W * kRowsPerGroup<W>) void layernorm_grad(const LayerNormArgs a) {
+__global__ __launch_bounds__(64 * W * kRowsPerGroup<W>, kGradWaves) void layernorm_grad(const LayerNormArgs a) {
     using Lane = RowLane<T, P, W>;
     constexpr int N = Lane::N;
     __shared__ float slots[4][W];
     const Lane l(a.cols);
-    float gamma[kPieces][N], sum_gamma[SUMS ? kPieces : 1][N] = {}, sum_beta[SUMS ? kPieces : 1][N] = {};
+    const int64_t step = (int64_t)gridDim.x * Lane::R;
+    typename Lane::Param gamma[kPieces];
+    typename Lane::Raw ahead_x[kPieces], ahead_dy[kPieces];
+    float ahead_mean = 0.f, ahead_rstd = 0.f, sum_gamma[SUMS ? kPieces : 1][N] = {}, sum_beta[SUMS ? kPieces : 1][N] = {};
+    auto load = [&](int64_t row) {
+        ahead_mean = a.mean[row];
+        ahead_rstd = a.rstd[row];
+        l.load((const T *)a.x + row * a.ldx, ahead_x);
+        l.load((const T *)a.dy + row * a.lddy, ahead_dy);
+    };
+    if (l.group < a.rows) load(l.group);
     l.params(a.gamma, gamma, 1.f);
     int turn = 0;
-    for (int64_t row = l.group; row < a.rows; row += (int64_t)gridDim.x * Lane::R) {
-        const T *x = (const T *)a.x + row * a.ldx, *dy = (const T *)a.dy + row * a.lddy;
+    for (int64_t row = l.group; row < a.rows; row += step) {
         T *dx = (T *)a.out + row * a.ldo;
-        const float mean = a.mean[row], rstd = a.rstd[row];
-        float xh[kPieces][N], g[kPieces][N], s1 = 0.f, s2 = 0.f;
-        l.each([&](int c, int p) {
-            load_piece(x, p, a.cols, xh[c], mean);          // past the end: xh = 0, dy = 0
-            load_piece(dy, p, a.cols, g[c]);
-        });
-        l.each([&](int c, int p) {
+        const float mean = ahead_mean, rstd = ahead_rstd;
+        typename Lane::Raw x[kPieces], dy[kPieces];
+        l.each([&](int c, int) { x[c] = ahead_x[c]; dy[c] = ahead_dy[c]; });
+        if (row + step < a.rows) load(row + step);
+        float s1 = 0.f, s2 = 0.f;
+        // (past the end of a row dy is zero, and so are all terms)
+        l.each([&](int c, int) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                xh[c][i] = (xh[c][i] - mean) * rstd;
+                const float xh = ((float)x[c][i] - mean) * rstd, d = (float)dy[c][i], g = d * (float)gamma[c][i];
                 if constexpr (SUMS) {
-                    sum_gamma[c][i] += g[c][i] * xh[c][i];
-                    sum_beta[c][i] += g[c][i];
+                    sum_gamma[c][i] += d * xh;
+                    sum_beta[c][i] += d;
                 }
-                g[c][i] *= gamma[c][i];
-                s1 += g[c][i];
-                s2 += g[c][i] * xh[c][i];
+                s1 += g;
+                s2 += g * xh;
             }
         });
         const float c1 = group_sum<W>(s1, slots[turn]) / a.width, c2 = group_sum<W>(s2, slots[turn + 1]) / a.width;
         turn ^= 2;
         l.each([&](int c, int p) {
+            float o[N];
 #pragma unroll
-            for (int i = 0; i < N; ++i) g[c][i] = rstd * (g[c][i] - c1 - xh[c][i] * c2);
-            store_piece(dx, p, a.cols, g[c]);
+            for (int i = 0; i < N; ++i) {
+                const float xh = ((float)x[c][i] - mean) * rstd, g = (float)dy[c][i] * (float)gamma[c][i];
+                o[i] = rstd * (g - c1 - xh * c2);
+            }
+            store_piece(dx, p, a.cols, o);
         });
     }
     if constexpr (SUMS) {
         float *to = a.partial + l.group * 2 * a.cols;
         l.each([&](int c, int p) {
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (p * N + i < a.cols) {
-                    to[p * N + i] = sum_gamma[c][i];
-                    to[a.cols + p * N + i] = sum_beta[c][i];
-                }
+            store_piece(to, p, a.cols, sum_gamma[c]);
+            store_piece(to + a.cols, p, a.cols, sum_beta[c]);
         });
     }
 }
@@ -277,7 +297,7 @@ int waves_for(int64_t cols, int elem) {
 int64_t grad_groups(int64_t rows, int64_t cols, int elem) {
     const int w = waves_for(cols, elem);
     if (w == 0) return std::min<int64_t>(rows, 64);
-    const int64_t groups = std::min<int64_t>(rows, kNumCU * 8 / w);
+    const int64_t groups = std::min<int64_t>(rows, kNumCU * 4 * kGradWaves / w);
     return w == 1 ? (groups + 3) / 4 * 4 : groups;
 }
 
@@ -336,7 +356,11 @@ fg_status fg_layernorm(int64_t rows, int64_t cols, const fg_matrix *X, const voi
         if (w == 0) hipLaunchKernelGGL((layernorm_wide<T, P>), dim3((unsigned)rows), dim3(1024), 0, stream, a);
         else with_waves(w, [&](auto tag) {
             constexpr int W = tag, R = kRowsPerGroup<W>;
-            const unsigned grid = (unsigned)std::min<int64_t>((rows + R - 1) / R, kNumCU * 32 / (W * R));
+            static const int per_cu = [] {              // workgroups that fit a unit
+                int n = 0;
+                return hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, (const void *)layernorm<T, P, W>, 64 * W * R, 0) == hipSuccess && n > 0 ? n : 1;
+            }();
+            const unsigned grid = (unsigned)std::min<int64_t>((rows + R - 1) / R, kNumCU * per_cu);
             hipLaunchKernelGGL((layernorm<T, P, W>), dim3(grid), dim3(64 * W * R), 0, stream, a);
         });
         return check_launch("layernorm");

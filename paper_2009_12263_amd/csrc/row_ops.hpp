@@ -19,17 +19,21 @@ template <class T, int N_ = 16 / (int)sizeof(T)> struct RowPiece {
     typedef vec unaligned __attribute__((aligned(sizeof(T))));
 };
 
-// Piece p (of N elements) of a row of n elements as FP32; past the end: `fill`.
+// Piece p (of N elements) of a row of n elements as it is stored; past the end: `fill`.
+template <class T, int N>
+__device__ __forceinline__ typename RowPiece<T, N>::vec load_raw(const T *row, int p, int n, T fill = (T)0.f) {
+    if ((p + 1) * N <= n) return *(const typename RowPiece<T, N>::unaligned *)(row + p * N);
+    typename RowPiece<T, N>::vec v;
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = p * N + e < n ? row[p * N + e] : fill;
+    return v;
+}
+// The same as FP32.
 template <class T, int N>
 __device__ __forceinline__ void load_piece(const T *row, int p, int n, float (&out)[N], float fill = 0.f) {
-    if ((p + 1) * N <= n) {
-        const typename RowPiece<T, N>::vec v = *(const typename RowPiece<T, N>::unaligned *)(row + p * N);
+    const typename RowPiece<T, N>::vec v = load_raw<T, N>(row, p, n, (T)fill);
 #pragma unroll
-        for (int e = 0; e < N; ++e) out[e] = (float)v[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) out[e] = p * N + e < n ? (float)row[p * N + e] : fill;
-    }
+    for (int e = 0; e < N; ++e) out[e] = (float)v[e];
 }
 // Rounded to nearest even once.
 template <class T, int N>
