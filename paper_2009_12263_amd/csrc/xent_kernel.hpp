@@ -51,98 +51,117 @@ struct XentCfg : Base {
     template <class Blocks>
     __device__ static __forceinline__ void store(const Params &p, const Blocks &blocks, int m_base, int n_base, int lane) {
         if constexpr (Base::WIDE) own_acc();
-        const int lm = lane & 31, lh = lane >> 5;
-        const int n_first = n_base + RUN * lh;                          // the lane's first column
-        const bool edge = n_base + Base::WTN > p.N;
-        static_for<Base::TI>([&](auto i) {
-            const int row = m_base + 32 * (int)decltype(i)::value + lm;
-            const bool there = row < p.M;
-            if constexpr (KIND == XENT_STATS) {
-                float z[Base::TJ][16], m = -__builtin_inff(), s = 0.f;
-                static_for<Base::TJ>([&](auto j) {
-                    const floatx16 a = blocks(i, j);
+        // What the lane's rows need from memory is requested for all of them at once: a lone wave would wait for each.
+        constexpr int COUNT = Base::TI, ROWS = 32;
+        int target[COUNT];
+        float lse[COUNT], dloss[COUNT];
+        if constexpr (KIND != XENT_ROUND) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) z[j][r] = a[r] * p.alpha;
-                });
-                if (edge) {
-#pragma unroll
-                    for (int j = 0; j < Base::TJ; ++j)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (n_first + 32 * j + Base::acc_col(r) >= p.N) z[j][r] = -__builtin_inff();
-                }
-#pragma unroll
-                for (int j = 0; j < Base::TJ; ++j)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) m = __builtin_fmaxf(m, z[j][r]);
-                m = with_other_half(m, [](float x, float y) { return __builtin_fmaxf(x, y); });
-                const float base = base_of(m) * kLog2e;
-#pragma unroll
-                for (int j = 0; j < Base::TJ; ++j)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][r], kLog2e, -base));
-                s = with_other_half(s, [](float x, float y) { return x + y; });
-                if (there && lh == 0) p.stats[(int64_t)(n_base / Base::WTN) * p.stats_stride + row] = {m, s};
-                const int target = there ? load_index(p.targets, p.wide, row, p.vocab) - p.v0 : -1, at = target - n_first;
-                if (__ballot(target >= n_base && target < n_base + Base::WTN)) {
-                    float hit = 0.f;
-                    bool is = false;
-#pragma unroll
-                    for (int j = 0; j < Base::TJ; ++j)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const bool same = at == 32 * j + Base::acc_col(r);
-                            hit = same ? z[j][r] : hit;
-                            is |= same;
-                        }
-                    if (is && target >= 0) p.z_target[row] = hit;
-                }
-            } else {
-                float factor = 0.f, lse2 = 0.f;
-                int at = -1;
-                bool live = there, hits = false;
+            for (int i = 0; i < COUNT; ++i) {
+                const int row = m_base + ROWS * i + lane % ROWS, at = row < p.M ? row : p.M - 1;
+                const int word = load_index(p.targets, p.wide, at, p.vocab);
+                target[i] = row < p.M ? word : -1;
                 if constexpr (KIND == XENT_DZ) {
-                    const int target = there ? load_index(p.targets, p.wide, row, p.vocab) : -1;
-                    live = target >= 0;
-                    if (live) {
-                        factor = p.dloss[(int64_t)row * p.dloss_inc] * p.factor[0];
-                        lse2 = p.lse[row] * kLog2e;
-                    }
-                    const int col = target - p.v0;
-                    at = live ? col - n_first : -1;
-                    hits = __ballot(live && col >= n_base && col < n_base + Base::WTN) != 0;
-                } else {
-                    factor = p.factor[1];
+                    lse[i] = p.lse[at];
+                    dloss[i] = p.dloss[(int64_t)at * p.dloss_inc];
                 }
-                T *out = (T *)p.D + (int64_t)row * p.ldd + n_first;
-                const float zs = p.alpha * kLog2e;
-                static_for<Base::TJ>([&](auto j) {
-                    const floatx16 a = blocks(i, j);
-#pragma unroll
-                    for (int h = 0; h < RUNS; ++h) {
-                        const int c0 = 32 * (int)decltype(j)::value + 2 * RUN * h;         // (from n_first)
-                        typename RowPiece<T, RUN>::vec v;
-#pragma unroll
-                        for (int e = 0; e < RUN; ++e) {
-                            float d = a[RUN * h + e];
-                            if constexpr (KIND == XENT_DZ) {
-                                d = __builtin_amdgcn_exp2f(__builtin_fmaf(d, zs, -lse2));
-                                if (hits) d -= at == c0 + e ? 1.f : 0.f;
-                                d = live && !(edge && n_first + c0 + e >= p.N) ? d * factor : 0.f;
-                            } else {
-                                d *= factor;
-                            }
-                            v[e] = (T)d;
-                        }
-                        // rows of dz are as long as ldd, with zeros behind the last word; columns of dw are whole runs
-                        const bool inside = !edge || n_first + c0 < (KIND == XENT_DZ ? (int)p.ldd : p.N);
-                        if (there && inside) *(typename RowPiece<T, RUN>::unaligned *)(out + c0) = v;
-                    }
-                });
             }
+        }
+        const int n_first = n_base + RUN * (lane >> 5);                  // the lane's first column
+        const bool edge = n_base + Base::WTN > p.N;
+        static_for<COUNT>([&](auto i) {
+            const int row = m_base + ROWS * (int)decltype(i)::value + lane % ROWS;
+            if constexpr (KIND == XENT_STATS) stats_of_rows<decltype(i)::value>(p, blocks, row, target[i], n_base, n_first, edge, lane);
+            else if constexpr (KIND == XENT_DZ) dz_of_rows<decltype(i)::value>(p, blocks, row, target[i], lse[i], dloss[i], n_base, n_first, edge);
+            else rounded_rows<decltype(i)::value>(p, blocks, row, n_first, edge);
             if constexpr (Base::WIDE) {
                 __builtin_amdgcn_sched_barrier(0);
                 own_acc();
+            }
+        });
+    }
+
+    template <int I, class Blocks>
+    __device__ static __forceinline__ void stats_of_rows(const Params &p, const Blocks &blocks, int row, int word, int n_base, int n_first, bool edge, int lane) {
+        constexpr int COUNT = 16 * Base::TJ, CHAINS = 4;                                         // (sums in four chains: a lone wave waits for each addition)
+        constexpr auto col = [](int e) { return 32 * (e / 16) + Base::acc_col(e % 16); };
+        float z[COUNT], top[CHAINS], sum[CHAINS] = {};
+        static_for<Base::TJ>([&](auto j) {
+            const floatx16 a = blocks(ic<I>{}, j);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) z[16 * (int)decltype(j)::value + r] = a[r] * p.alpha;
+        });
+        if (edge) {
+#pragma unroll
+            for (int e = 0; e < COUNT; ++e) z[e] = col(e) < p.N - n_first ? z[e] : -__builtin_inff();
+        }
+#pragma unroll
+        for (int e = 0; e < COUNT; ++e) top[e % CHAINS] = e < CHAINS ? z[e] : __builtin_fmaxf(top[e % CHAINS], z[e]);
+        const float m = with_other_half(__builtin_fmaxf(__builtin_fmaxf(top[0], top[1]), __builtin_fmaxf(top[2], top[3])), [](float x, float y) { return __builtin_fmaxf(x, y); });
+        const float base = base_of(m) * kLog2e;
+#pragma unroll
+        for (int e = 0; e < COUNT; ++e) sum[e % CHAINS] += __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], kLog2e, -base));
+        const float s = with_other_half((sum[0] + sum[1]) + (sum[2] + sum[3]), [](float x, float y) { return x + y; });
+        if (row < p.M && lane < 32) p.stats[(int64_t)(n_base / Base::WTN) * p.stats_stride + row] = {m, s};
+        const int target = word - p.v0;
+        if (__ballot(word >= 0 && target >= n_base && target < n_base + Base::WTN)) {
+            const int at = target - n_first;
+            float hit = 0.f;
+            bool is = false;
+#pragma unroll
+            for (int e = 0; e < COUNT; ++e) {
+                const bool same = at == col(e);
+                hit = same ? z[e] : hit;
+                is |= same;
+            }
+            if (is && word >= 0) p.z_target[row] = hit;
+        }
+    }
+
+    // Rows that are left out: relative to an lse of infinity their exponentials are zero.
+    template <int I, class Blocks>
+    __device__ static __forceinline__ void dz_of_rows(const Params &p, const Blocks &blocks, int row, int word, float row_lse, float dloss, int n_base, int n_first, bool edge) {
+        const bool there = row < p.M, live = word >= 0;
+        const int col = word - p.v0;
+        const float factor = live ? dloss * p.factor[0] : 0.f, lse = live ? row_lse * kLog2e : __builtin_inff();
+        const float scale = p.alpha * kLog2e;
+        const bool hits = __ballot(live && col >= n_base && col < n_base + Base::WTN) != 0;
+        T *out = (T *)p.D + (int64_t)row * p.ldd + n_first;
+        if (!edge && !hits) {
+            runs<I>(blocks, out, there, [&](float a, int) { return __builtin_amdgcn_exp2f(__builtin_fmaf(a, scale, -lse)) * factor; }, [](int) { return true; });
+        } else {
+            // with the target's column, and columns past the last word: zeros, to the end of the row
+            const int at = live ? col - n_first : -1, left = p.N - n_first, room = (int)p.ldd - n_first;
+            runs<I>(blocks, out, there, [&](float a, int c) {
+                const float d = (__builtin_amdgcn_exp2f(__builtin_fmaf(a, scale, -lse)) - (at == c ? 1.f : 0.f)) * factor;
+                return c < left ? d : 0.f;
+            }, [&](int c) { return c < room; });
+        }
+    }
+
+    // (the number of columns is a multiple of 8: runs are whole)
+    template <int I, class Blocks>
+    __device__ static __forceinline__ void rounded_rows(const Params &p, const Blocks &blocks, int row, int n_first, bool edge) {
+        const float factor = p.factor[1];
+        const int left = edge ? p.N - n_first : Base::WTN;
+        runs<I>(blocks, (T *)p.D + (int64_t)row * p.ldd + n_first, row < p.M, [&](float a, int) { return a * factor; }, [&](int c) { return c < left; });
+    }
+
+    // Stores value(result, column), rounded, where the row is there and the run's first column is `inside`.
+    template <int I, class Blocks, class Value, class Inside>
+    __device__ static __forceinline__ void runs(const Blocks &blocks, T *out, bool there, Value &&value, Inside &&inside) {
+        typedef float floats __attribute__((ext_vector_type(RUN)));
+        using Vec = typename RowPiece<T, RUN>::vec;
+        typedef __attribute__((address_space(1))) typename RowPiece<T, RUN>::unaligned *Global;
+        static_for<Base::TJ>([&](auto j) {
+            const floatx16 a = blocks(ic<I>{}, j);
+#pragma unroll
+            for (int h = 0; h < RUNS; ++h) {
+                const int c0 = 32 * (int)decltype(j)::value + 2 * RUN * h;
+                floats v;
+#pragma unroll
+                for (int e = 0; e < RUN; ++e) v[e] = value(a[RUN * h + e], c0 + e);
+                if (there && inside(c0)) *(Global)(out + c0) = __builtin_convertvector(v, Vec);
             }
         });
     }
