@@ -6,7 +6,7 @@
 // sorted by id, stably, and the sorted list is cut into tiles of kTile tokens.  A wave takes a tile and 64 pieces of its columns
 // and walks the tokens in order; the sum of an id whose tokens all lie in the tile is a row of the result, and the sums of an
 // id that reaches over the tile's edges are kept and joined in the order of the tiles by a last pass.  So an
-// id that half of the tokens have costs as little as a rare one.  Rows without tokens are filled by other waves of the same launch.
+// id that half of the tokens have costs as little as a rare one.  Other waves of that last pass fill the rows without tokens.
 //
 // Sorting: runs of kRun tokens are sorted in LDS, one workgroup each, and merged in one step: a token's place in the whole list is
 // the number of tokens in front of it in every run, found by bisection.
@@ -55,9 +55,9 @@ __global__ __launch_bounds__(256) void embedding(const T *table, int64_t ld, con
 
 // ---- sorting ----------------------------------------------------------------------------------------
 // Sorts run blockIdx.x of ITEMS * 1024 tokens by id, stably; ids that name no row count as `vocab` and come last.  Also clears the
-// bits of the rows that have tokens.
+// bits of the rows that have tokens, and the count of open ids; a single run is the whole list, and its rows' bits are set here.
 template <int ITEMS>
-__global__ __launch_bounds__(kRunThreads) void embedding_sort(const void *ids, bool wide, int tokens, int vocab, int passes, uint32_t *keys, uint32_t *order, uint32_t *present) {
+__global__ __launch_bounds__(kRunThreads) void embedding_sort(const void *ids, bool wide, int tokens, int vocab, int passes, uint32_t *keys, uint32_t *order, uint32_t *present, uint32_t *open_count) {
     constexpr int RUN = ITEMS * kRunThreads;
     __shared__ uint32_t key[RUN];
     __shared__ uint16_t pos[RUN];
@@ -65,6 +65,8 @@ __global__ __launch_bounds__(kRunThreads) void embedding_sort(const void *ids, b
     static_assert(kRunWaves << kDigit == kRunThreads, "one thread per counter");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.x * RUN, n = min(tokens - first, RUN);
     for (int64_t w = (int64_t)blockIdx.x * kRunThreads + threadIdx.x; w < (vocab + 31) / 32; w += (int64_t)gridDim.x * kRunThreads) present[w] = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *open_count = 0;
+    if (gridDim.x == 1) __threadfence();                                // (before the first __syncthreads: bits are set behind the last)
 #pragma unroll
     for (int r = 0; r < ITEMS; ++r) {
         const int i = (wave * ITEMS + r) * 64 + lane;
@@ -122,30 +124,38 @@ __global__ __launch_bounds__(kRunThreads) void embedding_sort(const void *ids, b
     for (int i = threadIdx.x; i < n; i += kRunThreads) {
         keys[first + i] = key[i];
         order[first + i] = first + pos[i];
+        if (gridDim.x == 1 && key[i] < (uint32_t)vocab && (i == 0 || key[i - 1] != key[i])) atomicOr(&present[key[i] >> 5], 1u << (key[i] & 31));
     }
 }
 
-// How many of the n sorted keys are below k (or equal to it, with `equal`).
-__device__ __forceinline__ int keys_before(const uint32_t *keys, int n, uint32_t k, bool equal) {
-    int lo = 0;
-    for (int left = n; left > 0;) {
-        const int half = left >> 1;
-        const uint32_t at = keys[lo + half];
-        if (at < k || (equal && at == k)) { lo += half + 1; left -= half + 1; }
-        else left = half;
-    }
-    return lo;
-}
-// Token i of the sorted runs goes to its place in the whole list: behind all smaller ids, and behind equal ones of earlier runs.
+// Token i of the sorted runs goes to its place in the whole list: behind all smaller ids, and behind equal ones of earlier runs.  Four runs
+// are searched side by side, each a fixed number of steps (one after the other, 16384 tokens: 10.2 us, 8.6 so).
 __global__ __launch_bounds__(256) void embedding_merge(const uint32_t *keys, const uint32_t *order, int tokens, int run, uint32_t *all_keys, uint32_t *all_order,
                                                        int vocab, uint32_t *present) {
+    constexpr int SIDE = 4;
     const int i = blockIdx.x * 256 + threadIdx.x;
     if (i >= tokens) return;
     const int own = i / run, runs = (tokens + run - 1) / run;
     const uint32_t k = keys[i];
     int place = i - own * run;
-    for (int r = 0; r < runs; ++r)
-        if (r != own) place += keys_before(keys + (int64_t)r * run, min(run, tokens - r * run), k, r < own);
+    for (int r0 = 0; r0 < runs; r0 += SIDE) {
+        int before[SIDE] = {};              // keys of the run that are in front
+        for (int step = run; step > 0; step /= 2) {                     // (a power of two)
+            uint32_t at[SIDE];
+            bool in[SIDE];
+#pragma unroll
+            for (int s = 0; s < SIDE; ++s) {
+                const int r = r0 + s, to = before[s] + step, n = min(run, tokens - r * run);
+                in[s] = r < runs && r != own && to <= n;
+                at[s] = keys[in[s] ? r * run + to - 1 : i];
+            }
+#pragma unroll
+            for (int s = 0; s < SIDE; ++s)
+                if (in[s] && (at[s] < k || (at[s] == k && r0 + s < own))) before[s] += step;
+        }
+#pragma unroll
+        for (int s = 0; s < SIDE; ++s) place += before[s];
+    }
     all_keys[place] = k;
     all_order[place] = order[i];
     if (k < (uint32_t)vocab && (i == own * run || keys[i - 1] != k)) atomicOr(&present[k >> 5], 1u << (k & 31));      // (bits: in any order)
@@ -158,46 +168,33 @@ struct EmbeddingGradArgs {
     void *out;
     const uint32_t *keys, *order, *present;
     float *open;                            // tile t: the sum of the id that comes in over its front at 2 t dim, of the one that goes out at (2 t + 1) dim
+    uint32_t *open_count, *open_tiles;      // tiles that an id which began there goes out of, in any order
     int64_t lddy, ldc, ldo;
     int tokens, vocab, dim, tiles, chunks;  // chunks: of 64 pieces, that cover the columns
-    int sum_groups;                         // workgroups of sums in front of those that fill rows
+    int join_groups;                        // workgroups that join sums, in front of those that fill rows
     int shift;                              // lanes of a row to fill
     float scale;
 };
 
-// A row's sum becomes the result: scaled, what is there added, rounded once.
+// Piece p of what is there in row id.
 template <class D, int N>
-__device__ __forceinline__ void embedding_finish(const EmbeddingGradArgs &a, uint32_t id, int p, float (&sum)[N]) {
-    float c[N];
-    if (a.c) load_piece((const D *)a.c + (int64_t)id * a.ldc, p, a.dim, c);
+__device__ __forceinline__ typename RowPiece<D, N>::vec embedding_there(const EmbeddingGradArgs &a, uint32_t id, int p) {
+    return load_raw<D, N>((const D *)a.c + (int64_t)id * a.ldc, p, a.dim);
+}
+// A row's sum becomes the result: scaled, what is there added, rounded once.
+template <class D, bool ADD, int N>
+__device__ __forceinline__ void embedding_finish(const EmbeddingGradArgs &a, uint32_t id, int p, const typename RowPiece<D, N>::vec &there, float (&sum)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) sum[i] = a.c ? sum[i] * a.scale + c[i] : sum[i] * a.scale;
+    for (int i = 0; i < N; ++i) sum[i] = ADD ? sum[i] * a.scale + (float)there[i] : sum[i] * a.scale;
     store_piece((D *)a.out + (int64_t)id * a.ldo, p, a.dim, sum);
 }
 
-template <class T, class D>
-__global__ __launch_bounds__(256) void embedding_grad(const EmbeddingGradArgs a) {
+// ADD: there is a matrix to add to.  Its rows are requested with those of dy (when each was read at the end of its sum: 9999 tokens of 1001 FP32
+// 38.9 us, 33.1 so).
+template <class T, class D, bool ADD>
+__global__ __launch_bounds__(256) void embedding_sums(const EmbeddingGradArgs a) {
     constexpr int N = RowPiece<T>::N;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pieces = (a.dim + N - 1) / N;
-    if ((int)blockIdx.x >= a.sum_groups) {
-        // rows without tokens: zeros, or what is there
-        constexpr int AHEAD = 4;
-        const int at = lane & ((1 << a.shift) - 1), rows = 64 >> a.shift, chunks = (pieces + (AHEAD << a.shift) - 1) / (AHEAD << a.shift);
-        const int64_t item = (int64_t)(blockIdx.x - a.sum_groups) * 4 + wave;
-        const int64_t row = item / chunks * rows + (lane >> a.shift);
-        const int first = (int)(item % chunks) * (AHEAD << a.shift) + at;
-        if (row >= a.vocab || (a.present[row >> 5] >> (row & 31) & 1)) return;
-        float v[AHEAD][N] = {};
-        if (a.c) {
-#pragma unroll
-            for (int c = 0; c < AHEAD; ++c)
-                if (first + (c << a.shift) < pieces) load_piece((const D *)a.c + row * a.ldc, first + (c << a.shift), a.dim, v[c]);
-        }
-#pragma unroll
-        for (int c = 0; c < AHEAD; ++c)
-            if (first + (c << a.shift) < pieces) store_piece((D *)a.out + row * a.ldo, first + (c << a.shift), a.dim, v[c]);
-        return;
-    }
     const int item = blockIdx.x * 4 + wave, tile = item / a.chunks, p = item % a.chunks * 64 + lane;
     if (tile >= a.tiles) return;
     const int i0 = tile * kTile, n = min(kTile, a.tokens - i0);
@@ -205,22 +202,33 @@ __global__ __launch_bounds__(256) void embedding_grad(const EmbeddingGradArgs a)
     // the tokens of the tile, one per lane; and whether the ids at its edges reach beyond it
     const uint32_t key_of_lane = a.keys[i0 + min(lane, n - 1)], token_of_lane = a.order[i0 + min(lane, n - 1)];
     const bool comes_in = i0 > 0 && a.keys[i0 - 1] == a.keys[i0], goes_out = i0 + n < a.tokens && a.keys[i0 + n] == a.keys[i0 + n - 1];
-    float sum[N] = {}, v[kTile][N];
+    // the tokens that end an id's sum, and those of them whose sum is all of the tile's
+    const uint32_t next_of_lane = __shfl_down(key_of_lane, 1);
+    const uint64_t ends = __ballot(lane < n && key_of_lane < (uint32_t)a.vocab && (lane + 1 == n || next_of_lane != key_of_lane));
+    uint64_t closed = ends;
+    if (comes_in) closed &= ~(ends & -ends);                            // (the first)
+    if (goes_out) closed &= ~(1ull << (n - 1));
+    float sum[N] = {};
+    typename RowPiece<T>::vec v[kTile];     // (as stored: as FP32 they take the registers of three waves per SIMD)
+    typename RowPiece<D, N>::vec there[ADD ? kTile : 1];
 #pragma unroll
     for (int e = 0; e < kTile; ++e)
-        if (e < n && on) load_piece((const T *)a.dy + (int64_t)(uint32_t)__builtin_amdgcn_readlane(token_of_lane, e) * a.lddy, p, a.dim, v[e]);
+        if (ADD && on && (closed >> e & 1)) there[ADD ? e : 0] = embedding_there<D, N>(a, __builtin_amdgcn_readlane(key_of_lane, e), p);
+#pragma unroll
+    for (int e = 0; e < kTile; ++e)
+        if (e < n && on) v[e] = load_raw<T, N>((const T *)a.dy + (int64_t)(uint32_t)__builtin_amdgcn_readlane(token_of_lane, e) * a.lddy, p, a.dim);
     bool in = comes_in;                     // the current id began in an earlier tile
 #pragma unroll
     for (int e = 0; e < kTile; ++e) {
         const uint32_t id = __builtin_amdgcn_readlane(key_of_lane, e);
         if (e < n && id < (uint32_t)a.vocab) {                          // (ids that name no row are the last)
 #pragma unroll
-            for (int i = 0; i < N; ++i) sum[i] += v[e][i];
-            const bool last = e + 1 == n;
-            if (last || (uint32_t)__builtin_amdgcn_readlane(key_of_lane, (e + 1) % kTile) != id) {
+            for (int i = 0; i < N; ++i) sum[i] += (float)v[e][i];
+            if (ends >> e & 1) {
                 if (on) {
-                    if (in || (last && goes_out)) store_piece(a.open + ((int64_t)tile * 2 + (in ? 0 : 1)) * a.dim, p, a.dim, sum);
-                    else embedding_finish<D>(a, id, p, sum);
+                    if (closed >> e & 1) embedding_finish<D, ADD>(a, id, p, there[ADD ? e : 0], sum);
+                    else store_piece(a.open + ((int64_t)tile * 2 + (in ? 0 : 1)) * a.dim, p, a.dim, sum);
+                    if (!in && e + 1 == n && goes_out && p == 0) a.open_tiles[atomicAdd(a.open_count, 1u)] = tile;
                 }
                 in = false;
 #pragma unroll
@@ -230,40 +238,82 @@ __global__ __launch_bounds__(256) void embedding_grad(const EmbeddingGradArgs a)
     }
 }
 
-// Joins the sums of an id that goes out of a tile it began in: that tile's, then one of each tile that it comes into.
+// Rows without tokens: zeros, or what is there.
 template <class T, class D>
+__device__ __forceinline__ void embedding_fill(const EmbeddingGradArgs &a, int64_t item, int lane, int pieces) {
+    constexpr int N = RowPiece<T>::N, AHEAD = 4;
+    const int at = lane & ((1 << a.shift) - 1), rows = 64 >> a.shift, chunks = (pieces + (AHEAD << a.shift) - 1) / (AHEAD << a.shift);
+    const int64_t row = item / chunks * rows + (lane >> a.shift);
+    const int first = (int)(item % chunks) * (AHEAD << a.shift) + at;
+    if (row >= a.vocab || (a.present[row >> 5] >> (row & 31) & 1)) return;
+    float v[AHEAD][N] = {};
+    if (a.c) {
+#pragma unroll
+        for (int c = 0; c < AHEAD; ++c)
+            if (first + (c << a.shift) < pieces) load_piece((const D *)a.c + row * a.ldc, first + (c << a.shift), a.dim, v[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < AHEAD; ++c)
+        if (first + (c << a.shift) < pieces) store_piece((D *)a.out + row * a.ldo, first + (c << a.shift), a.dim, v[c]);
+}
+
+// Joins the sums of an id that goes out of a tile it began in: that tile's, then those of the tiles that it comes into.  A workgroup takes one such id
+// at a time and 64 pieces of its columns; its waves add up a quarter of the tiles each, and the quarters are added in order.  That is a chain of
+// latencies (20 us for 16384 tokens in a launch of its own), which the filling of rows in the other workgroups covers.
+template <class T, class D, bool ADD>
 __global__ __launch_bounds__(256) void embedding_join(const EmbeddingGradArgs a) {
-    constexpr int N = RowPiece<T>::N, AHEAD = 8;
+    constexpr int N = RowPiece<T>::N, AHEAD = 8, WAVES = 4;
+    __shared__ float part[WAVES][N][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pieces = (a.dim + N - 1) / N;
-    const int item = blockIdx.x * 4 + wave, tile = item / a.chunks, p = item % a.chunks * 64 + lane;
-    if (tile + 1 >= a.tiles) return;
-    const int i0 = tile * kTile, next = i0 + kTile;
-    const uint32_t id = a.keys[next - 1];
-    if (id >= (uint32_t)a.vocab || a.keys[next] != id || (a.keys[i0] == id && i0 > 0 && a.keys[i0 - 1] == id)) return;
-    // tiles that it comes into
-    int into = 0;
-    for (;;) {
-        const int t = tile + 1 + into + lane;
-        const uint64_t same = __ballot(t < a.tiles && a.keys[(int64_t)t * kTile] == id);
-        const int more = same == ~0ull ? 64 : __builtin_ctzll(~same);
-        into += more;
-        if (more < 64) break;
+    if ((int)blockIdx.x >= a.join_groups) {
+        embedding_fill<T, D>(a, (int64_t)(blockIdx.x - a.join_groups) * WAVES + wave, lane, pieces);
+        return;
     }
-    if (p >= pieces) return;
-    float sum[N];
-    load_piece(a.open + ((int64_t)tile * 2 + 1) * a.dim, p, a.dim, sum);
-    for (int t0 = 0; t0 < into; t0 += AHEAD) {
-        float v[AHEAD][N];
+    const int p = blockIdx.x % a.chunks * 64 + lane;
+    const uint32_t ids = *a.open_count;
+    for (uint32_t n = blockIdx.x / a.chunks; n < ids; n += a.join_groups / a.chunks) {
+        const int tile = a.open_tiles[n];
+        const uint32_t id = a.keys[(int64_t)tile * kTile + kTile - 1];
+        // how many tiles it comes into: those behind, as long as they begin with it
+        int into = 0;
+        for (int stride = 64; stride > 0; stride /= 64)
+            for (;;) {
+                const int64_t t = tile + into + (int64_t)stride * (lane + 1);
+                const uint64_t same = __ballot(t < a.tiles && a.keys[t * kTile] == id);
+                const int more = same == ~0ull ? 64 : __builtin_ctzll(~same);
+                into += more * stride;
+                if (more < 64) break;
+            }
+        const int each = (into + WAVES - 1) / WAVES, first = wave * each, last = min(first + each, into);
+        float sum[N] = {};
+        if (p < pieces) {
+            if (wave == 0) load_piece(a.open + ((int64_t)tile * 2 + 1) * a.dim, p, a.dim, sum);
+            for (int t0 = first; t0 < last; t0 += AHEAD) {
+                float v[AHEAD][N];
 #pragma unroll
-        for (int t = 0; t < AHEAD; ++t)
-            if (t0 + t < into) load_piece(a.open + (int64_t)(tile + 1 + t0 + t) * 2 * a.dim, p, a.dim, v[t]);
+                for (int t = 0; t < AHEAD; ++t)
+                    if (t0 + t < last) load_piece(a.open + (int64_t)(tile + 1 + t0 + t) * 2 * a.dim, p, a.dim, v[t]);
 #pragma unroll
-        for (int t = 0; t < AHEAD; ++t)
-            if (t0 + t < into)
+                for (int t = 0; t < AHEAD; ++t)
+                    if (t0 + t < last)
 #pragma unroll
-                for (int i = 0; i < N; ++i) sum[i] += v[t][i];
+                        for (int i = 0; i < N; ++i) sum[i] += v[t][i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) part[wave][i][lane] = sum[i];
+        __syncthreads();
+        if (wave == 0 && p < pieces) {
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[i] += part[w][i][lane];
+            typename RowPiece<D, N>::vec there = {};
+            if (ADD) there = embedding_there<D, N>(a, id, p);
+            embedding_finish<D, ADD>(a, id, p, there, sum);
+        }
+        __syncthreads();
     }
-    embedding_finish<D>(a, id, p, sum);
 }
 
 // ---- host ----------------------------------------------------------------------------------------------
@@ -273,11 +323,11 @@ int lanes_shift(int pieces) {
     while (s < 6 && (1 << s) < pieces) ++s;
     return s;
 }
-int run_items(int64_t tokens) { return tokens <= 65536 ? 4 : 8; }
+int run_items(int64_t tokens) { return tokens <= kRunThreads ? 1 : tokens <= 65536 ? 4 : 16; }
 
 // The workspace: sorted runs, the whole list, the rows that have tokens, open sums.
 struct EmbeddingSpace {
-    int64_t keys, order, all_keys, all_order, present, open, bytes;
+    int64_t keys, order, all_keys, all_order, present, open_count, open_tiles, open, bytes;
     EmbeddingSpace(int64_t tokens, int64_t vocab, int64_t dim) {
         auto up = [](int64_t b) { return (b + 255) / 256 * 256; };
         keys = 0;
@@ -285,7 +335,9 @@ struct EmbeddingSpace {
         all_keys = order + up(4 * tokens);
         all_order = all_keys + up(4 * tokens);
         present = all_order + up(4 * tokens);
-        open = present + up((vocab + 31) / 32 * 4);
+        open_count = present + up((vocab + 31) / 32 * 4);
+        open_tiles = open_count + 256;
+        open = open_tiles + up((tokens + kTile - 1) / kTile * 4);
         bytes = open + (tokens + kTile - 1) / kTile * 2 * dim * 4;
     }
 };
@@ -300,7 +352,7 @@ template <class F> void with_element(int dtype, F &&f) {
 
 fg_status check_embedding(int64_t tokens, int64_t vocab, int64_t dim, const void *ids, int32_t index_dtype) {
     if (tokens < 0 || vocab < 0 || dim < 0) return fail(FG_ERR_SHAPE, "negative size: %lld tokens, %lld rows of %lld", (long long)tokens, (long long)vocab, (long long)dim);
-    if (tokens > (1 << 30) || vocab > (1 << 30) || dim > (1 << 30)) return fail(FG_ERR_UNSUPPORTED, "sizes above 2^30 are not supported");
+    if (tokens > (1 << 30) || vocab > (1 << 30) || dim > (1 << 24)) return fail(FG_ERR_UNSUPPORTED, "sizes above 2^30 (rows of more than 2^24) are not supported");
     return check_indices("ids", ids, index_dtype, tokens);
 }
 
@@ -349,6 +401,7 @@ fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg
     if (fg_status st = check_workspace(workspace, workspace_bytes, at.bytes)) return st;
     char *w = (char *)workspace;
     uint32_t *keys = (uint32_t *)(w + at.keys), *order = (uint32_t *)(w + at.order), *present = (uint32_t *)(w + at.present);
+    uint32_t *open_count = (uint32_t *)(w + at.open_count), *open_tiles = (uint32_t *)(w + at.open_tiles);
     uint32_t *all_keys = (uint32_t *)(w + at.all_keys), *all_order = (uint32_t *)(w + at.all_order);
     hipStream_t stream = (hipStream_t)hip_stream;
     int passes = 1;
@@ -356,9 +409,15 @@ fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg
     const bool wide = index_dtype == FG_I64;
     const int items = run_items(tokens), run = items * kRunThreads;
     const unsigned runs = (unsigned)std::max<int64_t>(1, (tokens + run - 1) / run);
-    if (items == 4) hipLaunchKernelGGL((embedding_sort<4>), dim3(runs), dim3(kRunThreads), 0, stream, ids, wide, (int)tokens, (int)vocab, passes, keys, order, present);
-    else hipLaunchKernelGGL((embedding_sort<8>), dim3(runs), dim3(kRunThreads), 0, stream, ids, wide, (int)tokens, (int)vocab, passes, keys, order, present);
-    if (tokens > 0)
+    auto sort = [&](auto tag) {
+        constexpr int ITEMS = decltype(tag)::value;
+        hipLaunchKernelGGL((embedding_sort<ITEMS>), dim3(runs), dim3(kRunThreads), 0, stream, ids, wide, (int)tokens, (int)vocab, passes, runs == 1 ? all_keys : keys,
+                           runs == 1 ? all_order : order, present, open_count);
+    };
+    if (items == 1) sort(std::integral_constant<int, 1>{});
+    else if (items == 4) sort(std::integral_constant<int, 4>{});
+    else sort(std::integral_constant<int, 16>{});
+    if (runs > 1)
         hipLaunchKernelGGL(embedding_merge, dim3((unsigned)((tokens + 255) / 256)), dim3(256), 0, stream, keys, order, (int)tokens, run, all_keys, all_order, (int)vocab, present);
     if (fg_status st = check_launch("embedding_sort")) return st;
     const bool in_place = Cin && Cin->re == dtable->re;
@@ -368,12 +427,16 @@ fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg
         const int64_t pieces = (dim + RowPiece<T>::N - 1) / RowPiece<T>::N, tiles = (tokens + kTile - 1) / kTile, chunks = (pieces + 63) / 64;
         const int shift = lanes_shift((int)((pieces + 3) / 4));
         const int64_t fills = in_place ? 0 : (vocab + (64 >> shift) - 1) / (64 >> shift) * ((pieces + (4 << shift) - 1) / (4 << shift));
-        const int64_t sum_groups = (tiles * chunks + 3) / 4;
-        EmbeddingGradArgs a = {dY->re, Cin ? Cin->re : nullptr, dtable->re, all_keys, all_order, present, (float *)(w + at.open), dY->ld, Cin ? Cin->ld : 0,
-                               dtable->ld, (int)tokens, (int)vocab, (int)dim, (int)tiles, (int)chunks, (int)sum_groups, shift, scale};
-        const int64_t groups = sum_groups + (fills + 3) / 4;
-        if (groups > 0) hipLaunchKernelGGL((embedding_grad<T, D>), dim3((unsigned)groups), dim3(256), 0, stream, a);
-        if (tiles > 1) hipLaunchKernelGGL((embedding_join<T, D>), dim3((unsigned)sum_groups), dim3(256), 0, stream, a);
+        const int64_t joins = tiles > 1 ? std::min<int64_t>(tiles - 1, 512) * chunks : 0, rest = joins + (fills + 3) / 4;
+        const EmbeddingGradArgs a = {dY->re, Cin ? Cin->re : nullptr, dtable->re, all_keys, all_order, present, (float *)(w + at.open), open_count, open_tiles, dY->ld,
+                                     Cin ? Cin->ld : 0, dtable->ld, (int)tokens, (int)vocab, (int)dim, (int)tiles, (int)chunks, (int)joins, shift, scale};
+        auto run = [&](auto tag) {
+            constexpr bool ADD = decltype(tag)::value;
+            if (tiles > 0) hipLaunchKernelGGL((embedding_sums<T, D, ADD>), dim3((unsigned)((tiles * chunks + 3) / 4)), dim3(256), 0, stream, a);
+            if (rest > 0) hipLaunchKernelGGL((embedding_join<T, D, ADD>), dim3((unsigned)rest), dim3(256), 0, stream, a);
+        };
+        if (Cin) run(std::true_type{});
+        else run(std::false_type{});
     };
     with_element(dY->dtype, [&](auto t) {
         if (dtable->dtype == FG_F32) launch(t, float{});

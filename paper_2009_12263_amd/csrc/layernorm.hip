@@ -50,7 +50,17 @@ struct RowLane {
         for (int c = 0; c < kPieces; ++c)
             if (lane + c * NT < pieces) f(c, lane + c * NT);
     }
-    __device__ __forceinline__ void load(const T *row, Raw (&out)[kPieces]) const {      // zeros past the end
+    // f(e, own) for the elements of a piece; `own` is a constant but in a row's last piece, which can hold its neighbour's elements too
+    template <class F> __device__ __forceinline__ void elements(int piece, F &&f) const {
+        if ((piece + 1) * N <= cols) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) f(e, true);
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) f(e, own_element<N>(piece, cols, e));
+        }
+    }
+    __device__ __forceinline__ void load(const T *row, Raw (&out)[kPieces]) const {
         each([&](int c, int p) { out[c] = load_raw<T, N>(row, p, cols); });
     }
     __device__ __forceinline__ void params(const void *p, Param (&out)[kPieces], float otherwise) const {
@@ -80,21 +90,12 @@ __global__ __launch_bounds__(64 * W * kRowsPerGroup<W>) void layernorm(const Lay
             for (int i = 0; i < N; ++i) v[c][i] = (float)ahead[c][i];
         });
         if (row + step < a.rows) l.load((const T *)a.x + (row + step) * a.ldx, ahead);
-        l.each([&](int c, int) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) sum += v[c][i];
-        });
+        l.each([&](int c, int p) { l.elements(p, [&](int i, bool own) { sum += own ? v[c][i] : 0.f; }); });
         const float mean = group_sum<W>(sum, slots[0]) / a.width;
         l.each([&](int c, int p) {
 #pragma unroll
             for (int i = 0; i < N; ++i) v[c][i] -= mean;
-            if ((p + 1) * N <= a.cols) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) square += v[c][i] * v[c][i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) square += p * N + i < a.cols ? v[c][i] * v[c][i] : 0.f;
-            }
+            l.elements(p, [&](int i, bool own) { square += own ? v[c][i] * v[c][i] : 0.f; });
         });
         const float rstd = 1.f / __builtin_sqrtf(group_sum<W>(square, slots[1]) / a.width + a.eps);
         l.each([&](int c, int p) {
@@ -135,18 +136,16 @@ __global__ __launch_bounds__(64 * W * kRowsPerGroup<W>, kGradWaves) void layerno
         l.each([&](int c, int) { x[c] = ahead_x[c]; dy[c] = ahead_dy[c]; });
         if (row + step < a.rows) load(row + step);
         float s1 = 0.f, s2 = 0.f;
-        // (past the end of a row dy is zero, and so are all terms)
-        l.each([&](int c, int) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
+        l.each([&](int c, int p) {
+            l.elements(p, [&](int i, bool own) {
                 const float xh = ((float)x[c][i] - mean) * rstd, d = (float)dy[c][i], g = d * (float)gamma[c][i];
-                if constexpr (SUMS) {
+                if constexpr (SUMS) {                                   // (those of other pieces' elements are not stored)
                     sum_gamma[c][i] += d * xh;
                     sum_beta[c][i] += d;
                 }
-                s1 += g;
-                s2 += g * xh;
-            }
+                s1 += own ? g : 0.f;
+                s2 += own ? g * xh : 0.f;
+            });
         });
         const float c1 = group_sum<W>(s1, slots[turn]) / a.width, c2 = group_sum<W>(s2, slots[turn + 1]) / a.width;
         turn ^= 2;
@@ -183,13 +182,13 @@ __global__ __launch_bounds__(1024) void layernorm_wide(const LayerNormArgs a) {
     for (int p = threadIdx.x; p < pieces; p += 1024) {
         load_piece(x, p, n, v);
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum += v[i];
+        for (int i = 0; i < N; ++i) sum += own_element<N>(p, n, i) ? v[i] : 0.f;
     }
     const float mean = group_sum<16>(sum, slots[0]) / a.width;
     for (int p = threadIdx.x; p < pieces; p += 1024) {
-        load_piece(x, p, n, v, mean);
+        load_piece(x, p, n, v);
 #pragma unroll
-        for (int i = 0; i < N; ++i) square += (v[i] - mean) * (v[i] - mean);
+        for (int i = 0; i < N; ++i) square += own_element<N>(p, n, i) ? (v[i] - mean) * (v[i] - mean) : 0.f;
     }
     const float rstd = 1.f / __builtin_sqrtf(group_sum<16>(square, slots[1]) / a.width + a.eps);
     const P *gamma = (const P *)a.gamma, *beta = (const P *)a.beta;
@@ -197,7 +196,7 @@ __global__ __launch_bounds__(1024) void layernorm_wide(const LayerNormArgs a) {
         load_piece(x, p, n, v);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int col = p * N + i < n ? p * N + i : n - 1;
+            const int col = first_of_piece<N>(p, n) + i;
             v[i] = (v[i] - mean) * rstd * (gamma ? (float)gamma[col] : 1.f) + (beta ? (float)beta[col] : 0.f);
         }
         store_piece(y, p, n, v);
@@ -220,20 +219,20 @@ __global__ __launch_bounds__(1024) void layernorm_grad_wide(const LayerNormArgs 
     const float mean = a.mean[row], rstd = a.rstd[row];
     float xh[N], g[N], s1 = 0.f, s2 = 0.f;
     auto load = [&](int p) {
-        load_piece(x, p, n, xh, mean);
+        load_piece(x, p, n, xh);
         load_piece(dy, p, n, g);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             xh[i] = (xh[i] - mean) * rstd;
-            if (gamma) g[i] *= (float)gamma[p * N + i < n ? p * N + i : n - 1];
+            if (gamma) g[i] *= (float)gamma[first_of_piece<N>(p, n) + i];
         }
     };
     for (int p = threadIdx.x; p < pieces; p += 1024) {
         load(p);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            s1 += g[i];
-            s2 += g[i] * xh[i];
+            s1 += own_element<N>(p, n, i) ? g[i] : 0.f;
+            s2 += own_element<N>(p, n, i) ? g[i] * xh[i] : 0.f;
         }
     }
     const float c1 = group_sum<16>(s1, slots[0]) / a.width, c2 = group_sum<16>(s2, slots[1]) / a.width;

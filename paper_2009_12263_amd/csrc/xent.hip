@@ -33,7 +33,7 @@ __device__ __forceinline__ float group_max(float v, float *slot) {
 }
 
 // ---- pieces of the logits in memory ---------------------------------------------------------------------
-// Statistics of token blockIdx.x over the n logits of a piece that begins at word v0.
+// Statistics of token blockIdx.x over the n logits of a piece that begins at word v0; rows are long enough for whole pieces of 8.
 __global__ __launch_bounds__(256) void xent_row_stats(const float *z, int64_t ld, int n, int v0, const void *targets, bool wide, int vocab, Stat *stats, float *z_target) {
     __shared__ float slots[2][4];
     const int64_t t = blockIdx.x;
@@ -41,16 +41,16 @@ __global__ __launch_bounds__(256) void xent_row_stats(const float *z, int64_t ld
     const int pieces = (n + 3) / 4;
     float m = -__builtin_inff(), s = 0.f, v[4];
     for (int p = threadIdx.x; p < pieces; p += 256) {
-        load_piece(row, p, n, v, -__builtin_inff());
+        load_piece(row, p, pieces * 4, v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) m = __builtin_fmaxf(m, v[i]);
+        for (int i = 0; i < 4; ++i) m = __builtin_fmaxf(m, p * 4 + i < n ? v[i] : -__builtin_inff());
     }
     m = group_max<4>(m, slots[0]);
     const float base = base_of(m);
     for (int p = threadIdx.x; p < pieces; p += 256) {
-        load_piece(row, p, n, v, -__builtin_inff());
+        load_piece(row, p, pieces * 4, v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s += __builtin_amdgcn_exp2f((v[i] - base) * kLog2e);
+        for (int i = 0; i < 4; ++i) s += p * 4 + i < n ? __builtin_amdgcn_exp2f((v[i] - base) * kLog2e) : 0.f;
     }
     s = group_sum<4>(s, slots[1]);
     if (threadIdx.x == 0) {
@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256) void xent_row_grad(const float *z, int64_t ldz
     const float g = target < 0 ? 0.f : dloss[t * dloss_inc] * factor[0], base = lse[t];
     for (int p = threadIdx.x; p < (n + 7) / 8; p += 256) {
         float v[8];
-        load_piece(row, p, n, v, -__builtin_inff());
+        load_piece(row, p, p * 8 + 8, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int col = p * 8 + i;
