@@ -129,7 +129,7 @@ _in_bad_fork = getattr(torch._C, "_cuda_isInBadFork", lambda: False)
 
 class _CtypesOnly:
     """In place of the native marshalling where it is not built: leaves every call to the binding (4 to 8 us more each)."""
-    gemm = dual = contract = staticmethod(lambda *args: -1)
+    gemm = dual = contract = layernorm = layernorm_grad = embedding = embedding_grad = xent = xent_grad = staticmethod(lambda *args: -1)
 
 
 def _load_fastcall(lib: C.CDLL) -> None:
@@ -144,6 +144,9 @@ def _load_fastcall(lib: C.CDLL) -> None:
     spec.loader.exec_module(fast)
     fast.setup(Matrix, _current_raw_stream, _current_device,
                *(C.cast(fn, C.c_void_p).value for fn in (lib.fg_gemm, lib.fg_gemm_ex, lib.fg_gemm_noalloc, lib.fg_gemm_dual, lib.fg_contract)))
+    fast.setup_rows(*(C.cast(fn, C.c_void_p).value for fn in (
+        lib.fg_layernorm, lib.fg_layernorm_grad, lib.fg_layernorm_grad_workspace, lib.fg_embedding, lib.fg_embedding_grad, lib.fg_embedding_grad_workspace,
+        lib.fg_linear_xent, lib.fg_linear_xent_workspace, lib.fg_linear_xent_grad, lib.fg_linear_xent_grad_workspace)))
     _fast = fast
 
 
@@ -403,6 +406,9 @@ def fg_layernorm(X: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[
                  mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, stream=None, raise_on_error: bool = True) -> int:
     """Y = layer norm of the rows of X; mean and rstd of the rows are kept for fg_layernorm_grad."""
     lib = _lib or load_library()
+    st = _fast.layernorm(X, gamma, beta, eps, Y, mean, rstd, stream)
+    if st >= 0:
+        return st if st == FG_OK else _check(st, raise_on_error)
     dev = _current_device()
     x = _rows(X, "X", None, dev)
     y = _rows(Y, "Y", X.shape, dev)
@@ -423,6 +429,9 @@ def fg_layernorm_grad(dY: torch.Tensor, X: torch.Tensor, gamma: Optional[torch.T
                       stream=None, raise_on_error: bool = True) -> int:
     """Gradients of fg_layernorm with respect to X, gamma and beta."""
     lib = _lib or load_library()
+    st = _fast.layernorm_grad(dY, X, gamma, mean, rstd, dX, dgamma, dbeta, workspace, stream)
+    if st >= 0:
+        return st if st == FG_OK else _check(st, raise_on_error)
     dev = _current_device()
     x = _rows(X, "X", None, dev)
     dy = _rows(dY, "dY", X.shape, dev)
@@ -446,6 +455,9 @@ def _indices(t: torch.Tensor, n: int, name: str, dev: int):
 def fg_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float, Y: torch.Tensor, stream=None, raise_on_error: bool = True) -> int:
     """Y[t] = scale * table[ids[t]]; zeros where ids[t] names no row."""
     lib = _lib or load_library()
+    st = _fast.embedding(table, ids, scale, Y, stream)
+    if st >= 0:
+        return st if st == FG_OK else _check(st, raise_on_error)
     dev = _current_device()
     m = _rows(table, "table", None, dev)
     vocab, dim = table.shape
@@ -463,6 +475,9 @@ def fg_embedding_grad(dY: torch.Tensor, ids: torch.Tensor, scale: float, Cin: Op
                       workspace: Optional[torch.Tensor] = None, stream=None, raise_on_error: bool = True) -> int:
     """dtable[v] = scale * sum of dY[t] over the t with ids[t] == v, + Cin[v] (None: nothing; dtable itself: only rows with tokens are touched)."""
     lib = _lib or load_library()
+    st = _fast.embedding_grad(dY, ids, scale, Cin, dtable, workspace, stream)
+    if st >= 0:
+        return st if st == FG_OK else _check(st, raise_on_error)
     dev = _current_device()
     d = _rows(dtable, "dtable", None, dev)
     vocab, dim = dtable.shape
@@ -483,6 +498,9 @@ def fg_linear_xent(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, scal
                    workspace: Optional[torch.Tensor] = None, stream=None, raise_on_error: bool = True) -> int:
     """loss[t] = lse[t] - z[t][targets[t]] with z = scale * X W^T, lse its log-sum-exp over the words; 0 where the target names no word."""
     lib = _lib or load_library()
+    st = _fast.xent(X, W, targets, scale, loss, lse, workspace, stream)
+    if st >= 0:
+        return st if st == FG_OK else _check(st, raise_on_error)
     dev = _current_device()
     x, w = _rows(X, "X", None, dev), _rows(W, "W", None, dev)
     (tokens, dim), vocab = X.shape, W.shape[0]
@@ -503,6 +521,9 @@ def fg_linear_xent_grad(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor,
                         dX: torch.Tensor, dW: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None, raise_on_error: bool = True) -> int:
     """Gradients of the losses of fg_linear_xent, weighted with dloss (one value per token, which may be a single one expanded)."""
     lib = _lib or load_library()
+    st = _fast.xent_grad(X, W, targets, scale, lse, dloss, dX, dW, workspace, stream)
+    if st >= 0:
+        return st if st == FG_OK else _check(st, raise_on_error)
     dev = _current_device()
     x, w = _rows(X, "X", None, dev), _rows(W, "W", None, dev)
     (tokens, dim), vocab = X.shape, W.shape[0]

@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/ops/empty.h>
 #include <pthread.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -229,6 +230,228 @@ PyObject *contract(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }
 }
 
+// ---- operators on rows --------------------------------------------------------------------------------
+typedef fg_status (*LayerNormFn)(int64_t, int64_t, const fg_matrix *, const void *, const void *, int32_t, float, const fg_matrix *, float *, float *, void *);
+typedef fg_status (*LayerNormGradFn)(int64_t, int64_t, const fg_matrix *, const fg_matrix *, const void *, int32_t, const float *, const float *, const fg_matrix *,
+                                     void *, void *, void *, int64_t, void *);
+typedef fg_status (*EmbeddingFn)(int64_t, int64_t, int64_t, const fg_matrix *, const void *, int32_t, float, const fg_matrix *, void *);
+typedef fg_status (*EmbeddingGradFn)(int64_t, int64_t, int64_t, const fg_matrix *, const void *, int32_t, float, const fg_matrix *, const fg_matrix *, void *, int64_t, void *);
+typedef fg_status (*XentFn)(int64_t, int64_t, int64_t, const fg_matrix *, const fg_matrix *, const void *, int32_t, float, float *, float *, void *, int64_t, void *);
+typedef fg_status (*XentGradFn)(int64_t, int64_t, int64_t, const fg_matrix *, const fg_matrix *, const void *, int32_t, float, const float *, const float *, int64_t,
+                                const fg_matrix *, const fg_matrix *, void *, int64_t, void *);
+typedef int64_t (*LayerNormSpaceFn)(int64_t, int64_t, int32_t);
+typedef int64_t (*SpaceFn)(int64_t, int64_t, int64_t);
+struct RowEntry {
+    LayerNormFn layernorm; LayerNormGradFn layernorm_grad; LayerNormSpaceFn layernorm_grad_space;
+    EmbeddingFn embedding; EmbeddingGradFn embedding_grad; SpaceFn embedding_grad_space;
+    XentFn xent; SpaceFn xent_space; XentGradFn xent_grad; SpaceFn xent_grad_space;
+} g_rows;
+
+// What the binding's own marshalling checks of a call: tensors on the current GPU, of the sizes that the others have.
+struct RowCall {
+    int dev = -1;
+    void *stream = nullptr;
+    at::Tensor made;                        // a workspace from torch's allocator
+
+    bool begin(PyObject *stream_arg) {
+        PyObject *d = PyObject_CallNoArgs(g_device);
+        int64_t v;
+        const bool ok = as_int(d, v);
+        Py_XDECREF(d);
+        dev = ok ? (int)v : -1;
+        return ok && current_stream(stream_arg, stream);
+    }
+    static int dtype_of(const at::Tensor &t) {
+        switch (t.scalar_type()) {
+            case at::kHalf: return FG_F16;
+            case at::kBFloat16: return FG_BF16;
+            case at::kFloat: return FG_F32;
+            case at::kInt: return FG_I32;
+            case at::kLong: return FG_I64;
+            default: return -1;
+        }
+    }
+    const at::Tensor *tensor(PyObject *o) const {
+        if (!THPVariable_CheckExact(o)) return nullptr;
+        const at::Tensor &t = THPVariable_Unpack(o);
+        return t.is_cuda() && t.get_device() == dev ? &t : nullptr;
+    }
+    // rows, cols: -1 where they are to be read off
+    bool matrix(PyObject *o, int64_t &rows, int64_t &cols, fg_matrix &m) const {
+        const at::Tensor *t = tensor(o);
+        if (!t || t->dim() != 2 || (rows >= 0 && t->size(0) != rows) || (cols >= 0 && t->size(1) != cols)) return false;
+        rows = t->size(0);
+        cols = t->size(1);
+        const int dtype = dtype_of(*t);
+        if ((cols > 1 && t->stride(1) != 1) || dtype < 0 || dtype > FG_F32) return false;
+        m = {t->data_ptr(), nullptr, dtype, FG_ROW, rows > 1 ? t->stride(0) : t->stride(0) > cols ? t->stride(0) : cols};
+        return true;
+    }
+    // n contiguous values of type dtype (-1: read off); absent if o is None
+    bool vector(PyObject *o, int64_t n, int &dtype, void *&p) const {
+        p = nullptr;
+        if (o == Py_None) return true;
+        const at::Tensor *t = tensor(o);
+        if (!t || t->dim() != 1 || t->size(0) != n || (n > 1 && t->stride(0) != 1)) return false;
+        const int is = dtype_of(*t);
+        if (is < 0 || (dtype >= 0 && is != dtype)) return false;
+        dtype = is;
+        p = t->data_ptr();
+        return true;
+    }
+    bool floats(PyObject *o, int64_t n, float *&p) const {
+        int dtype = FG_F32;
+        void *v;
+        if (!vector(o, n, dtype, v)) return false;
+        p = (float *)v;
+        return true;
+    }
+    bool indices(PyObject *o, int64_t n, int &dtype, void *&p) const {
+        dtype = -1;
+        return o != Py_None && vector(o, n, dtype, p) && (dtype == FG_I32 || dtype == FG_I64);
+    }
+    bool workspace(PyObject *o, int64_t need, void *&p, int64_t &bytes) {
+        p = nullptr;
+        bytes = 0;
+        if (o != Py_None) {
+            const at::Tensor *t = tensor(o);
+            if (!t || !t->is_contiguous()) return false;
+            p = t->data_ptr();
+            bytes = t->numel() * t->element_size();
+        } else if (need > 0) {
+            made = at::empty({need}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, (at::DeviceIndex)dev));
+            p = made.data_ptr();
+            bytes = need;
+        }
+        return true;
+    }
+};
+template <class F> PyObject *run_rows(PyObject *const *a, Py_ssize_t n, Py_ssize_t args, F &&f) {
+    if (g_forked || n != args || !g_rows.layernorm) return not_here();
+    try {
+        RowCall c;
+        fg_status st = FG_OK;
+        if (!c.begin(a[n - 1]) || !f(c, st)) return not_here();
+        return PyLong_FromLong(st);
+    } catch (...) {                          // no memory for a workspace, ...: the binding's own call says what is wrong
+        return not_here();
+    }
+}
+template <class F> fg_status without_gil(F &&call) {
+    fg_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = call();
+    Py_END_ALLOW_THREADS
+    return st;
+}
+
+// layernorm(X, gamma, beta, eps, Y, mean, rstd, stream) -> status
+PyObject *layernorm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return run_rows(a, n, 8, [&](RowCall &c, fg_status &st) {
+        int64_t rows = -1, cols = -1;
+        fg_matrix x, y;
+        int ptype = -1;
+        void *gamma, *beta;
+        float eps, *mean, *rstd;
+        if (!c.matrix(a[0], rows, cols, x) || !c.matrix(a[4], rows, cols, y) || !c.vector(a[1], cols, ptype, gamma) || !c.vector(a[2], cols, ptype, beta)) return false;
+        if (!as_float(a[3], eps) || !c.floats(a[5], rows, mean) || !c.floats(a[6], rows, rstd)) return false;
+        st = without_gil([&]() noexcept { return g_rows.layernorm(rows, cols, &x, gamma, beta, ptype < 0 ? x.dtype : ptype, eps, &y, mean, rstd, c.stream); });
+        return true;
+    });
+}
+// layernorm_grad(dY, X, gamma, mean, rstd, dX, dgamma, dbeta, workspace, stream) -> status
+PyObject *layernorm_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return run_rows(a, n, 10, [&](RowCall &c, fg_status &st) {
+        int64_t rows = -1, cols = -1, bytes;
+        fg_matrix x, dy, dx;
+        int ptype = -1;
+        void *gamma, *dgamma, *dbeta, *ws;
+        float *mean, *rstd;
+        if (!c.matrix(a[1], rows, cols, x) || !c.matrix(a[0], rows, cols, dy) || !c.matrix(a[5], rows, cols, dx)) return false;
+        if (!c.vector(a[2], cols, ptype, gamma) || !c.vector(a[6], cols, ptype, dgamma) || !c.vector(a[7], cols, ptype, dbeta)) return false;
+        if (!c.floats(a[3], rows, mean) || !c.floats(a[4], rows, rstd)) return false;
+        if (!c.workspace(a[8], dgamma || dbeta ? g_rows.layernorm_grad_space(rows, cols, x.dtype) : 0, ws, bytes)) return false;
+        st = without_gil([&]() noexcept { return g_rows.layernorm_grad(rows, cols, &dy, &x, gamma, ptype < 0 ? x.dtype : ptype, mean, rstd, &dx, dgamma, dbeta, ws, bytes, c.stream); });
+        return true;
+    });
+}
+// embedding(table, ids, scale, Y, stream) -> status
+PyObject *embedding(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return run_rows(a, n, 5, [&](RowCall &c, fg_status &st) {
+        int64_t vocab = -1, dim = -1, tokens = -1;
+        fg_matrix table, y;
+        int kind;
+        void *ids;
+        float scale;
+        if (!c.matrix(a[0], vocab, dim, table) || !c.matrix(a[3], tokens, dim, y) || !c.indices(a[1], tokens, kind, ids) || !as_float(a[2], scale)) return false;
+        st = without_gil([&]() noexcept { return g_rows.embedding(tokens, vocab, dim, &table, ids, kind, scale, &y, c.stream); });
+        return true;
+    });
+}
+// embedding_grad(dY, ids, scale, Cin, dtable, workspace, stream) -> status
+PyObject *embedding_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return run_rows(a, n, 7, [&](RowCall &c, fg_status &st) {
+        int64_t vocab = -1, dim = -1, tokens = -1, bytes;
+        fg_matrix dy, cin, d;
+        int kind;
+        void *ids, *ws;
+        float scale;
+        if (!c.matrix(a[4], vocab, dim, d) || !c.matrix(a[0], tokens, dim, dy) || !c.indices(a[1], tokens, kind, ids) || !as_float(a[2], scale)) return false;
+        const bool add = a[3] != Py_None;
+        if (add && !c.matrix(a[3], vocab, dim, cin)) return false;
+        if (!c.workspace(a[5], g_rows.embedding_grad_space(tokens, vocab, dim), ws, bytes)) return false;
+        st = without_gil([&]() noexcept { return g_rows.embedding_grad(tokens, vocab, dim, &dy, ids, kind, scale, add ? &cin : nullptr, &d, ws, bytes, c.stream); });
+        return true;
+    });
+}
+// xent(X, W, targets, scale, loss, lse, workspace, stream) -> status
+PyObject *xent(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return run_rows(a, n, 8, [&](RowCall &c, fg_status &st) {
+        int64_t vocab = -1, dim = -1, tokens = -1, bytes;
+        fg_matrix x, w;
+        int kind;
+        void *targets, *ws;
+        float scale, *loss, *lse;
+        if (!c.matrix(a[0], tokens, dim, x) || !c.matrix(a[1], vocab, dim, w) || !c.indices(a[2], tokens, kind, targets) || !as_float(a[3], scale)) return false;
+        if (!c.floats(a[4], tokens, loss) || !c.floats(a[5], tokens, lse) || !c.workspace(a[6], g_rows.xent_space(tokens, vocab, dim), ws, bytes)) return false;
+        st = without_gil([&]() noexcept { return g_rows.xent(tokens, vocab, dim, &x, &w, targets, kind, scale, loss, lse, ws, bytes, c.stream); });
+        return true;
+    });
+}
+// xent_grad(X, W, targets, scale, lse, dloss, dX, dW, workspace, stream) -> status
+PyObject *xent_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return run_rows(a, n, 10, [&](RowCall &c, fg_status &st) {
+        int64_t vocab = -1, dim = -1, tokens = -1, bytes;
+        fg_matrix x, w, dx, dw;
+        int kind;
+        void *targets, *ws;
+        float scale, *lse;
+        if (!c.matrix(a[0], tokens, dim, x) || !c.matrix(a[1], vocab, dim, w) || !c.matrix(a[6], tokens, dim, dx) || !c.matrix(a[7], vocab, dim, dw)) return false;
+        if (!c.indices(a[2], tokens, kind, targets) || !as_float(a[3], scale) || !c.floats(a[4], tokens, lse)) return false;
+        const at::Tensor *g = c.tensor(a[5]);
+        if (!g || g->dim() != 1 || g->size(0) != tokens || g->scalar_type() != at::kFloat) return false;
+        const int64_t inc = tokens > 1 && g->stride(0) == 0 ? 0 : 1;
+        if (inc && tokens > 1 && g->stride(0) != 1) return false;
+        if (!c.workspace(a[8], g_rows.xent_grad_space(tokens, vocab, dim), ws, bytes)) return false;
+        const float *dloss = (const float *)g->data_ptr();
+        st = without_gil([&]() noexcept { return g_rows.xent_grad(tokens, vocab, dim, &x, &w, targets, kind, scale, lse, dloss, inc, &dx, &dw, ws, bytes, c.stream); });
+        return true;
+    });
+}
+
+// setup_rows(addresses of the entry points in the order of RowEntry)
+PyObject *setup_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 10) { PyErr_SetString(PyExc_TypeError, "setup_rows takes 10 arguments"); return nullptr; }
+    void *f[10];
+    for (int i = 0; i < 10; ++i) {
+        f[i] = PyLong_AsVoidPtr(a[i]);
+        if (PyErr_Occurred()) return nullptr;
+    }
+    g_rows = RowEntry{(LayerNormFn)f[0], (LayerNormGradFn)f[1], (LayerNormSpaceFn)f[2], (EmbeddingFn)f[3], (EmbeddingGradFn)f[4], (SpaceFn)f[5],
+                      (XentFn)f[6], (SpaceFn)f[7], (XentGradFn)f[8], (SpaceFn)f[9]};
+    Py_RETURN_NONE;
+}
+
 // setup(Matrix, raw_stream, device, addresses of fg_gemm, fg_gemm_ex, fg_gemm_noalloc, fg_gemm_dual, fg_contract)
 PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (n != 8) { PyErr_SetString(PyExc_TypeError, "setup takes 8 arguments"); return nullptr; }
@@ -247,6 +470,13 @@ PyMethodDef g_methods[] = {{"setup", (PyCFunction)(void (*)(void))setup, METH_FA
                            {"gemm", (PyCFunction)(void (*)(void))gemm, METH_FASTCALL, nullptr},
                            {"dual", (PyCFunction)(void (*)(void))dual, METH_FASTCALL, nullptr},
                            {"contract", (PyCFunction)(void (*)(void))contract, METH_FASTCALL, nullptr},
+                           {"setup_rows", (PyCFunction)(void (*)(void))setup_rows, METH_FASTCALL, nullptr},
+                           {"layernorm", (PyCFunction)(void (*)(void))layernorm, METH_FASTCALL, nullptr},
+                           {"layernorm_grad", (PyCFunction)(void (*)(void))layernorm_grad, METH_FASTCALL, nullptr},
+                           {"embedding", (PyCFunction)(void (*)(void))embedding, METH_FASTCALL, nullptr},
+                           {"embedding_grad", (PyCFunction)(void (*)(void))embedding_grad, METH_FASTCALL, nullptr},
+                           {"xent", (PyCFunction)(void (*)(void))xent, METH_FASTCALL, nullptr},
+                           {"xent_grad", (PyCFunction)(void (*)(void))xent_grad, METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_fastcall", "Native marshalling of binding.py's calls.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
