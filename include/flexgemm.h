@@ -330,9 +330,8 @@ int64_t fg_embedding_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim);
  * that of its logits all the same).  No logits are kept: the vocabulary is walked in pieces, of which the statistics remain.
  *   X : tokens x dim, W : vocab x dim, both FG_F16 or both FG_BF16 (multiplied exactly, summed in FP32); targets : `tokens` indices of type
  *   index_dtype (FG_I32, FG_I64); loss, lse : `tokens` FP32 values each; vocab >= 1.
- * Infinite logits give a NaN.  16-byte aligned pointers and leading dimensions and a dim of multiples of 8 are served by kernels that form the statistics
- * of a tile of logits in its registers, with a bounded leading dimension as in fg_gemm; anything else by general ones, which pass pieces of the logits
- * through the workspace.  Splits of K use the workspace of fg_gemm (fg_init before a graph capture).
+ * Infinite logits give a NaN.  Rows that are not 16-byte aligned, or not of a multiple of 8 values, are copied into the workspace first, W a piece at a
+ * time (FG_ERR_UNSUPPORTED for rows of 2^21 values or more).
  */
 fg_status fg_linear_xent(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *X, const fg_matrix *W, const void *targets, int32_t index_dtype,
                          float scale, float *loss, float *lse, void *workspace, int64_t workspace_bytes, void *hip_stream);
@@ -345,7 +344,7 @@ int64_t fg_linear_xent_workspace(int64_t tokens, int64_t vocab, int64_t dim);
  * largest dloss, so that it neither overflows nor vanishes where dX and dW do not) and multiplied by W and X into FP32.
  *   dloss  : FP32, one value per token, or with dloss_inc 0 a single one for all (1 otherwise).
  *   dX, dW : of the type of X, the shapes of X and W.
- * A larger workspace than the query's is used for larger pieces.
+ * The product with dX splits K through the workspace of fg_gemm where that pays (fg_init before a graph capture).
  */
 fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *X, const fg_matrix *W, const void *targets, int32_t index_dtype,
                               float scale, const float *lse, const float *dloss, int64_t dloss_inc, const fg_matrix *dX, const fg_matrix *dW,

@@ -104,7 +104,8 @@ struct XentCfg : Base {
         const float s = with_other_half((sum[0] + sum[1]) + (sum[2] + sum[3]), [](float x, float y) { return x + y; });
         if (row < p.M && lane < 32) p.stats[(int64_t)(n_base / Base::WTN) * p.stats_stride + row] = {m, s};
         const int target = word - p.v0;
-        if (__ballot(word >= 0 && target >= n_base && target < n_base + Base::WTN)) {
+        const bool live = word >= 0 && target < p.N;
+        if (__ballot(live && target >= n_base && target < n_base + Base::WTN)) {
             const int at = target - n_first;
             float hit = 0.f;
             bool is = false;
@@ -114,7 +115,7 @@ struct XentCfg : Base {
                 hit = same ? z[e] : hit;
                 is |= same;
             }
-            if (is && word >= 0) p.z_target[row] = hit;
+            if (is && live) p.z_target[row] = hit;
         }
     }
 
@@ -139,12 +140,23 @@ struct XentCfg : Base {
         }
     }
 
-    // (the number of columns is a multiple of 8: runs are whole)
     template <int I, class Blocks>
     __device__ static __forceinline__ void rounded_rows(const Params &p, const Blocks &blocks, int row, int n_first, bool edge) {
         const float factor = p.factor[1];
         const int left = edge ? p.N - n_first : Base::WTN;
-        runs<I>(blocks, (T *)p.D + (int64_t)row * p.ldd + n_first, row < p.M, [&](float a, int) { return a * factor; }, [&](int c) { return c < left; });
+        T *out = (T *)p.D + (int64_t)row * p.ldd + n_first;
+        runs<I>(blocks, out, row < p.M, [&](float a, int) { return a * factor; }, [&](int c) { return c + RUN <= left; });
+        // the row's last columns, if they are no whole run
+        if (edge && p.N % RUN != 0 && row < p.M) {
+            static_for<Base::TJ>([&](auto j) {
+                const floatx16 a = blocks(ic<I>{}, j);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int c = 32 * (int)decltype(j)::value + Base::acc_col(r), c0 = c - r % RUN;
+                    if (c0 < left && c0 + RUN > left && c < left) out[c] = (T)(a[r] * factor);
+                }
+            });
+        }
     }
 
     // Stores value(result, column), rounded, where the row is there and the run's first column is `inside`.
