@@ -19,31 +19,35 @@ namespace {
 
 constexpr int kPieces = 2;                  // of 16 bytes per lane and row
 constexpr int kMaxWaves = 16;
-constexpr int kGradWaves = 4;               // waves per SIMD that the registers of the gradient's kernels leave room for
+// Waves per SIMD that the registers of the gradient's kernels leave room for: with four, workgroups of eight and sixteen waves fill a unit; smaller ones
+// do as well with three, and with fewer sums to add up (16384 x 2048 bfloat16 50.4 us with four, 45.2 with three).
+constexpr int grad_waves(int w) { return w <= 4 ? 3 : 4; }
 
 struct LayerNormArgs {
     const void *x, *dy;
     void *out;                              // y, or dx
     const void *gamma, *beta;
     float *mean, *rstd;
-    float *partial;                         // per wave group: dgamma's sums over its rows, then dbeta's (cols each)
+    float *partial;                         // per workgroup: dgamma's sums over its rows, then dbeta's (cols each)
     int64_t ldx, lddy, ldo, rows;
     int32_t cols;
     float eps, width;                       // width: cols, to divide by
 };
 
-// Workgroups of one wave a row hold four rows.
+// Workgroups of one wave a row hold four rows, those of the gradient with two waves a row two: the sums of a workgroup's rows are added up before they
+// are written (16384 x 1024 bfloat16, gradient: 40.9 us with sums of each wave, 24.1 so).
 template <int W> constexpr int kRowsPerGroup = W == 1 ? 4 : 1;
+template <int W> constexpr int kGradRows = W == 1 ? 4 : W == 2 ? 2 : 1;
 
-template <class T, class P, int W>
+template <class T, class P, int W, int R_>
 struct RowLane {
-    static constexpr int N = RowPiece<T>::N, NT = 64 * W, R = kRowsPerGroup<W>;
+    static constexpr int N = RowPiece<T>::N, NT = 64 * W, R = R_;
     using Raw = typename RowPiece<T>::vec;
     using Param = typename RowPiece<P, N>::vec;
     int lane, cols, pieces;
-    int64_t group;                          // of W waves, among all of the launch
-    __device__ RowLane(int n) : lane(W == 1 ? threadIdx.x & 63 : threadIdx.x), cols(n), pieces((n + N - 1) / N),
-                                group((int64_t)blockIdx.x * R + (W == 1 ? threadIdx.x >> 6 : 0)) {}
+    int sub;                                // which of the workgroup's rows
+    __device__ RowLane(int n) : lane(threadIdx.x % NT), cols(n), pieces((n + N - 1) / N), sub(R == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT)) {}
+    __device__ __forceinline__ int64_t first_row() const { return (int64_t)blockIdx.x * R + sub; }
     // f(c, piece) for the pieces of this lane
     template <class F> __device__ __forceinline__ void each(F &&f) const {
 #pragma unroll
@@ -72,17 +76,17 @@ struct RowLane {
 // bfloat16 97 us.)
 template <class T, class P, int W>
 __global__ __launch_bounds__(64 * W * kRowsPerGroup<W>) void layernorm(const LayerNormArgs a) {
-    using Lane = RowLane<T, P, W>;
+    using Lane = RowLane<T, P, W, kRowsPerGroup<W>>;
     constexpr int N = Lane::N;
     __shared__ float slots[2][W];
     const Lane l(a.cols);
     const int64_t step = (int64_t)gridDim.x * Lane::R;
     typename Lane::Param gamma[kPieces], beta[kPieces];
     typename Lane::Raw ahead[kPieces];
-    if (l.group < a.rows) l.load((const T *)a.x + l.group * a.ldx, ahead);
+    if (l.first_row() < a.rows) l.load((const T *)a.x + l.first_row() * a.ldx, ahead);
     l.params(a.gamma, gamma, 1.f);
     l.params(a.beta, beta, 0.f);
-    for (int64_t row = l.group; row < a.rows; row += step) {
+    for (int64_t row = l.first_row(); row < a.rows; row += step) {
         T *y = (T *)a.out + row * a.ldo;
         float v[kPieces][N], sum = 0.f, square = 0.f;
         l.each([&](int c, int) {
@@ -111,12 +115,16 @@ __global__ __launch_bounds__(64 * W * kRowsPerGroup<W>) void layernorm(const Lay
 }
 
 template <class T, class P, int W, bool SUMS>
-__global__ __launch_bounds__(64 * W * kRowsPerGroup<W>, kGradWaves) void layernorm_grad(const LayerNormArgs a) {
-    using Lane = RowLane<T, P, W>;
-    constexpr int N = Lane::N;
-    __shared__ float slots[4][W];
+__global__ __launch_bounds__(64 * W * kGradRows<W>, grad_waves(W)) void layernorm_grad(const LayerNormArgs a) {
+    using Lane = RowLane<T, P, W, kGradRows<W>>;
+    constexpr int N = Lane::N, R = Lane::R;
+    __shared__ float slots[4][R][W], pool[SUMS && R > 1 ? 2 : 1][SUMS && R > 1 ? 64 * W * kPieces * N : 1];
+    // Large workgroups have no registers left for gamma: each lane keeps its part in LDS.  (A spilled register is reloaded in the order of the loads, behind
+    // the next row: 16384 x 8192 binary16, FP32 parameters, 182 us with four spilled, 163 so.)
+    constexpr bool LDS = W >= 8;
+    __shared__ __attribute__((aligned(16))) float4 gamma_of[LDS ? kPieces : 1][LDS ? N / 4 : 1][LDS ? 64 * W : 1];
     const Lane l(a.cols);
-    const int64_t step = (int64_t)gridDim.x * Lane::R;
+    const int64_t step = (int64_t)gridDim.x * R;
     typename Lane::Param gamma[kPieces];
     typename Lane::Raw ahead_x[kPieces], ahead_dy[kPieces];
     float ahead_mean = 0.f, ahead_rstd = 0.f, sum_gamma[SUMS ? kPieces : 1][N] = {}, sum_beta[SUMS ? kPieces : 1][N] = {};
@@ -126,45 +134,94 @@ __global__ __launch_bounds__(64 * W * kRowsPerGroup<W>, kGradWaves) void layerno
         l.load((const T *)a.x + row * a.ldx, ahead_x);
         l.load((const T *)a.dy + row * a.lddy, ahead_dy);
     };
-    if (l.group < a.rows) load(l.group);
     l.params(a.gamma, gamma, 1.f);
+    if constexpr (LDS)
+        l.each([&](int c, int) {
+#pragma unroll
+            for (int q = 0; q < N / 4; ++q) gamma_of[c][q][threadIdx.x] = make_float4((float)gamma[c][4 * q], (float)gamma[c][4 * q + 1], (float)gamma[c][4 * q + 2], (float)gamma[c][4 * q + 3]);
+        });
+    auto times_gamma = [&](int c, const float (&d)[N], float (&g)[N]) {
+#pragma unroll
+        for (int q = 0; q < N / 4; ++q) {
+            if constexpr (LDS) {
+                const float4 v = gamma_of[c][q][threadIdx.x];
+                g[4 * q] = d[4 * q] * v.x; g[4 * q + 1] = d[4 * q + 1] * v.y; g[4 * q + 2] = d[4 * q + 2] * v.z; g[4 * q + 3] = d[4 * q + 3] * v.w;
+            } else {
+#pragma unroll
+                for (int i = 4 * q; i < 4 * q + 4; ++i) g[i] = d[i] * (float)gamma[c][i];
+            }
+        }
+    };
+    if (l.first_row() < a.rows) load(l.first_row());
     int turn = 0;
-    for (int64_t row = l.group; row < a.rows; row += step) {
-        T *dx = (T *)a.out + row * a.ldo;
+    // All rows of a workgroup go round together, for the barriers of their sums; those past the last row do nothing in between.
+    for (int64_t row = l.first_row(); row - l.sub < a.rows; row += step) {
+        const bool on = R == 1 || row < a.rows;
         const float mean = ahead_mean, rstd = ahead_rstd;
         typename Lane::Raw x[kPieces], dy[kPieces];
-        l.each([&](int c, int) { x[c] = ahead_x[c]; dy[c] = ahead_dy[c]; });
-        if (row + step < a.rows) load(row + step);
         float s1 = 0.f, s2 = 0.f;
-        l.each([&](int c, int p) {
-            l.elements(p, [&](int i, bool own) {
-                const float xh = ((float)x[c][i] - mean) * rstd, d = (float)dy[c][i], g = d * (float)gamma[c][i];
-                if constexpr (SUMS) {                                   // (those of other pieces' elements are not stored)
-                    sum_gamma[c][i] += d * xh;
-                    sum_beta[c][i] += d;
-                }
-                s1 += own ? g : 0.f;
-                s2 += own ? g * xh : 0.f;
+        if (on) {
+            l.each([&](int c, int) { x[c] = ahead_x[c]; dy[c] = ahead_dy[c]; });
+            if (row + step < a.rows) load(row + step);
+            l.each([&](int c, int p) {
+                float d[N], g[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) d[i] = (float)dy[c][i];
+                times_gamma(c, d, g);
+                l.elements(p, [&](int i, bool own) {
+                    const float xh = ((float)x[c][i] - mean) * rstd;
+                    if constexpr (SUMS) {                               // (those of other pieces' elements are not stored)
+                        sum_gamma[c][i] += d[i] * xh;
+                        sum_beta[c][i] += d[i];
+                    }
+                    s1 += own ? g[i] : 0.f;
+                    s2 += own ? g[i] * xh : 0.f;
+                });
             });
-        });
-        const float c1 = group_sum<W>(s1, slots[turn]) / a.width, c2 = group_sum<W>(s2, slots[turn + 1]) / a.width;
+        }
+        const float c1 = group_sum<W>(s1, slots[turn][l.sub]) / a.width, c2 = group_sum<W>(s2, slots[turn + 1][l.sub]) / a.width;
         turn ^= 2;
+        if (!on) continue;
+        T *dx = (T *)a.out + row * a.ldo;
         l.each([&](int c, int p) {
-            float o[N];
+            float d[N], o[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) d[i] = (float)dy[c][i];
+            times_gamma(c, d, o);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float xh = ((float)x[c][i] - mean) * rstd, g = (float)dy[c][i] * (float)gamma[c][i];
-                o[i] = rstd * (g - c1 - xh * c2);
+                const float xh = ((float)x[c][i] - mean) * rstd;
+                o[i] = rstd * (o[i] - c1 - xh * c2);
             }
             store_piece(dx, p, a.cols, o);
         });
     }
     if constexpr (SUMS) {
-        float *to = a.partial + l.group * 2 * a.cols;
-        l.each([&](int c, int p) {
-            store_piece(to, p, a.cols, sum_gamma[c]);
-            store_piece(to + a.cols, p, a.cols, sum_beta[c]);
-        });
+        float *to = a.partial + (int64_t)blockIdx.x * 2 * a.cols;
+        if constexpr (R == 1) {
+            l.each([&](int c, int p) {
+                store_piece(to, p, a.cols, sum_gamma[c]);
+                store_piece(to + a.cols, p, a.cols, sum_beta[c]);
+            });
+        } else {
+            for (int r = 0; r < R; ++r) {               // in the order of the rows
+                if (l.sub == r)
+                    l.each([&](int c, int p) {
+#pragma unroll
+                        for (int i = 0; i < N; ++i)
+                            if (own_element<N>(p, a.cols, i)) {
+                                const int col = first_of_piece<N>(p, a.cols) + i;
+                                pool[0][col] = (r ? pool[0][col] : 0.f) + sum_gamma[c][i];
+                                pool[1][col] = (r ? pool[1][col] : 0.f) + sum_beta[c][i];
+                            }
+                    });
+                __syncthreads();
+            }
+            for (int col = threadIdx.x; col < a.cols; col += 64 * W * R) {
+                to[col] = pool[0][col];
+                to[a.cols + col] = pool[1][col];
+            }
+        }
     }
 }
 
@@ -292,12 +349,12 @@ int waves_for(int64_t cols, int elem) {
         if (pieces <= (int64_t)64 * w * kPieces) return w;
     return 0;
 }
-// How many wave groups share the rows of a gradient: enough to fill the GPU, and no more sums than that for the second pass.
+// How many workgroups share the rows of a gradient: enough to fill the GPU, and no more sums than that for the second pass.
 int64_t grad_groups(int64_t rows, int64_t cols, int elem) {
     const int w = waves_for(cols, elem);
     if (w == 0) return std::min<int64_t>(rows, 64);
-    const int64_t groups = std::min<int64_t>(rows, kNumCU * 4 * kGradWaves / w);
-    return w == 1 ? (groups + 3) / 4 * 4 : groups;
+    const int rows_each = w == 1 ? kGradRows<1> : w == 2 ? kGradRows<2> : 1;
+    return std::min<int64_t>((rows + rows_each - 1) / rows_each, kNumCU * 4 * grad_waves(w) / (w * rows_each));
 }
 
 template <class F> fg_status with_type(int dtype, F &&f) {
@@ -397,8 +454,8 @@ fg_status fg_layernorm_grad(int64_t rows, int64_t cols, const fg_matrix *dY, con
             if (sums) hipLaunchKernelGGL((layernorm_column_sums<T>), dim3((unsigned)((cols + 255) / 256), (unsigned)groups), dim3(256), 0, stream, a);
             hipLaunchKernelGGL((layernorm_grad_wide<T, P>), dim3((unsigned)rows), dim3(1024), 0, stream, a);
         } else if (rows > 0) with_waves(w, [&](auto tag) {
-            constexpr int W = tag, R = kRowsPerGroup<W>;
-            const dim3 grid((unsigned)((groups + R - 1) / R)), block(64 * W * R);
+            constexpr int W = tag;
+            const dim3 grid((unsigned)groups), block(64 * W * kGradRows<W>);
             if (sums) hipLaunchKernelGGL((layernorm_grad<T, P, W, true>), grid, block, 0, stream, a);
             else hipLaunchKernelGGL((layernorm_grad<T, P, W, false>), grid, block, 0, stream, a);
         });

@@ -79,13 +79,13 @@ __device__ __forceinline__ float wave_reduce(float v, Op op) {
 __device__ __forceinline__ float wave_sum(float v) { return wave_reduce(v, [](float a, float b) { return a + b; }); }
 __device__ __forceinline__ float wave_max(float v) { return wave_reduce(v, [](float a, float b) { return __builtin_fmaxf(a, b); }); }
 
-// Sum over the W waves of a workgroup, in the order of the waves.  `slot` (W floats of LDS) must not be in use by a sum less than
+// Sum over W waves of a workgroup (the first W, the next W, ...), in the order of the waves; every wave of the workgroup takes part.  `slot` (W floats of LDS for each W waves) must not be in use by a sum less than
 // two barriers ago: callers alternate between two.
 template <int W>
 __device__ __forceinline__ float group_sum(float v, float *slot) {
     v = wave_sum(v);
     if constexpr (W > 1) {
-        if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+        if ((threadIdx.x & 63) == 0) slot[(threadIdx.x >> 6) % W] = v;
         __syncthreads();
         v = slot[0];
 #pragma unroll
