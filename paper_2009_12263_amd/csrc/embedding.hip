@@ -357,6 +357,12 @@ fg_status check_embedding(int64_t tokens, int64_t vocab, int64_t dim, const void
 }
 
 }  // namespace
+
+hipError_t load_embedding_kernels() {
+    hipFuncAttributes a;
+    return hipFuncGetAttributes(&a, (const void *)embedding<float>);
+}
+
 }  // namespace fg
 
 using namespace fg;

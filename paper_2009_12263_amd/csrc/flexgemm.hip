@@ -1321,6 +1321,8 @@ fg_status fg_init(void) {
             if (!tb.t[i].fn) continue;          // a variant that is not built for this tile
             if (fg_status st = prepare(tb.t[i], dev, per_cu)) return st;
         }
+    for (hipError_t e : {fg::load_layernorm_kernels(), fg::load_embedding_kernels(), fg::load_xent_kernels()})
+        if (e != hipSuccess) return fail(FG_ERR_LAUNCH, "loading the kernels on rows failed: %s", hipGetErrorString(e));
     float *st = nullptr;
     if (fg_status s2 = static_scratch(dev, &st)) return s2;
     std::lock_guard<std::mutex> lock(g_ws_mutex);

@@ -91,6 +91,11 @@ enum { CTILE_64x64 = 2, CTILE_64x64_KG2 = 3, CTILE_COUNT = 4 };
 int plan_tile(int64_t M, int64_t N, int64_t K);
 fg_status launch_product(const KernelEntry &k, GemmParams &p, hipStream_t stream);
 
+// Load the kernels of the operators on rows (each file's are one image), which their first launch would do otherwise.
+hipError_t load_layernorm_kernels();
+hipError_t load_embedding_kernels();
+hipError_t load_xent_kernels();
+
 // Second pass of a split-K product (splitk_reduce.hip).
 hipError_t launch_splitk_reduce(const float *W, int splits, int tile_begin, int tile_count, int bm, int bn, int tiles_m,
                                 int tiles_n, int M, int N, float alpha, float beta, const float *C, int64_t ldc, float *D,

@@ -390,6 +390,12 @@ fg_status check_layernorm(int64_t rows, int64_t cols, const fg_matrix *X, const 
 }
 
 }  // namespace
+
+hipError_t load_layernorm_kernels() {
+    hipFuncAttributes a;
+    return hipFuncGetAttributes(&a, (const void *)layernorm<float, float, 1>);
+}
+
 }  // namespace fg
 
 using namespace fg;

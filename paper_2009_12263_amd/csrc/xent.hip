@@ -266,6 +266,12 @@ const KernelEntry *kernel_table_xent(int kind, bool bf16) {
     return bf16 ? kernel_table_xent_round_bf16() : kernel_table_xent_round_f16();
 }
 
+
+hipError_t load_xent_kernels() {
+    hipFuncAttributes a;
+    return hipFuncGetAttributes(&a, (const void *)xent_join<16>);
+}
+
 }  // namespace fg
 
 using namespace fg;

@@ -156,3 +156,23 @@ def test_repeats_streams_and_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(first, captured)
+
+
+def test_offsets_beyond_32_bits():
+    """A table of which the last rows begin past 2^32 bytes: small integers, exact."""
+    vocab, dim, tokens = 600000, 4096, 200
+    g = torch.Generator().manual_seed(7)
+    ids = torch.cat([torch.randint(vocab - 50, vocab, (tokens // 2,), generator=g), torch.randint(0, vocab, (tokens // 2,), generator=g)]).cuda()
+    table = torch.zeros(vocab, dim, dtype=torch.float16, device="cuda")
+    table[ids] = rows(tokens, dim, torch.float16, g, ints=True)
+    y = torch.empty(tokens, dim, dtype=torch.float16, device="cuda")
+    fg.fg_embedding(table, ids, 2.0, y)
+    assert torch.equal(y, table[ids] * 2)
+    dy = rows(tokens, dim, torch.float16, g, ints=True)
+    fg.fg_embedding_grad(dy, ids, 1.0, None, table)
+    want = torch.zeros(tokens, dim, device="cuda")
+    rows_of, at = torch.unique(ids, return_inverse=True)
+    want.index_add_(0, at, dy.float())
+    assert torch.equal(table[rows_of].float(), want[:len(rows_of)])
+    table[rows_of] = 0
+    assert not table.any()

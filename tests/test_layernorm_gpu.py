@@ -188,3 +188,22 @@ def test_streams_repeats_and_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(first, captured))
+
+
+def test_offsets_beyond_32_bits():
+    """Rows of which the last begin past 2^32 bytes; first and last against the same rows by themselves (which the other tests check)."""
+    rows, cols = 270000, 8192
+    x = torch.empty(rows, cols, dtype=torch.float16, device="cuda")
+    part, dy, gamma, beta = make(64, cols, torch.float16, torch.float32, 3)
+    pick = torch.cat([torch.arange(32), torch.arange(rows - 32, rows)]).cuda()
+    x.zero_(); x[pick] = part
+    y, m, s = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    fg.fg_layernorm(x, gamma, beta, 1e-5, y, m, s)
+    y2, m2, s2 = torch.empty_like(part), torch.empty(64, device="cuda"), torch.empty(64, device="cuda")
+    fg.fg_layernorm(part, gamma, beta, 1e-5, y2, m2, s2)
+    assert torch.equal(y[pick], y2) and torch.equal(m[pick], m2) and torch.equal(s[pick], s2)
+    dx2 = torch.empty_like(part)
+    fg.fg_layernorm_grad(dy, part, gamma, m2, s2, dx2)
+    y.zero_(); y[pick] = dy
+    fg.fg_layernorm_grad(y, x, gamma, m, s, x)
+    assert torch.equal(x[pick], dx2)

@@ -191,3 +191,38 @@ def test_repeats_streams_and_graph(K):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(first, captured))
+
+
+@pytest.mark.parametrize("K,ld", [(4096, 4096), (4095, 4096)])
+def test_offsets_beyond_32_bits(K, ld):
+    """A vocabulary matrix of which the last rows begin past 2^32 bytes, with and without copies.  All rows but a few are zero, so that the
+    logits of the others are exactly zero and the formulas can be evaluated on the few."""
+    T, V = 24, 600000
+    gen = torch.Generator().manual_seed(6)
+    few = torch.cat([torch.arange(20), torch.arange(V - 20, V)])
+    w = torch.zeros(V, ld, dtype=torch.bfloat16, device="cuda")[:, :K]
+    some = rows(40, K, torch.bfloat16, gen, 4.0 / math.sqrt(K))
+    w[few.cuda()] = some
+    x = rows(T, K, torch.bfloat16, gen, 1.0)
+    targets = few[torch.randint(0, 40, (T,), generator=gen)]
+    loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    fg.fg_linear_xent(x, w, targets.cuda(), 1.0, loss, lse)
+    z = x.double().cpu() @ some.double().cpu().T
+    want = torch.log(torch.exp(z).sum(1) + (V - 40))
+    at = (targets[:, None] == few[None]).long().argmax(1)
+    tol = 4 * math.sqrt(K) * U * (x.double().cpu().abs() @ some.double().cpu().abs().T).max() + (V / 256 + 400) * U + 16 * U * (want.abs() + z.abs().max())
+    assert ((lse.double().cpu() - want).abs() <= tol).all()
+    assert ((loss.double().cpu() - (want - z.gather(1, at[:, None])[:, 0])).abs() <= 2 * tol).all()
+    dloss = torch.full((1,), 0.5).expand(T)
+    dx, dw = torch.empty_like(x), torch.empty(V, ld, dtype=torch.bfloat16, device="cuda")[:, :K]
+    fg.fg_linear_xent_grad(x, w, targets.cuda(), 1.0, lse, dloss.cuda(), dx, dw)
+    dz = (torch.exp(z - want[:, None]) - torch.zeros_like(z).scatter_(1, at[:, None], 1.0)) * 0.5
+    got, exact = dw[few.cuda()].double().cpu(), dz.T @ x.double().cpu()
+    bar = 2.0 ** -8 * 1.02 * (dz.abs().T @ x.double().cpu().abs() + exact.abs()) + 2 * tol.max() * (dz.abs().T @ x.double().cpu().abs())
+    assert ((got - exact).abs() <= bar).all()
+    bar = 2.0 ** -8 * 1.02 * (dz.abs() @ some.double().cpu().abs() + (dz @ some.double().cpu()).abs()) + 2 * tol.max() * (dz.abs() @ some.double().cpu().abs())
+    assert ((dx.double().cpu() - dz @ some.double().cpu()).abs() <= bar + 1e-30).all()
+    # a row of zero logits, in the middle: p is the same for all of them
+    p0 = (torch.exp(-want) * 0.5)[None] @ x.double().cpu()
+    mags = (torch.exp(-want) * 0.5)[None] @ x.double().cpu().abs()
+    assert ((dw[V // 2].double().cpu() - p0[0]).abs() <= 2.0 ** -8 * 1.02 * (p0[0].abs() + mags[0]) + 2 * tol.max() * mags[0]).all()
