@@ -8,7 +8,7 @@
 // id that reaches over the tile's edges are kept and joined in the order of the tiles by a last pass.  So an
 // id that half of the tokens have costs as little as a rare one.  Other waves of that last pass fill the rows without tokens.
 //
-// Sorting: runs of kRun tokens are sorted in LDS, one workgroup each, and merged in one step: a token's place in the whole list is
+// Sorting: runs of tokens are sorted in LDS, one workgroup each, and merged in one step: a token's place in the whole list is
 // the number of tokens in front of it in every run, found by bisection.
 #include "row_ops.hpp"
 
@@ -18,7 +18,6 @@ namespace fg {
 namespace {
 
 constexpr int kTile = 16;                   // sorted tokens per tile
-constexpr int kRunThreads = 1024, kRunWaves = kRunThreads / 64;
 constexpr int kDigit = 6;                   // bits that one pass of the sort takes
 
 // ---- lookup -----------------------------------------------------------------------------------------
@@ -54,19 +53,21 @@ __global__ __launch_bounds__(256) void embedding(const T *table, int64_t ld, con
 }
 
 // ---- sorting ----------------------------------------------------------------------------------------
-// Sorts run blockIdx.x of ITEMS * 1024 tokens by id, stably; ids that name no row count as `vocab` and come last.  Also clears the
-// bits of the rows that have tokens, and the count of open ids; a single run is the whole list, and its rows' bits are set here.
-template <int ITEMS>
-__global__ __launch_bounds__(kRunThreads) void embedding_sort(const void *ids, bool wide, int tokens, int vocab, int passes, uint32_t *keys, uint32_t *order, uint32_t *present, uint32_t *open_count) {
-    constexpr int RUN = ITEMS * kRunThreads;
+// Sorts run blockIdx.x of ITEMS * 64 WAVES tokens by id, stably; ids that name no row count as `vocab` and come last.  Also clears the
+// marks of the rows that have tokens, and the count of open ids; a single run is the whole list, and its rows' marks are set here.
+// A pass counts, per wave, the tokens of each of 64 digits, token by token in order (lanes with the same digit find each other by ballots), turns the counts
+// into places, digits first and then waves, and moves the tokens.
+template <int WAVES, int ITEMS>
+__global__ __launch_bounds__(64 * WAVES) void embedding_sort(const void *ids, bool wide, int tokens, int vocab, int passes, uint32_t *keys, uint32_t *order, uint4 *present,
+                                                             uint32_t *open_count) {
+    constexpr int THREADS = 64 * WAVES, RUN = ITEMS * THREADS;
     __shared__ uint32_t key[RUN];
     __shared__ uint16_t pos[RUN];
-    __shared__ uint32_t count[kRunWaves][1 << kDigit], total[kRunWaves];
-    static_assert(kRunWaves << kDigit == kRunThreads, "one thread per counter");
+    __shared__ uint32_t count[WAVES][1 << kDigit], total[WAVES];
+    static_assert(WAVES << kDigit == THREADS, "one thread per counter");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.x * RUN, n = min(tokens - first, RUN);
-    for (int64_t w = (int64_t)blockIdx.x * kRunThreads + threadIdx.x; w < (vocab + 31) / 32; w += (int64_t)gridDim.x * kRunThreads) present[w] = 0;
+    for (int64_t w = (int64_t)blockIdx.x * THREADS + threadIdx.x; w < (vocab + 15) / 16; w += (int64_t)gridDim.x * THREADS) present[w] = make_uint4(0, 0, 0, 0);
     if (blockIdx.x == 0 && threadIdx.x == 0) *open_count = 0;
-    if (gridDim.x == 1) __threadfence();                                // (before the first __syncthreads: bits are set behind the last)
 #pragma unroll
     for (int r = 0; r < ITEMS; ++r) {
         const int i = (wave * ITEMS + r) * 64 + lane;
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(kRunThreads) void embedding_sort(const void *ids, b
         }
         __syncthreads();
         // where the tokens of (digit, wave) begin: the sum of all counters in front of it, digits first
-        const int d = threadIdx.x / kRunWaves, w = threadIdx.x % kRunWaves;
+        const int d = threadIdx.x / WAVES, w = threadIdx.x % WAVES;
         const uint32_t own = count[w][d];
         uint32_t sum = own;
 #pragma unroll
@@ -110,8 +111,10 @@ __global__ __launch_bounds__(kRunThreads) void embedding_sort(const void *ids, b
         }
         if (lane == 63) total[wave] = sum;
         __syncthreads();
-        for (int o = 0; o < wave; ++o) sum += total[o];
-        count[w][d] = sum - own;
+        uint32_t front = lane < wave ? total[lane] : 0;                 // of the waves in front (at most 16)
+#pragma unroll
+        for (int s = 8; s > 0; s /= 2) front += __shfl_xor(front, s);
+        count[w][d] = sum - own + (uint32_t)__builtin_amdgcn_readfirstlane(front);
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < ITEMS; ++r) {
@@ -121,18 +124,19 @@ __global__ __launch_bounds__(kRunThreads) void embedding_sort(const void *ids, b
         }
         __syncthreads();
     }
-    for (int i = threadIdx.x; i < n; i += kRunThreads) {
+    for (int i = threadIdx.x; i < n; i += THREADS) {
         keys[first + i] = key[i];
         order[first + i] = first + pos[i];
-        if (gridDim.x == 1 && key[i] < (uint32_t)vocab && (i == 0 || key[i - 1] != key[i])) atomicOr(&present[key[i] >> 5], 1u << (key[i] & 31));
+        if (gridDim.x == 1 && key[i] < (uint32_t)vocab && (i == 0 || key[i - 1] != key[i])) ((uint8_t *)present)[key[i]] = 1;      // (cleared barriers ago)
     }
 }
 
-// Token i of the sorted runs goes to its place in the whole list: behind all smaller ids, and behind equal ones of earlier runs.  Four runs
-// are searched side by side, each a fixed number of steps (one after the other, 16384 tokens: 10.2 us, 8.6 so).
+// Token i of the sorted runs goes to its place in the whole list: behind all smaller ids, and behind equal ones of earlier runs.  SIDE runs are
+// searched side by side, a fixed number of steps: 8 where there are more than 4 (20624 tokens, six runs: 9.4 us, 11.7 four at a time).  Bound by the latency
+// of the steps, one load each.
+template <int SIDE>
 __global__ __launch_bounds__(256) void embedding_merge(const uint32_t *keys, const uint32_t *order, int tokens, int run, uint32_t *all_keys, uint32_t *all_order,
-                                                       int vocab, uint32_t *present) {
-    constexpr int SIDE = 4;
+                                                      int vocab, uint8_t *present) {
     const int i = blockIdx.x * 256 + threadIdx.x;
     if (i >= tokens) return;
     const int own = i / run, runs = (tokens + run - 1) / run;
@@ -142,23 +146,22 @@ __global__ __launch_bounds__(256) void embedding_merge(const uint32_t *keys, con
         int before[SIDE] = {};              // keys of the run that are in front
         for (int step = run; step > 0; step /= 2) {                     // (a power of two)
             uint32_t at[SIDE];
-            bool in[SIDE];
 #pragma unroll
             for (int s = 0; s < SIDE; ++s) {
-                const int r = r0 + s, to = before[s] + step, n = min(run, tokens - r * run);
-                in[s] = r < runs && r != own && to <= n;
-                at[s] = keys[in[s] ? r * run + to - 1 : i];
+                const int r = r0 + s, to = before[s] + step;
+                // (what is not there counts as behind)
+                at[s] = r < runs && r != own && to <= min(run, tokens - r * run) ? keys[r * run + to - 1] : ~0u;
             }
 #pragma unroll
             for (int s = 0; s < SIDE; ++s)
-                if (in[s] && (at[s] < k || (at[s] == k && r0 + s < own))) before[s] += step;
+                if (at[s] < k || (at[s] == k && r0 + s < own)) before[s] += step;
         }
 #pragma unroll
         for (int s = 0; s < SIDE; ++s) place += before[s];
     }
     all_keys[place] = k;
     all_order[place] = order[i];
-    if (k < (uint32_t)vocab && (i == own * run || keys[i - 1] != k)) atomicOr(&present[k >> 5], 1u << (k & 31));      // (bits: in any order)
+    if (k < (uint32_t)vocab && (i == own * run || keys[i - 1] != k)) present[k] = 1;
 }
 
 // ---- sums -------------------------------------------------------------------------------------------
@@ -166,7 +169,9 @@ struct EmbeddingGradArgs {
     const void *dy;
     const void *c;
     void *out;
-    const uint32_t *keys, *order, *present;
+    const uint32_t *keys, *order;
+    const uint8_t *present;                 // a byte for each row: it has tokens.  (Bits would be set by atomics, which the XCDs take one after another: 20624
+                                            // tokens of 4993 ids 29 us in embedding_merge, 9.4 so.)
     float *open;                            // tile t: the sum of the id that comes in over its front at 2 t dim, of the one that goes out at (2 t + 1) dim
     uint32_t *open_count, *open_tiles;      // tiles that an id which began there goes out of, in any order
     int64_t lddy, ldc, ldo;
@@ -238,23 +243,31 @@ __global__ __launch_bounds__(256) void embedding_sums(const EmbeddingGradArgs a)
     }
 }
 
-// Rows without tokens: zeros, or what is there.
-template <class T, class D>
+// Rows without tokens: zeros, or what is there.  A lane looks at the marks of ROWS rows at once: 4 where it only stores (65536 rows of 4096 bfloat16 74 us, 79 one
+// by one, 77 with 16), one where it loads too (50001 of 1001 FP32 73 us, 81 with 4: rows follow each other).
+template <bool ADD> constexpr int kFillRows = ADD ? 1 : 4;
+template <class T, class D, bool ADD>
 __device__ __forceinline__ void embedding_fill(const EmbeddingGradArgs &a, int64_t item, int lane, int pieces) {
-    constexpr int N = RowPiece<T>::N, AHEAD = 4;
+    constexpr int N = RowPiece<T>::N, AHEAD = 4, ROWS = kFillRows<ADD>;
     const int at = lane & ((1 << a.shift) - 1), rows = 64 >> a.shift, chunks = (pieces + (AHEAD << a.shift) - 1) / (AHEAD << a.shift);
-    const int64_t row = item / chunks * rows + (lane >> a.shift);
+    const int64_t row0 = (item / chunks * rows + (lane >> a.shift)) * ROWS;
     const int first = (int)(item % chunks) * (AHEAD << a.shift) + at;
-    if (row >= a.vocab || (a.present[row >> 5] >> (row & 31) & 1)) return;
-    float v[AHEAD][N] = {};
-    if (a.c) {
+    if (row0 >= a.vocab) return;
+    const uint32_t marks = ROWS == 1 ? a.present[row0] : ((const uint32_t *)a.present)[row0 / 4];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const int64_t row = row0 + r;
+        if (row >= a.vocab || (marks >> r * 8 & 1)) continue;
+        float v[AHEAD][N] = {};
+        if (ADD) {
+#pragma unroll
+            for (int c = 0; c < AHEAD; ++c)
+                if (first + (c << a.shift) < pieces) load_piece((const D *)a.c + row * a.ldc, first + (c << a.shift), a.dim, v[c]);
+        }
 #pragma unroll
         for (int c = 0; c < AHEAD; ++c)
-            if (first + (c << a.shift) < pieces) load_piece((const D *)a.c + row * a.ldc, first + (c << a.shift), a.dim, v[c]);
+            if (first + (c << a.shift) < pieces) store_piece((D *)a.out + row * a.ldo, first + (c << a.shift), a.dim, v[c]);
     }
-#pragma unroll
-    for (int c = 0; c < AHEAD; ++c)
-        if (first + (c << a.shift) < pieces) store_piece((D *)a.out + row * a.ldo, first + (c << a.shift), a.dim, v[c]);
 }
 
 // Joins the sums of an id that goes out of a tile it began in: that tile's, then those of the tiles that it comes into.  A workgroup takes one such id
@@ -266,7 +279,7 @@ __global__ __launch_bounds__(256) void embedding_join(const EmbeddingGradArgs a)
     __shared__ float part[WAVES][N][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pieces = (a.dim + N - 1) / N;
     if ((int)blockIdx.x >= a.join_groups) {
-        embedding_fill<T, D>(a, (int64_t)(blockIdx.x - a.join_groups) * WAVES + wave, lane, pieces);
+        embedding_fill<T, D, ADD>(a, (int64_t)(blockIdx.x - a.join_groups) * WAVES + wave, lane, pieces);
         return;
     }
     const int p = blockIdx.x % a.chunks * 64 + lane;
@@ -323,7 +336,9 @@ int lanes_shift(int pieces) {
     while (s < 6 && (1 << s) < pieces) ++s;
     return s;
 }
-int run_items(int64_t tokens) { return tokens <= kRunThreads ? 1 : tokens <= 65536 ? 4 : 16; }
+// Tokens of a run (powers of two: embedding_merge).  Few tokens are sorted by few waves or few items a lane: up to 256 tokens 4.5 us, and 11.6 in a run of 4096;
+// 1024 tokens 7.2 us and 11.
+int run_of(int64_t tokens) { return tokens <= 256 ? 256 : tokens <= 1024 ? 1024 : tokens <= 65536 ? 4096 : 16384; }
 
 // The workspace: sorted runs, the whole list, the rows that have tokens, open sums.
 struct EmbeddingSpace {
@@ -335,7 +350,7 @@ struct EmbeddingSpace {
         all_keys = order + up(4 * tokens);
         all_order = all_keys + up(4 * tokens);
         present = all_order + up(4 * tokens);
-        open_count = present + up((vocab + 31) / 32 * 4);
+        open_count = present + up(vocab);
         open_tiles = open_count + 256;
         open = open_tiles + up((tokens + kTile - 1) / kTile * 4);
         bytes = open + (tokens + kTile - 1) / kTile * 2 * dim * 4;
@@ -406,25 +421,32 @@ fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg
     const EmbeddingSpace at(tokens, vocab, dim);
     if (fg_status st = check_workspace(workspace, workspace_bytes, at.bytes)) return st;
     char *w = (char *)workspace;
-    uint32_t *keys = (uint32_t *)(w + at.keys), *order = (uint32_t *)(w + at.order), *present = (uint32_t *)(w + at.present);
+    uint32_t *keys = (uint32_t *)(w + at.keys), *order = (uint32_t *)(w + at.order);
+    uint8_t *present = (uint8_t *)(w + at.present);
     uint32_t *open_count = (uint32_t *)(w + at.open_count), *open_tiles = (uint32_t *)(w + at.open_tiles);
     uint32_t *all_keys = (uint32_t *)(w + at.all_keys), *all_order = (uint32_t *)(w + at.all_order);
     hipStream_t stream = (hipStream_t)hip_stream;
     int passes = 1;
     while (((vocab + 1) >> (passes * kDigit)) != 0) ++passes;             // the largest key is vocab + 1
     const bool wide = index_dtype == FG_I64;
-    const int items = run_items(tokens), run = items * kRunThreads;
+    const int run = run_of(tokens);
     const unsigned runs = (unsigned)std::max<int64_t>(1, (tokens + run - 1) / run);
-    auto sort = [&](auto tag) {
-        constexpr int ITEMS = decltype(tag)::value;
-        hipLaunchKernelGGL((embedding_sort<ITEMS>), dim3(runs), dim3(kRunThreads), 0, stream, ids, wide, (int)tokens, (int)vocab, passes, runs == 1 ? all_keys : keys,
-                           runs == 1 ? all_order : order, present, open_count);
+    auto sort = [&](auto waves, auto items) {
+        constexpr int WAVES = decltype(waves)::value, ITEMS = decltype(items)::value;
+        hipLaunchKernelGGL((embedding_sort<WAVES, ITEMS>), dim3(runs), dim3(64 * WAVES), 0, stream, ids, wide, (int)tokens, (int)vocab, passes, runs == 1 ? all_keys : keys,
+                           runs == 1 ? all_order : order, (uint4 *)present, open_count);
     };
-    if (items == 1) sort(std::integral_constant<int, 1>{});
-    else if (items == 4) sort(std::integral_constant<int, 4>{});
-    else sort(std::integral_constant<int, 16>{});
-    if (runs > 1)
-        hipLaunchKernelGGL(embedding_merge, dim3((unsigned)((tokens + 255) / 256)), dim3(256), 0, stream, keys, order, (int)tokens, run, all_keys, all_order, (int)vocab, present);
+    using std::integral_constant;
+    if (run == 256) sort(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+    else if (run == 1024) sort(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+    else if (run == 4096) sort(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+    else sort(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+    auto merge = [&](auto side) {
+        hipLaunchKernelGGL((embedding_merge<decltype(side)::value>), dim3((unsigned)((tokens + 255) / 256)), dim3(256), 0, stream, keys, order, (int)tokens, run, all_keys,
+                           all_order, (int)vocab, present);
+    };
+    if (runs > 4) merge(integral_constant<int, 8>{});
+    else if (runs > 1) merge(integral_constant<int, 4>{});
     if (fg_status st = check_launch("embedding_sort")) return st;
     const bool in_place = Cin && Cin->re == dtable->re;
     auto launch = [&](auto t, auto d) {
@@ -432,12 +454,13 @@ fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg
         using D = decltype(d);
         const int64_t pieces = (dim + RowPiece<T>::N - 1) / RowPiece<T>::N, tiles = (tokens + kTile - 1) / kTile, chunks = (pieces + 63) / 64;
         const int shift = lanes_shift((int)((pieces + 3) / 4));
-        const int64_t fills = in_place ? 0 : (vocab + (64 >> shift) - 1) / (64 >> shift) * ((pieces + (4 << shift) - 1) / (4 << shift));
-        const int64_t joins = tiles > 1 ? std::min<int64_t>(tiles - 1, 512) * chunks : 0, rest = joins + (fills + 3) / 4;
+        const int64_t joins = tiles > 1 ? std::min<int64_t>(tiles - 1, 512) * chunks : 0;
         const EmbeddingGradArgs a = {dY->re, Cin ? Cin->re : nullptr, dtable->re, all_keys, all_order, present, (float *)(w + at.open), open_count, open_tiles, dY->ld,
                                      Cin ? Cin->ld : 0, dtable->ld, (int)tokens, (int)vocab, (int)dim, (int)tiles, (int)chunks, (int)joins, shift, scale};
         auto run = [&](auto tag) {
             constexpr bool ADD = decltype(tag)::value;
+            const int64_t rows = (64 >> shift) * kFillRows<ADD>, fills = in_place ? 0 : (vocab + rows - 1) / rows * ((pieces + (4 << shift) - 1) / (4 << shift));
+            const int64_t rest = joins + (fills + 3) / 4;
             if (tiles > 0) hipLaunchKernelGGL((embedding_sums<T, D, ADD>), dim3((unsigned)((tiles * chunks + 3) / 4)), dim3(256), 0, stream, a);
             if (rest > 0) hipLaunchKernelGGL((embedding_join<T, D, ADD>), dim3((unsigned)rest), dim3(256), 0, stream, a);
         };
