@@ -13,6 +13,7 @@
 // memory, from the general matrix kernel to kernels on rows: 8192 tokens x 50000 words x 1001 with gradients 6516 us, 3122 so).
 #include <algorithm>
 #include <cstring>
+#include <type_traits>
 
 #include "cache_policy.hpp"
 #include "xent_kernel.hpp"
@@ -115,10 +116,72 @@ __global__ __launch_bounds__(256) void xent_round(const float *in, int64_t ld, c
     }
 }
 
+// ---- dw of few tokens ------------------------------------------------------------------------------------------
+// dw = scale dz^T x where the tokens fit KS steps of 32 k of the matrix units: all of it is writing dw.  A wave takes 128 words and 128 columns
+// with one read of both operands.  A lane reads 16 bytes of 8 tokens' rows and turns the 8 x 8 values over in registers (one byte permutation each
+// pair): 8 vectors of 8 tokens, of which the j-th of dz and the i-th of x serve the product of words 8 m + j with columns 8 n + i.  A lane's
+// results of i = 0 .. 7 are then 16 bytes of a row of dw, and those of 16 lanes two lines.  Bound by the writes (65536 words x 2048: 16 tokens 42.8 us or 6.3 TB/s, 64 tokens
+// 58); the tiled kernels, whose one wave a SIMD does not write while it multiplies, take 84 and 87 (50001 x 1001, 33 tokens: 32 and 81).
+template <class T>
+__device__ __forceinline__ floatx4 mfma_16x16x32(typename RowPiece<T>::vec a, typename RowPiece<T>::vec b, floatx4 c) {
+    if constexpr (std::is_same<T, bf16_t>::value) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+template <class T, int KS>
+__global__ __launch_bounds__(256) void xent_dw_few(const T *dz, int64_t ld_dz, const T *x, int64_t ldx, const float *factor, T *out, int64_t ldo, int tokens,
+                                                   int words, int dim, int strips) {
+    typedef typename RowPiece<T>::vec vec;
+    const int lane = threadIdx.x & 63, at = lane & 15, quarter = lane >> 4;
+    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t word0 = item / strips * 128;
+    if (word0 >= words) return;
+    const int p = (int)(item % strips) * 16 + at, pieces = (dim + 7) / 8, there = min(p, pieces - 1);
+    const bool in = word0 + at * 8 < ld_dz;
+    vec a[KS][8], b[KS][8];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        vec w[8] = {}, v[8] = {};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int t = s * 32 + quarter * 8 + e;
+            if (t < tokens) {
+                if (in) w[e] = *(const vec *)(dz + t * ld_dz + word0 + at * 8);
+                v[e] = load_raw<T, 8>(x + t * ldx, there, dim);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                a[s][j][e] = w[e][j];
+                b[s][j][e] = v[e][j];
+            }
+    }
+    const float f = factor[1];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        floatx4 sum[8] = {};
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = mfma_16x16x32<T>(a[s][j], b[s][i], sum[i]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int64_t word = word0 + (quarter * 4 + r) * 8 + j;
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = sum[i][r] * f;
+            if (word < words && p < pieces) store_piece(out + word * ldo, p, dim, v);
+        }
+    }
+}
+
 // ---- host ----------------------------------------------------------------------------------------------------
 constexpr int64_t kPieceBytes = 256ll << 20;        // of dz: what the memory-side cache holds
 constexpr int64_t kCopyBytes = 64ll << 20;          // of a piece of W that is copied
 constexpr int64_t kTokenBlock = 16384;              // tokens whose statistics are kept at a time
+constexpr int64_t kFewTokens = 64;                  // whose dw xent_dw_few writes
 constexpr int64_t kFewestWords = 256;               // of a piece; pieces begin at multiples of it
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -368,12 +431,27 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
         p.lse = lse; p.dloss = dloss; p.dloss_inc = (int32_t)dloss_inc; p.factor = factor;
         p.D = (float *)dz.re; p.ldd = at.ld_dz;
         if (fg_status st = launch_product(kz, p, stream)) return st;
-        // neither operand is K-contiguous: any number of tokens
-        const KernelEntry &kw = kernel_table_xent(XENT_ROUND, bf16)[xent_tile(n, dim, tokens)];
-        XentParams q = product(kw, false, n, dim, tokens, dz.re, at.ld_dz, x.re, x.ld);
-        q.factor = factor;
-        q.D = (float *)row_at(dW, v0); q.ldd = dW->ld;
-        if (fg_status st = launch_product(kw, q, stream)) return st;
+        if (tokens <= kFewTokens) {
+            const int strips = (int)((dim + 127) / 128);
+            const int64_t waves = (n + 127) / 128 * strips;
+            with_half(X->dtype, [&](auto t) {
+                using T = decltype(t);
+                auto few = [&](auto steps) {
+                    hipLaunchKernelGGL((xent_dw_few<T, decltype(steps)::value>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, (const T *)dz.re, at.ld_dz, (const T *)x.re, x.ld,
+                                       factor, (T *)row_at(dW, v0), dW->ld, (int)tokens, (int)n, (int)dim, strips);
+                };
+                if (tokens <= 32) few(std::integral_constant<int, 1>{});
+                else few(std::integral_constant<int, 2>{});
+            });
+            if (fg_status st = check_launch("xent_dw_few")) return st;
+        } else {
+            // neither operand is K-contiguous: any number of tokens
+            const KernelEntry &kw = kernel_table_xent(XENT_ROUND, bf16)[xent_tile(n, dim, tokens)];
+            XentParams q = product(kw, false, n, dim, tokens, dz.re, at.ld_dz, x.re, x.ld);
+            q.factor = factor;
+            q.D = (float *)row_at(dW, v0); q.ldd = dW->ld;
+            if (fg_status st = launch_product(kw, q, stream)) return st;
+        }
         // dz has zeros from n on to the next multiple of 8
         if (fg_status st = gemm_stored(tokens, dim, up(n, 8), n, 1.f, &dz, &w, v0 == 0 ? 0.f : 1.f, &sum_dx, &sum_dx, stream)) return st;
     }

@@ -102,6 +102,18 @@ def test_more_words_than_a_piece(dtype):
     check(9000, 8500, 16, dtype)                # (pieces of fewer words)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T", [7, 8, 9, 31, 32, 33, 63, 64, 65])
+@pytest.mark.parametrize("V,K,ld,offset", [(127, 129, 131, 1), (129, 128, 128, 0), (1030, 7, 7, 0), (264, 264, 272, 8)])
+def test_few_tokens(T, V, K, ld, offset, dtype):
+    check(T, V, K, dtype, ld=ld, offset=offset)
+
+
+def test_few_tokens_in_small_pieces():
+    """A workspace of four pieces of 256 words, full of NaNs: the last piece ends inside a run of 128 words."""
+    check(40, 1001, 72, torch.bfloat16, grad_workspace=torch.full((fg.fg_linear_xent_grad_workspace(40, 256, 72),), 255, dtype=torch.uint8, device="cuda"))
+
+
 @pytest.mark.parametrize("kind", ["all", "some", "none"])
 @pytest.mark.parametrize("K", [64, 63])
 def test_targets_and_gradients_of_the_loss(kind, K):
