@@ -117,50 +117,53 @@ __global__ __launch_bounds__(256) void xent_round(const float *in, int64_t ld, c
 }
 
 // ---- dw of few tokens ------------------------------------------------------------------------------------------
-// dw = scale dz^T x where the tokens fit KS steps of 32 k of the matrix units: all of it is writing dw.  A wave takes 128 words and 128 columns
-// with one read of both operands.  A lane reads 16 bytes of 8 tokens' rows and turns the 8 x 8 values over in registers (one byte permutation each
-// pair): 8 vectors of 8 tokens, of which the j-th of dz and the i-th of x serve the product of words 8 m + j with columns 8 n + i.  A lane's
-// results of i = 0 .. 7 are then 16 bytes of a row of dw, and those of 16 lanes two lines.  Bound by the writes (65536 words x 2048: 16 tokens 42.8 us or 6.3 TB/s, 64 tokens
-// 58); the tiled kernels, whose one wave a SIMD does not write while it multiplies, take 84 and 87 (50001 x 1001, 33 tokens: 32 and 81).
+// dw = scale dz^T x where the tokens fit KS steps of 32 k of the matrix units: all of it is writing dw.  A wave takes 16 J words and 128 columns
+// with one read of both operands.  A lane reads J words and 8 columns of 8 tokens' rows and turns the values over in registers (one byte permutation each
+// pair): vectors of 8 tokens, of which the j-th of dz and the i-th of x serve the product of words J m + j with columns 8 n + i.  A lane's
+// results of i = 0 .. 7 are then 16 bytes of a row of dw, and those of 16 lanes two lines.  Bound by the writes (65536 words x 2048: 16 tokens 41 us or 6.5 TB/s, 64 tokens
+// 56); the tiled kernels, whose one wave a SIMD does not write while it multiplies, take 84 and 88 (50001 x 1001, 33 tokens: 25 and 81).  With 128 tokens the operands fill
+// the registers: 103 us and 103.
 template <class T>
 __device__ __forceinline__ floatx4 mfma_16x16x32(typename RowPiece<T>::vec a, typename RowPiece<T>::vec b, floatx4 c) {
     if constexpr (std::is_same<T, bf16_t>::value) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-template <class T, int KS>
-__global__ __launch_bounds__(256) void xent_dw_few(const T *dz, int64_t ld_dz, const T *x, int64_t ldx, const float *factor, T *out, int64_t ldo, int tokens,
+template <class T, int KS, int J>
+__global__ __launch_bounds__(256, 2) void xent_dw_few(const T *dz, int64_t ld_dz, const T *x, int64_t ldx, const float *factor, T *out, int64_t ldo, int tokens,
                                                    int words, int dim, int strips) {
     typedef typename RowPiece<T>::vec vec;
     const int lane = threadIdx.x & 63, at = lane & 15, quarter = lane >> 4;
     const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t word0 = item / strips * 128;
+    typedef typename RowPiece<T, J>::vec words_vec;
+    const int64_t word0 = item / strips * (16 * J);
     if (word0 >= words) return;
     const int p = (int)(item % strips) * 16 + at, pieces = (dim + 7) / 8, there = min(p, pieces - 1);
-    const bool in = word0 + at * 8 < ld_dz;
-    vec a[KS][8], b[KS][8];
+    const bool in = word0 + at * J < ld_dz;
+    vec a[KS][J], b[KS][8];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-        vec w[8] = {}, v[8] = {};
+        words_vec w[8] = {};
+        vec v[8] = {};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int t = s * 32 + quarter * 8 + e;
             if (t < tokens) {
-                if (in) w[e] = *(const vec *)(dz + t * ld_dz + word0 + at * 8);
+                if (in) w[e] = *(const words_vec *)(dz + t * ld_dz + word0 + at * J);
                 v[e] = load_raw<T, 8>(x + t * ldx, there, dim);
             }
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int e = 0; e < 8; ++e) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                a[s][j][e] = w[e][j];
-                b[s][j][e] = v[e][j];
-            }
+            for (int j = 0; j < J; ++j) a[s][j][e] = w[e][j];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) b[s][i][e] = v[e][i];
+        }
     }
     const float f = factor[1];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < J; ++j) {
         floatx4 sum[8] = {};
 #pragma unroll
         for (int s = 0; s < KS; ++s)
@@ -168,11 +171,12 @@ __global__ __launch_bounds__(256) void xent_dw_few(const T *dz, int64_t ld_dz, c
             for (int i = 0; i < 8; ++i) sum[i] = mfma_16x16x32<T>(a[s][j], b[s][i], sum[i]);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int64_t word = word0 + (quarter * 4 + r) * 8 + j;
+            const int64_t word = word0 + (quarter * 4 + r) * J + j;
+            if (word >= words || p >= pieces) continue;
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = sum[i][r] * f;
-            if (word < words && p < pieces) store_piece(out + word * ldo, p, dim, v);
+            store_piece(out + word * ldo, p, dim, v);
         }
     }
 }
@@ -433,15 +437,20 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
         if (fg_status st = launch_product(kz, p, stream)) return st;
         if (tokens <= kFewTokens) {
             const int strips = (int)((dim + 127) / 128);
-            const int64_t waves = (n + 127) / 128 * strips;
             with_half(X->dtype, [&](auto t) {
                 using T = decltype(t);
-                auto few = [&](auto steps) {
-                    hipLaunchKernelGGL((xent_dw_few<T, decltype(steps)::value>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, (const T *)dz.re, at.ld_dz, (const T *)x.re, x.ld,
-                                       factor, (T *)row_at(dW, v0), dW->ld, (int)tokens, (int)n, (int)dim, strips);
+                auto few = [&](auto steps, auto run) {
+                    constexpr int KS = decltype(steps)::value, J = decltype(run)::value;
+                    const int64_t waves = (n + 16 * J - 1) / (16 * J) * strips;
+                    hipLaunchKernelGGL((xent_dw_few<T, KS, J>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, (const T *)dz.re, at.ld_dz, (const T *)x.re, x.ld, factor,
+                                       (T *)row_at(dW, v0), dW->ld, (int)tokens, (int)n, (int)dim, strips);
                 };
-                if (tokens <= 32) few(std::integral_constant<int, 1>{});
-                else few(std::integral_constant<int, 2>{});
+                using std::integral_constant;
+                // Fewer waves than there are SIMDs: 64 words each instead of 128 (2496 words x 1000: 16 tokens 5.0 us and 6.7, 64 tokens 5.9 and 8.0;
+                // 65536 x 2048: 53 and 41, 73 and 56).
+                const bool small = (n + 127) / 128 * strips < 1024;
+                if (tokens <= 32) small ? few(integral_constant<int, 1>{}, integral_constant<int, 4>{}) : few(integral_constant<int, 1>{}, integral_constant<int, 8>{});
+                else small ? few(integral_constant<int, 2>{}, integral_constant<int, 4>{}) : few(integral_constant<int, 2>{}, integral_constant<int, 8>{});
             });
             if (fg_status st = check_launch("xent_dw_few")) return st;
         } else {
