@@ -250,11 +250,15 @@ template <class Space> Space space_within(int64_t bytes, int64_t tokens, int64_t
     while (words > kFewestWords && Space(words, tokens, vocab, dim, c).bytes > bytes) words = std::max(kFewestWords, words / 2 / kFewestWords * kFewestWords);
     return Space(words, tokens, vocab, dim, c);
 }
-// What the queries give serves rows of any alignment: where dim lets the kernels take them as they are, copies with the smallest pieces.
+// What the queries give serves rows of any alignment: where dim lets the kernels take them as they are, each of the four combinations of copies, with W
+// copied in the smallest pieces.  (No combination stands for another: the tile, and with it the statistics, follows the words of a piece.)
 template <class Space> int64_t space_for(int64_t tokens, int64_t vocab, int64_t dim) {
     const int64_t words = Space::preferred(tokens, vocab, dim);
     if (dim % 8 != 0) return Space(words, tokens, vocab, dim, Copies(true, true)).bytes;
-    return std::max(Space(words, tokens, vocab, dim, Copies(false, false)).bytes, Space(std::min(kFewestWords, up(vocab, 8)), tokens, vocab, dim, Copies(true, true)).bytes);
+    int64_t bytes = 0;
+    for (bool x : {false, true})
+        for (bool w : {false, true}) bytes = std::max(bytes, Space(w ? std::min(kFewestWords, words) : words, tokens, vocab, dim, Copies(x, w)).bytes);
+    return bytes;
 }
 
 fg_status check_xent(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *X, const fg_matrix *W, const void *targets, int32_t index_dtype) {

@@ -1,0 +1,38 @@
+"""CPU test: the workspace that the queries of the linear cross entropy give is enough for rows of any alignment.  Without a GPU a call that
+passes its checks ends at its first launch (FG_ERR_LAUNCH); the addresses are made up, so this does not run where there is one."""
+import ctypes as C
+import random
+
+import pytest
+import torch
+
+from paper_2009_12263_amd import binding as fg
+
+pytestmark = pytest.mark.skipif(torch.cuda.device_count() > 0, reason="made-up addresses: not where a GPU would follow them")
+
+PTR = 0x100000
+
+
+def rows(ld, shift=0):
+    return C.byref(fg.fg_matrix(PTR + 2 * shift, None, fg.FG_BF16, fg.FG_ROW, ld))
+
+
+def forward(T, V, K, x_shift, w_shift):
+    lib = fg.load_library()
+    return lib.fg_linear_xent(T, V, K, rows(K, x_shift), rows(K, w_shift), PTR, fg.FG_I64, 1.0, PTR, PTR, PTR, lib.fg_linear_xent_workspace(T, V, K), None)
+
+
+def gradient(T, V, K, x_shift, w_shift):
+    lib = fg.load_library()
+    return lib.fg_linear_xent_grad(T, V, K, rows(K, x_shift), rows(K, w_shift), PTR, fg.FG_I64, 1.0, PTR, PTR, 1, rows(K), rows(K), PTR,
+                                   lib.fg_linear_xent_grad_workspace(T, V, K), None)
+
+
+@pytest.mark.parametrize("call", [forward, gradient])
+@pytest.mark.parametrize("x_shift,w_shift", [(0, 0), (1, 0), (0, 1), (1, 1)])
+def test_the_queried_workspace_serves_any_alignment(call, x_shift, w_shift):
+    rng = random.Random(5)
+    sizes = [(16384, 320, 256), (15348, 1044, 8), (32277, 548, 304), (13148, 636, 24), (4784, 3338, 728), (1, 1, 1), (1, 1, 8), (64, 100000, 72)]
+    sizes += [(rng.randrange(1, 1 << rng.randrange(1, 17)), rng.randrange(1, 1 << rng.randrange(1, 18)), rng.randrange(1, 600) * rng.choice([1, 8])) for _ in range(2000)]
+    refused = [s for s in sizes if call(*s, x_shift, w_shift) != fg.FG_ERR_LAUNCH]
+    assert not refused, (len(refused), refused[:5], fg.fg_last_error())
