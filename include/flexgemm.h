@@ -343,7 +343,7 @@ int64_t fg_linear_xent_workspace(int64_t tokens, int64_t vocab, int64_t dim);
  * The logits are formed again, a piece of the vocabulary at a time; dz is rounded to the type of X (binary16: relative to the
  * largest dloss, so that it neither overflows nor vanishes where dX and dW do not) and multiplied by W and X into FP32.
  *   dloss  : FP32, one value per token, or with dloss_inc 0 a single one for all (1 otherwise).
- *   dX, dW : of the type of X, the shapes of X and W.
+ *   dX, dW : of the type of X, the shapes of X and W (FG_ERR_UNSUPPORTED for rows of more than 2^21 - 4 values).
  * The product with dX splits K through the workspace of fg_gemm where that pays (fg_init before a graph capture).
  */
 fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *X, const fg_matrix *W, const void *targets, int32_t index_dtype,

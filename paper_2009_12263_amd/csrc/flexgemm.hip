@@ -1364,7 +1364,8 @@ static fg_status gemm_impl(int64_t M, int64_t N, int64_t K, float alpha, const f
     auto reach = [&](bool kc, int64_t ld) { return (kc ? 255 * ld + 64 : 64 * ld + 256) * ab_elem_bytes; };
     if ((!q.a_diag && reach(q.a_kc, q.lda) >= (1ll << 31)) || (!q.b_diag && reach(q.b_kc, q.ldb) >= (1ll << 31)))
         return fail(FG_ERR_UNSUPPORTED, "leading dimension of A or B too large (row-of-K operands: below 2^22 elements, others below 2^24)");
-    const int64_t cd_limit = q.ilv ? (1ll << 20) : (1ll << 21);
+    static_assert((255 * (fg::kKContiguousLd - 1) + 64) * 2 < (1ll << 31), "");
+    const int64_t cd_limit = q.ilv ? (1ll << 20) : fg::kResultLd;
     if (q.ldc >= cd_limit || q.ldd >= cd_limit) return fail(FG_ERR_UNSUPPORTED, "leading dimension of C or D must be below 2^21 elements (2^20 interleaved)");
     p.C = q.C; p.D = q.D; p.C_im = q.C_im; p.D_im = q.D_im; p.ldc = q.ldc; p.ldd = q.ldd;
     p.bias = q.bias; p.bias_dim = q.bias_dim; p.act = q.act; p.has_c = q.C != nullptr;

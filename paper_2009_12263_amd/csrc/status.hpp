@@ -14,6 +14,10 @@ fg_status fail(fg_status st, const char *fmt, ...) __attribute__((format(printf,
 fg_status gemm_stored(int64_t M, int64_t N, int64_t K, int64_t k_rows, float alpha, const fg_matrix *A, const fg_matrix *B, float beta,
                       const fg_matrix *C, const fg_matrix *D, void *hip_stream);
 
+// Leading dimensions that the tiled kernels take stay below these: of A and B where they are K-contiguous (a lane's offsets within a tile's rows fit 31 bits),
+// and of C and D.
+constexpr int64_t kKContiguousLd = 1ll << 22, kResultLd = 1ll << 21;
+
 inline bool aligned_to(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 }  // namespace fg

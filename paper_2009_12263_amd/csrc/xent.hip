@@ -187,6 +187,7 @@ constexpr int64_t kCopyBytes = 64ll << 20;          // of a piece of W that is c
 constexpr int64_t kTokenBlock = 16384;              // tokens whose statistics are kept at a time
 constexpr int64_t kFewTokens = 64;                  // whose dw xent_dw_few writes
 constexpr int64_t kFewestWords = 256;               // of a piece; pieces begin at multiples of it
+constexpr int64_t kMostWords = kKContiguousLd - kFewestWords;          // of a piece of dz, whose rows the product with dX reads along the words
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
@@ -211,7 +212,7 @@ struct Copies {
     bool x, w;
     Copies(bool x_, bool w_) : x(x_), w(w_) {}
     Copies(int64_t dim, const fg_matrix *X, const fg_matrix *W) {
-        auto fits = [&](const fg_matrix *m) { return dim % 8 == 0 && aligned_to(m->re, 16) && m->ld % 8 == 0 && m->ld < (1 << 22); };
+        auto fits = [&](const fg_matrix *m) { return dim % 8 == 0 && aligned_to(m->re, 16) && m->ld % 8 == 0 && m->ld < kKContiguousLd; };
         x = !fits(X);
         w = !fits(W);
     }
@@ -242,7 +243,7 @@ struct GradSpace {
         w = x + (c.x ? up(tokens * ld * 2, 256) : 0);
         bytes = w + (c.w ? words * ld * 2 : 0);
     }
-    static int64_t preferred(int64_t tokens, int64_t vocab, int64_t) { return words_of(kPieceBytes, 2 * tokens, 2048, vocab); }
+    static int64_t preferred(int64_t tokens, int64_t vocab, int64_t) { return std::min(words_of(kPieceBytes, 2 * tokens, 2048, vocab), kMostWords); }
 };
 // The space of a call: pieces of the preferred size, or smaller ones that fit `bytes`.
 template <class Space> Space space_within(int64_t bytes, int64_t tokens, int64_t vocab, int64_t dim, Copies c) {
@@ -404,6 +405,7 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
     if (fg_status st = check_rows("dX", dX, tokens, dim)) return st;
     if (fg_status st = check_rows("dW", dW, vocab, dim)) return st;
     if (dX->dtype != X->dtype || dW->dtype != X->dtype) return fail(FG_ERR_UNSUPPORTED, "dX and dW must have the element type of X");
+    if (up(dim, 4) >= kResultLd) return fail(FG_ERR_UNSUPPORTED, "gradients of rows of more than 2^21 - 4 values are not supported");
     if (dloss_inc != 0 && dloss_inc != 1) return fail(FG_ERR_SHAPE, "dloss_inc must be 0 or 1");
     if (dim == 0) return FG_OK;
     if (tokens > 0 && (!lse || !dloss)) return fail(FG_ERR_NULL, "lse or dloss is NULL");

@@ -80,3 +80,12 @@ def test_statistics_of_a_copied_operand_fit_the_queried_workspace():
     plain, plain_lse = torch.empty_like(loss), torch.empty_like(lse)
     fg.fg_linear_xent(x.contiguous().clone(), w, targets.cuda(), 1.0, plain, plain_lse)
     assert torch.equal(loss, plain) and torch.equal(lse, plain_lse)
+
+
+@pytest.mark.parametrize("T,V", [(3, 2 ** 22 + 5000), (31, 2 ** 22 + 3)])
+def test_more_words_than_a_row_of_dz_holds(T, V):
+    """Few tokens whose dz would be one piece by its size, but of rows longer than a product takes."""
+    print("[case] many words", T, V, flush=True)
+    x, w, targets, dloss = inputs(T, V, 8, torch.bfloat16, 6)
+    targets[1] = V - 1
+    compare(x, w, targets, 1.0, dloss, run(x, w, targets.cuda(), 1.0, dloss.cuda()), norms=False)
