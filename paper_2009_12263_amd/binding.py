@@ -388,6 +388,16 @@ def _vector(t: Optional[torch.Tensor], n: int, name: str, dtype, dev: int) -> Op
     return t.data_ptr()
 
 
+def _torch_stream(stream):
+    """A stream argument as torch's allocator knows streams."""
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = _stream_handle(stream)
+    if handle == 2:                 # hipStreamPerThread: one handle for the streams of all threads, which the allocator would take for one
+        raise ValueError("workspace: a call on hipStreamPerThread needs one from the caller")
+    return torch.cuda.ExternalStream(0 if handle == 1 else handle)        # (1: the default stream by its other name)
+
+
 def _workspace(given: Optional[torch.Tensor], need: int, stream, dev: int):
     """(address, bytes, what keeps it alive) of the caller's workspace, or of one from torch's allocator for the stream of the call."""
     if given is not None:
@@ -396,9 +406,14 @@ def _workspace(given: Optional[torch.Tensor], need: int, stream, dev: int):
         return given.data_ptr(), given.numel() * given.element_size(), given
     if need <= 0:
         return None, 0, None
-    t = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", dev))
-    if stream is not None:          # torch takes it for memory of the current stream
-        t.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream_handle(stream)))
+    make = lambda: torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", dev))
+    if stream is None:
+        t = make()
+    else:
+        # Memory of the call's own stream: what the current stream has freed may still be written by kernels waiting there, and nothing
+        # orders the call behind them.
+        with torch.cuda.stream(_torch_stream(stream)):
+            t = make()
     return t.data_ptr(), need, t
 
 
