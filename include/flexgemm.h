@@ -279,8 +279,9 @@ fg_status fg_contract_plan(int32_t nA, const int32_t *modesA, const int64_t *str
  * dimension of any size from the row's length on and element-aligned pointers, of FG_F16, FG_BF16 or (where it is said) FG_F32
  * elements.  All arithmetic is FP32 or wider; every result is rounded to nearest even once, when it is stored.  Results do not
  * depend on scheduling: the same call gives the same bits.  Calls that need scratch memory take a 16-byte aligned workspace from the
- * caller, of at least the bytes that the query beside it gives; it holds nothing from one call to the next, needs no clearing and may be
- * reused by the next call on the same stream.  These calls allocate nothing and only enqueue kernels: they may be recorded into a HIP graph.
+ * caller, of the bytes that the query beside it gives; it holds nothing from one call to the next, needs no clearing and may be
+ * reused by the next call on the same stream.  These calls allocate nothing, share no memory with other calls and only enqueue kernels: they may be recorded into
+ * HIP graphs (fg_init first: a kernel's first launch loads it), and graphs with workspaces of their own may run side by side.
  * Sizes of zero are accepted.
  */
 
@@ -344,7 +345,8 @@ int64_t fg_linear_xent_workspace(int64_t tokens, int64_t vocab, int64_t dim);
  * largest dloss, so that it neither overflows nor vanishes where dX and dW do not) and multiplied by W and X into FP32.
  *   dloss  : FP32, one value per token, or with dloss_inc 0 a single one for all (1 otherwise).
  *   dX, dW : of the type of X, the shapes of X and W (FG_ERR_UNSUPPORTED for rows of more than 2^21 - 4 values).
- * The product with dX splits K through the workspace of fg_gemm where that pays (fg_init before a graph capture).
+ * The product with dX splits its K where that pays, through the workspace.  A smaller workspace than the query gives is accepted as long as it holds pieces of
+ * 256 words; sums are then formed in another order.
  */
 fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *X, const fg_matrix *W, const void *targets, int32_t index_dtype,
                               float scale, const float *lse, const float *dloss, int64_t dloss_inc, const fg_matrix *dX, const fg_matrix *dW,

@@ -1333,10 +1333,11 @@ fg_status fg_init(void) {
 // static_only: the allocation-free entry point.  Same plan as the ordinary call; partial products
 // of a K split go to the static scratch array (FG_ERR_UNSUPPORTED if they do not fit), and nothing
 // on this path allocates, frees or creates anything.
-// k_rows (0: K): an operand that is not K-contiguous stores its first k_rows k's only, and the others count as zero.
+// stored: what gemm_stored adds.
+struct Stored { int64_t k_rows; float *scratch; int64_t scratch_bytes; };
 static fg_status gemm_impl(int64_t M, int64_t N, int64_t K, float alpha, const fg_matrix *A, const fg_matrix *B,
                            float beta, const fg_matrix *C, const fg_matrix *D, const fg_epilogue *ep, bool dual,
-                           const fg_load_transforms *lt, void *hip_stream, bool static_only = false, int64_t k_rows = 0) {
+                           const fg_load_transforms *lt, void *hip_stream, bool static_only = false, const Stored *stored = nullptr) {
     Problem q;
     if (fg_status st = normalise(M, N, K, alpha, A, B, beta, C, D, ep, dual, lt, q)) return st;
     if (q.M == 0 || q.N == 0) return FG_OK;
@@ -1356,6 +1357,7 @@ static fg_status gemm_impl(int64_t M, int64_t N, int64_t K, float alpha, const f
     p.b_rs = q.b_kc ? q.ldb : 1; p.b_ks = q.b_kc ? 1 : q.ldb;
     // stored span of each operand, rounded up to whole 16-byte chunks (see TileLoader::begin)
     auto span8 = [](bool kc, int64_t rows, int64_t k, int64_t ld) { int64_t s = kc ? (rows - 1) * ld + k : (k - 1) * ld + rows; return (s + 7) / 8 * 8; };
+    const int64_t k_rows = stored ? stored->k_rows : 0;
     p.a_span = q.K > 0 ? span8(q.a_kc, q.M, q.a_kc || !k_rows ? q.K : k_rows, q.lda) : 0;
     p.b_span = q.K > 0 ? span8(q.b_kc, q.N, q.b_kc || !k_rows ? q.K : k_rows, q.ldb) : 0;
     // A and B may be of any size; what must fit 32 bits is the byte offset a lane forms inside one
@@ -1402,7 +1404,10 @@ static fg_status gemm_impl(int64_t M, int64_t N, int64_t K, float alpha, const f
                                         "static scratch array of the allocation-free entry point holds %lld (use fg_gemm_ex)",
                     S, (long long)need, (long long)kStaticScratchBytes);
     Scratch scratch;
-    if (fg_status st = scratch.acquire(static_only, dev, stream)) return st;
+    if (stored) {
+        if (need > stored->scratch_bytes) return launch(k, p, stream);
+        scratch.ptr = stored->scratch;
+    } else if (fg_status st = scratch.acquire(static_only, dev, stream)) return st;
     if (first > 0) {
         fg::GemmParams head = p;
         head.tile_count = first;
@@ -1434,8 +1439,16 @@ fg_status fg::launch_product(const KernelEntry &k, GemmParams &p, hipStream_t st
 }
 
 fg_status fg::gemm_stored(int64_t M, int64_t N, int64_t K, int64_t k_rows, float alpha, const fg_matrix *A, const fg_matrix *B, float beta,
-                          const fg_matrix *C, const fg_matrix *D, void *hip_stream) {
-    return gemm_impl(M, N, K, alpha, A, B, beta, C, D, nullptr, false, nullptr, hip_stream, false, k_rows);
+                          const fg_matrix *C, const fg_matrix *D, float *scratch, int64_t scratch_bytes, void *hip_stream) {
+    const Stored stored = {k_rows, scratch, scratch_bytes};
+    return gemm_impl(M, N, K, alpha, A, B, beta, C, D, nullptr, false, nullptr, hip_stream, false, &stored);
+}
+int64_t fg::gemm_stored_scratch(int64_t M, int64_t N, int64_t K) {
+    Problem q = {};
+    q.M = N; q.N = M; q.K = K;          // as normalise() exchanges them
+    q.b_kc = true;                      // (the element type decides nothing about a split)
+    Plan plan{0, 1, 1};
+    return select_kernel(q, &plan) ? scratch_need(plan, q.M, q.N) : 0;
 }
 
 extern "C" {

@@ -10,9 +10,12 @@ namespace fg {
 fg_status fail(fg_status st, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 
 // fg_gemm where an operand that is not K-contiguous stores its first k_rows k's only (0: all of them); the others count as zero, and K can be
-// rounded up to what the tiled kernels take.  For operands that meet their alignment (aligned16 pointers, leading dimensions of 8).
+// rounded up to what the tiled kernels take.  For operands that meet their alignment (aligned16 pointers, leading dimensions of 8).  Partial products of a split of
+// K go to `scratch` (16-byte aligned); one that does not fit its scratch_bytes is computed in one pass.  Nothing is allocated.
 fg_status gemm_stored(int64_t M, int64_t N, int64_t K, int64_t k_rows, float alpha, const fg_matrix *A, const fg_matrix *B, float beta,
-                      const fg_matrix *C, const fg_matrix *D, void *hip_stream);
+                      const fg_matrix *C, const fg_matrix *D, float *scratch, int64_t scratch_bytes, void *hip_stream);
+// The scratch that gemm_stored has a use for, where A, B and D are row-major.
+int64_t gemm_stored_scratch(int64_t M, int64_t N, int64_t K);
 
 // Leading dimensions that the tiled kernels take stay below these: of A and B where they are K-contiguous (a lane's offsets within a tile's rows fit 31 bits),
 // and of C and D.

@@ -232,7 +232,7 @@ struct StatsSpace {
     }
     static int64_t preferred(int64_t, int64_t vocab, int64_t dim) { return words_of(kCopyBytes, up(dim, 8) * 2, kFewestWords, vocab); }
 };
-// Gradient: dz of a piece, the sums of dx, and copies of operands.
+// Gradient: dz of a piece, the sums of dx, and copies of operands.  What the workspace has behind them serves a split of the product with dX.
 struct GradSpace {
     int64_t words, ld, ld_dz, ld_dx, dz, dx, factor, x, w, bytes;
     GradSpace(int64_t words_, int64_t tokens, int64_t, int64_t dim, Copies c) : words(words_), ld(up(dim, 8)), ld_dz(up(words, 8)), ld_dx(up(dim, 4)) {
@@ -241,7 +241,7 @@ struct GradSpace {
         factor = dx + up(tokens * ld_dx * 4, 256);
         x = factor + 256;
         w = x + (c.x ? up(tokens * ld * 2, 256) : 0);
-        bytes = w + (c.w ? words * ld * 2 : 0);
+        bytes = w + (c.w ? up(words * ld * 2, 256) : 0);
     }
     static int64_t preferred(int64_t tokens, int64_t vocab, int64_t) { return std::min(words_of(kPieceBytes, 2 * tokens, 2048, vocab), kMostWords); }
 };
@@ -259,6 +259,14 @@ template <class Space> int64_t space_for(int64_t tokens, int64_t vocab, int64_t 
     int64_t bytes = 0;
     for (bool x : {false, true})
         for (bool w : {false, true}) bytes = std::max(bytes, Space(w ? std::min(kFewestWords, words) : words, tokens, vocab, dim, Copies(x, w)).bytes);
+    return bytes;
+}
+
+// The partial products of dX's product, of the pieces that the preferred size gives.
+int64_t grad_scratch(int64_t tokens, int64_t vocab, int64_t dim) {
+    const int64_t words = GradSpace::preferred(tokens, vocab, dim), last = vocab % words;
+    int64_t bytes = last > 0 ? gemm_stored_scratch(tokens, dim, up(last, 8)) : 0;
+    if (vocab >= words) bytes = std::max(bytes, gemm_stored_scratch(tokens, dim, up(words, 8)));
     return bytes;
 }
 
@@ -395,7 +403,7 @@ fg_status fg_linear_xent(int64_t tokens, int64_t vocab, int64_t dim, const fg_ma
 
 int64_t fg_linear_xent_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim) {
     if (tokens < 0 || vocab <= 0 || dim <= 0) return 0;
-    return space_for<GradSpace>(tokens, vocab, dim);
+    return space_for<GradSpace>(tokens, vocab, dim) + (tokens > 0 ? grad_scratch(tokens, vocab, dim) : 0);
 }
 
 fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *X, const fg_matrix *W, const void *targets, int32_t index_dtype,
@@ -468,7 +476,9 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
             if (fg_status st = launch_product(kw, q, stream)) return st;
         }
         // dz has zeros from n on to the next multiple of 8
-        if (fg_status st = gemm_stored(tokens, dim, up(n, 8), n, 1.f, &dz, &w, v0 == 0 ? 0.f : 1.f, &sum_dx, &sum_dx, stream)) return st;
+        if (fg_status st = gemm_stored(tokens, dim, up(n, 8), n, 1.f, &dz, &w, v0 == 0 ? 0.f : 1.f, &sum_dx, &sum_dx, (float *)(space + at.bytes),
+                                        workspace_bytes - at.bytes, stream))
+            return st;
     }
     return round(sums, dX, tokens);
 }

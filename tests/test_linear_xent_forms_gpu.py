@@ -89,3 +89,33 @@ def test_more_words_than_a_row_of_dz_holds(T, V):
     x, w, targets, dloss = inputs(T, V, 8, torch.bfloat16, 6)
     targets[1] = V - 1
     compare(x, w, targets, 1.0, dloss, run(x, w, targets.cuda(), 1.0, dloss.cuda()), norms=False)
+
+
+def test_captured_calls_with_workspaces_of_their_own_run_side_by_side():
+    """Two graphs, each with the gradient of its own loss (a product with dX that is split over K), replayed on two streams at a time."""
+    fg.fg_init()
+    T, V, K = 300, 20000, 256
+    graphs, outs, firsts, keep = [], [], [], []
+    for seed in (1, 2):
+        x, w, targets, dloss = inputs(T, V, K, torch.bfloat16, seed)
+        targets, dloss = targets.cuda(), dloss.cuda()
+        loss, lse, dx, dw = run(x, w, targets, 0.5, dloss)
+        firsts.append((dx, dw))
+        mine, ws = (torch.empty_like(dx), torch.empty_like(dw)), torch.empty(fg.fg_linear_xent_grad_workspace(T, V, K), dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            fg.fg_linear_xent_grad(x, w, targets, 0.5, lse, dloss, *mine, workspace=ws)
+        graphs.append(graph); outs.append(mine); keep.append((x, w, targets, dloss, lse, ws))
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(10):
+        for o in outs:
+            for t in o:
+                t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(outs, firsts):
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
