@@ -327,8 +327,8 @@ int64_t fg_embedding_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim);
 /*
  * Softmax cross entropy of a linear layer over a vocabulary, without the logits in memory: with z[t][v] = scale * sum over k of X[t][k] * W[v][k],
  *   lse[t] = log of the sum over v of exp(z[t][v]),   loss[t] = lse[t] - z[t][targets[t]].
- * A token whose target is not in [0, vocab) is left out: its loss is 0, and it has no part in a gradient (its lse is
- * that of its logits all the same).  No logits are kept: the vocabulary is walked in pieces, of which the statistics remain.
+ * A token whose target is not in [0, vocab) is left out: its loss is 0, and it has no part in a gradient, whatever its row of X or its dloss holds (its
+ * lse is that of its logits all the same).  No logits are kept: the vocabulary is walked in pieces, of which the statistics remain.
  *   X : tokens x dim, W : vocab x dim, both FG_F16 or both FG_BF16 (multiplied exactly, summed in FP32); targets : `tokens` indices of type
  *   index_dtype (FG_I32, FG_I64); loss, lse : `tokens` FP32 values each; vocab >= 1.
  * Infinite logits give a NaN.  Rows that are not 16-byte aligned, or not of a multiple of 8 values, are copied into the workspace first, W a piece at a

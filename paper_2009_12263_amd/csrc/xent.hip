@@ -32,6 +32,16 @@ __device__ __forceinline__ float group_max(float v, float *slot) {
     return v;
 }
 
+// Piece p of eight of a row of `cols` values, zeros behind them.
+template <class T>
+__device__ __forceinline__ typename RowPiece<T>::vec padded_piece(const T *row, int p, int cols) {
+    if ((p + 1) * 8 <= cols) return load_raw<T, 8>(row, p, cols);
+    typename RowPiece<T>::vec v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = p * 8 + e < cols ? row[p * 8 + e] : (T)0.f;
+    return v;
+}
+
 // Copies rows of `cols` values to rows of ldo (a multiple of 8) that are aligned, with zeros behind them.
 template <class T>
 __global__ __launch_bounds__(256) void xent_pad(const T *in, int64_t ld, T *out, int64_t ldo, int64_t rows, int cols) {
@@ -39,12 +49,7 @@ __global__ __launch_bounds__(256) void xent_pad(const T *in, int64_t ld, T *out,
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (int64_t)gridDim.x * 256) {
         const int64_t row = i / pieces;
         const int p = (int)(i - row * pieces);
-        typename RowPiece<T>::vec v;
-        if ((p + 1) * 8 <= cols) v = load_raw<T, 8>(in + row * ld, p, cols);
-        else
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = p * 8 + e < cols ? in[row * ld + p * 8 + e] : (T)0.f;
-        *(typename RowPiece<T>::vec *)(out + row * ldo + p * 8) = v;
+        *(typename RowPiece<T>::vec *)(out + row * ldo + p * 8) = padded_piece(in + row * ld, p, cols);
     }
 }
 
@@ -80,13 +85,28 @@ __global__ __launch_bounds__(1024) void xent_join(const XentStat *stats, int par
     loss[t] = load_index(targets, wide, t, vocab) < 0 ? 0.f : total - z_target[t];
 }
 
-// ---- scaling of dz ------------------------------------------------------------------------------------------
-// dz is kept as c dz, c = 2^k / max |dloss|.  With one dloss for all tokens (the mean of the losses) what is rounded is then exp(z - lse) - 1 or exp(z -
+// ---- what the gradient's products begin with ---------------------------------------------------------------
+// The first workgroup: the scaling of dz.  dz is kept as c dz, c = 2^k / max |dloss|.  With one dloss for all tokens (the mean of the losses) what is rounded is then exp(z - lse) - 1 or exp(z -
 // lse) itself: relative to dloss, the same rounding of nearly -1 in every token would shift all of dx and dw one way (8192 tokens,
 // bfloat16: error against 64 bits 2.6e-3 so, half of which is the rounding of the results).  Binary16: k = 14, so that |c dz|
 // is at most 2^14 and what is 2^-38 of the largest is still a number.  factor[0] = c, factor[1] = scale / c.
-__global__ __launch_bounds__(1024) void xent_factor(const float *dloss, int64_t dloss_inc, const void *targets, bool wide, int vocab, int64_t tokens, bool half,
-                                                    float scale, float *factor) {
+//
+// The others: x's rows for the products, aligned and padded like xent_pad's, with zeros for the tokens that are left out.  Their dz is zero, but a row of a
+// token nobody asks for may hold anything, and in dw = dz^T x zero times infinity or NaN would reach every word.
+template <class T>
+__global__ __launch_bounds__(1024) void xent_prepare(const float *dloss, int64_t dloss_inc, const void *targets, bool wide, int vocab, int64_t tokens, float scale,
+                                                     float *factor, const T *x, int64_t ldx, T *out, int64_t ldo, int cols) {
+    if (blockIdx.x > 0) {
+        const int pieces = (int)(ldo / 8);
+        for (int64_t i = (int64_t)(blockIdx.x - 1) * 1024 + threadIdx.x; i < tokens * pieces; i += (int64_t)(gridDim.x - 1) * 1024) {
+            const int64_t t = i / pieces;
+            const int p = (int)(i - t * pieces);
+            typename RowPiece<T>::vec v = {};
+            if (load_index(targets, wide, t, vocab) >= 0) v = padded_piece(x + t * ldx, p, cols);
+            *(typename RowPiece<T>::vec *)(out + t * ldo + p * 8) = v;
+        }
+        return;
+    }
     __shared__ float slots[16];
     float top = 0.f;
     for (int64_t t = threadIdx.x; t < tokens; t += 1024)
@@ -94,24 +114,26 @@ __global__ __launch_bounds__(1024) void xent_factor(const float *dloss, int64_t 
     top = group_max<16>(top, slots);
     if (threadIdx.x == 0) {
         const bool usable = top > 0.f && top < __builtin_inff();
-        const float range = half ? 16384.f : 1.f, unit = usable ? __builtin_fmaxf(top, 1e-30f) : 1.f;
+        const float range = std::is_same<T, f16_t>::value ? 16384.f : 1.f, unit = usable ? __builtin_fmaxf(top, 1e-30f) : 1.f;
         factor[0] = usable ? range / unit : 1.f;
         factor[1] = usable ? scale * (unit / range) : scale;
     }
 }
 
-// rows x cols FP32 values times *factor (no `in`: zeros), rounded into `out`
+// rows x cols FP32 values times *factor (no `in`: zeros; no target: zeros in that row), rounded into `out`
 template <class T>
-__global__ __launch_bounds__(256) void xent_round(const float *in, int64_t ld, const float *factor, T *out, int64_t ldo, int64_t rows, int cols) {
+__global__ __launch_bounds__(256) void xent_round(const float *in, int64_t ld, const float *factor, const void *targets, bool wide, int vocab, T *out, int64_t ldo,
+                                                  int64_t rows, int cols) {
     const int pieces = (cols + 7) / 8;
     const float f = *factor;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (int64_t)gridDim.x * 256) {
         const int64_t row = i / pieces;
         const int p = (int)(i - row * pieces);
+        const bool live = in && load_index(targets, wide, row, vocab) >= 0;
         float v[8];
-        if (in) load_piece(in + row * ld, p, cols, v);
+        if (live) load_piece(in + row * ld, p, cols, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = in ? v[e] * f : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = live ? v[e] * f : 0.f;
         store_piece(out + row * ldo, p, cols, v);
     }
 }
@@ -130,8 +152,8 @@ __device__ __forceinline__ floatx4 mfma_16x16x32(typename RowPiece<T>::vec a, ty
 }
 
 template <class T, int KS, int J>
-__global__ __launch_bounds__(256, 2) void xent_dw_few(const T *dz, int64_t ld_dz, const T *x, int64_t ldx, const float *factor, T *out, int64_t ldo, int tokens,
-                                                   int words, int dim, int strips) {
+__global__ __launch_bounds__(256, 2) void xent_dw_few(const T *dz, int64_t ld_dz, const T *x, int64_t ldx, const void *targets, bool wide, int vocab, const float *factor,
+                                                   T *out, int64_t ldo, int tokens, int words, int dim, int strips) {
     typedef typename RowPiece<T>::vec vec;
     const int lane = threadIdx.x & 63, at = lane & 15, quarter = lane >> 4;
     const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -145,14 +167,20 @@ __global__ __launch_bounds__(256, 2) void xent_dw_few(const T *dz, int64_t ld_dz
     for (int s = 0; s < KS; ++s) {
         words_vec w[8] = {};
         vec v[8] = {};
+        int target[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int t = s * 32 + quarter * 8 + e;
+            target[e] = -1;
             if (t < tokens) {
+                target[e] = load_index(targets, wide, t, vocab);
                 if (in) w[e] = *(const words_vec *)(dz + t * ld_dz + word0 + at * J);
                 v[e] = load_raw<T, 8>(x + t * ldx, there, dim);
             }
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (target[e] < 0) v[e] = vec{};                            // (left out: see xent_prepare)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
 #pragma unroll
@@ -235,12 +263,14 @@ struct StatsSpace {
 // Gradient: dz of a piece, the sums of dx, and copies of operands.  What the workspace has behind them serves a split of the product with dX.
 struct GradSpace {
     int64_t words, ld, ld_dz, ld_dx, dz, dx, factor, x, w, bytes;
-    GradSpace(int64_t words_, int64_t tokens, int64_t, int64_t dim, Copies c) : words(words_), ld(up(dim, 8)), ld_dz(up(words, 8)), ld_dx(up(dim, 4)) {
+    bool copy_x;                            // (the tiled product with dw reads rows without those of left-out tokens; xent_dw_few looks at the targets itself)
+    GradSpace(int64_t words_, int64_t tokens, int64_t, int64_t dim, Copies c)
+        : words(words_), ld(up(dim, 8)), ld_dz(up(words, 8)), ld_dx(up(dim, 4)), copy_x(c.x || tokens > kFewTokens) {
         dz = 0;
         dx = dz + up(tokens * ld_dz * 2, 256);
         factor = dx + up(tokens * ld_dx * 4, 256);
         x = factor + 256;
-        w = x + (c.x ? up(tokens * ld * 2, 256) : 0);
+        w = x + (copy_x ? up(tokens * ld * 2, 256) : 0);
         bytes = w + (c.w ? up(words * ld * 2, 256) : 0);
     }
     static int64_t preferred(int64_t tokens, int64_t vocab, int64_t) { return std::min(words_of(kPieceBytes, 2 * tokens, 2048, vocab), kMostWords); }
@@ -429,15 +459,21 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
         const unsigned groups = (unsigned)std::min<int64_t>((rows * ((dim + 7) / 8) + 255) / 256, 8192);
         with_half(X->dtype, [&](auto t) {
             using T = decltype(t);
-            hipLaunchKernelGGL((xent_round<T>), dim3(groups), dim3(256), 0, stream, in, at.ld_dx, factor + 1, (T *)out->re, out->ld, rows, (int)dim);
+            hipLaunchKernelGGL((xent_round<T>), dim3(groups), dim3(256), 0, stream, in, at.ld_dx, factor + 1, targets, wide, (int)vocab, (T *)out->re, out->ld, rows,
+                               (int)dim);
         });
         return check_launch("xent_round");
     };
-    hipLaunchKernelGGL(xent_factor, dim3(1), dim3(1024), 0, stream, dloss, dloss_inc, targets, wide, (int)vocab, tokens, !bf16, scale, factor);
-    if (fg_status st = check_launch("xent_factor")) return st;
+    fg_matrix x = rows_of(X->re, X->dtype, X->ld), w;
+    with_half(X->dtype, [&](auto t) {
+        using T = decltype(t);
+        const int64_t pieces = at.copy_x ? tokens * (at.ld / 8) : 0;
+        hipLaunchKernelGGL((xent_prepare<T>), dim3((unsigned)(1 + std::min<int64_t>((pieces + 1023) / 1024, 2048))), dim3(1024), 0, stream, dloss, dloss_inc, targets, wide,
+                           (int)vocab, tokens, scale, factor, (const T *)X->re, X->ld, (T *)(space + at.x), at.ld, (int)dim);
+    });
+    if (fg_status st = check_launch("xent_prepare")) return st;
     if (tokens == 0) return round(nullptr, dW, vocab);
-    fg_matrix x, w;
-    if (fg_status st = aligned_rows(X, 0, tokens, dim, copies.x, space + at.x, at.ld, x, stream)) return st;
+    if (at.copy_x) x = rows_of(space + at.x, X->dtype, at.ld);
     const fg_matrix dz = rows_of(space + at.dz, X->dtype, at.ld_dz), sum_dx = rows_of(sums, FG_F32, at.ld_dx);
     for (int64_t v0 = 0; v0 < vocab; v0 += at.words) {
         const int64_t n = std::min(at.words, vocab - v0);
@@ -456,8 +492,8 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
                 auto few = [&](auto steps, auto run) {
                     constexpr int KS = decltype(steps)::value, J = decltype(run)::value;
                     const int64_t waves = (n + 16 * J - 1) / (16 * J) * strips;
-                    hipLaunchKernelGGL((xent_dw_few<T, KS, J>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, (const T *)dz.re, at.ld_dz, (const T *)x.re, x.ld, factor,
-                                       (T *)row_at(dW, v0), dW->ld, (int)tokens, (int)n, (int)dim, strips);
+                    hipLaunchKernelGGL((xent_dw_few<T, KS, J>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, (const T *)dz.re, at.ld_dz, (const T *)x.re, x.ld, targets, wide,
+                                       (int)vocab, factor, (T *)row_at(dW, v0), dW->ld, (int)tokens, (int)n, (int)dim, strips);
                 };
                 using std::integral_constant;
                 // Fewer waves than there are SIMDs: 64 words each instead of 128 (2496 words x 1000: 16 tokens 5.0 us and 6.7, 64 tokens 5.9 and 8.0;

@@ -119,23 +119,26 @@ struct XentCfg : Base {
         }
     }
 
-    // Rows that are left out: relative to an lse of infinity their exponentials are zero.
+    // Rows that are left out are zeros whatever their logits are, NaN and infinities too.
     template <int I, class Blocks>
     __device__ static __forceinline__ void dz_of_rows(const Params &p, const Blocks &blocks, int row, int word, float row_lse, float dloss, int n_base, int n_first, bool edge) {
         const bool there = row < p.M, live = word >= 0;
         const int col = word - p.v0;
-        const float factor = live ? dloss * p.factor[0] : 0.f, lse = live ? row_lse * kLog2e : __builtin_inff();
+        const float factor = dloss * p.factor[0], lse = row_lse * kLog2e;
         const float scale = p.alpha * kLog2e;
         const bool hits = __ballot(live && col >= n_base && col < n_base + Base::WTN) != 0;
         T *out = (T *)p.D + (int64_t)row * p.ldd + n_first;
         if (!edge && !hits) {
-            runs<I>(blocks, out, there, [&](float a, int) { return __builtin_amdgcn_exp2f(__builtin_fmaf(a, scale, -lse)) * factor; }, [](int) { return true; });
+            runs<I>(blocks, out, there, [&](float a, int) {
+                const float d = __builtin_amdgcn_exp2f(__builtin_fmaf(a, scale, -lse)) * factor;
+                return live ? d : 0.f;
+            }, [](int) { return true; });
         } else {
             // with the target's column, and columns past the last word: zeros, to the end of the row
             const int at = live ? col - n_first : -1, left = p.N - n_first, room = (int)p.ldd - n_first;
             runs<I>(blocks, out, there, [&](float a, int c) {
                 const float d = (__builtin_amdgcn_exp2f(__builtin_fmaf(a, scale, -lse)) - (at == c ? 1.f : 0.f)) * factor;
-                return c < left ? d : 0.f;
+                return live && c < left ? d : 0.f;
             }, [&](int c) { return c < room; });
         }
     }

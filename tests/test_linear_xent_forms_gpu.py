@@ -119,3 +119,34 @@ def test_captured_calls_with_workspaces_of_their_own_run_side_by_side():
         torch.cuda.synchronize()
         for got, want in zip(outs, firsts):
             assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("T,V,K,shift", [(20, 700, 64, 0), (50, 700, 63, 0), (64, 300, 128, 1), (65, 700, 64, 0), (300, 2000, 128, 0), (300, 1001, 99, 1)])
+def test_what_a_left_out_token_holds_has_no_part_in_a_gradient(T, V, K, shift, value, dtype):
+    """Rows of X, and values of dloss, of tokens without a target: dX is zero there, and dW that of a call where they hold nothing unusual, bit by bit."""
+    print("[case] left out", T, V, K, shift, value, dtype, flush=True)
+    x, w, targets, dloss = inputs(T, V, K, dtype, 9, x_ld=K + shift)
+    out = targets < 0
+    targets[out & (torch.arange(T) % 2 == 0)] = V
+    targets, dloss = targets.cuda(), dloss.cuda()
+    loss, lse, dx, dw = run(x, w, targets, 0.5, dloss)
+    x[out.cuda()] = value
+    dloss[out.cuda()] = value
+    loss2, lse2, dx2, dw2 = run(x, w, targets, 0.5, dloss)
+    assert torch.isfinite(dw).all() and torch.equal(dw, dw2) and torch.equal(dx, dx2) and torch.equal(loss, loss2)
+    assert (dx2[out.cuda()] == 0).all() and torch.equal(lse[~out.cuda()], lse2[~out.cuda()])
+
+
+@pytest.mark.parametrize("T", [20, 300])
+def test_left_out_tokens_have_no_gradient_where_the_vocabulary_matrix_is_not_finite(T):
+    """A word whose logits are all minus infinity (its probability is zero): dX of left-out tokens stays zero."""
+    x, w, targets, dloss = inputs(T, 700, 64, torch.bfloat16, 10)
+    x.abs_()
+    w[13] = float("-inf")
+    targets[targets == 13] = 14
+    loss, lse, dx, dw = run(x, w, targets.cuda(), 1.0, dloss.cuda())
+    assert torch.isfinite(lse).all() and (dx[(targets < 0).cuda()] == 0).all()
+    keep = torch.arange(700) != 13
+    assert torch.isfinite(dw[keep.cuda()]).all() and (dw[13] == 0).all()
