@@ -32,6 +32,7 @@ struct LayerNormArgs {
     int64_t ldx, lddy, ldo, rows;
     int32_t cols;
     float eps, width;                       // width: cols, to divide by
+    int64_t row0;                           // kernels with a workgroup for each row: the first one's
 };
 
 // Workgroups of one wave a row hold four rows, those of the gradient with two waves a row two: the sums of a workgroup's rows are added up before they
@@ -232,7 +233,7 @@ __global__ __launch_bounds__(1024) void layernorm_wide(const LayerNormArgs a) {
     constexpr int N = RowPiece<T>::N;
     __shared__ float slots[2][16];
     const int n = a.cols, pieces = (n + N - 1) / N;
-    const int64_t row = blockIdx.x;
+    const int64_t row = a.row0 + blockIdx.x;
     const T *x = (const T *)a.x + row * a.ldx;
     T *y = (T *)a.out + row * a.ldo;
     float v[N], sum = 0.f, square = 0.f;
@@ -269,7 +270,7 @@ __global__ __launch_bounds__(1024) void layernorm_grad_wide(const LayerNormArgs 
     constexpr int N = RowPiece<T>::N;
     __shared__ float slots[2][16];
     const int n = a.cols, pieces = (n + N - 1) / N;
-    const int64_t row = blockIdx.x;
+    const int64_t row = a.row0 + blockIdx.x;
     const T *x = (const T *)a.x + row * a.ldx, *dy = (const T *)a.dy + row * a.lddy;
     T *dx = (T *)a.out + row * a.ldo;
     const P *gamma = (const P *)a.gamma;
@@ -321,14 +322,15 @@ __global__ __launch_bounds__(256) void layernorm_column_sums(const LayerNormArgs
 // A workgroup adds the `groups` sums of 32 of the 2 cols columns: 32 lanes along the columns, 32 runs of groups side by
 // side, which are then added in order.
 template <class P>
-__global__ __launch_bounds__(1024) void layernorm_sums(const float *partial, int groups, int cols, P *dgamma, P *dbeta) {
+__global__ __launch_bounds__(1024) void layernorm_sums(const float *partial, int groups, int64_t cols, int64_t group0, P *dgamma, P *dbeta) {
     __shared__ float part[32][33];
-    const int at = threadIdx.x & 31, run = threadIdx.x >> 5, col = blockIdx.x * 32 + at;
+    const int at = threadIdx.x & 31, run = threadIdx.x >> 5;
+    const int64_t col = (group0 + blockIdx.x) * 32 + at;
     const int each = (groups + 31) / 32, first = run * each, last = min(first + each, groups);
     float sum = 0.f;
     if (col < 2 * cols) {
 #pragma unroll 4
-        for (int g = first; g < last; ++g) sum += partial[(int64_t)g * 2 * cols + col];
+        for (int g = first; g < last; ++g) sum += partial[g * 2 * cols + col];
     }
     part[run][at] = sum;
     __syncthreads();
@@ -409,13 +411,16 @@ fg_status fg_layernorm(int64_t rows, int64_t cols, const fg_matrix *X, const voi
     if (!aligned_to(beta, element_bytes(param_dtype)) || !aligned_to(mean, 4) || !aligned_to(rstd, 4))
         return fail(FG_ERR_ALIGN, "beta, mean and rstd must be aligned to an element");
     if (rows == 0 || cols == 0) return FG_OK;
-    LayerNormArgs a = {X->re, nullptr, Y->re, gamma, beta, mean, rstd, nullptr, X->ld, 0, Y->ld, rows, (int32_t)cols, eps, (float)cols};
+    LayerNormArgs a = {X->re, nullptr, Y->re, gamma, beta, mean, rstd, nullptr, X->ld, 0, Y->ld, rows, (int32_t)cols, eps, (float)cols, 0};
     hipStream_t stream = (hipStream_t)hip_stream;
     const int w = waves_for(cols, element_bytes(X->dtype));
     return with_types(X->dtype, param_dtype, [&](auto t, auto p) {
         using T = decltype(t);
         using P = decltype(p);
-        if (w == 0) hipLaunchKernelGGL((layernorm_wide<T, P>), dim3((unsigned)rows), dim3(1024), 0, stream, a);
+        if (w == 0) in_parts(rows, [&](int64_t first, dim3 grid) {
+            a.row0 = first;
+            hipLaunchKernelGGL((layernorm_wide<T, P>), grid, dim3(1024), 0, stream, a);
+        });
         else with_waves(w, [&](auto tag) {
             constexpr int W = tag, R = kRowsPerGroup<W>;
             static const int per_cu = [] {              // workgroups that fit a unit
@@ -449,7 +454,7 @@ fg_status fg_layernorm_grad(int64_t rows, int64_t cols, const fg_matrix *dY, con
     const int64_t need = sums ? fg_layernorm_grad_workspace(rows, cols, X->dtype) : 0;
     if (fg_status st = check_workspace(workspace, workspace_bytes, need)) return st;
     LayerNormArgs a = {X->re, dY->re, dX->re, gamma, nullptr, const_cast<float *>(mean), const_cast<float *>(rstd), (float *)workspace,
-                       X->ld, dY->ld, dX->ld, rows, (int32_t)cols, 0.f, (float)cols};
+                       X->ld, dY->ld, dX->ld, rows, (int32_t)cols, 0.f, (float)cols, 0};
     hipStream_t stream = (hipStream_t)hip_stream;
     const int w = waves_for(cols, element_bytes(X->dtype));
     const int64_t groups = rows > 0 ? grad_groups(rows, cols, element_bytes(X->dtype)) : 0;      // no row: the sums are zero
@@ -458,7 +463,10 @@ fg_status fg_layernorm_grad(int64_t rows, int64_t cols, const fg_matrix *dY, con
         using P = decltype(p);
         if (rows > 0 && w == 0) {
             if (sums) hipLaunchKernelGGL((layernorm_column_sums<T>), dim3((unsigned)((cols + 255) / 256), (unsigned)groups), dim3(256), 0, stream, a);
-            hipLaunchKernelGGL((layernorm_grad_wide<T, P>), dim3((unsigned)rows), dim3(1024), 0, stream, a);
+            in_parts(rows, [&](int64_t first, dim3 grid) {
+                a.row0 = first;
+                hipLaunchKernelGGL((layernorm_grad_wide<T, P>), grid, dim3(1024), 0, stream, a);
+            });
         } else if (rows > 0) with_waves(w, [&](auto tag) {
             constexpr int W = tag;
             const dim3 grid((unsigned)groups), block(64 * W * kGradRows<W>);
@@ -467,8 +475,9 @@ fg_status fg_layernorm_grad(int64_t rows, int64_t cols, const fg_matrix *dY, con
         });
         if (fg_status st = check_launch("layernorm_grad")) return st;
         if (!sums) return FG_OK;
-        hipLaunchKernelGGL((layernorm_sums<P>), dim3((unsigned)((2 * cols + 31) / 32)), dim3(1024), 0, stream, (const float *)workspace, (int)groups, (int)cols,
-                           (P *)dgamma, (P *)dbeta);
+        in_parts((2 * cols + 31) / 32, [&](int64_t first, dim3 grid) {
+            hipLaunchKernelGGL((layernorm_sums<P>), grid, dim3(1024), 0, stream, (const float *)workspace, (int)groups, cols, first, (P *)dgamma, (P *)dbeta);
+        });
         return check_launch("layernorm_sums");
     });
 }

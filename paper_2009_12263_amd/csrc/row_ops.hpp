@@ -129,6 +129,12 @@ inline fg_status check_workspace(const void *workspace, int64_t bytes, int64_t n
     if (bytes < need) return fail(FG_ERR_SHAPE, "the workspace has %lld bytes, %lld are needed", (long long)bytes, (long long)need);
     return FG_OK;
 }
+// f(first, n) for groups first .. first + n - 1 of a launch's `groups` workgroups (up to 1024 threads): a launch holds fewer than 2^32 threads, so
+// larger ones are made in parts.
+template <class F> void in_parts(int64_t groups, F &&f) {
+    constexpr int64_t kMost = 1 << 21;
+    for (int64_t first = 0; first < groups; first += kMost) f(first, dim3((unsigned)(groups - first < kMost ? groups - first : kMost)));
+}
 inline fg_status check_launch(const char *what) {
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? FG_OK : fail(FG_ERR_LAUNCH, "launch of %s failed: %s", what, hipGetErrorString(e));
