@@ -24,11 +24,11 @@ constexpr int kDigit = 6;                   // bits that one pass of the sort ta
 // A wave takes rows << shift lanes: 64 >> shift rows at a time, 2^shift lanes each.
 template <class T>
 __global__ __launch_bounds__(256) void embedding(const T *table, int64_t ld, const void *ids, bool wide, float scale, T *y, int64_t ldy, int64_t tokens,
-                                                 int vocab, int dim, int shift) {
+                                                 int vocab, int dim, int shift, int64_t group0) {
     constexpr int N = RowPiece<T>::N, AHEAD = 4;
     const int lane = threadIdx.x & 63, at = lane & ((1 << shift) - 1), rows = 64 >> shift, pieces = (dim + N - 1) / N;
     const int chunks = (pieces + (AHEAD << shift) - 1) / (AHEAD << shift);
-    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t wave = (group0 + blockIdx.x) * 4 + (threadIdx.x >> 6);
     const int64_t t = wave / chunks * rows + (lane >> shift);
     const int first = (int)(wave % chunks) * (AHEAD << shift) + at;
     if (t >= tokens) return;
@@ -176,7 +176,8 @@ struct EmbeddingGradArgs {
     uint32_t *open_count, *open_tiles;      // tiles that an id which began there goes out of, in any order
     int64_t lddy, ldc, ldo;
     int tokens, vocab, dim, tiles, chunks;  // chunks: of 64 pieces, that cover the columns
-    int join_groups;                        // workgroups that join sums, in front of those that fill rows
+    int64_t join_groups;                    // workgroups that join sums, in front of those that fill rows
+    int64_t group0;                         // the launch's first workgroup
     int shift;                              // lanes of a row to fill
     float scale;
 };
@@ -200,7 +201,8 @@ template <class T, class D, bool ADD>
 __global__ __launch_bounds__(256) void embedding_sums(const EmbeddingGradArgs a) {
     constexpr int N = RowPiece<T>::N;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pieces = (a.dim + N - 1) / N;
-    const int item = blockIdx.x * 4 + wave, tile = item / a.chunks, p = item % a.chunks * 64 + lane;
+    const int64_t item = (a.group0 + blockIdx.x) * 4 + wave;
+    const int tile = (int)(item / a.chunks), p = (int)(item % a.chunks) * 64 + lane;
     if (tile >= a.tiles) return;
     const int i0 = tile * kTile, n = min(kTile, a.tokens - i0);
     const bool on = p < pieces;             // (lanes without columns hold tokens all the same)
@@ -278,13 +280,14 @@ __global__ __launch_bounds__(256) void embedding_join(const EmbeddingGradArgs a)
     constexpr int N = RowPiece<T>::N, AHEAD = 8, WAVES = 4;
     __shared__ float part[WAVES][N][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pieces = (a.dim + N - 1) / N;
-    if ((int)blockIdx.x >= a.join_groups) {
-        embedding_fill<T, D, ADD>(a, (int64_t)(blockIdx.x - a.join_groups) * WAVES + wave, lane, pieces);
+    const int64_t group = a.group0 + blockIdx.x;
+    if (group >= a.join_groups) {
+        embedding_fill<T, D, ADD>(a, (group - a.join_groups) * WAVES + wave, lane, pieces);
         return;
     }
-    const int p = blockIdx.x % a.chunks * 64 + lane;
+    const int p = (int)(group % a.chunks) * 64 + lane;
     const uint32_t ids = *a.open_count;
-    for (uint32_t n = blockIdx.x / a.chunks; n < ids; n += a.join_groups / a.chunks) {
+    for (int64_t n = group / a.chunks; n < ids; n += a.join_groups / a.chunks) {
         const int tile = a.open_tiles[n];
         const uint32_t id = a.keys[(int64_t)tile * kTile + kTile - 1];
         // how many tiles it comes into: those behind, as long as they begin with it
@@ -395,8 +398,10 @@ fg_status fg_embedding(int64_t tokens, int64_t vocab, int64_t dim, const fg_matr
         using T = decltype(t);
         const int pieces = (int)((dim + RowPiece<T>::N - 1) / RowPiece<T>::N), shift = lanes_shift((pieces + 3) / 4);
         const int64_t waves = (tokens + (64 >> shift) - 1) / (64 >> shift) * ((pieces + (4 << shift) - 1) / (4 << shift));
-        hipLaunchKernelGGL((embedding<T>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, (hipStream_t)hip_stream, (const T *)table->re, table->ld, ids,
-                           index_dtype == FG_I64, scale, (T *)Y->re, Y->ld, tokens, (int)vocab, (int)dim, shift);
+        in_parts((waves + 3) / 4, [&](int64_t first, dim3 grid) {
+            hipLaunchKernelGGL((embedding<T>), grid, dim3(256), 0, (hipStream_t)hip_stream, (const T *)table->re, table->ld, ids, index_dtype == FG_I64, scale,
+                               (T *)Y->re, Y->ld, tokens, (int)vocab, (int)dim, shift, first);
+        });
     });
     return check_launch("embedding");
 }
@@ -455,14 +460,20 @@ fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg
         const int64_t pieces = (dim + RowPiece<T>::N - 1) / RowPiece<T>::N, tiles = (tokens + kTile - 1) / kTile, chunks = (pieces + 63) / 64;
         const int shift = lanes_shift((int)((pieces + 3) / 4));
         const int64_t joins = tiles > 1 ? std::min<int64_t>(tiles - 1, 512) * chunks : 0;
-        const EmbeddingGradArgs a = {dY->re, Cin ? Cin->re : nullptr, dtable->re, all_keys, all_order, present, (float *)(w + at.open), open_count, open_tiles, dY->ld,
-                                     Cin ? Cin->ld : 0, dtable->ld, (int)tokens, (int)vocab, (int)dim, (int)tiles, (int)chunks, (int)joins, shift, scale};
+        EmbeddingGradArgs a = {dY->re, Cin ? Cin->re : nullptr, dtable->re, all_keys, all_order, present, (float *)(w + at.open), open_count, open_tiles, dY->ld,
+                                     Cin ? Cin->ld : 0, dtable->ld, (int)tokens, (int)vocab, (int)dim, (int)tiles, (int)chunks, joins, 0, shift, scale};
         auto run = [&](auto tag) {
             constexpr bool ADD = decltype(tag)::value;
             const int64_t rows = (64 >> shift) * kFillRows<ADD>, fills = in_place ? 0 : (vocab + rows - 1) / rows * ((pieces + (4 << shift) - 1) / (4 << shift));
             const int64_t rest = joins + (fills + 3) / 4;
-            if (tiles > 0) hipLaunchKernelGGL((embedding_sums<T, D, ADD>), dim3((unsigned)((tiles * chunks + 3) / 4)), dim3(256), 0, stream, a);
-            if (rest > 0) hipLaunchKernelGGL((embedding_join<T, D, ADD>), dim3((unsigned)rest), dim3(256), 0, stream, a);
+            in_parts((tiles * chunks + 3) / 4, [&](int64_t first, dim3 grid) {
+                a.group0 = first;
+                hipLaunchKernelGGL((embedding_sums<T, D, ADD>), grid, dim3(256), 0, stream, a);
+            });
+            in_parts(rest, [&](int64_t first, dim3 grid) {
+                a.group0 = first;
+                hipLaunchKernelGGL((embedding_join<T, D, ADD>), grid, dim3(256), 0, stream, a);
+            });
         };
         if (Cin) run(std::true_type{});
         else run(std::false_type{});

@@ -61,3 +61,17 @@ def test_sums_of_more_columns_than_a_launch_holds():
     assert torch.equal(dbeta, dy[0].float())
     want = dy[0].double() * ((x[0].double() - 0.25) * 1.5)
     assert ((dgamma.double() - want).abs() <= 4 * 2.0 ** -24 * want.abs()).all()
+
+
+def test_more_tokens_than_a_launch_holds():
+    """2^30 tokens of rows of 66 values, 16 to a wave: 2^32 lanes."""
+    _needs(200)
+    tokens, dim, vocab = 1 << 30, 66, 5
+    print("[case] embedding", tokens, dim, flush=True)
+    table = torch.randint(-9, 10, (vocab, dim), device="cuda").half()
+    ids = torch.empty(tokens, dtype=torch.int32, device="cuda").random_(-1, vocab)
+    y = torch.full((tokens, dim), float("nan"), dtype=torch.float16, device="cuda")
+    fg.fg_embedding(table, ids, 2.0, y)
+    twice = torch.cat([table * 2, torch.zeros(1, dim, dtype=torch.float16, device="cuda")])
+    for i in range(0, tokens, 1 << 25):
+        assert torch.equal(y[i:i + (1 << 25)], twice[ids[i:i + (1 << 25)].long() % (vocab + 1)]), i
