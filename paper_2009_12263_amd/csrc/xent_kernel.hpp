@@ -184,6 +184,8 @@ struct XentCfg : Base {
 
 // The five tiles a plan can name: 256x256, 256x128, 128x128 with four buffers, 64x64 and 64x128 with two groups of waves (kernel_table.hpp).
 enum { XENT_TILES = 5 };
+// Columns of a wave on each: those of one run of XentParams::stats, whose space the host counts by them.
+constexpr int kXentWaveColumns[XENT_TILES] = {128, 64, 64, 32, 64};
 const KernelEntry *kernel_table_xent(int kind, bool bf16);
 
 #define FG_XENT_TABLE(FUNC, KIND, AKC, BKC, BF, NAME)                                                                      \
@@ -193,6 +195,8 @@ const KernelEntry *kernel_table_xent(int kind, bool bf16);
         using C = XentCfg<FG_CFG_K32(128, 128, 64, 4, 2, 2, AKC, BKC, BF, false), KIND>;                                   \
         using D = XentCfg<FG_CFG_KG(AKC, BKC, BF, false, false, 64, 4, true), KIND>;                                       \
         using E = XentCfg<FG_CFG_KG(AKC, BKC, BF, false, false, 128, 3, true), KIND>;                                      \
+        static_assert(A::WTN == kXentWaveColumns[0] && B::WTN == kXentWaveColumns[1] && C::WTN == kXentWaveColumns[2] &&   \
+                      D::WTN == kXentWaveColumns[3] && E::WTN == kXentWaveColumns[4], "");                                 \
         static const KernelEntry t[XENT_TILES] = {                                                                         \
             {(const void *)gemm_kernel<A>, NAME "_256x256x64", 256, 256, A::NTHREADS, A::LDS_BYTES},                       \
             {(const void *)gemm_kernel<B>, NAME "_256x128x64", 256, 128, B::NTHREADS, B::LDS_BYTES},                       \
@@ -202,7 +206,5 @@ const KernelEntry *kernel_table_xent(int kind, bool bf16);
         };                                                                                                                 \
         return t;                                                                                                          \
     }
-// columns of a wave, on each tile: those of one run of XentParams::stats
-constexpr int kXentWaveColumns[XENT_TILES] = {128, 64, 64, 32, 64};
 
 }  // namespace fg
