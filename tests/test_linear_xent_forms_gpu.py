@@ -150,3 +150,25 @@ def test_left_out_tokens_have_no_gradient_where_the_vocabulary_matrix_is_not_fin
     assert torch.isfinite(lse).all() and (dx[(targets < 0).cuda()] == 0).all()
     keep = torch.arange(700) != 13
     assert torch.isfinite(dw[keep.cuda()]).all() and (dw[13] == 0).all()
+
+
+@pytest.mark.parametrize("K", [16, 15])
+def test_more_tokens_than_a_block(K):
+    """The statistics of 16384 tokens are kept at a time; the last block is shorter.  With 15 values a row both operands are copied, block by block."""
+    T, V = 16384 + 77, 300
+    print("[case] blocks", T, V, K, flush=True)
+    x, w, targets, dloss = inputs(T, V, K, torch.bfloat16, 12)
+    compare(x, w, targets, 1.0, dloss, run(x, w, targets.cuda(), 1.0, dloss.cuda()))
+
+
+def test_rows_without_values():
+    """All logits are zero."""
+    for T, V in ((5, 7), (300, 3000)):
+        x, w = torch.empty(T, 0, dtype=torch.float16, device="cuda"), torch.empty(V, 0, dtype=torch.float16, device="cuda")
+        targets = torch.arange(T, device="cuda") % V
+        targets[2] = -1
+        loss, lse, dx, dw = run(x, w, targets, 1.0, torch.ones(T, device="cuda"))
+        want = torch.full((T,), math.log(V), dtype=torch.float64)
+        assert ((lse.double().cpu() - want).abs() <= (V / 256 + 400) * U).all()
+        want[2] = 0
+        assert ((loss.double().cpu() - want).abs() <= (V / 256 + 400) * U).all() and loss[2] == 0
