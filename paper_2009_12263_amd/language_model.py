@@ -107,7 +107,7 @@ def main(argv=None) -> float:
     for i in range(a.steps):
         loss = model.step(*chain(a.tokens, a.vocab, i), a.rate)
         if i % 20 == 0 or i + 1 == a.steps:
-            mean = float(loss.sum() / (a.tokens - 1))
+            mean = float(loss.sum() / max(a.tokens - 1, 1))
             print("step %4d  loss %.4f" % (i, mean), flush=True)
     return mean
 
