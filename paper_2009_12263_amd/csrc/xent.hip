@@ -92,7 +92,8 @@ __global__ __launch_bounds__(1024) void xent_join(const XentStat *stats, int par
 // is at most 2^14 and what is 2^-38 of the largest is still a number.  factor[0] = c, factor[1] = scale / c.
 //
 // The others: x's rows for the products, aligned and padded like xent_pad's, with zeros for the tokens that are left out.  Their dz is zero, but a row of a
-// token nobody asks for may hold anything, and in dw = dz^T x zero times infinity or NaN would reach every word.
+// token nobody asks for may hold anything, and in dw = dz^T x zero times infinity or NaN would reach every word.  (Beside the scaling's chain of latencies up
+// to 64 tokens cost nothing, 4.1 us either way; looked up by xent_dw_few instead, the targets took it from 41 to 47 us, with 64 tokens from 56 to 80.)
 template <class T>
 __global__ __launch_bounds__(1024) void xent_prepare(const float *dloss, int64_t dloss_inc, const void *targets, bool wide, int vocab, int64_t tokens, float scale,
                                                      float *factor, const T *x, int64_t ldx, T *out, int64_t ldo, int cols) {
@@ -152,8 +153,8 @@ __device__ __forceinline__ floatx4 mfma_16x16x32(typename RowPiece<T>::vec a, ty
 }
 
 template <class T, int KS, int J>
-__global__ __launch_bounds__(256, 2) void xent_dw_few(const T *dz, int64_t ld_dz, const T *x, int64_t ldx, const void *targets, bool wide, int vocab, const float *factor,
-                                                   T *out, int64_t ldo, int tokens, int words, int dim, int strips) {
+__global__ __launch_bounds__(256, 2) void xent_dw_few(const T *dz, int64_t ld_dz, const T *x, int64_t ldx, const float *factor, T *out, int64_t ldo, int tokens,
+                                                   int words, int dim, int strips) {
     typedef typename RowPiece<T>::vec vec;
     const int lane = threadIdx.x & 63, at = lane & 15, quarter = lane >> 4;
     const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -167,20 +168,14 @@ __global__ __launch_bounds__(256, 2) void xent_dw_few(const T *dz, int64_t ld_dz
     for (int s = 0; s < KS; ++s) {
         words_vec w[8] = {};
         vec v[8] = {};
-        int target[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int t = s * 32 + quarter * 8 + e;
-            target[e] = -1;
             if (t < tokens) {
-                target[e] = load_index(targets, wide, t, vocab);
                 if (in) w[e] = *(const words_vec *)(dz + t * ld_dz + word0 + at * J);
                 v[e] = load_raw<T, 8>(x + t * ldx, there, dim);
             }
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (target[e] < 0) v[e] = vec{};                            // (left out: see xent_prepare)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
 #pragma unroll
@@ -260,17 +255,15 @@ struct StatsSpace {
     }
     static int64_t preferred(int64_t, int64_t vocab, int64_t dim) { return words_of(kCopyBytes, up(dim, 8) * 2, kFewestWords, vocab); }
 };
-// Gradient: dz of a piece, the sums of dx, and copies of operands.  What the workspace has behind them serves a split of the product with dX.
+// Gradient: dz of a piece, the sums of dx, x without the rows of left-out tokens (xent_prepare), and a copy of w.  What the workspace has behind them serves a split of the product with dX.
 struct GradSpace {
     int64_t words, ld, ld_dz, ld_dx, dz, dx, factor, x, w, bytes;
-    bool copy_x;                            // (the tiled product with dw reads rows without those of left-out tokens; xent_dw_few looks at the targets itself)
-    GradSpace(int64_t words_, int64_t tokens, int64_t, int64_t dim, Copies c)
-        : words(words_), ld(up(dim, 8)), ld_dz(up(words, 8)), ld_dx(up(dim, 4)), copy_x(c.x || tokens > kFewTokens) {
+    GradSpace(int64_t words_, int64_t tokens, int64_t, int64_t dim, Copies c) : words(words_), ld(up(dim, 8)), ld_dz(up(words, 8)), ld_dx(up(dim, 4)) {
         dz = 0;
         dx = dz + up(tokens * ld_dz * 2, 256);
         factor = dx + up(tokens * ld_dx * 4, 256);
         x = factor + 256;
-        w = x + (copy_x ? up(tokens * ld * 2, 256) : 0);
+        w = x + up(tokens * ld * 2, 256);
         bytes = w + (c.w ? up(words * ld * 2, 256) : 0);
     }
     static int64_t preferred(int64_t tokens, int64_t vocab, int64_t) { return std::min(words_of(kPieceBytes, 2 * tokens, 2048, vocab), kMostWords); }
@@ -464,16 +457,16 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
         });
         return check_launch("xent_round");
     };
-    fg_matrix x = rows_of(X->re, X->dtype, X->ld), w;
+    const fg_matrix x = rows_of(space + at.x, X->dtype, at.ld);
+    fg_matrix w;
     with_half(X->dtype, [&](auto t) {
         using T = decltype(t);
-        const int64_t pieces = at.copy_x ? tokens * (at.ld / 8) : 0;
-        hipLaunchKernelGGL((xent_prepare<T>), dim3((unsigned)(1 + std::min<int64_t>((pieces + 1023) / 1024, 2048))), dim3(1024), 0, stream, dloss, dloss_inc, targets, wide,
+        const int64_t groups = std::min<int64_t>((tokens * (at.ld / 8) + 1023) / 1024, 2048);
+        hipLaunchKernelGGL((xent_prepare<T>), dim3((unsigned)(1 + groups)), dim3(1024), 0, stream, dloss, dloss_inc, targets, wide,
                            (int)vocab, tokens, scale, factor, (const T *)X->re, X->ld, (T *)(space + at.x), at.ld, (int)dim);
     });
     if (fg_status st = check_launch("xent_prepare")) return st;
     if (tokens == 0) return round(nullptr, dW, vocab);
-    if (at.copy_x) x = rows_of(space + at.x, X->dtype, at.ld);
     const fg_matrix dz = rows_of(space + at.dz, X->dtype, at.ld_dz), sum_dx = rows_of(sums, FG_F32, at.ld_dx);
     for (int64_t v0 = 0; v0 < vocab; v0 += at.words) {
         const int64_t n = std::min(at.words, vocab - v0);
@@ -492,8 +485,8 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
                 auto few = [&](auto steps, auto run) {
                     constexpr int KS = decltype(steps)::value, J = decltype(run)::value;
                     const int64_t waves = (n + 16 * J - 1) / (16 * J) * strips;
-                    hipLaunchKernelGGL((xent_dw_few<T, KS, J>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, (const T *)dz.re, at.ld_dz, (const T *)x.re, x.ld, targets, wide,
-                                       (int)vocab, factor, (T *)row_at(dW, v0), dW->ld, (int)tokens, (int)n, (int)dim, strips);
+                    hipLaunchKernelGGL((xent_dw_few<T, KS, J>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, (const T *)dz.re, at.ld_dz, (const T *)x.re, x.ld, factor,
+                                       (T *)row_at(dW, v0), dW->ld, (int)tokens, (int)n, (int)dim, strips);
                 };
                 using std::integral_constant;
                 // Fewer waves than there are SIMDs: 64 words each instead of 128 (2496 words x 1000: 16 tokens 5.0 us and 6.7, 64 tokens 5.9 and 8.0;
