@@ -277,7 +277,8 @@ fg_status fg_contract_plan(int32_t nA, const int32_t *modesA, const int64_t *str
 /* ---- operators on the rows of a matrix: the ends of a language model --------------------------------------
  * Hidden states, embedding tables and vocabulary matrices are row-major fg_matrix descriptors (layout FG_ROW, `im` NULL) with a leading
  * dimension of any size from the row's length on and element-aligned pointers, of FG_F16, FG_BF16 or (where it is said) FG_F32
- * elements.  All arithmetic is FP32 or wider; every result is rounded to nearest even once, when it is stored.  Results do not
+ * elements.  All arithmetic is FP32 or wider, but that fg_linear_xent_grad holds the logits' gradient in 16 bits between its products; every result is rounded to
+ * nearest even once, when it is stored.  Results do not
  * depend on scheduling: the same call gives the same bits.  Calls that need scratch memory take a 16-byte aligned workspace from the
  * caller, of the bytes that the query beside it gives; it holds nothing from one call to the next, needs no clearing and may be
  * reused by the next call on the same stream.  These calls allocate nothing, share no memory with other calls and only enqueue kernels: they may be recorded into
@@ -331,7 +332,7 @@ int64_t fg_embedding_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim);
  * lse is that of its logits all the same).  No logits are kept: the vocabulary is walked in pieces, of which the statistics remain.
  *   X : tokens x dim, W : vocab x dim, both FG_F16 or both FG_BF16 (multiplied exactly, summed in FP32); targets : `tokens` indices of type
  *   index_dtype (FG_I32, FG_I64); loss, lse : `tokens` FP32 values each; vocab >= 1.
- * Infinite logits give a NaN.  Rows that are not 16-byte aligned, or not of a multiple of 8 values, are copied into the workspace first, W a piece at a
+ * Logits of plus infinity or NaN give a NaN.  Rows that are not 16-byte aligned, or not of a multiple of 8 values, are copied into the workspace first, W a piece at a
  * time (FG_ERR_UNSUPPORTED for rows of 2^21 values or more).
  */
 fg_status fg_linear_xent(int64_t tokens, int64_t vocab, int64_t dim, const fg_matrix *X, const fg_matrix *W, const void *targets, int32_t index_dtype,

@@ -121,7 +121,8 @@ __global__ __launch_bounds__(64 * W * kGradRows<W>, grad_waves(W)) void layernor
     constexpr int N = Lane::N, R = Lane::R;
     __shared__ float slots[4][R][W], pool[SUMS && R > 1 ? 2 : 1][SUMS && R > 1 ? 64 * W * kPieces * N : 1];
     // Large workgroups have no registers left for gamma: each lane keeps its part in LDS.  (A spilled register is reloaded in the order of the loads, behind
-    // the next row: 16384 x 8192 binary16, FP32 parameters, 182 us with four spilled, 163 so.)
+    // the next row: 16384 x 8192 binary16, FP32 parameters, 182 us with four spilled, 163 so.  Of the kernels of eight waves those of bfloat16 have two spilled all the
+    // same: 16384 x 5120 118 to 122 us, binary16 102; 16384 x 8192 154 to 163, binary16 162 to 168.)
     constexpr bool LDS = W >= 8;
     __shared__ __attribute__((aligned(16))) float4 gamma_of[LDS ? kPieces : 1][LDS ? N / 4 : 1][LDS ? 64 * W : 1];
     const Lane l(a.cols);
