@@ -394,16 +394,17 @@ fg_status fg_embedding(int64_t tokens, int64_t vocab, int64_t dim, const fg_matr
     if (fg_status st = check_rows("Y", Y, tokens, dim)) return st;
     if (table->dtype != Y->dtype) return fail(FG_ERR_UNSUPPORTED, "the table and Y must have the same element type");
     if (tokens == 0 || dim == 0) return FG_OK;
+    Launches enqueue(hip_stream);
     with_element(Y->dtype, [&](auto t) {
         using T = decltype(t);
         const int pieces = (int)((dim + RowPiece<T>::N - 1) / RowPiece<T>::N), shift = lanes_shift((pieces + 3) / 4);
         const int64_t waves = (tokens + (64 >> shift) - 1) / (64 >> shift) * ((pieces + (4 << shift) - 1) / (4 << shift));
         in_parts((waves + 3) / 4, [&](int64_t first, dim3 grid) {
-            hipLaunchKernelGGL((embedding<T>), grid, dim3(256), 0, (hipStream_t)hip_stream, (const T *)table->re, table->ld, ids, index_dtype == FG_I64, scale,
+            enqueue(embedding<T>, grid, dim3(256), (const T *)table->re, table->ld, ids, index_dtype == FG_I64, scale,
                                (T *)Y->re, Y->ld, tokens, (int)vocab, (int)dim, shift, first);
         });
     });
-    return check_launch("embedding");
+    return enqueue.status("embedding");
 }
 
 int64_t fg_embedding_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim) {
@@ -430,7 +431,7 @@ fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg
     uint8_t *present = (uint8_t *)(w + at.present);
     uint32_t *open_count = (uint32_t *)(w + at.open_count), *open_tiles = (uint32_t *)(w + at.open_tiles);
     uint32_t *all_keys = (uint32_t *)(w + at.all_keys), *all_order = (uint32_t *)(w + at.all_order);
-    hipStream_t stream = (hipStream_t)hip_stream;
+    Launches enqueue(hip_stream);
     int passes = 1;
     while (((vocab + 1) >> (passes * kDigit)) != 0) ++passes;             // the largest key is vocab + 1
     const bool wide = index_dtype == FG_I64;
@@ -438,7 +439,7 @@ fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg
     const unsigned runs = (unsigned)std::max<int64_t>(1, (tokens + run - 1) / run);
     auto sort = [&](auto waves, auto items) {
         constexpr int WAVES = decltype(waves)::value, ITEMS = decltype(items)::value;
-        hipLaunchKernelGGL((embedding_sort<WAVES, ITEMS>), dim3(runs), dim3(64 * WAVES), 0, stream, ids, wide, (int)tokens, (int)vocab, passes, runs == 1 ? all_keys : keys,
+        enqueue(embedding_sort<WAVES, ITEMS>, dim3(runs), dim3(64 * WAVES), ids, wide, (int)tokens, (int)vocab, passes, runs == 1 ? all_keys : keys,
                            runs == 1 ? all_order : order, (uint4 *)present, open_count);
     };
     using std::integral_constant;
@@ -447,12 +448,12 @@ fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg
     else if (run == 4096) sort(integral_constant<int, 16>{}, integral_constant<int, 4>{});
     else sort(integral_constant<int, 16>{}, integral_constant<int, 16>{});
     auto merge = [&](auto side) {
-        hipLaunchKernelGGL((embedding_merge<decltype(side)::value>), dim3((unsigned)((tokens + 255) / 256)), dim3(256), 0, stream, keys, order, (int)tokens, run, all_keys,
+        enqueue(embedding_merge<decltype(side)::value>, dim3((unsigned)((tokens + 255) / 256)), dim3(256), keys, order, (int)tokens, run, all_keys,
                            all_order, (int)vocab, present);
     };
     if (runs > 4) merge(integral_constant<int, 8>{});
     else if (runs > 1) merge(integral_constant<int, 4>{});
-    if (fg_status st = check_launch("embedding_sort")) return st;
+    if (fg_status st = enqueue.status("embedding_sort")) return st;
     const bool in_place = Cin && Cin->re == dtable->re;
     auto launch = [&](auto t, auto d) {
         using T = decltype(t);
@@ -468,11 +469,11 @@ fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg
             const int64_t rest = joins + (fills + 3) / 4;
             in_parts((tiles * chunks + 3) / 4, [&](int64_t first, dim3 grid) {
                 a.group0 = first;
-                hipLaunchKernelGGL((embedding_sums<T, D, ADD>), grid, dim3(256), 0, stream, a);
+                enqueue(embedding_sums<T, D, ADD>, grid, dim3(256), a);
             });
             in_parts(rest, [&](int64_t first, dim3 grid) {
                 a.group0 = first;
-                hipLaunchKernelGGL((embedding_join<T, D, ADD>), grid, dim3(256), 0, stream, a);
+                enqueue(embedding_join<T, D, ADD>, grid, dim3(256), a);
             });
         };
         if (Cin) run(std::true_type{});
@@ -482,7 +483,7 @@ fg_status fg_embedding_grad(int64_t tokens, int64_t vocab, int64_t dim, const fg
         if (dtable->dtype == FG_F32) launch(t, float{});
         else launch(t, t);
     });
-    return check_launch("embedding_grad");
+    return enqueue.status("embedding_grad");
 }
 
 }  // extern "C"

@@ -21,6 +21,7 @@
 // 4095x4097x4099: 244 us, 563 TFLOP/s.
 #pragma once
 #include "kernel_table.hpp"
+#include "launch.hpp"
 #include "piece_address.hpp"
 
 namespace fg {
@@ -654,8 +655,7 @@ inline hipError_t launch_general(void (*fn)(const GeneralParams), int variant, G
     const int64_t items = (int64_t)p.tiles_m * p.tiles_n * (ranges ? 1 : p.splits) * p.batches;
     const unsigned per_row = (unsigned)(items < (1 << 22) ? items : (1 << 22));
     p.items = (int32_t)items;
-    hipLaunchKernelGGL(fn, dim3(per_row, (unsigned)((items + per_row - 1) / per_row)), dim3(variant == GENERAL_64x64_ONE ? 256 : 512), 0, stream, p);
-    return hipGetLastError();
+    return launch_kernel(fn, dim3(per_row, (unsigned)((items + per_row - 1) / per_row)), dim3(variant == GENERAL_64x64_ONE ? 256 : 512), stream, p);
 }
 
 typedef void (*GeneralFn)(const GeneralParams);

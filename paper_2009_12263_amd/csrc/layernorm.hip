@@ -413,14 +413,14 @@ fg_status fg_layernorm(int64_t rows, int64_t cols, const fg_matrix *X, const voi
         return fail(FG_ERR_ALIGN, "beta, mean and rstd must be aligned to an element");
     if (rows == 0 || cols == 0) return FG_OK;
     LayerNormArgs a = {X->re, nullptr, Y->re, gamma, beta, mean, rstd, nullptr, X->ld, 0, Y->ld, rows, (int32_t)cols, eps, (float)cols, 0};
-    hipStream_t stream = (hipStream_t)hip_stream;
+    Launches enqueue(hip_stream);
     const int w = waves_for(cols, element_bytes(X->dtype));
     return with_types(X->dtype, param_dtype, [&](auto t, auto p) {
         using T = decltype(t);
         using P = decltype(p);
         if (w == 0) in_parts(rows, [&](int64_t first, dim3 grid) {
             a.row0 = first;
-            hipLaunchKernelGGL((layernorm_wide<T, P>), grid, dim3(1024), 0, stream, a);
+            enqueue(layernorm_wide<T, P>, grid, dim3(1024), a);
         });
         else with_waves(w, [&](auto tag) {
             constexpr int W = tag, R = kRowsPerGroup<W>;
@@ -429,9 +429,9 @@ fg_status fg_layernorm(int64_t rows, int64_t cols, const fg_matrix *X, const voi
                 return hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, (const void *)layernorm<T, P, W>, 64 * W * R, 0) == hipSuccess && n > 0 ? n : 1;
             }();
             const unsigned grid = (unsigned)std::min<int64_t>((rows + R - 1) / R, kNumCU * per_cu);
-            hipLaunchKernelGGL((layernorm<T, P, W>), dim3(grid), dim3(64 * W * R), 0, stream, a);
+            enqueue(layernorm<T, P, W>, dim3(grid), dim3(64 * W * R), a);
         });
-        return check_launch("layernorm");
+        return enqueue.status("layernorm");
     });
 }
 
@@ -456,30 +456,30 @@ fg_status fg_layernorm_grad(int64_t rows, int64_t cols, const fg_matrix *dY, con
     if (fg_status st = check_workspace(workspace, workspace_bytes, need)) return st;
     LayerNormArgs a = {X->re, dY->re, dX->re, gamma, nullptr, const_cast<float *>(mean), const_cast<float *>(rstd), (float *)workspace,
                        X->ld, dY->ld, dX->ld, rows, (int32_t)cols, 0.f, (float)cols, 0};
-    hipStream_t stream = (hipStream_t)hip_stream;
+    Launches enqueue(hip_stream);
     const int w = waves_for(cols, element_bytes(X->dtype));
     const int64_t groups = rows > 0 ? grad_groups(rows, cols, element_bytes(X->dtype)) : 0;      // no row: the sums are zero
     return with_types(X->dtype, param_dtype, [&](auto t, auto p) {
         using T = decltype(t);
         using P = decltype(p);
         if (rows > 0 && w == 0) {
-            if (sums) hipLaunchKernelGGL((layernorm_column_sums<T>), dim3((unsigned)((cols + 255) / 256), (unsigned)groups), dim3(256), 0, stream, a);
+            if (sums) enqueue(layernorm_column_sums<T>, dim3((unsigned)((cols + 255) / 256), (unsigned)groups), dim3(256), a);
             in_parts(rows, [&](int64_t first, dim3 grid) {
                 a.row0 = first;
-                hipLaunchKernelGGL((layernorm_grad_wide<T, P>), grid, dim3(1024), 0, stream, a);
+                enqueue(layernorm_grad_wide<T, P>, grid, dim3(1024), a);
             });
         } else if (rows > 0) with_waves(w, [&](auto tag) {
             constexpr int W = tag;
             const dim3 grid((unsigned)groups), block(64 * W * kGradRows<W>);
-            if (sums) hipLaunchKernelGGL((layernorm_grad<T, P, W, true>), grid, block, 0, stream, a);
-            else hipLaunchKernelGGL((layernorm_grad<T, P, W, false>), grid, block, 0, stream, a);
+            if (sums) enqueue(layernorm_grad<T, P, W, true>, grid, block, a);
+            else enqueue(layernorm_grad<T, P, W, false>, grid, block, a);
         });
-        if (fg_status st = check_launch("layernorm_grad")) return st;
+        if (fg_status st = enqueue.status("layernorm_grad")) return st;
         if (!sums) return FG_OK;
         in_parts((2 * cols + 31) / 32, [&](int64_t first, dim3 grid) {
-            hipLaunchKernelGGL((layernorm_sums<P>), grid, dim3(1024), 0, stream, (const float *)workspace, (int)groups, cols, first, (P *)dgamma, (P *)dbeta);
+            enqueue(layernorm_sums<P>, grid, dim3(1024), (const float *)workspace, (int)groups, cols, first, (P *)dgamma, (P *)dbeta);
         });
-        return check_launch("layernorm_sums");
+        return enqueue.status("layernorm_sums");
     });
 }
 

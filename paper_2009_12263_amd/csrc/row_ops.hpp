@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "launch.hpp"
 #include "status.hpp"
 
 namespace fg {
@@ -135,9 +136,4 @@ template <class F> void in_parts(int64_t groups, F &&f) {
     constexpr int64_t kMost = 1 << 21;
     for (int64_t first = 0; first < groups; first += kMost) f(first, dim3((unsigned)(groups - first < kMost ? groups - first : kMost)));
 }
-inline fg_status check_launch(const char *what) {
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? FG_OK : fail(FG_ERR_LAUNCH, "launch of %s failed: %s", what, hipGetErrorString(e));
-}
-
 }  // namespace fg

@@ -5,6 +5,7 @@
 // across workgroups) in Section 4.2.5.  The partials are added in ascending s, so the result does
 // not depend on how the first pass was scheduled.
 #include "kernel_table.hpp"
+#include "launch.hpp"
 
 namespace fg {
 namespace {
@@ -77,9 +78,8 @@ hipError_t launch_splitk_reduce(const float *W, int splits, int tile_begin, int 
     const int64_t work = (int64_t)(bm / 4) * bn * tile_count;
     const unsigned blocks = (unsigned)((work + 255) / 256);
     auto vec = [](const void *p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 4 == 0; };
-    hipLaunchKernelGGL((vec(D, ldd) && (!C || vec(C, ldc)) ? splitk_reduce<true> : splitk_reduce<false>), dim3(blocks), dim3(256), 0, stream, W, splits, tile_begin, tile_count, bm, bn, tiles_m,
-                       tiles_n, M, N, alpha, beta, C, ldc, D, ldd, bias, bias_dim, act, c_act);
-    return hipGetLastError();
+    return launch_kernel(vec(D, ldd) && (!C || vec(C, ldc)) ? splitk_reduce<true> : splitk_reduce<false>, dim3(blocks), dim3(256), stream, W, splits, tile_begin, tile_count, bm, bn,
+                         tiles_m, tiles_n, M, N, alpha, beta, C, ldc, D, ldd, bias, bias_dim, act, c_act);
 }
 
 }  // namespace fg

@@ -331,29 +331,31 @@ XentParams product(const KernelEntry &k, bool kc, int64_t M, int64_t N, int64_t 
 
 fg_status run_join(const XentStat *stats, int64_t parts, int64_t stride, int64_t tokens, const void *targets, bool wide, int64_t vocab, const float *z_target, float *loss,
                    float *lse, hipStream_t stream) {
+    Launches enqueue(stream);
     auto launch = [&](auto tag) {
         constexpr int G = decltype(tag)::value, TOKENS = 1024 / G;
-        hipLaunchKernelGGL((xent_join<G>), dim3((unsigned)((tokens + TOKENS - 1) / TOKENS)), dim3(1024), 0, stream, stats, (int)parts, stride, tokens, targets, wide, (int)vocab,
+        enqueue(xent_join<G>, dim3((unsigned)((tokens + TOKENS - 1) / TOKENS)), dim3(1024), stats, (int)parts, stride, tokens, targets, wide, (int)vocab,
                            z_target, loss, lse);
     };
     // Enough workgroups to share the reads: 16 tokens of 2048 parts 20.2 us with 16 threads each, 6.0 with 256; 8192 of 1024 17.4 with 16.
     if (tokens <= 256) launch(std::integral_constant<int, 256>{});
     else if (tokens <= 4096) launch(std::integral_constant<int, 64>{});
     else launch(std::integral_constant<int, 16>{});
-    return check_launch("xent_join");
+    return enqueue.status("xent_join");
 }
 
 // Rows row0 .. row0 + n - 1 of m as the matrix kernels take them: themselves, or copied to `to`.
 fg_status aligned_rows(const fg_matrix *m, int64_t row0, int64_t n, int64_t dim, bool copy, void *to, int64_t ld, fg_matrix &out, hipStream_t stream) {
     out = rows_of(row_at(m, row0), m->dtype, m->ld);
     if (!copy || ld == 0) return FG_OK;
+    Launches enqueue(stream);
     with_half(m->dtype, [&](auto t) {
         using T = decltype(t);
         const unsigned groups = (unsigned)std::min<int64_t>((n * (ld / 8) + 255) / 256, 8192);
-        hipLaunchKernelGGL((xent_pad<T>), dim3(groups), dim3(256), 0, stream, (const T *)out.re, out.ld, (T *)to, ld, n, (int)dim);
+        enqueue(xent_pad<T>, dim3(groups), dim3(256), (const T *)out.re, out.ld, (T *)to, ld, n, (int)dim);
     });
     out = rows_of(to, m->dtype, ld);
-    return check_launch("xent_pad");
+    return enqueue.status("xent_pad");
 }
 
 }  // namespace
@@ -446,6 +448,7 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
     const auto at = space_within<GradSpace>(workspace_bytes, tokens, vocab, dim, copies);
     if (fg_status st = check_workspace(workspace, workspace_bytes, at.bytes)) return st;
     hipStream_t stream = (hipStream_t)hip_stream;
+    Launches enqueue(stream);
     char *space = (char *)workspace;
     const bool wide = index_dtype == FG_I64, bf16 = X->dtype == FG_BF16;
     float *sums = (float *)(space + at.dx), *factor = (float *)(space + at.factor);
@@ -453,20 +456,20 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
         const unsigned groups = (unsigned)std::min<int64_t>((rows * ((dim + 7) / 8) + 255) / 256, 8192);
         with_half(X->dtype, [&](auto t) {
             using T = decltype(t);
-            hipLaunchKernelGGL((xent_round<T>), dim3(groups), dim3(256), 0, stream, in, at.ld_dx, factor + 1, targets, wide, (int)vocab, (T *)out->re, out->ld, rows,
+            enqueue(xent_round<T>, dim3(groups), dim3(256), in, at.ld_dx, factor + 1, targets, wide, (int)vocab, (T *)out->re, out->ld, rows,
                                (int)dim);
         });
-        return check_launch("xent_round");
+        return enqueue.status("xent_round");
     };
     const fg_matrix x = rows_of(space + at.x, X->dtype, at.ld);
     fg_matrix w;
     with_half(X->dtype, [&](auto t) {
         using T = decltype(t);
         const int64_t groups = std::min<int64_t>((tokens * (at.ld / 8) + 1023) / 1024, 2048);
-        hipLaunchKernelGGL((xent_prepare<T>), dim3((unsigned)(1 + groups)), dim3(1024), 0, stream, dloss, dloss_inc, targets, wide,
+        enqueue(xent_prepare<T>, dim3((unsigned)(1 + groups)), dim3(1024), dloss, dloss_inc, targets, wide,
                            (int)vocab, tokens, scale, factor, (const T *)X->re, X->ld, (T *)(space + at.x), at.ld, (int)dim);
     });
-    if (fg_status st = check_launch("xent_prepare")) return st;
+    if (fg_status st = enqueue.status("xent_prepare")) return st;
     if (tokens == 0) return round(nullptr, dW, vocab);
     const fg_matrix dz = rows_of(space + at.dz, X->dtype, at.ld_dz), sum_dx = rows_of(sums, FG_F32, at.ld_dx);
     for (int64_t v0 = 0; v0 < vocab; v0 += at.words) {
@@ -486,7 +489,7 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
                 auto few = [&](auto steps, auto run) {
                     constexpr int KS = decltype(steps)::value, J = decltype(run)::value;
                     const int64_t waves = (n + 16 * J - 1) / (16 * J) * strips;
-                    hipLaunchKernelGGL((xent_dw_few<T, KS, J>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, (const T *)dz.re, at.ld_dz, (const T *)x.re, x.ld, factor,
+                    enqueue(xent_dw_few<T, KS, J>, dim3((unsigned)((waves + 3) / 4)), dim3(256), (const T *)dz.re, at.ld_dz, (const T *)x.re, x.ld, factor,
                                        (T *)row_at(dW, v0), dW->ld, (int)tokens, (int)n, (int)dim, strips);
                 };
                 using std::integral_constant;
@@ -496,7 +499,7 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
                 if (tokens <= 32) small ? few(integral_constant<int, 1>{}, integral_constant<int, 4>{}) : few(integral_constant<int, 1>{}, integral_constant<int, 8>{});
                 else small ? few(integral_constant<int, 2>{}, integral_constant<int, 4>{}) : few(integral_constant<int, 2>{}, integral_constant<int, 8>{});
             });
-            if (fg_status st = check_launch("xent_dw_few")) return st;
+            if (fg_status st = enqueue.status("xent_dw_few")) return st;
         } else {
             // neither operand is K-contiguous: any number of tokens
             const KernelEntry &kw = kernel_table_xent(XENT_ROUND, bf16)[xent_tile(n, dim, tokens)];
