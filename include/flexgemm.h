@@ -298,7 +298,7 @@ fg_status fg_layernorm(int64_t rows, int64_t cols, const fg_matrix *X, const voi
 /*
  * Its gradient: with xh = (X - mean) * rstd and g = dY * gamma, dX = rstd * (g - sum g / cols - xh * sum(g * xh) / cols); dgamma = sum over rows of
  * dY * xh, dbeta = sum over rows of dY (zero without rows).  mean and rstd are those of the forward call.  dgamma and dbeta (type
- * param_dtype) may be NULL; with both NULL no workspace is needed.  dX may alias dY or X exactly.
+ * param_dtype) may be NULL; with both NULL no workspace is needed.  dX may alias dY (not one of ld 0) or X exactly.
  * dY may have ld 0: the same row for all.
  */
 fg_status fg_layernorm_grad(int64_t rows, int64_t cols, const fg_matrix *dY, const fg_matrix *X, const void *gamma, int32_t param_dtype,
@@ -345,7 +345,7 @@ int64_t fg_linear_xent_workspace(int64_t tokens, int64_t vocab, int64_t dim);
  * The logits are formed again, a piece of the vocabulary at a time; dz is rounded to the type of X (binary16: relative to the
  * largest dloss, so that it neither overflows nor vanishes where dX and dW do not) and multiplied by W and X into FP32.
  *   dloss  : FP32, one value per token, or with dloss_inc 0 a single one for all (1 otherwise).
- *   dX, dW : of the type of X, the shapes of X and W (FG_ERR_UNSUPPORTED for rows of more than 2^21 - 4 values).
+ *   dX, dW : of the type of X, the shapes of X and W, in other memory (FG_ERR_UNSUPPORTED for rows of more than 2^21 - 4 values).
  * The product with dX splits its K where that pays, through the workspace.  A smaller workspace than the query gives is accepted as long as it holds pieces of
  * 256 words; sums are then formed in another order.
  */

@@ -381,12 +381,20 @@ template <class F> void with_waves(int w, F &&f) {
     }
 }
 
+// A result that lies where an operand does has its rows where the operand's are: a workgroup writes only rows that no other reads.
+fg_status check_in_place(const char *name, const fg_matrix *in, const char *out_name, const fg_matrix *out, int64_t rows) {
+    if (rows > 1 && in->re == out->re && in->ld != out->ld)
+        return fail(FG_ERR_LAYOUT, "%s in the place of %s must have its leading dimension", out_name, name);
+    return FG_OK;
+}
+
 fg_status check_layernorm(int64_t rows, int64_t cols, const fg_matrix *X, const char *name, const fg_matrix *Y, const void *gamma, int32_t param_dtype) {
     if (rows < 0 || cols < 0) return fail(FG_ERR_SHAPE, "negative size: %lld rows of %lld", (long long)rows, (long long)cols);
     if (rows > (1 << 30) || cols > (1 << 30)) return fail(FG_ERR_UNSUPPORTED, "sizes above 2^30 are not supported");
     if (fg_status st = check_rows("X", X, rows, cols)) return st;
     if (fg_status st = check_rows(name, Y, rows, cols)) return st;
     if (X->dtype != Y->dtype) return fail(FG_ERR_UNSUPPORTED, "X and %s must have the same element type", name);
+    if (cols > 0) if (fg_status st = check_in_place("X", X, name, Y, rows)) return st;
     if (param_dtype != FG_F32 && param_dtype != X->dtype) return fail(FG_ERR_LAYOUT, "gamma and beta must be FG_F32 or of the type of X");
     if (!aligned_to(gamma, element_bytes(param_dtype))) return fail(FG_ERR_ALIGN, "gamma must be aligned to an element");
     return FG_OK;
@@ -446,6 +454,7 @@ fg_status fg_layernorm_grad(int64_t rows, int64_t cols, const fg_matrix *dY, con
     if (fg_status st = check_layernorm(rows, cols, X, "dX", dX, gamma, param_dtype)) return st;
     if (fg_status st = check_rows("dY", dY, rows, cols, true)) return st;
     if (dY->dtype != X->dtype) return fail(FG_ERR_UNSUPPORTED, "X and dY must have the same element type");
+    if (cols > 0) if (fg_status st = check_in_place("dY", dY, "dX", dX, rows)) return st;
     const unsigned es = element_bytes(param_dtype);
     if (!aligned_to(dgamma, es) || !aligned_to(dbeta, es) || !aligned_to(mean, 4) || !aligned_to(rstd, 4))
         return fail(FG_ERR_ALIGN, "mean, rstd, dgamma and dbeta must be aligned to an element");
