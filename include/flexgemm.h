@@ -107,7 +107,9 @@ typedef enum {
     FG_ZERO = 3   /* all-zero matrix that is never read (C only; same as passing C == NULL)    */
 } fg_layout;
 
-typedef enum { FG_ACT_NONE = 0, FG_ACT_RELU = 1 } fg_act;       /* relu(y) = max(y, 0)         */
+/* relu(y) = max(y, 0); silu(y) = y / (1 + exp(-y)); gelu_tanh(y) = y (1 + tanh(sqrt(2 / pi) (y + 0.044715 y^3))) / 2.
+ * The last two belong to fg_gated_ffn; products have the first two. */
+typedef enum { FG_ACT_NONE = 0, FG_ACT_RELU = 1, FG_ACT_SILU = 2, FG_ACT_GELU_TANH = 3 } fg_act;
 
 /* A matrix operand.  `im == NULL`: real matrix, or, with dtype FG_CF16 / FG_CF32, a complex matrix
  * in interleaved storage (Section 5.4: the real and imaginary part of an element are adjacent;
@@ -353,6 +355,70 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
                               float scale, const float *lse, const float *dloss, int64_t dloss_inc, const fg_matrix *dX, const fg_matrix *dW,
                               void *workspace, int64_t workspace_bytes, void *hip_stream);
 int64_t fg_linear_xent_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim);
+
+/* ---- the middle of a language model, and its update ------------------------------------------------------------ */
+
+/*
+ * Gated feed-forward block: with [G U] = X * W_in^T and H = act(G) * U (element by element),   Y = H * W_out^T.
+ *   X, Y  : tokens x dim; W_in : 2 hidden x dim, the rows of G and then those of U; W_out : dim x hidden.  All FG_F16 or all FG_BF16,
+ *           multiplied exactly and summed in FP32; H is rounded to that type between the products.  Y may not overlap an operand.
+ *   act   : FG_ACT_NONE, FG_ACT_RELU, FG_ACT_SILU, FG_ACT_GELU_TANH.
+ *   GU    : tokens x 2 hidden, FG_F32: G and U, written for fg_gated_ffn_grad; NULL: not wanted.  (Rounded to 16 bits they would make the errors of
+ *           the gradients 1.4 times as large.)
+ * Rows that are not 16-byte aligned, or not of a multiple of 8 values, are copied into the workspace first.
+ * FG_ERR_UNSUPPORTED for dim or 2 hidden of 2^21 - 8 and more, and for products of more than 2^25 tiles of 64 x 64 results.
+ */
+fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_matrix *X, const fg_matrix *W_in, const fg_matrix *W_out, int32_t act,
+                       const fg_matrix *Y, const fg_matrix *GU, void *workspace, int64_t workspace_bytes, void *hip_stream);
+int64_t fg_gated_ffn_workspace(int64_t tokens, int64_t dim, int64_t hidden);
+
+/*
+ * Its gradient, from the GU of the forward call: with dH = dY * W_out, dG = dH * U * act'(G), dU = dH * act(G),
+ *   dX = [dG dU] * W_in,   dW_in = [dG dU]^T * X,   dW_out = dY^T * H        (zero without tokens; relu'(0) = 0).
+ * dG, dU and H are rounded to the type of X between the products (binary16: gradients are kept in range by a scaled loss).
+ * dX, dW_in and dW_out are of the type and shape of X, W_in and W_out, in other memory; each may be NULL: not wanted.
+ */
+fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const fg_matrix *dY, const fg_matrix *X, const fg_matrix *W_in,
+                            const fg_matrix *W_out, int32_t act, const fg_matrix *GU, const fg_matrix *dX, const fg_matrix *dW_in, const fg_matrix *dW_out,
+                            void *workspace, int64_t workspace_bytes, void *hip_stream);
+int64_t fg_gated_ffn_grad_workspace(int64_t tokens, int64_t dim, int64_t hidden);
+
+/* A run of n values in memory, of type FG_F16, FG_BF16 or FG_F32. */
+typedef struct { const void *values; int64_t n; int32_t dtype; } fg_values;
+
+/*
+ * Norm of many gradients: norm = scale * sqrt(sum of the squares of all values of all tensors), in 64 bits, and the factor that brings them to
+ * max_norm at most: factor = scale * min(1, max_norm / norm); NaN if the norm is no finite number.  (scale: one over a scaled loss's scale.)
+ *   grads  : `count` descriptions, in host memory, read before the call returns; norm, factor : one FP32 value each, factor may be NULL.
+ */
+fg_status fg_grad_norm(int64_t count, const fg_values *grads, float scale, float max_norm, float *norm, float *factor, void *workspace,
+                       int64_t workspace_bytes, void *hip_stream);
+int64_t fg_grad_norm_workspace(int64_t count);
+
+/* A parameter, its gradient and its state, n values each (contiguous). */
+typedef struct {
+    void *param;                       /* FG_F16, FG_BF16 or FG_F32                                                          */
+    const void *grad;                  /* of the type of param, or FG_F32                                                    */
+    float *master;                     /* FP32 values that 16-bit parameters are rounded from (and not read), or NULL        */
+    void *exp_avg, *exp_avg_sq;        /* the moments: FP32; in eight bits e4m3 numbers, 16-byte aligned                     */
+    float *avg_scale, *sq_scale;       /* moments in eight bits: a scale for each 256 values, (n + 255) / 256; NULL: in FP32 */
+    int64_t n;
+    int32_t param_dtype, grad_dtype;
+} fg_adamw_tensor;
+
+/*
+ * One step of AdamW on all tensors: with t = *step, counted from 1, g = grad_factor * grad and lr multiplied by lr_factor,
+ *   exp_avg = beta1 * exp_avg + (1 - beta1) * g,   exp_avg_sq = beta2 * exp_avg_sq + (1 - beta2) * g^2,
+ *   param = (1 - lr * weight_decay) * param - lr / (1 - beta1^t) * exp_avg / (sqrt(exp_avg_sq) / sqrt(1 - beta2^t) + eps).
+ *   tensors : `count` descriptions, in host memory, read before the call returns; they may not overlap.  All with moments in FP32 or all in eight bits.
+ *   step, grad_factor, lr_factor : one value each in device memory (a captured step is replayed with others); the factors may be NULL: 1.
+ * Nothing is changed where grad_factor is no finite number (gradients that overflowed, see fg_grad_norm) or *step is below 1.
+ * Moments in eight bits stand for number * scale, and the second one for (number * scale)^2: its root is kept.  The scale is the largest absolute
+ * value of 256 / 448 (0 below 1e-30 / 448), numbers are rounded to nearest even, a root above zero to the smallest number (2^-9) at least.  The step itself uses
+ * the moments before they are rounded.
+ */
+fg_status fg_adamw(int64_t count, const fg_adamw_tensor *tensors, const int64_t *step, double lr, double beta1, double beta2, double eps,
+                   double weight_decay, const float *grad_factor, const float *lr_factor, void *hip_stream);
 
 /* Message for the most recent failing call on this thread ("" if none).  The pointer refers to
  * thread-local static storage: valid until the next library call on the same thread. */

@@ -25,12 +25,13 @@ FG_OK = 0
 FG_ERR_NULL, FG_ERR_SHAPE, FG_ERR_LAYOUT, FG_ERR_ALIGN, FG_ERR_UNSUPPORTED, FG_ERR_MODES, FG_ERR_LAUNCH = range(1, 8)
 FG_F16, FG_BF16, FG_F32, FG_CF16, FG_CF32, FG_I32, FG_I64 = 0, 1, 2, 3, 4, 5, 6
 FG_COL, FG_ROW, FG_DIAG, FG_ZERO = 0, 1, 2, 3
-FG_ACT_NONE, FG_ACT_RELU = 0, 1
+FG_ACT_NONE, FG_ACT_RELU, FG_ACT_SILU, FG_ACT_GELU_TANH = 0, 1, 2, 3
 
 EXPORTS = ("fg_init", "fg_gemm", "fg_gemm_ex", "fg_gemm_noalloc", "fg_gemm_dual", "fg_contract", "fg_contract_plan", "fg_last_error", "fg_version",
            "fg_reload_tuning", "fg_gemm_plan", "fg_probe_mfma", "fg_probe_mfma_k32", "fg_probe_kloop_mix",
            "fg_layernorm", "fg_layernorm_grad", "fg_layernorm_grad_workspace", "fg_embedding", "fg_embedding_grad", "fg_embedding_grad_workspace",
-           "fg_linear_xent", "fg_linear_xent_workspace", "fg_linear_xent_grad", "fg_linear_xent_grad_workspace")
+           "fg_linear_xent", "fg_linear_xent_workspace", "fg_linear_xent_grad", "fg_linear_xent_grad_workspace",
+           "fg_gated_ffn", "fg_gated_ffn_workspace", "fg_gated_ffn_grad", "fg_gated_ffn_grad_workspace", "fg_adamw", "fg_grad_norm", "fg_grad_norm_workspace")
 FG_PLAN_REAL, FG_PLAN_COMPLEX, FG_PLAN_DUAL, FG_PLAN_REAL_BF16, FG_PLAN_COMPLEX_INTERLEAVED, FG_PLAN_REAL_F16_CD = 0, 1, 2, 3, 4, 5
 FG_PLAN_REAL_AB_ADD = 6
 
@@ -45,6 +46,15 @@ class fg_epilogue(C.Structure):
 
 class fg_load_transforms(C.Structure):
     _fields_ = [("a_add", C.c_float), ("b_add", C.c_float), ("c_act", C.c_int32)]
+
+
+class fg_adamw_tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("master", C.c_void_p), ("exp_avg", C.c_void_p), ("exp_avg_sq", C.c_void_p),
+                ("avg_scale", C.c_void_p), ("sq_scale", C.c_void_p), ("n", C.c_int64), ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32)]
+
+
+class fg_values(C.Structure):
+    _fields_ = [("values", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
 
 
 class FlexGemmError(RuntimeError):
@@ -119,6 +129,17 @@ def load_library() -> C.CDLL:
         lib.fg_linear_xent_grad.argtypes = [i64, i64, i64, mp, mp, vp, i32, f32, vp, vp, i64, mp, mp, vp, i64, vp]
         lib.fg_linear_xent_workspace.restype = lib.fg_linear_xent_grad_workspace.restype = i64
         lib.fg_linear_xent_workspace.argtypes = lib.fg_linear_xent_grad_workspace.argtypes = [i64, i64, i64]
+        lib.fg_gated_ffn.restype = lib.fg_gated_ffn_grad.restype = C.c_int
+        lib.fg_gated_ffn.argtypes = [i64, i64, i64, mp, mp, mp, i32, mp, mp, vp, i64, vp]
+        lib.fg_gated_ffn_grad.argtypes = [i64, i64, i64, mp, mp, mp, mp, i32, mp, mp, mp, mp, vp, i64, vp]
+        lib.fg_gated_ffn_workspace.restype = lib.fg_gated_ffn_grad_workspace.restype = i64
+        lib.fg_gated_ffn_workspace.argtypes = lib.fg_gated_ffn_grad_workspace.argtypes = [i64, i64, i64]
+        f64 = C.c_double
+        lib.fg_adamw.restype = lib.fg_grad_norm.restype = C.c_int
+        lib.fg_adamw.argtypes = [i64, C.POINTER(fg_adamw_tensor), vp, f64, f64, f64, f64, f64, vp, vp, vp]
+        lib.fg_grad_norm.argtypes = [i64, C.POINTER(fg_values), f32, f32, vp, vp, vp, i64, vp]
+        lib.fg_grad_norm_workspace.restype = i64
+        lib.fg_grad_norm_workspace.argtypes = [i64]
         _load_fastcall(lib)
         _lib = lib
     return _lib
@@ -129,7 +150,8 @@ _in_bad_fork = getattr(torch._C, "_cuda_isInBadFork", lambda: False)
 
 class _CtypesOnly:
     """In place of the native marshalling where it is not built: leaves every call to the binding (4 to 8 us more each)."""
-    gemm = dual = contract = layernorm = layernorm_grad = embedding = embedding_grad = xent = xent_grad = staticmethod(lambda *args: -1)
+    gemm = dual = contract = layernorm = layernorm_grad = embedding = embedding_grad = xent = xent_grad = \
+        gated_ffn = gated_ffn_grad = adamw = grad_norm = staticmethod(lambda *args: -1)
 
 
 def _load_fastcall(lib: C.CDLL) -> None:
@@ -146,7 +168,9 @@ def _load_fastcall(lib: C.CDLL) -> None:
                *(C.cast(fn, C.c_void_p).value for fn in (lib.fg_gemm, lib.fg_gemm_ex, lib.fg_gemm_noalloc, lib.fg_gemm_dual, lib.fg_contract)))
     fast.setup_rows(*(C.cast(fn, C.c_void_p).value for fn in (
         lib.fg_layernorm, lib.fg_layernorm_grad, lib.fg_layernorm_grad_workspace, lib.fg_embedding, lib.fg_embedding_grad, lib.fg_embedding_grad_workspace,
-        lib.fg_linear_xent, lib.fg_linear_xent_workspace, lib.fg_linear_xent_grad, lib.fg_linear_xent_grad_workspace)))
+        lib.fg_linear_xent, lib.fg_linear_xent_workspace, lib.fg_linear_xent_grad, lib.fg_linear_xent_grad_workspace,
+        lib.fg_gated_ffn, lib.fg_gated_ffn_workspace, lib.fg_gated_ffn_grad, lib.fg_gated_ffn_grad_workspace,
+        lib.fg_adamw, lib.fg_grad_norm, lib.fg_grad_norm_workspace)))
     _fast = fast
 
 
@@ -553,4 +577,130 @@ def fg_linear_xent_grad(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor,
     ws, ws_bytes, _keep = _workspace(workspace, lib.fg_linear_xent_grad_workspace(tokens, vocab, dim), stream, dev)
     st = lib.fg_linear_xent_grad(tokens, vocab, dim, C.byref(x), C.byref(w), at, kind, scale, _vector(lse, tokens, "lse", torch.float32, dev), g, inc,
                                  C.byref(dx), C.byref(dw), ws, ws_bytes, _stream_handle(stream))
+    return _check(st, raise_on_error)
+
+
+# ---- the middle of a language model, and its update --------------------------------------------------
+
+def fg_gated_ffn_workspace(tokens: int, dim: int, hidden: int) -> int:
+    return int(load_library().fg_gated_ffn_workspace(tokens, dim, hidden))
+
+
+def _block(X: torch.Tensor, W_in: torch.Tensor, W_out: torch.Tensor, dev: int):
+    """Descriptors and sizes of a gated block's operands."""
+    x = _rows(X, "X", None, dev)
+    tokens, dim = X.shape
+    if W_in.dim() != 2 or W_in.shape[0] % 2:
+        raise ValueError("W_in: expected a matrix with the rows of gate and up, got shape %s" % (tuple(W_in.shape),))
+    hidden = W_in.shape[0] // 2
+    return x, _rows(W_in, "W_in", (2 * hidden, dim), dev), _rows(W_out, "W_out", (dim, hidden), dev), tokens, dim, hidden
+
+
+def fg_gated_ffn(X: torch.Tensor, W_in: torch.Tensor, W_out: torch.Tensor, act: int, Y: torch.Tensor, GU: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None, stream=None, raise_on_error: bool = True) -> int:
+    """Y = (act(G) * U) W_out^T with [G U] = X W_in^T; W_in has the rows of G and then those of U.  GU (FP32) keeps both for fg_gated_ffn_grad."""
+    lib = _lib or load_library()
+    st = _fast.gated_ffn(X, W_in, W_out, act, Y, GU, workspace, stream)
+    if st >= 0:
+        return st if st == FG_OK else _check(st, raise_on_error)
+    dev = _current_device()
+    x, w_in, w_out, tokens, dim, hidden = _block(X, W_in, W_out, dev)
+    y = _rows(Y, "Y", X.shape, dev)
+    gu = None if GU is None else _rows(GU, "GU", (tokens, 2 * hidden), dev)
+    ws, ws_bytes, _keep = _workspace(workspace, lib.fg_gated_ffn_workspace(tokens, dim, hidden), stream, dev)
+    st = lib.fg_gated_ffn(tokens, dim, hidden, C.byref(x), C.byref(w_in), C.byref(w_out), act, C.byref(y), _ref(gu), ws, ws_bytes, _stream_handle(stream))
+    return _check(st, raise_on_error)
+
+
+def fg_gated_ffn_grad_workspace(tokens: int, dim: int, hidden: int) -> int:
+    return int(load_library().fg_gated_ffn_grad_workspace(tokens, dim, hidden))
+
+
+def fg_gated_ffn_grad(dY: torch.Tensor, X: torch.Tensor, W_in: torch.Tensor, W_out: torch.Tensor, act: int, GU: torch.Tensor,
+                      dX: Optional[torch.Tensor] = None, dW_in: Optional[torch.Tensor] = None, dW_out: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None, stream=None, raise_on_error: bool = True) -> int:
+    """Gradients of fg_gated_ffn with respect to X, W_in and W_out, from the GU that it kept."""
+    lib = _lib or load_library()
+    st = _fast.gated_ffn_grad(dY, X, W_in, W_out, act, GU, dX, dW_in, dW_out, workspace, stream)
+    if st >= 0:
+        return st if st == FG_OK else _check(st, raise_on_error)
+    dev = _current_device()
+    x, w_in, w_out, tokens, dim, hidden = _block(X, W_in, W_out, dev)
+    dy = _rows(dY, "dY", X.shape, dev)
+    gu = _rows(GU, "GU", (tokens, 2 * hidden), dev)
+    dx = None if dX is None else _rows(dX, "dX", X.shape, dev)
+    dw_in = None if dW_in is None else _rows(dW_in, "dW_in", W_in.shape, dev)
+    dw_out = None if dW_out is None else _rows(dW_out, "dW_out", W_out.shape, dev)
+    ws, ws_bytes, _keep = _workspace(workspace, lib.fg_gated_ffn_grad_workspace(tokens, dim, hidden), stream, dev)
+    st = lib.fg_gated_ffn_grad(tokens, dim, hidden, C.byref(dy), C.byref(x), C.byref(w_in), C.byref(w_out), act, C.byref(gu), _ref(dx), _ref(dw_in),
+                               _ref(dw_out), ws, ws_bytes, _stream_handle(stream))
+    return _check(st, raise_on_error)
+
+
+def _values(t: torch.Tensor, name: str, dev: int, shape=None, dtype=None) -> int:
+    """The address of a contiguous tensor."""
+    if not t.is_cuda or t.get_device() != dev:
+        raise ValueError("%s: a tensor on the current GPU is needed, got one on %s" % (name, t.device))
+    if (shape is not None and t.shape != shape) or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous tensor%s, got shape %s, strides %s" % (
+            name, "" if shape is None else " of shape %s" % (tuple(shape),), tuple(t.shape), t.stride()))
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError("%s: expected %s, got %s" % (name, dtype, t.dtype))
+    return t.data_ptr()
+
+
+def fg_adamw(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], exp_avg: Sequence[torch.Tensor], exp_avg_sq: Sequence[torch.Tensor],
+             step: torch.Tensor, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float,
+             masters: Optional[Sequence[Optional[torch.Tensor]]] = None, avg_scales: Optional[Sequence[torch.Tensor]] = None,
+             sq_scales: Optional[Sequence[torch.Tensor]] = None, grad_factor: Optional[torch.Tensor] = None, lr_factor: Optional[torch.Tensor] = None,
+             stream=None, raise_on_error: bool = True) -> int:
+    """One step of AdamW on all params, in place.  step: one int64 on the GPU, counted from 1.  masters: FP32 copies of 16-bit params, None for those
+    without.  With avg_scales and sq_scales (FP32, one value for each 256) the moments are float8_e4m3fn, exp_avg_sq the root."""
+    lib = _lib or load_library()
+    st = _fast.adamw(params, grads, exp_avg, exp_avg_sq, step, lr, beta1, beta2, eps, weight_decay, masters, avg_scales, sq_scales, grad_factor, lr_factor, stream)
+    if st >= 0:
+        return st if st == FG_OK else _check(st, raise_on_error)
+    dev = _current_device()
+    lists = dict(grads=grads, exp_avg=exp_avg, exp_avg_sq=exp_avg_sq, masters=masters, avg_scales=avg_scales, sq_scales=sq_scales)
+    for name, items in lists.items():
+        if items is not None and len(items) != len(params):
+            raise ValueError("%s: expected %d tensors, got %d" % (name, len(params), len(items)))
+    if (avg_scales is None) != (sq_scales is None):
+        raise ValueError("avg_scales, sq_scales: moments in eight bits need both")
+    moment = torch.float32 if avg_scales is None else torch.float8_e4m3fn
+    tensors = (fg_adamw_tensor * len(params))()
+    for i, (t, p) in enumerate(zip(tensors, params)):
+        t.n, t.param_dtype, t.grad_dtype = p.numel(), _DTYPES.get(p.dtype, -1), _DTYPES.get(grads[i].dtype, -1)
+        t.param, t.grad = _values(p, "params[%d]" % i, dev), _values(grads[i], "grads[%d]" % i, dev, p.shape)
+        t.exp_avg = _values(exp_avg[i], "exp_avg[%d]" % i, dev, p.shape, moment)
+        t.exp_avg_sq = _values(exp_avg_sq[i], "exp_avg_sq[%d]" % i, dev, p.shape, moment)
+        if masters is not None and masters[i] is not None:
+            t.master = _values(masters[i], "masters[%d]" % i, dev, p.shape, torch.float32)
+        if avg_scales is not None:
+            blocks = (t.n + 255) // 256
+            t.avg_scale = _vector(avg_scales[i], blocks, "avg_scales[%d]" % i, torch.float32, dev)
+            t.sq_scale = _vector(sq_scales[i], blocks, "sq_scales[%d]" % i, torch.float32, dev)
+    st = lib.fg_adamw(len(params), tensors, _vector(step, 1, "step", torch.int64, dev), lr, beta1, beta2, eps, weight_decay,
+                      _vector(grad_factor, 1, "grad_factor", torch.float32, dev), _vector(lr_factor, 1, "lr_factor", torch.float32, dev), _stream_handle(stream))
+    return _check(st, raise_on_error)
+
+
+def fg_grad_norm_workspace(count: int) -> int:
+    return int(load_library().fg_grad_norm_workspace(count))
+
+
+def fg_grad_norm(grads: Sequence[torch.Tensor], scale: float, max_norm: float, norm: torch.Tensor, factor: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None, stream=None, raise_on_error: bool = True) -> int:
+    """norm = scale * the norm of all grads; factor = scale * min(1, max_norm / norm), for fg_adamw's grad_factor."""
+    lib = _lib or load_library()
+    st = _fast.grad_norm(grads, scale, max_norm, norm, factor, workspace, stream)
+    if st >= 0:
+        return st if st == FG_OK else _check(st, raise_on_error)
+    dev = _current_device()
+    values = (fg_values * len(grads))()
+    for i, (v, g) in enumerate(zip(values, grads)):
+        v.values, v.n, v.dtype = _values(g, "grads[%d]" % i, dev), g.numel(), _DTYPES.get(g.dtype, -1)
+    ws, ws_bytes, _keep = _workspace(workspace, lib.fg_grad_norm_workspace(len(grads)), stream, dev)
+    st = lib.fg_grad_norm(len(grads), values, scale, max_norm, _vector(norm, 1, "norm", torch.float32, dev), _vector(factor, 1, "factor", torch.float32, dev),
+                          ws, ws_bytes, _stream_handle(stream))
     return _check(st, raise_on_error)

@@ -1,0 +1,488 @@
+// What follows a backward pass, over all tensors of a model at once: the norm of the gradients, and the AdamW step.
+//
+//   norm = scale sqrt(sum over all g^2),   factor = scale min(1, max_norm / norm)
+//   g' = factor g,  m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2,
+//   p = (1 - lr wd) p - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+//
+// Bound by memory: each value of a tensor is read and written once (28 bytes a 16-bit parameter with an FP32 copy, gradient and FP32 moments,
+// 10 with moments in eight bits and no copy).  A launch covers the tensors that a kernel's arguments hold; each workgroup takes a
+// chunk of one, found by bisection of the chunks' numbers.  Nothing is kept between calls: the tensors' addresses travel with the launch.
+//
+// Moments in eight bits (e4m3) have an FP32 scale for each 256 values, the largest of them / 448.  Of v the root is kept: its range
+// of 2^17 is one of 2^34 of v.  A root that is not zero is held at least as the smallest such number: m / (root + eps) of a v that was rounded
+// to zero would be m / eps.  The step itself uses m and v in FP32, as they are before they are rounded.
+//
+// The operations are written one by one, without fused ones: what eight bits hold changes by 1/16 where a sum falls on the other side of a border.
+#include "row_ops.hpp"
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <type_traits>
+#include <vector>
+
+namespace fg {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kStateBlock = 256;            // values that share a scale
+constexpr int kLaneBlock = 16;              // of them in a lane: 16 lanes, a row of the wave, share one
+constexpr int kChunk = 8192;                // values of a workgroup
+constexpr float kTop = 448.f, kLeast = 0x1p-9f;         // of e4m3: the largest number, the smallest one above zero
+constexpr float kNothing = 1e-30f;          // a block whose largest value is smaller is zero (its scale's reciprocal would overflow)
+
+struct TensorArg {
+    void *p;
+    const void *g;
+    float *master;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    int64_t n;
+    int32_t first;                          // number of its first chunk in the launch
+    int32_t kind;
+};
+// Arguments are copied through the command path: few tensors have a short list of them.
+template <int CAP> struct TensorArgs { TensorArg at[CAP]; };
+
+struct StepArgs {
+    double lr, beta1, beta2, eps, decay;
+    const int64_t *step;
+    const float *factor, *lr_factor;
+    int32_t count;
+};
+// What a step needs of them, in FP32.
+struct Rates {
+    float beta1, other1, beta2, other2, eps, keep, rate, root, factor;
+};
+
+// Which of `count` tensors chunk `c` is in: the last one whose first chunk is not behind it.
+template <class T>
+__device__ __forceinline__ int tensor_of(const T *at, int count, int c) {
+    int lo = 0, hi = count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (at[mid].first <= c) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// x^t by squaring; 64-bit, for 1 - x^t of an x near 1.
+__device__ __forceinline__ double power(double x, int64_t t) {
+    double y = 1.0;
+    for (; t > 0 && y != 0.0; t >>= 1, x *= x)
+        if (t & 1) y *= x;
+    return y;
+}
+
+// False where there is nothing to do: a factor that is no finite number (gradients that overflowed), or no step.
+__device__ __forceinline__ bool rates_of(const StepArgs &s, Rates &r) {
+    const int64_t t = *s.step;
+    r.factor = s.factor ? *s.factor : 1.f;
+    if (t < 1 || !(__builtin_fabsf(r.factor) < __builtin_inff())) return false;
+    const double lr = s.lr_factor ? s.lr * (double)*s.lr_factor : s.lr;
+    r.beta1 = (float)s.beta1; r.other1 = (float)(1.0 - s.beta1);
+    r.beta2 = (float)s.beta2; r.other2 = (float)(1.0 - s.beta2);
+    r.eps = (float)s.eps;
+    r.keep = (float)(1.0 - lr * s.decay);
+    r.rate = (float)(lr / (1.0 - power(s.beta1, t)));
+    r.root = (float)(1.0 / __builtin_sqrt(1.0 - power(s.beta2, t)));
+    return true;
+}
+
+// One value: m and v become the new ones, the new parameter and v's root are returned.
+__device__ __forceinline__ float stepped(const Rates &r, float p, float g, float &m, float &v, float &root) {
+#pragma clang fp contract(off)
+    g = g * r.factor;
+    m = m * r.beta1 + g * r.other1;
+    v = v * r.beta2 + g * g * r.other2;
+    root = __builtin_sqrtf(v);
+    return p * r.keep - r.rate * (m / (root * r.root + r.eps));
+}
+
+// N values from `at` on, those past the end of n left as they are.
+template <class T, int N>
+__device__ __forceinline__ void load_values(const T *from, int64_t at, int64_t n, float (&out)[N]) {
+    constexpr int E = 16 / (int)sizeof(T) < N ? 16 / (int)sizeof(T) : N;
+    if (at + N <= n) {
+#pragma unroll
+        for (int h = 0; h < N / E; ++h) {
+            const typename RowPiece<T, E>::vec v = *(const typename RowPiece<T, E>::unaligned *)(from + at + h * E);
+#pragma unroll
+            for (int e = 0; e < E; ++e) out[h * E + e] = (float)v[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) out[e] = at + e < n ? (float)from[at + e] : 0.f;
+    }
+}
+template <class T, int N>
+__device__ __forceinline__ void store_values(T *to, int64_t at, int64_t n, const float (&in)[N]) {
+    constexpr int E = 16 / (int)sizeof(T) < N ? 16 / (int)sizeof(T) : N;
+    if (at + N <= n) {
+#pragma unroll
+        for (int h = 0; h < N / E; ++h) {
+            typename RowPiece<T, E>::vec v;
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = (T)in[h * E + e];
+            *(typename RowPiece<T, E>::unaligned *)(to + at + h * E) = v;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (at + e < n) to[at + e] = (T)in[e];
+    }
+}
+
+// ---- moments in eight bits ----------------------------------------------------------------------------
+typedef uint32_t codes16 __attribute__((ext_vector_type(4)));
+typedef float float2v __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ void load_codes(const void *from, int64_t at, int64_t n, float scale, float (&out)[kLaneBlock]) {
+    codes16 c = {};
+    if (at + kLaneBlock <= n) c = *(const codes16 *)((const uint8_t *)from + at);
+    else
+        for (int e = 0; e < kLaneBlock; ++e)
+            if (at + e < n) c[e / 4] |= (uint32_t)((const uint8_t *)from)[at + e] << (e % 4 * 8);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float2v lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[w], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[w], true);
+        out[4 * w] = lo[0] * scale; out[4 * w + 1] = lo[1] * scale; out[4 * w + 2] = hi[0] * scale; out[4 * w + 3] = hi[1] * scale;
+    }
+}
+__device__ __forceinline__ void store_codes(void *to, int64_t at, int64_t n, const float (&in)[kLaneBlock]) {
+    codes16 c;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        int word = __builtin_amdgcn_cvt_pk_fp8_f32(in[4 * w], in[4 * w + 1], 0, false);
+        c[w] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(in[4 * w + 2], in[4 * w + 3], word, true);
+    }
+    if (at + kLaneBlock <= n) *(codes16 *)((uint8_t *)to + at) = c;
+    else
+        for (int e = 0; e < kLaneBlock; ++e)
+            if (at + e < n) ((uint8_t *)to)[at + e] = (uint8_t)(c[e / 4] >> (e % 4 * 8));
+}
+// The largest of a row of 16 lanes, in all of them.
+__device__ __forceinline__ float row_max(float v) {
+    auto turned = [](float x, auto ctrl) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, false));
+    };
+    v = __builtin_fmaxf(v, turned(v, std::integral_constant<int, 0x128>{}));
+    v = __builtin_fmaxf(v, turned(v, std::integral_constant<int, 0x124>{}));
+    v = __builtin_fmaxf(v, turned(v, std::integral_constant<int, 0x122>{}));
+    return __builtin_fmaxf(v, turned(v, std::integral_constant<int, 0x121>{}));
+}
+// A block's values relative to its scale, and the scale.  FLOOR: at least kLeast where they are not zero.
+template <bool FLOOR>
+__device__ __forceinline__ float relative(float (&x)[kLaneBlock]) {
+#pragma clang fp contract(off)
+    float top = 0.f;
+#pragma unroll
+    for (int e = 0; e < kLaneBlock; ++e) top = __builtin_fmaxf(top, __builtin_fabsf(x[e]));
+    top = row_max(top);
+    const float by = top >= kNothing ? kTop / top : 0.f;
+#pragma unroll
+    for (int e = 0; e < kLaneBlock; ++e) {
+        x[e] *= by;
+        if (FLOOR) x[e] = x[e] > 0.f && x[e] < kLeast ? kLeast : x[e];
+    }
+    return top >= kNothing ? top / kTop : 0.f;
+}
+
+// ---- the step -----------------------------------------------------------------------------------------
+// P: parameters, G: gradients, COPY: with an FP32 copy, which is what the step reads.
+template <class P, class G, bool COPY, bool SMALL>
+__device__ __forceinline__ void step_chunk(const TensorArg &t, const Rates &r, int64_t begin) {
+    constexpr int N = SMALL ? kLaneBlock : 8;
+    const int64_t end = begin + kChunk < t.n ? begin + kChunk : t.n;
+    // (the lanes of a row are in the same block, and go round together)
+    for (int64_t at = begin + threadIdx.x * N; SMALL ? at / kStateBlock * kStateBlock < end : at < end; at += kThreads * N) {
+        float p[N], g[N], m[N], v[N], root[N];
+        load_values<G, N>((const G *)t.g, at, t.n, g);
+        if constexpr (COPY) load_values<float, N>(t.master, at, t.n, p);
+        else load_values<P, N>((const P *)t.p, at, t.n, p);
+        if constexpr (SMALL) {
+            const int64_t block = at / kStateBlock;
+            load_codes(t.m, at, t.n, t.m_scale[block], m);
+            load_codes(t.v, at, t.n, t.v_scale[block], v);
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = v[e] * v[e];
+        } else {
+            load_values<float, N>((const float *)t.m, at, t.n, m);
+            load_values<float, N>((const float *)t.v, at, t.n, v);
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) p[e] = stepped(r, p[e], g[e], m[e], v[e], root[e]);
+        if constexpr (COPY) store_values<float, N>(t.master, at, t.n, p);
+        store_values<P, N>((P *)t.p, at, t.n, p);
+        if constexpr (SMALL) {
+            const float sm = relative<false>(m), sv = relative<true>(root);
+            store_codes(t.m, at, t.n, m);
+            store_codes(t.v, at, t.n, root);
+            if (at % kStateBlock == 0) {
+                t.m_scale[at / kStateBlock] = sm;
+                t.v_scale[at / kStateBlock] = sv;
+            }
+        } else {
+            store_values<float, N>((float *)t.m, at, t.n, m);
+            store_values<float, N>((float *)t.v, at, t.n, v);
+        }
+    }
+}
+
+// kind: the type of the parameters (FG_F16, FG_BF16, FG_F32), + 4 with FP32 gradients, + 8 with an FP32 copy of the parameters
+constexpr int kWideGrad = 4, kCopy = 8;
+
+template <int CAP, bool SMALL>
+__global__ __launch_bounds__(kThreads) void adamw(const TensorArgs<CAP> a, const StepArgs s) {
+    Rates r;
+    if (!rates_of(s, r)) return;
+    const TensorArg &t = a.at[tensor_of(a.at, s.count, (int)blockIdx.x)];
+    const int64_t begin = ((int64_t)blockIdx.x - t.first) * kChunk;
+    switch (t.kind) {
+        case FG_F16: return step_chunk<f16_t, f16_t, false, SMALL>(t, r, begin);
+        case FG_BF16: return step_chunk<bf16_t, bf16_t, false, SMALL>(t, r, begin);
+        case FG_F32 + kWideGrad: return step_chunk<float, float, false, SMALL>(t, r, begin);
+        case FG_F16 + kWideGrad: return step_chunk<f16_t, float, false, SMALL>(t, r, begin);
+        case FG_BF16 + kWideGrad: return step_chunk<bf16_t, float, false, SMALL>(t, r, begin);
+        case FG_F16 + kCopy: return step_chunk<f16_t, f16_t, true, SMALL>(t, r, begin);
+        case FG_BF16 + kCopy: return step_chunk<bf16_t, bf16_t, true, SMALL>(t, r, begin);
+        case FG_F16 + kCopy + kWideGrad: return step_chunk<f16_t, float, true, SMALL>(t, r, begin);
+        case FG_BF16 + kCopy + kWideGrad: return step_chunk<bf16_t, float, true, SMALL>(t, r, begin);
+    }
+}
+
+// ---- the norm -------------------------------------------------------------------------------------------
+constexpr int kNormGroups = 2048;           // of a launch, at most
+struct GradArg {
+    const void *g;
+    int64_t n;
+    int32_t first, dtype;
+};
+template <int CAP> struct GradArgs { GradArg at[CAP]; };
+
+template <class G>
+__device__ __forceinline__ double squares_of(const GradArg &t, int64_t begin) {
+    constexpr int N = 16 / (int)sizeof(G) * 2;
+    const int64_t end = begin + kChunk < t.n ? begin + kChunk : t.n;
+    double sum = 0.0;
+    for (int64_t at = begin + threadIdx.x * N; at < end; at += kThreads * N) {
+        float g[N];
+        load_values<G, N>((const G *)t.g, at, t.n, g);
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum += (double)g[e] * (double)g[e];
+    }
+    return sum;
+}
+
+// Sum over a workgroup of W waves, by halves; in the first thread.
+template <int W>
+__device__ __forceinline__ double group_total(double v, double *slots) {
+    slots[threadIdx.x] = v;
+    __syncthreads();
+    for (int half = 32 * W; half > 0; half /= 2) {
+        if ((int)threadIdx.x < half) slots[threadIdx.x] += slots[threadIdx.x + half];
+        __syncthreads();
+    }
+    return slots[0];
+}
+
+// Sums in 64 bits: of 10^9 squares nothing is lost, and those of the largest and smallest FP32 values have room.
+template <int CAP>
+__global__ __launch_bounds__(kThreads) void grad_squares(const GradArgs<CAP> a, int count, int chunks, double *partial) {
+    __shared__ double slots[kThreads];
+    double sum = 0.0;
+    for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
+        const GradArg &t = a.at[tensor_of(a.at, count, c)];
+        const int64_t begin = ((int64_t)c - t.first) * kChunk;
+        sum += t.dtype == FG_F16 ? squares_of<f16_t>(t, begin) : t.dtype == FG_BF16 ? squares_of<bf16_t>(t, begin) : squares_of<float>(t, begin);
+    }
+    sum = group_total<kThreads / 64>(sum, slots);
+    if (threadIdx.x == 0) partial[blockIdx.x] = sum;
+}
+
+__global__ __launch_bounds__(1024) void grad_norm(const double *partial, int64_t parts, double scale, double max_norm, float *norm, float *factor) {
+    __shared__ double slots[1024];
+    double sum = 0.0;
+    for (int64_t i = threadIdx.x; i < parts; i += 1024) sum += partial[i];
+    sum = group_total<16>(sum, slots);
+    if (threadIdx.x != 0) return;
+    const double n = __builtin_sqrt(sum) * scale;
+    *norm = (float)n;
+    // (a norm that is no finite FP32 number gives a factor that is none)
+    if (factor) *factor = !((float)n < __builtin_inff()) ? __builtin_nanf("") : (float)(n > max_norm ? max_norm / n * scale : scale);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------
+constexpr int kFewTensors = 6, kMostTensors = 48, kFewGrads = 16, kMostGrads = 128;
+constexpr int64_t kMostChunks = 1 << 23;    // of a launch: fewer than 2^32 threads
+
+int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
+
+fg_status check_tensor_count(int64_t count, const void *tensors) {
+    if (count < 0) return fail(FG_ERR_SHAPE, "negative number of tensors: %lld", (long long)count);
+    if (count > 0 && !tensors) return fail(FG_ERR_NULL, "the list of tensors is NULL");
+    return FG_OK;
+}
+fg_status check_values(const char *name, int64_t i, const void *p, int dtype, int64_t n) {
+    if (!element_bytes(dtype)) return fail(FG_ERR_LAYOUT, "tensor %lld: %s must be FG_F16, FG_BF16 or FG_F32", (long long)i, name);
+    if (n > 0 && !p) return fail(FG_ERR_NULL, "tensor %lld: %s is NULL", (long long)i, name);
+    if (!aligned_to(p, element_bytes(dtype))) return fail(FG_ERR_ALIGN, "tensor %lld: %s must be aligned to an element", (long long)i, name);
+    return FG_OK;
+}
+fg_status check_length(int64_t i, int64_t n) {
+    if (n < 0) return fail(FG_ERR_SHAPE, "tensor %lld: negative length %lld", (long long)i, (long long)n);
+    if (n > kMostChunks * kChunk) return fail(FG_ERR_UNSUPPORTED, "tensor %lld: more than 2^36 values are not supported", (long long)i);
+    return FG_OK;
+}
+
+fg_status check_adamw_tensor(int64_t i, const fg_adamw_tensor &t) {
+    if (fg_status st = check_length(i, t.n)) return st;
+    if (fg_status st = check_values("param", i, t.param, t.param_dtype, t.n)) return st;
+    if (fg_status st = check_values("grad", i, t.grad, t.grad_dtype, t.n)) return st;
+    if (t.grad_dtype != FG_F32 && t.grad_dtype != t.param_dtype) return fail(FG_ERR_LAYOUT, "tensor %lld: grad must be FG_F32 or of the type of param", (long long)i);
+    if (t.master && t.param_dtype == FG_F32) return fail(FG_ERR_LAYOUT, "tensor %lld: FG_F32 parameters have no other FP32 copy", (long long)i);
+    if (t.n > 0 && (!t.exp_avg || !t.exp_avg_sq)) return fail(FG_ERR_NULL, "tensor %lld: exp_avg or exp_avg_sq is NULL", (long long)i);
+    if (!t.avg_scale != !t.sq_scale) return fail(FG_ERR_NULL, "tensor %lld: moments in eight bits need both scales", (long long)i);
+    const unsigned align = t.avg_scale ? 16 : 4;
+    if (!aligned_to(t.exp_avg, align) || !aligned_to(t.exp_avg_sq, align)) return fail(FG_ERR_ALIGN, "tensor %lld: moments must be aligned to %u bytes", (long long)i, align);
+    if (!aligned_to(t.master, 4) || !aligned_to(t.avg_scale, 4) || !aligned_to(t.sq_scale, 4))
+        return fail(FG_ERR_ALIGN, "tensor %lld: master, avg_scale and sq_scale must be aligned to an element", (long long)i);
+    return FG_OK;
+}
+
+// The same values in two tensors would be updated by two workgroups at once.
+fg_status check_apart(int64_t count, const fg_adamw_tensor *tensors) {
+    auto end_of = [](const fg_adamw_tensor &t) { return (const char *)t.param + t.n * element_bytes(t.param_dtype); };
+    const char *last = nullptr;
+    bool in_order = true;
+    for (int64_t i = 0; i < count && in_order; ++i) {
+        if (tensors[i].n == 0) continue;
+        in_order = (const char *)tensors[i].param >= last;
+        last = end_of(tensors[i]);
+    }
+    if (in_order) return FG_OK;
+    try {
+        std::vector<int64_t> order;
+        for (int64_t i = 0; i < count; ++i)
+            if (tensors[i].n > 0) order.push_back(i);
+        std::sort(order.begin(), order.end(), [&](int64_t a, int64_t b) { return tensors[a].param < tensors[b].param; });
+        for (size_t k = 1; k < order.size(); ++k)
+            if (end_of(tensors[order[k - 1]]) > (const char *)tensors[order[k]].param)
+                return fail(FG_ERR_LAYOUT, "tensors %lld and %lld have values of param in common", (long long)order[k - 1], (long long)order[k]);
+    } catch (const std::bad_alloc &) {
+        return fail(FG_ERR_UNSUPPORTED, "no host memory for a list of %lld tensors", (long long)count);
+    }
+    return FG_OK;
+}
+
+// Hands out tensors to launches: f(first tensor, tensors, chunks) with as many as `most` and kMostChunks allow; tensors without values count as well.
+template <class Length, class F> void in_launches(int64_t count, int most, Length &&length, F &&f) {
+    int64_t begin = 0, chunks = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        const int64_t c = chunks_of(length(i));
+        if (i > begin && (i - begin == most || chunks + c > kMostChunks)) {
+            f(begin, (int)(i - begin), chunks);
+            begin = i;
+            chunks = 0;
+        }
+        chunks += c;
+    }
+    if (count > begin) f(begin, (int)(count - begin), chunks);
+}
+
+}  // namespace
+
+hipError_t load_adamw_kernels() {
+    hipFuncAttributes a;
+    return hipFuncGetAttributes(&a, (const void *)grad_norm);
+}
+
+}  // namespace fg
+
+using namespace fg;
+
+extern "C" {
+
+fg_status fg_adamw(int64_t count, const fg_adamw_tensor *tensors, const int64_t *step, double lr, double beta1, double beta2, double eps,
+                   double weight_decay, const float *grad_factor, const float *lr_factor, void *hip_stream) {
+    if (fg_status st = check_tensor_count(count, tensors)) return st;
+    if (!std::isfinite(lr) || !std::isfinite(weight_decay)) return fail(FG_ERR_SHAPE, "lr and weight_decay must be finite");
+    if (!(beta1 >= 0 && beta1 < 1 && beta2 >= 0 && beta2 < 1)) return fail(FG_ERR_SHAPE, "beta1 and beta2 must be at least 0 and below 1");
+    if (!(eps >= 0) || !std::isfinite(eps)) return fail(FG_ERR_SHAPE, "eps must not be negative");
+    if (!step) return fail(FG_ERR_NULL, "step is NULL");
+    if (!aligned_to(step, 8) || !aligned_to(grad_factor, 4) || !aligned_to(lr_factor, 4))
+        return fail(FG_ERR_ALIGN, "step, grad_factor and lr_factor must be aligned to an element");
+    bool some[2] = {};
+    for (int64_t i = 0; i < count; ++i) {
+        if (fg_status st = check_adamw_tensor(i, tensors[i])) return st;
+        if (tensors[i].n > 0) some[tensors[i].avg_scale != nullptr] = true;
+    }
+    if (some[0] && some[1]) return fail(FG_ERR_UNSUPPORTED, "moments in FP32 and in eight bits need calls of their own");
+    if (!some[0] && !some[1]) return FG_OK;
+    if (fg_status st = check_apart(count, tensors)) return st;
+    Launches enqueue(hip_stream);
+    auto launch = [&](auto cap, int64_t begin, int n, int64_t chunks) {
+        constexpr int CAP = decltype(cap)::value;
+        TensorArgs<CAP> a = {};
+        int64_t first = 0;
+        for (int i = 0; i < n; ++i) {
+            const fg_adamw_tensor &t = tensors[begin + i];
+            a.at[i] = {t.param, t.grad, t.master, t.exp_avg, t.exp_avg_sq, t.avg_scale, t.sq_scale, t.n, (int32_t)first,
+                       t.param_dtype + (t.grad_dtype == FG_F32 ? kWideGrad : 0) + (t.master ? kCopy : 0)};
+            first += chunks_of(t.n);
+        }
+        const StepArgs s = {lr, beta1, beta2, eps, weight_decay, step, grad_factor, lr_factor, n};
+        if (some[1]) enqueue(adamw<CAP, true>, dim3((unsigned)chunks), dim3(kThreads), a, s);
+        else enqueue(adamw<CAP, false>, dim3((unsigned)chunks), dim3(kThreads), a, s);
+    };
+    in_launches(count, kMostTensors, [&](int64_t i) { return tensors[i].n; }, [&](int64_t begin, int n, int64_t chunks) {
+        if (chunks == 0) return;
+        if (n <= kFewTensors) launch(std::integral_constant<int, kFewTensors>{}, begin, n, chunks);
+        else launch(std::integral_constant<int, kMostTensors>{}, begin, n, chunks);
+    });
+    return enqueue.status("adamw");
+}
+
+// (a launch more for each 2^36 values: more than four of those have no room on a GPU)
+int64_t fg_grad_norm_workspace(int64_t count) { return count <= 0 ? 0 : ((count + kMostGrads - 1) / kMostGrads + 4) * kNormGroups * 8; }
+
+fg_status fg_grad_norm(int64_t count, const fg_values *grads, float scale, float max_norm, float *norm, float *factor, void *workspace,
+                       int64_t workspace_bytes, void *hip_stream) {
+    if (fg_status st = check_tensor_count(count, grads)) return st;
+    if (!norm) return fail(FG_ERR_NULL, "norm is NULL");
+    if (!aligned_to(norm, 4) || !aligned_to(factor, 4)) return fail(FG_ERR_ALIGN, "norm and factor must be aligned to an element");
+    if (!(scale > 0) || !std::isfinite(scale)) return fail(FG_ERR_SHAPE, "scale must be positive");
+    if (!(max_norm > 0)) return fail(FG_ERR_SHAPE, "max_norm must be positive");
+    for (int64_t i = 0; i < count; ++i) {
+        if (fg_status st = check_length(i, grads[i].n)) return st;
+        if (fg_status st = check_values("grad", i, grads[i].values, grads[i].dtype, grads[i].n)) return st;
+    }
+    int64_t parts = 0;
+    auto launches = [&](auto &&f) { in_launches(count, kMostGrads, [&](int64_t i) { return grads[i].n; }, f); };
+    launches([&](int64_t, int, int64_t chunks) { parts += std::min<int64_t>(chunks, kNormGroups); });
+    if (fg_status st = check_workspace(workspace, workspace_bytes, parts * 8)) return st;
+    Launches enqueue(hip_stream);
+    double *partial = (double *)workspace;
+    launches([&](int64_t begin, int n, int64_t chunks) {
+        if (chunks == 0) return;
+        const unsigned groups = (unsigned)std::min<int64_t>(chunks, kNormGroups);
+        auto launch = [&](auto cap) {
+            constexpr int CAP = decltype(cap)::value;
+            GradArgs<CAP> a = {};
+            int64_t first = 0;
+            for (int i = 0; i < n; ++i) {
+                const fg_values &t = grads[begin + i];
+                a.at[i] = {t.values, t.n, (int32_t)first, t.dtype};
+                first += chunks_of(t.n);
+            }
+            enqueue(grad_squares<CAP>, dim3(groups), dim3(kThreads), a, n, (int)chunks, partial);
+        };
+        if (n <= kFewGrads) launch(std::integral_constant<int, kFewGrads>{});
+        else launch(std::integral_constant<int, kMostGrads>{});
+        partial += groups;
+    });
+    enqueue(grad_norm, dim3(1), dim3(1024), (const double *)workspace, parts, (double)scale, (double)max_norm, norm, factor);
+    return enqueue.status("grad_norm");
+}
+
+}  // extern "C"

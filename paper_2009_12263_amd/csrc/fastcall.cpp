@@ -11,6 +11,8 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <pthread.h>
+
+#include <vector>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/flexgemm.h"
@@ -239,12 +241,21 @@ typedef fg_status (*EmbeddingGradFn)(int64_t, int64_t, int64_t, const fg_matrix 
 typedef fg_status (*XentFn)(int64_t, int64_t, int64_t, const fg_matrix *, const fg_matrix *, const void *, int32_t, float, float *, float *, void *, int64_t, void *);
 typedef fg_status (*XentGradFn)(int64_t, int64_t, int64_t, const fg_matrix *, const fg_matrix *, const void *, int32_t, float, const float *, const float *, int64_t,
                                 const fg_matrix *, const fg_matrix *, void *, int64_t, void *);
+typedef fg_status (*GatedFn)(int64_t, int64_t, int64_t, const fg_matrix *, const fg_matrix *, const fg_matrix *, int32_t, const fg_matrix *, const fg_matrix *, void *,
+                             int64_t, void *);
+typedef fg_status (*GatedGradFn)(int64_t, int64_t, int64_t, const fg_matrix *, const fg_matrix *, const fg_matrix *, const fg_matrix *, int32_t, const fg_matrix *,
+                                 const fg_matrix *, const fg_matrix *, const fg_matrix *, void *, int64_t, void *);
+typedef fg_status (*AdamWFn)(int64_t, const fg_adamw_tensor *, const int64_t *, double, double, double, double, double, const float *, const float *, void *);
+typedef fg_status (*GradNormFn)(int64_t, const fg_values *, float, float, float *, float *, void *, int64_t, void *);
+typedef int64_t (*CountSpaceFn)(int64_t);
 typedef int64_t (*LayerNormSpaceFn)(int64_t, int64_t, int32_t);
 typedef int64_t (*SpaceFn)(int64_t, int64_t, int64_t);
 struct RowEntry {
     LayerNormFn layernorm; LayerNormGradFn layernorm_grad; LayerNormSpaceFn layernorm_grad_space;
     EmbeddingFn embedding; EmbeddingGradFn embedding_grad; SpaceFn embedding_grad_space;
     XentFn xent; SpaceFn xent_space; XentGradFn xent_grad; SpaceFn xent_grad_space;
+    GatedFn gated; SpaceFn gated_space; GatedGradFn gated_grad; SpaceFn gated_grad_space;
+    AdamWFn adamw; GradNormFn grad_norm; CountSpaceFn grad_norm_space;
 } g_rows;
 
 // What the binding's own marshalling checks of a call: tensors on the current GPU, of the sizes that the others have.
@@ -439,16 +450,133 @@ PyObject *xent_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// gated_ffn(X, W_in, W_out, act, Y, GU, workspace, stream) -> status
+PyObject *gated_ffn(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return run_rows(a, n, 8, [&](RowCall &c, fg_status &st) {
+        int64_t tokens = -1, dim = -1, twice = -1, act, bytes;
+        fg_matrix x, w_in, w_out, y, gu;
+        void *ws;
+        if (!c.matrix(a[0], tokens, dim, x) || !c.matrix(a[1], twice, dim, w_in) || twice % 2 != 0) return false;
+        int64_t hidden = twice / 2;
+        if (!c.matrix(a[2], dim, hidden, w_out) || !as_int(a[3], act) || !c.matrix(a[4], tokens, dim, y)) return false;
+        const bool keep = a[5] != Py_None;
+        if (keep && !c.matrix(a[5], tokens, twice, gu)) return false;
+        if (!c.workspace(a[6], g_rows.gated_space(tokens, dim, hidden), ws, bytes)) return false;
+        st = without_gil([&]() noexcept { return g_rows.gated(tokens, dim, hidden, &x, &w_in, &w_out, (int32_t)act, &y, keep ? &gu : nullptr, ws, bytes, c.stream); });
+        return true;
+    });
+}
+// gated_ffn_grad(dY, X, W_in, W_out, act, GU, dX, dW_in, dW_out, workspace, stream) -> status
+PyObject *gated_ffn_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return run_rows(a, n, 11, [&](RowCall &c, fg_status &st) {
+        int64_t tokens = -1, dim = -1, twice = -1, act, bytes;
+        fg_matrix dy, x, w_in, w_out, gu, dx, dw_in, dw_out;
+        void *ws;
+        if (!c.matrix(a[1], tokens, dim, x) || !c.matrix(a[0], tokens, dim, dy) || !c.matrix(a[2], twice, dim, w_in) || twice % 2 != 0) return false;
+        int64_t hidden = twice / 2;
+        if (!c.matrix(a[3], dim, hidden, w_out) || !as_int(a[4], act) || !c.matrix(a[5], tokens, twice, gu)) return false;
+        if ((a[6] != Py_None && !c.matrix(a[6], tokens, dim, dx)) || (a[7] != Py_None && !c.matrix(a[7], twice, dim, dw_in)) ||
+            (a[8] != Py_None && !c.matrix(a[8], dim, hidden, dw_out))) return false;
+        if (!c.workspace(a[9], g_rows.gated_grad_space(tokens, dim, hidden), ws, bytes)) return false;
+        st = without_gil([&]() noexcept {
+            return g_rows.gated_grad(tokens, dim, hidden, &dy, &x, &w_in, &w_out, (int32_t)act, &gu, a[6] != Py_None ? &dx : nullptr, a[7] != Py_None ? &dw_in : nullptr,
+                                     a[8] != Py_None ? &dw_out : nullptr, ws, bytes, c.stream);
+        });
+        return true;
+    });
+}
+
+// The items of a list or tuple of tensors; none (and size 0) if it is None.
+struct Items {
+    PyObject *const *at = nullptr;
+    Py_ssize_t n = 0;
+    bool read(PyObject *o) {
+        if (o == Py_None) return true;
+        if (!PyList_CheckExact(o) && !PyTuple_CheckExact(o)) return false;
+        at = PySequence_Fast_ITEMS(o);
+        n = PySequence_Fast_GET_SIZE(o);
+        return true;
+    }
+};
+// adamw(params, grads, exp_avg, exp_avg_sq, step, lr, beta1, beta2, eps, weight_decay, masters, avg_scales, sq_scales, grad_factor, lr_factor, stream) -> status
+PyObject *adamw(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return run_rows(a, n, 16, [&](RowCall &c, fg_status &st) {
+        Items params, grads, avg, sq, masters, avg_scales, sq_scales;
+        if (!params.read(a[0]) || !grads.read(a[1]) || !avg.read(a[2]) || !sq.read(a[3]) || !masters.read(a[10]) || !avg_scales.read(a[11]) || !sq_scales.read(a[12])) return false;
+        const Py_ssize_t count = params.n;
+        if (grads.n != count || avg.n != count || sq.n != count || (masters.at && masters.n != count) || !avg_scales.at != !sq_scales.at) return false;
+        const bool small = avg_scales.at != nullptr;
+        if (small && (avg_scales.n != count || sq_scales.n != count)) return false;
+        double rates[5];
+        for (int i = 0; i < 5; ++i) {
+            if (!PyFloat_CheckExact(a[5 + i])) return false;
+            rates[i] = PyFloat_AS_DOUBLE(a[5 + i]);
+        }
+        int kind = FG_I64;
+        void *step;
+        float *grad_factor, *lr_factor;
+        if (a[4] == Py_None || !c.vector(a[4], 1, kind, step) || !c.floats(a[13], 1, grad_factor) || !c.floats(a[14], 1, lr_factor)) return false;
+        const at::ScalarType moment = small ? at::kFloat8_e4m3fn : at::kFloat;
+        std::vector<fg_adamw_tensor> list((size_t)count);
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            const at::Tensor *p = c.tensor(params.at[i]), *g = c.tensor(grads.at[i]), *m = c.tensor(avg.at[i]), *v = c.tensor(sq.at[i]);
+            if (!p || !g || !m || !v || !p->is_contiguous() || !g->is_contiguous() || !m->is_contiguous() || !v->is_contiguous()) return false;
+            if (g->sizes() != p->sizes() || m->sizes() != p->sizes() || v->sizes() != p->sizes() || m->scalar_type() != moment || v->scalar_type() != moment) return false;
+            fg_adamw_tensor &t = list[(size_t)i];
+            t.n = p->numel();
+            t.param_dtype = RowCall::dtype_of(*p);
+            t.grad_dtype = RowCall::dtype_of(*g);
+            if (t.param_dtype < 0 || t.param_dtype > FG_F32 || t.grad_dtype < 0 || t.grad_dtype > FG_F32) return false;
+            t.param = p->data_ptr(); t.grad = g->data_ptr(); t.exp_avg = m->data_ptr(); t.exp_avg_sq = v->data_ptr();
+            t.master = t.avg_scale = t.sq_scale = nullptr;
+            if (masters.at && masters.at[i] != Py_None) {
+                const at::Tensor *w = c.tensor(masters.at[i]);
+                if (!w || !w->is_contiguous() || w->sizes() != p->sizes() || w->scalar_type() != at::kFloat) return false;
+                t.master = (float *)w->data_ptr();
+            }
+            const int64_t blocks = (t.n + 255) / 256;
+            if (small && (avg_scales.at[i] == Py_None || sq_scales.at[i] == Py_None || !c.floats(avg_scales.at[i], blocks, t.avg_scale) || !c.floats(sq_scales.at[i], blocks, t.sq_scale)))
+                return false;
+        }
+        st = without_gil([&]() noexcept {
+            return g_rows.adamw(count, list.data(), (const int64_t *)step, rates[0], rates[1], rates[2], rates[3], rates[4], grad_factor, lr_factor, c.stream);
+        });
+        return true;
+    });
+}
+// grad_norm(grads, scale, max_norm, norm, factor, workspace, stream) -> status
+PyObject *grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return run_rows(a, n, 7, [&](RowCall &c, fg_status &st) {
+        Items grads;
+        float scale, most, *norm, *factor;
+        void *ws;
+        int64_t bytes;
+        if (a[0] == Py_None || !grads.read(a[0]) || !as_float(a[1], scale) || !as_float(a[2], most) || a[3] == Py_None || !c.floats(a[3], 1, norm) || !c.floats(a[4], 1, factor)) return false;
+        std::vector<fg_values> list((size_t)grads.n);
+        for (Py_ssize_t i = 0; i < grads.n; ++i) {
+            const at::Tensor *g = c.tensor(grads.at[i]);
+            if (!g || !g->is_contiguous()) return false;
+            const int dtype = RowCall::dtype_of(*g);
+            if (dtype < 0 || dtype > FG_F32) return false;
+            list[(size_t)i] = {g->data_ptr(), g->numel(), dtype};
+        }
+        if (!c.workspace(a[5], g_rows.grad_norm_space(grads.n), ws, bytes)) return false;
+        st = without_gil([&]() noexcept { return g_rows.grad_norm(grads.n, list.data(), scale, most, norm, factor, ws, bytes, c.stream); });
+        return true;
+    });
+}
+
 // setup_rows(addresses of the entry points in the order of RowEntry)
 PyObject *setup_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    if (n != 10) { PyErr_SetString(PyExc_TypeError, "setup_rows takes 10 arguments"); return nullptr; }
-    void *f[10];
-    for (int i = 0; i < 10; ++i) {
+    if (n != 17) { PyErr_SetString(PyExc_TypeError, "setup_rows takes 17 arguments"); return nullptr; }
+    void *f[17];
+    for (int i = 0; i < 17; ++i) {
         f[i] = PyLong_AsVoidPtr(a[i]);
         if (PyErr_Occurred()) return nullptr;
     }
     g_rows = RowEntry{(LayerNormFn)f[0], (LayerNormGradFn)f[1], (LayerNormSpaceFn)f[2], (EmbeddingFn)f[3], (EmbeddingGradFn)f[4], (SpaceFn)f[5],
-                      (XentFn)f[6], (SpaceFn)f[7], (XentGradFn)f[8], (SpaceFn)f[9]};
+                      (XentFn)f[6], (SpaceFn)f[7], (XentGradFn)f[8], (SpaceFn)f[9], (GatedFn)f[10], (SpaceFn)f[11], (GatedGradFn)f[12], (SpaceFn)f[13],
+                      (AdamWFn)f[14], (GradNormFn)f[15], (CountSpaceFn)f[16]};
     Py_RETURN_NONE;
 }
 
@@ -477,6 +605,10 @@ PyMethodDef g_methods[] = {{"setup", (PyCFunction)(void (*)(void))setup, METH_FA
                            {"embedding_grad", (PyCFunction)(void (*)(void))embedding_grad, METH_FASTCALL, nullptr},
                            {"xent", (PyCFunction)(void (*)(void))xent, METH_FASTCALL, nullptr},
                            {"xent_grad", (PyCFunction)(void (*)(void))xent_grad, METH_FASTCALL, nullptr},
+                           {"gated_ffn", (PyCFunction)(void (*)(void))gated_ffn, METH_FASTCALL, nullptr},
+                           {"gated_ffn_grad", (PyCFunction)(void (*)(void))gated_ffn_grad, METH_FASTCALL, nullptr},
+                           {"adamw", (PyCFunction)(void (*)(void))adamw, METH_FASTCALL, nullptr},
+                           {"grad_norm", (PyCFunction)(void (*)(void))grad_norm, METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_fastcall", "Native marshalling of binding.py's calls.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

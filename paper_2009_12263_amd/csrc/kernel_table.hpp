@@ -95,6 +95,8 @@ fg_status launch_product(const KernelEntry &k, GemmParams &p, hipStream_t stream
 hipError_t load_layernorm_kernels();
 hipError_t load_embedding_kernels();
 hipError_t load_xent_kernels();
+hipError_t load_gated_kernels();
+hipError_t load_adamw_kernels();
 
 // Second pass of a split-K product (splitk_reduce.hip).
 hipError_t launch_splitk_reduce(const float *W, int splits, int tile_begin, int tile_count, int bm, int bn, int tiles_m,
