@@ -185,7 +185,7 @@ __device__ __forceinline__ float relative(float (&x)[kLaneBlock]) {
         x[e] *= by;
         if (FLOOR) x[e] = x[e] > 0.f && x[e] < kLeast ? kLeast : x[e];
     }
-    return top >= kNothing ? top / kTop : 0.f;
+    return top >= kNothing ? top * (1.f / kTop) : 0.f;
 }
 
 // ---- the step -----------------------------------------------------------------------------------------

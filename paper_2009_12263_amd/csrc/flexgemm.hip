@@ -1315,6 +1315,12 @@ fg_status fg_init(void) {
                 int per_cu = 0;
                 if (fg_status st = prepare(fg::kernel_table_xent(kind, bf16)[i], dev, per_cu)) return st;
             }
+    for (int kind = 0; kind < fg::GATED_KINDS; ++kind)
+        for (bool bf16 : {false, true})
+            for (int i = 0; i < fg::GATED_TILES; ++i) {
+                int per_cu = 0;
+                if (fg_status st = prepare(fg::kernel_table_gated(kind, bf16)[i], dev, per_cu)) return st;
+            }
     for (auto &tb : tables)
         for (int i = 0; i < tb.n; ++i) {
             int per_cu = 0;

@@ -3,41 +3,25 @@
 //   [G U] = X W_in^T,   H = act(G) U,   Y = H W_out^T
 //   dH = dY W_out,   dG = dH U act'(G),   dU = dH act(G),   dX = [dG dU] W_in,   dW_in = [dG dU]^T X,   dW_out = dY^T H
 //
-// 6 T D H operations forward (T tokens of D values, H hidden ones), 12 T D H backward, on the matrix units.
+// 6 T D H operations forward (T tokens of D values, H hidden ones) and 12 T D H backward, on the matrix units, whose epilogues are the activation, its
+// gradient and the rounding (gated_kernel.hpp).  A product that the planner splits along K (few tiles, a long K) goes through FP32 sums instead, and
+// a pass over them is the epilogue.
+//
+// H, dG and dU are rounded to the operands' 16 bits, the only roundings but those of the results: an error of half a step each, so that
+// results are 1.4 times as far from 64 bits as rounding alone makes them.  G and U are kept in FP32: in 16 bits theirs came on top (dX 1.9 times).
+// With up to kPartsTokens tokens the error of single values shows in a result's norm, and the matrix units have time: there
+// H, dG and dU are two 16-bit numbers each, a value and what its rounding left, in rows of their own of the same products.
+//
+// Up to kFewTokens tokens the forward products are all reading of weights: gated_few.
 #include <algorithm>
 #include <cstring>
 #include <type_traits>
 
-#include "kernel_table.hpp"
-#include "row_ops.hpp"
+#include "cache_policy.hpp"
+#include "gated_kernel.hpp"
 
 namespace fg {
 namespace {
-
-constexpr float kLog2eG = 1.44269504088896340736f;
-
-__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + __builtin_amdgcn_exp2f(-kLog2eG * x)); }
-// act(g), and its derivative
-template <int ACT>
-__device__ __forceinline__ void activate(float g, float &a, float &d) {
-    if constexpr (ACT == FG_ACT_NONE) { a = g; d = 1.f; }
-    else if constexpr (ACT == FG_ACT_RELU) { a = g > 0.f ? g : 0.f; d = g > 0.f ? 1.f : 0.f; }
-    else if constexpr (ACT == FG_ACT_SILU) { const float q = sigmoid(g); a = g * q; d = q * (1.f + g * (1.f - q)); }
-    else {
-        // (1 + tanh u) / 2 = sigmoid(2 u), u = c (g + 0.044715 g^3)
-        const float c2 = 2.f * 0.79788456080286535588f, q = sigmoid(c2 * (g + 0.044715f * g * g * g));
-        a = g * q;
-        d = q + c2 * g * q * (1.f - q) * (1.f + 3.f * 0.044715f * g * g);
-    }
-}
-template <class F> void with_act(int act, F &&f) {
-    switch (act) {
-        case FG_ACT_NONE: f(std::integral_constant<int, FG_ACT_NONE>{}); break;
-        case FG_ACT_RELU: f(std::integral_constant<int, FG_ACT_RELU>{}); break;
-        case FG_ACT_SILU: f(std::integral_constant<int, FG_ACT_SILU>{}); break;
-        default: f(std::integral_constant<int, FG_ACT_GELU_TANH>{});
-    }
-}
 
 // Copies rows of `cols` values to rows of ldo (a multiple of 8), with zeros behind them.
 template <class T>
@@ -56,52 +40,249 @@ __global__ __launch_bounds__(256) void gated_pad(const T *in, int64_t ld, T *out
     }
 }
 
-// h = act(g) u, rounded, in rows of ldh with zeros behind them; g and u are copied to `keep` where it is given
-template <class T, int ACT>
-__global__ __launch_bounds__(256) void gated_product(const float *gu, int64_t ldgu, T *h, int64_t ldh, int64_t rows, int hidden, float *keep, int64_t ldkeep) {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * ldh; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / ldh;
-        const int c = (int)(i - row * ldh);
-        float a = 0.f, d = 0.f;
-        if (c < hidden) {
-            const float g = gu[row * ldgu + c], u = gu[row * ldgu + hidden + c];
-            activate<ACT>(g, a, d);
-            a *= u;
-            if (keep) {
-                keep[row * ldkeep + c] = g;
-                keep[row * ldkeep + hidden + c] = u;
-            }
-        }
-        h[i] = (T)a;
+// Piece p of eight values of FP32 rows; zeros from `cols` on.
+__device__ __forceinline__ void load_eight(const float *row, int c0, int cols, float (&v)[8]) {
+    typedef float four __attribute__((ext_vector_type(4)));
+    typedef four anywhere __attribute__((aligned(4)));
+    if (c0 + 8 <= cols) {
+        const four a = *(const anywhere *)(row + c0), b = *(const anywhere *)(row + c0 + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c0 + e < cols ? row[c0 + e] : 0.f;
     }
 }
-// h as above, dg and du behind each other in rows of ldd with zeros behind them
-template <class T, int ACT>
-__global__ __launch_bounds__(256) void gated_product_grad(const float *gu, int64_t ldgu, const float *dh, int64_t lddh, T *h, int64_t ldh, T *dgu, int64_t ldd,
-                                                          int64_t rows, int hidden) {
-    const int64_t wide = ldd > ldh ? ldd : ldh;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * wide; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / wide;
-        const int c = (int)(i - row * wide);
-        if (c < hidden) {
-            float a, d;
-            activate<ACT>(gu[row * ldgu + c], a, d);
-            const float u = gu[row * ldgu + hidden + c], x = dh[row * lddh + c];
-            dgu[row * ldd + c] = (T)(x * u * d);
-            dgu[row * ldd + hidden + c] = (T)(x * a);
-            h[row * ldh + c] = (T)(a * u);
-        } else {
-            if (c < ldh) h[row * ldh + c] = (T)0.f;
-            if (c >= 2 * hidden && c < ldd) dgu[row * ldd + c] = (T)0.f;
-        }
-    }
-}
+// Eight values of a 16-bit row, those before `cols`; with `rest` also what their rounding leaves.
 template <class T>
+__device__ __forceinline__ void store_eight(T *row, int c0, int cols, const float (&v)[8], T *rest) {
+    typedef typename RowPiece<T, 8>::vec vec;
+    typedef typename RowPiece<T, 8>::unaligned anywhere;
+    vec hi, lo;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        hi[e] = (T)v[e];
+        const float off = v[e] - (float)hi[e];
+        lo[e] = __builtin_fabsf(off) < __builtin_inff() ? (T)off : (T)0.f;           // (of an infinity nothing is left)
+    }
+    if (c0 + 8 <= cols) {
+        *(anywhere *)(row + c0) = hi;
+        if (rest) *(anywhere *)(rest + c0) = lo;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c0 + e < cols) {
+                row[c0 + e] = hi[e];
+                if (rest) rest[c0 + e] = lo[e];
+            }
+    }
+}
+// f(row, first column) for pieces of eight columns
+template <class F> __device__ __forceinline__ void each_piece(int64_t rows, int cols, F &&f) {
+    const int pieces = (cols + 7) / 8;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / pieces;
+        f(row, (int)(i - row * pieces) * 8);
+    }
+}
+
+// h = act(g) u, rounded, with zeros to the end of its rows; g and u are copied to `keep` where it is given
+template <class T>
+__global__ __launch_bounds__(256) void gated_product(const float *gu, int64_t ldgu, T *h, int64_t ldh, int64_t rows, int hidden, Activation act, float *keep, int64_t ldkeep) {
+    each_piece(rows, hidden, [&](int64_t row, int c) {
+        float g[8], u[8], v[8];
+        load_eight(gu + row * ldgu, c, hidden, g);
+        load_eight(gu + row * ldgu + hidden, c, hidden, u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c + e < hidden ? act.operator()<false>(g[e], nullptr) * u[e] : 0.f;
+        store_eight<T>(h + row * ldh, c, (int)ldh, v, nullptr);
+        if (keep) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e < hidden) {
+                    keep[row * ldkeep + c + e] = g[e];
+                    keep[row * ldkeep + hidden + c + e] = u[e];
+                }
+        }
+    });
+}
+// dg and du behind each other, and h, with zeros to the end of their rows; PARTS: what their rounding leaves `rows` rows further on
+template <class T, bool PARTS>
+__global__ __launch_bounds__(256) void gated_product_grad(const float *gu, int64_t ldgu, const float *dh, int64_t lddh, T *h, int64_t ldh, T *dgu, int64_t ldd,
+                                                          int64_t rows, int hidden, Activation act) {
+    each_piece(rows, hidden, [&](int64_t row, int c) {
+        float g[8], u[8], x[8], vg[8], vu[8], vh[8];
+        load_eight(gu + row * ldgu, c, hidden, g);
+        load_eight(gu + row * ldgu + hidden, c, hidden, u);
+        load_eight(dh + row * lddh, c, hidden, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float d;
+            const float a = act.operator()<true>(g[e], &d);
+            vg[e] = x[e] * u[e] * d;
+            vu[e] = x[e] * a;
+            vh[e] = c + e < hidden ? a * u[e] : 0.f;
+        }
+        T *to = dgu + row * ldd, *rest = PARTS ? to + rows * ldd : nullptr;
+        store_eight<T>(to, c, hidden, vg, rest);
+        store_eight<T>(to + hidden, c, hidden, vu, PARTS ? rest + hidden : nullptr);
+        store_eight<T>(h + row * ldh, c, (int)ldh, vh, PARTS ? h + (rows + row) * ldh : nullptr);
+        if (c + 8 >= hidden)
+            for (int z = 2 * hidden; z < (int)ldd; ++z) {
+                to[z] = (T)0.f;
+                if (PARTS) rest[z] = (T)0.f;
+            }
+    });
+}
+// Rounded; PARTS: the sums of row r and row rows + r.  No `in`: zeros.
+template <class T, bool PARTS>
 __global__ __launch_bounds__(256) void gated_round(const float *in, int64_t ldi, T *out, int64_t ldo, int64_t rows, int cols) {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / cols;
-        const int c = (int)(i - row * cols);
-        out[row * ldo + c] = in ? (T)in[row * ldi + c] : (T)0.f;
+    each_piece(rows, cols, [&](int64_t row, int c) {
+        float v[8] = {}, w[8];
+        if (in) load_eight(in + row * ldi, c, cols, v);
+        if constexpr (PARTS) {
+            load_eight(in + (rows + row) * ldi, c, cols, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += w[e];
+        }
+        store_eight<T>(out + row * ldo, c, cols, v, nullptr);
+    });
+}
+// Copies W_in for GATED_UP: 32 rows of G, 32 of U, and so on, rows of ldo values with zeros behind them and behind the last row.
+template <class T>
+__global__ __launch_bounds__(256) void gated_interleave(const T *in, int64_t ld, T *out, int64_t ldo, int hidden, int cols) {
+    each_piece((int64_t)(hidden + 31) / 32 * 64, (int)ldo, [&](int64_t row, int c) {
+        const int at = (int)(row / 64) * 32 + (int)(row % 32);
+        const T *from = in + (at + ((row / 32) % 2 ? hidden : 0)) * ld;
+        typename RowPiece<T>::vec v = {};
+        if (at < hidden) {
+            if (c + 8 <= cols) v = load_raw<T, 8>(from, c / 8, cols);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? from[c + e] : (T)0.f;
+        }
+        *(typename RowPiece<T>::vec *)(out + row * ldo + c) = v;
+    });
+}
+
+// ---- few tokens -------------------------------------------------------------------------------------------------
+// Sums over k of w[n][k] x[r][k] for up to 16 NB rows r of x: reading w.  A workgroup takes 16 rows of w (UP: and as many of U), its waves 64 k each in
+// turn: a lane reads its row's 16 bytes straight into the operand of a 16x16x32 matrix instruction, a wave two whole lines of each row.  The waves' sums are added
+// up through LDS in their order.  x is read from the L2 by every workgroup, 16 bytes for each 16 of w and 16 rows.
+// UP: h = act(g) u of the sums, in 16 bits, and what its rounding leaves `lo` rows further on (lo > 0); g and u are kept in FP32 where that is wanted.
+// Otherwise: rounded; with lo > 0 the sums of rows r and lo + r.
+struct FewArgs {
+    const void *x, *w;
+    void *out;
+    float *keep;
+    int64_t ldx, ldw, ldo, ldkeep;
+    int32_t rows, lo, n, k;             // of x; see above; rows of w (UP: of G), and their values
+    Activation act;
+};
+template <class T>
+__device__ __forceinline__ floatx4 mfma_16x16x32(typename RowPiece<T>::vec a, typename RowPiece<T>::vec b, floatx4 c) {
+    if constexpr (std::is_same<T, bf16_t>::value) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+template <class T, int NB, bool UP>
+__global__ __launch_bounds__(NB == 4 ? 512 : 1024) void gated_few(const FewArgs a) {
+    typedef typename RowPiece<T>::vec vec;
+    typedef typename RowPiece<T>::unaligned anywhere;
+    constexpr int G = UP ? 2 : 1;
+    extern __shared__ __attribute__((aligned(16))) char few_parts[];
+    floatx4 *part = (floatx4 *)few_parts;               // [wave][G][NB][lane]
+    const int lane = threadIdx.x & 63, at = lane & 15, quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int n0 = blockIdx.x * 16, row = min(n0 + at, a.n - 1);
+    const T *w[G], *x[NB];
+#pragma unroll
+    for (int g = 0; g < G; ++g) w[g] = (const T *)a.w + ((int64_t)row + (g ? a.n : 0)) * a.ldw + quarter * 8;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) x[b] = (const T *)a.x + (int64_t)min(b * 16 + at, a.rows - 1) * a.ldx + quarter * 8;
+    floatx4 sum[G][NB] = {};
+    const int k_whole = a.k / 64 * 64, stride = waves * 64;
+    // S turns of 64 k at once, all their loads first
+    auto turns = [&](int k, auto count) {
+        constexpr int S = 2 * decltype(count)::value;
+        vec wv[S][G], xv[S][NB];
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int at_k = k + s / 2 * stride + s % 2 * 32;
+#pragma unroll
+            for (int g = 0; g < G; ++g) wv[s][g] = *(const anywhere *)(w[g] + at_k);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) xv[s][b] = *(const anywhere *)(x[b] + at_k);
+        }
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int b = 0; b < NB; ++b) sum[g][b] = mfma_16x16x32<T>(wv[s][g], xv[s][b], sum[g][b]);
+    };
+    int k = wave * 64;
+    for (; k + stride < k_whole; k += 2 * stride) turns(k, std::integral_constant<int, 2>{});
+    if (k < k_whole) turns(k, std::integral_constant<int, 1>{});
+    if (k_whole < a.k && wave == k_whole / 64 % waves) {            // the last values: element by element at the end of a row
+        auto piece = [&](const T *p, int k) {
+            vec v = {};
+            const int left = a.k - k - quarter * 8;
+            if (left >= 8) v = *(const anywhere *)(p + k);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e < left) v[e] = p[k + e];
+            return v;
+        };
+        for (int last = k_whole; last < a.k; last += 32)
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const vec v = piece(w[g], last);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) sum[g][b] = mfma_16x16x32<T>(v, piece(x[b], last), sum[g][b]);
+            }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) part[((wave * G + g) * NB + b) * 64 + lane] = sum[g][b];
+    __syncthreads();
+    // A thread has row r of x and four columns.
+    auto total = [&](int g, int r, int q) {
+        const int slot = (g * NB + (r >> 4)) * 64 + q * 16 + (r & 15);
+        floatx4 s = part[slot];
+        for (int v = 1; v < waves; ++v) s += part[v * (G * NB * 64) + slot];
+        return s;
+    };
+    const int rows = UP || a.lo == 0 ? a.rows : a.lo;
+    for (int i = threadIdx.x; i < rows * 4; i += blockDim.x) {
+        const int r = i >> 2, q = i & 3, c = n0 + 4 * q, left = a.n - c;
+        floatx4 v = total(0, r, q);
+        if (left <= 0) continue;
+        T *out = (T *)a.out + (int64_t)r * a.ldo + c;
+        if constexpr (UP) {
+            const floatx4 u = total(1, r, q);
+            if (a.keep) {
+                float *g_out = a.keep + (int64_t)r * a.ldkeep + c, *u_out = g_out + a.n;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < left) { g_out[e] = v[e]; u_out[e] = u[e]; }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = a.act.operator()<false>(v[e], nullptr) * u[e];
+            T *rest = out + (int64_t)a.lo * a.ldo;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < left) {
+                    out[e] = (T)v[e];
+                    const float off = v[e] - (float)(T)v[e];
+                    if (a.lo) rest[e] = __builtin_fabsf(off) < __builtin_inff() ? (T)off : (T)0.f;
+                }
+        } else {
+            if (a.lo) v += total(0, a.lo + r, q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < left) out[e] = (T)v[e];
+        }
     }
 }
 
@@ -117,38 +298,63 @@ fg_matrix rows_of(const void *p, int32_t dtype, int64_t ld, int32_t layout = FG_
 fg_matrix turned(fg_matrix m) { m.layout = FG_COL; return m; }
 bool as_it_is(int64_t cols, const fg_matrix *m) { return cols % 8 == 0 && aligned_to(m->re, 16) && m->ld % 8 == 0 && m->ld < kKContiguousLd; }
 
+constexpr int64_t kFewTokens = 64, kPartsTokens = 32;
+
+// Whether a product goes through FP32 sums: the planner splits its K.
+bool by_sums(int64_t M, int64_t N, int64_t K) { return gemm_stored_scratch(M, N, K) > 0; }
+// A lane of GATED_UP reaches U from G's rows with a 32-bit offset.
+bool in_reach(int64_t H, const fg_matrix *W_in) { return (H + 128) * W_in->ld * 2 < (1ll << 31); }
+
 // Where the parts of a workspace are.
 struct Space {
-    int64_t bytes = 0;
+    int64_t bytes = 0, scratch = 0, scratch_bytes = 0;
     int64_t take(int64_t n) { const int64_t at = bytes; bytes += up(n, 256); return at; }
+    void partial(int64_t M, int64_t N, int64_t K) { scratch_bytes = std::max(scratch_bytes, gemm_stored_scratch(M, N, K)); }
 };
 struct ForwardSpace : Space {
-    int64_t x, w_in, w_out, gu, h, sums, scratch, scratch_bytes;
-    ForwardSpace(int64_t T, int64_t D, int64_t H, bool copy_x, bool copy_in, bool copy_out, bool has_gu) {
+    bool few, up_by_sums, down_by_sums;
+    int64_t x = 0, w_in = 0, w_out = 0, gu = 0, h, sums = 0;
+    ForwardSpace(int64_t T, int64_t D, int64_t H, bool copy_x, bool copy_in, bool copy_out, bool own_gu) {
         const int64_t dp = up(D, 8), hp = up(H, 8);
-        x = copy_x ? take(T * dp * 2) : 0;
-        w_in = copy_in ? take(2 * H * dp * 2) : 0;
-        w_out = copy_out ? take(D * hp * 2) : 0;
-        gu = has_gu ? 0 : take(T * up(2 * H, 4) * 4);
-        h = take(T * hp * 2);
-        sums = take(T * up(D, 4) * 4);
-        scratch_bytes = std::max(gemm_stored_scratch(T, 2 * H, dp), gemm_stored_scratch(T, D, hp));
+        few = T <= kFewTokens;
+        up_by_sums = !few && by_sums(T, 2 * H, dp);
+        down_by_sums = !few && by_sums(T, D, hp);
+        h = take((T <= kPartsTokens ? 2 : 1) * T * hp * 2);
+        if (few) return;
+        if (copy_x) x = take(T * dp * 2);
+        if (copy_in) w_in = take(2 * up(H, 32) * dp * 2);
+        if (copy_out) w_out = take(D * hp * 2);
+        if (up_by_sums && own_gu) gu = take(T * up(2 * H, 4) * 4);
+        if (down_by_sums) sums = take(T * up(D, 4) * 4);
+        if (up_by_sums) partial(T, 2 * H, dp);
+        if (down_by_sums) partial(T, D, hp);
         scratch = take(scratch_bytes);
     }
 };
 struct GradSpace : Space {
-    int64_t dy, x, w_in, w_out, dh, h, dgu, sums, scratch, scratch_bytes;
+    int64_t parts;
+    bool down_by_sums, x_by_sums, in_by_sums, out_by_sums;
+    int64_t dy = 0, x = 0, w_in = 0, w_out = 0, dh = 0, h, dgu, sums = 0;
     GradSpace(int64_t T, int64_t D, int64_t H, bool copy_dy, bool copy_x, bool copy_in, bool copy_out) {
-        const int64_t dp = up(D, 8), hp = up(H, 8), gp = up(2 * H, 8), tp = up(T, 8);
-        dy = copy_dy ? take(T * dp * 2) : 0;
-        x = copy_x ? take(T * dp * 2) : 0;
-        w_in = copy_in ? take(2 * H * dp * 2) : 0;
-        w_out = copy_out ? take(D * hp * 2) : 0;
-        dh = take(T * up(H, 4) * 4);
-        h = take(T * hp * 2);
-        dgu = take(T * gp * 2);
-        sums = take(std::max({T, 2 * H}) * up(D, 4) * 4 > D * up(H, 4) * 4 ? std::max({T, 2 * H}) * up(D, 4) * 4 : D * up(H, 4) * 4);
-        scratch_bytes = std::max({gemm_stored_scratch(T, H, dp), gemm_stored_scratch(T, D, gp), gemm_stored_scratch(2 * H, D, tp), gemm_stored_scratch(D, H, tp)});
+        const int64_t dp = up(D, 8), hp = up(H, 8), gp = up(2 * H, 8);
+        parts = T <= kPartsTokens ? 2 : 1;
+        const int64_t tp = up(parts * T, 8);
+        down_by_sums = parts == 2 || by_sums(T, H, dp);
+        x_by_sums = parts == 2 || by_sums(T, D, gp);
+        in_by_sums = by_sums(2 * H, D, tp);
+        out_by_sums = by_sums(D, H, tp);
+        if (copy_dy || parts == 2) dy = take(parts * T * dp * 2);
+        if (copy_x || parts == 2) x = take(parts * T * dp * 2);
+        if (copy_in) w_in = take(2 * H * dp * 2);
+        if (copy_out) w_out = take(D * hp * 2);
+        h = take(parts * T * hp * 2);
+        dgu = take(parts * T * gp * 2);
+        if (down_by_sums) { dh = take(T * up(H, 4) * 4); partial(T, H, dp); }
+        int64_t most = 0;
+        if (x_by_sums) { most = std::max(most, parts * T * up(D, 4)); partial(parts * T, D, gp); }
+        if (in_by_sums) { most = std::max(most, 2 * H * up(D, 4)); partial(2 * H, D, tp); }
+        if (out_by_sums) { most = std::max(most, D * up(H, 4)); partial(D, H, tp); }
+        sums = take(most * 4);
         scratch = take(scratch_bytes);
     }
 };
@@ -172,40 +378,109 @@ fg_status check_like(const char *name, const fg_matrix *m, int64_t rows, int64_t
     return FG_OK;
 }
 
-unsigned groups_for(int64_t values, int each) { return (unsigned)std::min<int64_t>((values + 256 * each - 1) / (256 * each), 8192); }
+unsigned groups_for(int64_t rows, int64_t cols) { return (unsigned)std::min<int64_t>((rows * ((cols + 7) / 8) + 255) / 256, 8192); }
+
+// Which tile of kernel_table_gated serves a product.
+int gated_tile(int64_t M, int64_t N, int64_t K) {
+    switch (plan_tile(M, N, K)) {
+        case TILE_256x256: case TILE_256x256_K32: return 0;
+        case TILE_256x128: case TILE_256x128_PASS: return 1;
+        case TILE_64x64: case TILE_64x64_KG2: case TILE_64x64_KG2_DEEP: return 3;
+        case TILE_64x128_KG2: return 4;
+        default: return 2;
+    }
+}
 
 // A call's operands and launches.
 struct Call {
     Launches enqueue;
     char *space;
     int dtype;
-    int64_t scratch, scratch_bytes;
-    // m, or a copy at `at` whose rows are aligned and padded
-    fg_matrix aligned(const fg_matrix *m, int64_t rows, int64_t cols, bool copy, int64_t at) {
-        if (!copy) return *m;
-        const int64_t ld = up(cols, 8);
+    // m, or a copy at `at` whose rows are aligned and padded (`times`: so many, one behind the other)
+    fg_matrix aligned(const fg_matrix *m, int64_t rows, int64_t cols, bool copy, int64_t at, int64_t times = 1) {
+        if (!copy && times == 1) return *m;
+        const int64_t ld = fg::up(cols, 8);
         with_half(dtype, [&](auto t) {
             using T = decltype(t);
-            enqueue(gated_pad<T>, dim3(groups_for(rows * ld, 8)), dim3(256), (const T *)m->re, m->ld, (T *)(space + at), ld, rows, (int)cols);
+            for (int64_t k = 0; k < times; ++k)
+                enqueue(gated_pad<T>, dim3(groups_for(rows, ld)), dim3(256), (const T *)m->re, m->ld, (T *)(space + at) + k * rows * ld, ld, rows, (int)cols);
         });
         return rows_of(space + at, dtype, ld);
     }
-    fg_status product(int64_t M, int64_t N, int64_t K, int64_t k_rows, const fg_matrix &a, const fg_matrix &b, const fg_matrix &d) {
-        return gemm_stored(M, N, K, k_rows, 1.f, &a, &b, 0.f, nullptr, &d, (float *)(space + scratch), scratch_bytes, enqueue.stream);
+    fg_status by_sums(const Space &s, int64_t M, int64_t N, int64_t K, int64_t k_rows, const fg_matrix &a, const fg_matrix &b, const fg_matrix &d) {
+        if (fg_status st = enqueue.status("gated_pad")) return st;
+        return gemm_stored(M, N, K, k_rows, 1.f, &a, &b, 0.f, nullptr, &d, (float *)(space + s.scratch), s.scratch_bytes, enqueue.stream);
     }
-    void round(const fg_matrix &in, const fg_matrix *out, int64_t rows, int64_t cols) {
+    template <bool PARTS> void round(const fg_matrix &in, const fg_matrix *out, int64_t rows, int64_t cols) {
         with_half(dtype, [&](auto t) {
             using T = decltype(t);
-            enqueue(gated_round<T>, dim3(groups_for(rows * cols, 1)), dim3(256), (const float *)in.re, in.ld, (T *)out->re, out->ld, rows, (int)cols);
+            enqueue(gated_round<T, PARTS>, dim3(groups_for(rows, cols)), dim3(256), (const float *)in.re, in.ld, (T *)out->re, out->ld, rows, (int)cols);
+        });
+    }
+    // A product of the tiled kernels; k_rows: those that an operand has which is not K-contiguous (others count as zero).  f sets the parameters of its epilogue.
+    template <class F> fg_status product(int kind, int64_t M, int64_t N, int64_t K, int64_t k_rows, const fg_matrix &a, const fg_matrix &b, F &&f) {
+        if (fg_status st = enqueue.status("gated_pad")) return st;
+        const bool a_kc = kind != GATED_ROUND_NN, b_kc = kind == GATED_UP || kind == GATED_ROUND_KK;
+        const KernelEntry &k = kernel_table_gated(kind, dtype == FG_BF16)[gated_tile(M, N, K)];
+        GatedParams p;
+        memset(&p, 0, sizeof p);
+        p.M = (int32_t)M; p.N = (int32_t)N; p.K = (int32_t)K;
+        p.tiles_m = (int32_t)((M + k.bm - 1) / k.bm); p.tiles_n = (int32_t)((N + k.bn - 1) / k.bn);
+        p.A = (const _Float16 *)a.re; p.B = (const _Float16 *)b.re;
+        p.a_rs = a_kc ? a.ld : 1; p.a_ks = a_kc ? 1 : a.ld;
+        p.b_rs = b_kc ? b.ld : 1; p.b_ks = b_kc ? 1 : b.ld;
+        p.a_span = fg::up(a_kc ? (M - 1) * a.ld + K : (k_rows - 1) * a.ld + M, 8);
+        p.b_span = fg::up(b_kc ? (N - 1) * b.ld + K : (k_rows - 1) * b.ld + N, 8);
+        p.alpha = 1.f;
+        p.rotate = (p.tiles_m == 1 && b_kc) || (p.tiles_n == 1 && a_kc);
+        p.once = p.tiles_m == 1 && streams_once((uintptr_t)b.re, b.ld, N * K * 2) ? 1 : p.tiles_n == 1 && streams_once((uintptr_t)a.re, a.ld, M * K * 2) ? 2 : 0;
+        f(p);
+        return launch_product(k, p, enqueue.stream);
+    }
+    // out = a b, rounded, by the tiled kernels or through sums at s.sums; kind: GATED_ROUND_..
+    fg_status rounded(const Space &s, int64_t sums, bool through_sums, int kind, int64_t M, int64_t N, int64_t K, int64_t k_rows, const fg_matrix &a, const fg_matrix &b, const fg_matrix *out) {
+        if (!through_sums)
+            return product(kind, M, N, K, k_rows, a, b, [&](GatedParams &p) { p.D = (float *)out->re; p.ldd = out->ld; });
+        const fg_matrix d = rows_of(space + sums, FG_F32, fg::up(N, 4));
+        if (fg_status st = by_sums(s, M, N, K, kind == GATED_ROUND_KK ? 0 : k_rows, kind == GATED_ROUND_NN ? turned(a) : a, kind == GATED_ROUND_KK ? turned(b) : b, d)) return st;
+        round<false>(d, out, M, N);
+        return enqueue.status("gated_round");
+    }
+    template <bool UP> void few(const FewArgs &a) {
+        with_half(dtype, [&](auto t) {
+            using T = decltype(t);
+            auto launch = [&](auto nb) {
+                constexpr int NB = decltype(nb)::value;
+                const int tiles = (a.n + 15) / 16, steps = (a.k + 63) / 64, most = std::min(NB == 4 ? 8 : 16, 64 / ((UP ? 2 : 1) * NB));      // (64 KB of LDS)
+                int waves = 1;
+                while (waves < most && tiles * waves < 4096 && steps >= 4 * waves) waves *= 2;
+                enqueue.with_lds(waves * (UP ? 2 : 1) * NB * 1024, gated_few<T, NB, UP>, dim3((unsigned)tiles), dim3(64 * waves), a);
+            };
+            if (a.rows <= 16) launch(std::integral_constant<int, 1>{});
+            else if (a.rows <= 32) launch(std::integral_constant<int, 2>{});
+            else launch(std::integral_constant<int, 4>{});
         });
     }
 };
 
 }  // namespace
 
+#define FG_GATED(NAME) const KernelEntry *kernel_table_gated_##NAME##_f16(); const KernelEntry *kernel_table_gated_##NAME##_bf16();
+FG_GATED(up) FG_GATED(down) FG_GATED(round_kk) FG_GATED(round_kn) FG_GATED(round_nn)
+#undef FG_GATED
+const KernelEntry *kernel_table_gated(int kind, bool bf16) {
+    switch (kind) {
+        case GATED_UP: return bf16 ? kernel_table_gated_up_bf16() : kernel_table_gated_up_f16();
+        case GATED_DOWN: return bf16 ? kernel_table_gated_down_bf16() : kernel_table_gated_down_f16();
+        case GATED_ROUND_KK: return bf16 ? kernel_table_gated_round_kk_bf16() : kernel_table_gated_round_kk_f16();
+        case GATED_ROUND_KN: return bf16 ? kernel_table_gated_round_kn_bf16() : kernel_table_gated_round_kn_f16();
+        default: return bf16 ? kernel_table_gated_round_nn_bf16() : kernel_table_gated_round_nn_f16();
+    }
+}
+
 hipError_t load_gated_kernels() {
     hipFuncAttributes a;
-    return hipFuncGetAttributes(&a, (const void *)gated_round<f16_t>);
+    return hipFuncGetAttributes(&a, (const void *)gated_round<f16_t, false>);
 }
 
 }  // namespace fg
@@ -225,32 +500,57 @@ fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_mat
     if (fg_status st = check_like("Y", Y, tokens, dim, X->dtype)) return st;
     if (GU) if (fg_status st = check_like("GU", GU, tokens, 2 * hidden, FG_F32)) return st;
     if (tokens == 0 || dim == 0) return FG_OK;
-    Call call = {Launches(hip_stream), (char *)workspace, X->dtype, 0, 0};
+    Call call = {Launches(hip_stream), (char *)workspace, X->dtype};
     if (hidden == 0) {
-        call.round(rows_of(nullptr, FG_F32, 0), Y, tokens, dim);
+        call.round<false>(rows_of(nullptr, FG_F32, 0), Y, tokens, dim);
         return call.enqueue.status("gated_round");
     }
-    const bool copy_x = !as_it_is(dim, X), copy_in = !as_it_is(dim, W_in), copy_out = !as_it_is(hidden, W_out);
+    const bool copy_x = !as_it_is(dim, X), copy_out = !as_it_is(hidden, W_out), copy_in = !as_it_is(dim, W_in) || !in_reach(hidden, W_in);
     const bool own_gu = !GU || !aligned_to(GU->re, 16) || GU->ld % 4 != 0 || GU->ld >= kResultLd;        // (so that results do not depend on where GU is)
-    const ForwardSpace at(tokens, dim, hidden, copy_x, copy_in, copy_out, !own_gu);
+    const ForwardSpace at(tokens, dim, hidden, copy_x, copy_in, copy_out, own_gu);
     if (fg_status st = check_workspace(workspace, workspace_bytes, at.bytes)) return st;
-    call.scratch = at.scratch; call.scratch_bytes = at.scratch_bytes;
     const int64_t dp = up(dim, 8), hp = up(hidden, 8);
-    const fg_matrix x = call.aligned(X, tokens, dim, copy_x, at.x), w_in = call.aligned(W_in, 2 * hidden, dim, copy_in, at.w_in),
-                    w_out = call.aligned(W_out, dim, hidden, copy_out, at.w_out);
-    const fg_matrix gu = !own_gu ? *GU : rows_of(call.space + at.gu, FG_F32, up(2 * hidden, 4)), h = rows_of(call.space + at.h, X->dtype, hp),
-                    sums = rows_of(call.space + at.sums, FG_F32, up(dim, 4));
-    if (fg_status st = call.product(tokens, 2 * hidden, dp, 0, x, turned(w_in), gu)) return st;
-    with_half(X->dtype, [&](auto t) {
-        using T = decltype(t);
-        with_act(act, [&](auto a) {
-            call.enqueue(gated_product<T, decltype(a)::value>, dim3(groups_for(tokens * hp, 1)), dim3(256), (const float *)gu.re, gu.ld, (T *)h.re, hp, tokens, (int)hidden,
-                         own_gu && GU ? (float *)GU->re : nullptr, GU ? GU->ld : 0);
+    const fg_matrix h = rows_of(call.space + at.h, X->dtype, hp);
+    float *keep = GU ? (float *)GU->re : nullptr;
+    const int64_t ldkeep = GU ? GU->ld : 0;
+    const Activation activation = Activation::of(act);
+    if (at.few) {
+        const int32_t lo = tokens <= kPartsTokens ? (int32_t)tokens : 0;
+        call.few<true>({X->re, W_in->re, h.re, keep, X->ld, W_in->ld, hp, ldkeep, (int32_t)tokens, lo, (int32_t)hidden, (int32_t)dim, activation});
+        call.few<false>({h.re, W_out->re, Y->re, nullptr, hp, W_out->ld, Y->ld, 0, (int32_t)tokens + lo, lo, (int32_t)dim, (int32_t)hidden, activation});
+        return call.enqueue.status("gated_few");
+    }
+    const fg_matrix x = call.aligned(X, tokens, dim, copy_x, at.x), w_out = call.aligned(W_out, dim, hidden, copy_out, at.w_out);
+    if (at.up_by_sums) {
+        const fg_matrix w_in = call.aligned(W_in, 2 * hidden, dim, copy_in, at.w_in), gu = !own_gu ? *GU : rows_of(call.space + at.gu, FG_F32, up(2 * hidden, 4));
+        if (fg_status st = call.by_sums(at, tokens, 2 * hidden, dp, 0, x, turned(w_in), gu)) return st;
+        with_half(X->dtype, [&](auto t) {
+            using T = decltype(t);
+            call.enqueue(gated_product<T>, dim3(groups_for(tokens, hidden)), dim3(256), (const float *)gu.re, gu.ld, (T *)h.re, hp, tokens, (int)hidden, activation,
+                         own_gu ? keep : nullptr, ldkeep);
         });
-    });
-    if (fg_status st = call.product(tokens, dim, hp, 0, h, turned(w_out), sums)) return st;
-    call.round(sums, Y, tokens, dim);
-    return call.enqueue.status("gated_ffn");
+    } else {
+        fg_matrix w_in = *W_in;
+        int64_t pair = hidden, pair_step = 32;
+        if (copy_in) {
+            w_in = rows_of(call.space + at.w_in, X->dtype, dp);
+            pair = 32;
+            pair_step = 64;
+            with_half(X->dtype, [&](auto t) {
+                using T = decltype(t);
+                call.enqueue(gated_interleave<T>, dim3(groups_for(2 * up(hidden, 32), dp)), dim3(256), (const T *)W_in->re, W_in->ld, (T *)w_in.re, dp, (int)hidden, (int)dim);
+            });
+        }
+        const int64_t columns = 2 * up(hidden, 32);
+        if (fg_status st = call.product(GATED_UP, tokens, columns, dp, 0, x, w_in, [&](GatedParams &p) {
+                p.b_span = up(((copy_in ? columns : 2 * hidden) - 1) * w_in.ld + dp, 8);
+                p.D = (float *)h.re; p.ldd = hp;
+                p.keep = keep; p.ldgu = ldkeep;
+                p.pair = pair; p.pair_step = pair_step;
+                p.hidden = (int32_t)hidden; p.act = activation;
+            })) return st;
+    }
+    return call.rounded(at, at.sums, at.down_by_sums, GATED_ROUND_KK, tokens, dim, hp, 0, h, w_out, Y);
 }
 
 int64_t fg_gated_ffn_grad_workspace(int64_t tokens, int64_t dim, int64_t hidden) {
@@ -267,47 +567,56 @@ fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const f
     if (dX) if (fg_status st = check_like("dX", dX, tokens, dim, X->dtype)) return st;
     if (dW_in) if (fg_status st = check_like("dW_in", dW_in, 2 * hidden, dim, X->dtype)) return st;
     if (dW_out) if (fg_status st = check_like("dW_out", dW_out, dim, hidden, X->dtype)) return st;
-    Call call = {Launches(hip_stream), (char *)workspace, X->dtype, 0, 0};
+    Call call = {Launches(hip_stream), (char *)workspace, X->dtype};
     if (dim == 0) return FG_OK;
     if (tokens == 0 || hidden == 0) {
         const fg_matrix none = rows_of(nullptr, FG_F32, 0);
-        if (dX && tokens > 0) call.round(none, dX, tokens, dim);
-        if (dW_in && hidden > 0) call.round(none, dW_in, 2 * hidden, dim);
-        if (dW_out && hidden > 0) call.round(none, dW_out, dim, hidden);
+        if (dX && tokens > 0) call.round<false>(none, dX, tokens, dim);
+        if (dW_in && hidden > 0) call.round<false>(none, dW_in, 2 * hidden, dim);
+        if (dW_out && hidden > 0) call.round<false>(none, dW_out, dim, hidden);
         return call.enqueue.status("gated_round");
     }
     if (!dX && !dW_in && !dW_out) return FG_OK;
     const bool copy_dy = !as_it_is(dim, dY), copy_x = !as_it_is(dim, X), copy_in = !as_it_is(dim, W_in), copy_out = !as_it_is(hidden, W_out);
     const GradSpace at(tokens, dim, hidden, copy_dy, copy_x, copy_in, copy_out);
     if (fg_status st = check_workspace(workspace, workspace_bytes, at.bytes)) return st;
-    call.scratch = at.scratch; call.scratch_bytes = at.scratch_bytes;
-    const int64_t dp = up(dim, 8), hp = up(hidden, 8), gp = up(2 * hidden, 8), tp = up(tokens, 8);
-    const fg_matrix dy = call.aligned(dY, tokens, dim, copy_dy, at.dy), x = call.aligned(X, tokens, dim, copy_x, at.x),
-                    w_in = call.aligned(W_in, 2 * hidden, dim, copy_in, at.w_in), w_out = call.aligned(W_out, dim, hidden, copy_out, at.w_out);
-    const fg_matrix dh = rows_of(call.space + at.dh, FG_F32, up(hidden, 4)), h = rows_of(call.space + at.h, X->dtype, hp),
-                    dgu = rows_of(call.space + at.dgu, X->dtype, gp);
-    auto sums = [&](int64_t cols) { return rows_of(call.space + at.sums, FG_F32, up(cols, 4)); };
-    if (fg_status st = call.product(tokens, hidden, dp, dim, dy, w_out, dh)) return st;
-    with_half(X->dtype, [&](auto t) {
-        using T = decltype(t);
-        with_act(act, [&](auto a) {
-            call.enqueue(gated_product_grad<T, decltype(a)::value>, dim3(groups_for(tokens * gp, 1)), dim3(256), (const float *)GU->re, GU->ld, (const float *)dh.re, dh.ld,
-                         (T *)h.re, hp, (T *)dgu.re, gp, tokens, (int)hidden);
+    const int64_t dp = up(dim, 8), hp = up(hidden, 8), gp = up(2 * hidden, 8), rows = at.parts * tokens, tp = up(rows, 8);
+    const fg_matrix dy = call.aligned(dY, tokens, dim, copy_dy, at.dy, at.parts), w_out = call.aligned(W_out, dim, hidden, copy_out, at.w_out);
+    const fg_matrix h = rows_of(call.space + at.h, X->dtype, hp), dgu = rows_of(call.space + at.dgu, X->dtype, gp);
+    const Activation activation = Activation::of(act);
+    if (at.down_by_sums) {
+        const fg_matrix dh = rows_of(call.space + at.dh, FG_F32, up(hidden, 4));
+        if (fg_status st = call.by_sums(at, tokens, hidden, dp, dim, dy, w_out, dh)) return st;
+        with_half(X->dtype, [&](auto t) {
+            using T = decltype(t);
+            auto pass = [&](auto kernel) {
+                call.enqueue(kernel, dim3(groups_for(tokens, hidden)), dim3(256), (const float *)GU->re, GU->ld, (const float *)dh.re, dh.ld, (T *)h.re, hp, (T *)dgu.re, gp,
+                             tokens, (int)hidden, activation);
+            };
+            if (at.parts == 2) pass(gated_product_grad<T, true>);
+            else pass(gated_product_grad<T, false>);
         });
-    });
-    if (fg_status st = call.enqueue.status("gated_product_grad")) return st;
+        if (fg_status st = call.enqueue.status("gated_product_grad")) return st;
+    } else if (fg_status st = call.product(GATED_DOWN, tokens, hidden, dp, dim, dy, w_out, [&](GatedParams &p) {
+                   p.D = (float *)dgu.re; p.ldd = gp;
+                   p.h = h.re; p.ldh = hp;
+                   p.gu = (const float *)GU->re; p.ldgu = GU->ld;
+                   p.hidden = (int32_t)hidden; p.act = activation;
+               })) return st;
     if (dX) {
-        if (fg_status st = call.product(tokens, dim, gp, 2 * hidden, dgu, w_in, sums(dim))) return st;
-        call.round(sums(dim), dX, tokens, dim);
+        const fg_matrix w_in = call.aligned(W_in, 2 * hidden, dim, copy_in, at.w_in);
+        if (at.parts == 2) {
+            const fg_matrix sums = rows_of(call.space + at.sums, FG_F32, up(dim, 4));
+            if (fg_status st = call.by_sums(at, rows, dim, gp, 2 * hidden, dgu, w_in, sums)) return st;
+            call.round<true>(sums, dX, tokens, dim);
+        } else if (fg_status st = call.rounded(at, at.sums, at.x_by_sums, GATED_ROUND_KN, tokens, dim, gp, 2 * hidden, dgu, w_in, dX)) return st;
     }
     if (dW_in) {
-        if (fg_status st = call.product(2 * hidden, dim, tp, tokens, turned(dgu), x, sums(dim))) return st;
-        call.round(sums(dim), dW_in, 2 * hidden, dim);
+        const fg_matrix x = call.aligned(X, tokens, dim, copy_x, at.x, at.parts);
+        if (fg_status st = call.rounded(at, at.sums, at.in_by_sums, GATED_ROUND_NN, 2 * hidden, dim, at.in_by_sums ? tp : rows, rows, dgu, x, dW_in)) return st;
     }
-    if (dW_out) {
-        if (fg_status st = call.product(dim, hidden, tp, tokens, turned(dy), h, sums(hidden))) return st;
-        call.round(sums(hidden), dW_out, dim, hidden);
-    }
+    if (dW_out)
+        if (fg_status st = call.rounded(at, at.sums, at.out_by_sums, GATED_ROUND_NN, dim, hidden, at.out_by_sums ? tp : rows, rows, dy, h, dW_out)) return st;
     return call.enqueue.status("gated_ffn_grad");
 }
 

@@ -161,6 +161,8 @@ struct TileCfg {
     // OWN_STORE: results do not become D = act(alpha A.B + beta C + bias); what becomes of them is said by a configuration derived
     // from this one, in store(parameters, blocks, m_base, n_base, lane): blocks(i, j), with compile-time indices, is a 32x32 block.
     static constexpr bool OWN_STORE = false;
+    // PAIRED (derived configurations with B contiguous along K): blocks of 32 of B's rows come from two places in turn, GatedParams::pair rows apart.
+    static constexpr bool PAIRED = false;
     // 0: real; 1: complex (i^2 = -1), 2: dual (eps^2 = 0) numbers in planar-split storage
     static constexpr int CPLX = CPLX_;
     static constexpr bool SPLITK_KERNEL = !STRIDED_ && DIAG_ == 0 && CPLX_ == 0;
@@ -358,8 +360,11 @@ __device__ __forceinline__ T load_param(unsigned offset) {
 // layout (commit), the conversion the paper places in the global-to-shared copy.
 // FLIP (M/N-contiguous tiles read as 16-row fragments, TileCfg::M16): see mc_swz.
 // KINC (plain matrices): advance() moves on by so many K steps.
-template <int R, int BK, bool KC, int SLABS, bool STRIDED, int ES = 1, bool FLIP = false, int KINC = 1>
+// PAIRED: see TileCfg; LDS row r holds source row `pair_row` (pair, pair_step: GatedParams).
+__device__ __forceinline__ int64_t pair_row(int r, int64_t pair, int64_t pair_step) { return (r >> 6) * pair_step + (r & 31) + ((r >> 5) & 1) * pair; }
+template <int R, int BK, bool KC, int SLABS, bool STRIDED, int ES = 1, bool FLIP = false, int KINC = 1, bool PAIRED = false>
 struct TileLoader {
+    static_assert(!PAIRED || (KC && !STRIDED && ES == 1), "");
     static_assert(ES == 1 || (ES == 2 && !STRIDED), "interleaved elements: plain matrices only");
     static_assert(!FLIP || ES == 1, "");
     static_assert(KINC == 1 || !STRIDED, "");
@@ -380,7 +385,7 @@ struct TileLoader {
 
     __device__ __forceinline__ void init(const _Float16 *ptr, int row0, int wave, int lane,
                                          int64_t rs, int64_t ks, const ModeGroup &rg, const ModeGroup &kgrp,
-                                         int64_t span = 0, int kdim_ = 0, int rdim = 0) {
+                                         int64_t span = 0, int kdim_ = 0, int rdim = 0, int64_t pair = 0, int64_t pair_step = 0) {
         ktile = 0;
         klim = BK;
         if constexpr (!STRIDED) {
@@ -409,7 +414,8 @@ struct TileLoader {
                 int r = slab * (64 / CPR) + lane / CPR;
                 int c = (lane % CPR) ^ kc_swz<BK>(r);
                 kchunk[s] = c * 8;
-                if constexpr (!STRIDED) off = (int64_t)r * rs + c * 8;
+                if constexpr (PAIRED) off = pair_row(r, pair, pair_step) * rs + c * 8;
+                else if constexpr (!STRIDED) off = (int64_t)r * rs + c * 8;
                 else off = group_offset(rg, row0 + r) + c * 8;     // leading K mode has stride 1
                 if constexpr (STRIDED) {
                     // a row past the merged row extent: the load is dropped and LDS gets zeros
@@ -1158,14 +1164,14 @@ __global__ __launch_bounds__(Cfg::NTHREADS, Cfg::WAVES) void gemm_kernel(const t
     FG_LDS char *lds_b = lds_a + Cfg::A_BYTES;
 
     using PlainA = TileLoader<BM, BK, Cfg::A_KC, Cfg::A_SLABS, Cfg::STRIDED, Cfg::ILV ? 2 : 1, Cfg::M16, Cfg::KINC>;
-    using PlainB = TileLoader<BN, BK, Cfg::B_KC, Cfg::B_SLABS, Cfg::STRIDED, Cfg::ILV ? 2 : 1, Cfg::M16, Cfg::KINC>;
+    using PlainB = TileLoader<BN, BK, Cfg::B_KC, Cfg::B_SLABS, Cfg::STRIDED, Cfg::ILV ? 2 : 1, Cfg::M16, Cfg::KINC, Cfg::PAIRED>;
     constexpr int NLOADERS = Cfg::ILV ? 1 : P;      // an interleaved operand is one array, not one per plane
     using LoaderA = typename std::conditional<Cfg::DIAG == 1, DiagLoader<BM, BK, Cfg::A_SLABS>, PlainA>::type;
     using LoaderB = typename std::conditional<Cfg::DIAG == 2, DiagLoader<BN, BK, Cfg::B_SLABS>, PlainB>::type;
     LoaderA la[P];
     LoaderB lb[P];
     [[maybe_unused]] WideLoader<BM, Cfg::A_KC> wide_a;      // TileCfg::WIDE, in place of la and lb
-    [[maybe_unused]] WideLoader<BN, Cfg::B_KC> wide_b;
+    [[maybe_unused]] WideLoader<BN, Cfg::B_KC, Cfg::PAIRED> wide_b;
     FragReader<BM, BK, Cfg::A_KC, TI, Cfg::M16> fa;
     FragReader<BN, BK, Cfg::B_KC, TJ, Cfg::M16> fb;
     auto init_readers = [&] {
@@ -1237,11 +1243,15 @@ __global__ __launch_bounds__(Cfg::NTHREADS, Cfg::WAVES) void gemm_kernel(const t
             const uint32_t to_a = (uint32_t)(uintptr_t)lds_a + (uint32_t)wave * (Cfg::A_SLABS * 1024u);
             const uint32_t to_b = (uint32_t)(uintptr_t)lds_b + (uint32_t)wave * (Cfg::B_SLABS * 1024u);
             wide_a.init(wave, lane, tp.a_rs, tp.a_ks);
-            wide_b.init(wave, lane, tp.b_rs, tp.b_ks);
+            int b_row0 = n0;
+            if constexpr (Cfg::PAIRED) {
+                b_row0 = n0 / 64 * (int)tp.pair_step;
+                wide_b.init_pairs(wave, lane, tp.b_rs, tp.pair, tp.pair_step);
+            } else wide_b.init(wave, lane, tp.b_rs, tp.b_ks);
             const int first = kt0 + turn;
             const bool a_once = Cfg::ONCE && tp.once == 2, b_once = Cfg::ONCE && tp.once == 1;
             wide_a.at(ap[0], m0, tp.a_rs, tp.a_ks, tp.a_span, first, nkt > 0, circle);
-            wide_b.at(bp[0], n0, tp.b_rs, tp.b_ks, tp.b_span, first, nkt > 0, circle);
+            wide_b.at(bp[0], b_row0, tp.b_rs, tp.b_ks, tp.b_span, first, nkt > 0, circle);
             if (last_first) {
                 wide_a.moved(nk - 1 - first).issue_part(to_a, rest, lane);
                 wide_b.moved(nk - 1 - first).issue_part(to_b, rest, lane);
@@ -1278,6 +1288,7 @@ __global__ __launch_bounds__(Cfg::NTHREADS, Cfg::WAVES) void gemm_kernel(const t
             if constexpr (Cfg::DIAG == 1) la[q].init(ap[q], m0, tp.M < tp.K ? tp.M : tp.K, wave, lane);
             else la[q].init(ap[q], m0, wave, lane, tp.a_rs, tp.a_ks, none, none, tp.a_span, tp.K, tp.M);
             if constexpr (Cfg::DIAG == 2) lb[q].init(bp[q], n0, tp.N < tp.K ? tp.N : tp.K, wave, lane);
+            else if constexpr (Cfg::PAIRED) lb[q].init(bp[q], n0 / 64 * (int)tp.pair_step, wave, lane, tp.b_rs, tp.b_ks, none, none, tp.b_span, tp.K, tp.N, tp.pair, tp.pair_step);
             else lb[q].init(bp[q], n0, wave, lane, tp.b_rs, tp.b_ks, none, none, tp.b_span, tp.K, tp.N);
             if constexpr (Cfg::DIAG != 0 || Cfg::SPLITK_KERNEL || Cfg::KG > 1) {
                 if (kt0 > 0) { la[q].skip(kt0); lb[q].skip(kt0); }

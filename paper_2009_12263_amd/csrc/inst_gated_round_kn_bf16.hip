@@ -1,0 +1,5 @@
+// Gated feed-forward block, bfloat16: rounded products, A contiguous along K (gated_kernel.hpp).
+#include "gated_kernel.hpp"
+namespace fg {
+FG_GATED_TABLE(kernel_table_gated_round_kn_bf16, GATED_ROUND_KN, true, false, true, "gated_round_kn_bf16")
+}

@@ -77,7 +77,7 @@ __device__ __forceinline__ void mfma_acc_load(half8 a, half8 b, u32x4 rsrc, uint
 // One operand of a plain matrix, R rows x 64 k per K tile, in the LDS layout of TileLoader (16-row fragments); a wave
 // fetches SLABS pieces of 1 KB.  The descriptor is advanced in place.  Its size, the bytes from the current K tile
 // to the end of the operand, is counted in 64 bits (negative past the end).
-template <int R, bool KC>
+template <int R, bool KC, bool PAIRED = false>
 struct WideLoader {
     static constexpr int SLABS = R / 32;
     uint32_t voff[SLABS];
@@ -123,6 +123,13 @@ struct WideLoader {
         const uint32_t first = (uint32_t)(wave * (SLABS * SLAB_ROWS) + row) * pitch;
 #pragma unroll
         for (int s = 0; s < SLABS; ++s) voff[s] = first + (uint32_t)((c ^ flips(s)) * 16) + (uint32_t)(s * SLAB_ROWS) * pitch;
+    }
+    // the same for rows that come from two places in turn (TileCfg::PAIRED)
+    __device__ __forceinline__ void init_pairs(int wave, int lane, int64_t rs, int64_t pair, int64_t pair_step) {
+        static_assert(!PAIRED || KC, "");
+        const int row = wave * (SLABS * SLAB_ROWS) + lane / 8, c = (lane & 7) ^ (lane >> 4);
+#pragma unroll
+        for (int s = 0; s < SLABS; ++s) voff[s] = (uint32_t)(pair_row(row + s * SLAB_ROWS, pair, pair_step) * rs * 2) + (uint32_t)((c ^ flips(s)) * 16);
     }
     // KC: which chunk of eight k of its row a lane fetches
     __device__ __forceinline__ int chunk(int s, int lane) const { return (lane & 7) ^ (lane >> 4) ^ flips(s); }
