@@ -9,10 +9,10 @@
 //
 // H, dG and dU are rounded to the operands' 16 bits, the only roundings but those of the results: an error of half a step each, so that
 // results are 1.4 times as far from 64 bits as rounding alone makes them.  G and U are kept in FP32: in 16 bits theirs came on top (dX 1.9 times).
-// With up to kPartsTokens tokens the error of single values shows in a result's norm, and the matrix units have time: there
-// H, dG and dU are two 16-bit numbers each, a value and what its rounding left, in rows of their own of the same products.
+// Of few results (parts_of) the error of single values shows in the norm, 1.6 times that of rounding alone (2 tokens of 224 values), and the matrix units have time:
+// there H, dG and dU are two 16-bit numbers each, a value and what its rounding left, in rows of their own of the same products.
 //
-// Up to kFewTokens tokens the forward products are all reading of weights: gated_few.
+// Of few tokens the forward products are all reading of weights: gated_few.
 #include <algorithm>
 #include <cstring>
 #include <type_traits>
@@ -86,8 +86,8 @@ template <class F> __device__ __forceinline__ void each_piece(int64_t rows, int 
     }
 }
 
-// h = act(g) u, rounded, with zeros to the end of its rows; g and u are copied to `keep` where it is given
-template <class T>
+// h = act(g) u, rounded, with zeros to the end of its rows, PARTS: and what its rounding leaves `rows` rows further on; g and u are copied to `keep` where it is given
+template <class T, bool PARTS>
 __global__ __launch_bounds__(256) void gated_product(const float *gu, int64_t ldgu, T *h, int64_t ldh, int64_t rows, int hidden, Activation act, float *keep, int64_t ldkeep) {
     each_piece(rows, hidden, [&](int64_t row, int c) {
         float g[8], u[8], v[8];
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256) void gated_product(const float *gu, int64_t ld
         load_eight(gu + row * ldgu + hidden, c, hidden, u);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = c + e < hidden ? act.operator()<false>(g[e], nullptr) * u[e] : 0.f;
-        store_eight<T>(h + row * ldh, c, (int)ldh, v, nullptr);
+        store_eight<T>(h + row * ldh, c, (int)ldh, v, PARTS ? h + (rows + row) * ldh : nullptr);
         if (keep) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -168,9 +168,12 @@ __global__ __launch_bounds__(256) void gated_interleave(const T *in, int64_t ld,
 // ---- few tokens -------------------------------------------------------------------------------------------------
 // Sums over k of w[n][k] x[r][k] for up to 16 NB rows r of x: reading w.  A workgroup takes 16 rows of w (UP: and as many of U), its waves 64 k each in
 // turn: a lane reads its row's 16 bytes straight into the operand of a 16x16x32 matrix instruction, a wave two whole lines of each row.  The waves' sums are added
-// up through LDS in their order.  x is read from the L2 by every workgroup, 16 bytes for each 16 of w and 16 rows.
-// UP: h = act(g) u of the sums, in 16 bits, and what its rounding leaves `lo` rows further on (lo > 0); g and u are kept in FP32 where that is wanted.
+// up through LDS in their order.
+// UP: h = act(g) u of the sums, in 16 bits, and what its rounding leaves `lo` rows further on (lo > 0); g and u are kept in FP32 where that is wanted.  x is row-major; h
+// is written as the other form reads its x: operands of matrix instructions, those of 32 k and 16 rows one after the other.
 // Otherwise: rounded; with lo > 0 the sums of rows r and lo + r.
+// Bound by reading w with one token (4096 x 10240: 252 MB in 50 us); with more, x costs as well, which each workgroup reads from the L2: every row of it is a
+// line of its own (16 tokens 61 us), and from 17 on the tiled kernels, which share x through LDS, are as fast.
 struct FewArgs {
     const void *x, *w;
     void *out;
@@ -184,8 +187,12 @@ __device__ __forceinline__ floatx4 mfma_16x16x32(typename RowPiece<T>::vec a, ty
     if constexpr (std::is_same<T, bf16_t>::value) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
+// Where h's value of row r and column c is, and the values of all of it.
+template <int NB> __host__ __device__ __forceinline__ int64_t few_place(int r, int c) { return ((int64_t)(c >> 5) * NB + (r >> 4)) * 512 + ((c >> 3) & 3) * 128 + (r & 15) * 8 + (c & 7); }
+constexpr int64_t few_values(int64_t rows, int64_t k) { return (k + 31) / 32 * 512 * ((rows + 15) / 16); }
+
 template <class T, int NB, bool UP>
-__global__ __launch_bounds__(NB == 4 ? 512 : 1024) void gated_few(const FewArgs a) {
+__global__ __launch_bounds__(1024) void gated_few(const FewArgs a) {
     typedef typename RowPiece<T>::vec vec;
     typedef typename RowPiece<T>::unaligned anywhere;
     constexpr int G = UP ? 2 : 1;
@@ -197,21 +204,27 @@ __global__ __launch_bounds__(NB == 4 ? 512 : 1024) void gated_few(const FewArgs 
 #pragma unroll
     for (int g = 0; g < G; ++g) w[g] = (const T *)a.w + ((int64_t)row + (g ? a.n : 0)) * a.ldw + quarter * 8;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) x[b] = (const T *)a.x + (int64_t)min(b * 16 + at, a.rows - 1) * a.ldx + quarter * 8;
+    for (int b = 0; b < NB; ++b) x[b] = UP ? (const T *)a.x + (int64_t)min(b * 16 + at, a.rows - 1) * a.ldx + quarter * 8 : (const T *)a.x + b * 512 + lane * 8;
+    auto x_at = [&](int b, int k) { return UP ? x[b] + k : x[b] + (int64_t)(k >> 5) * (NB * 512); };
     floatx4 sum[G][NB] = {};
-    const int k_whole = a.k / 64 * 64, stride = waves * 64;
-    // S turns of 64 k at once, all their loads first
-    auto turns = [&](int k, auto count) {
+    // Workgroups begin at places of their own and walk K in a circle: side by side from its start they read, of rows that often lie a power of two
+    // apart, the same few address bits, and those choose the memory channel (16 tokens, 4096 x 10240: 46.6 and 38.0 us the two forms, 39.7 and 34.2 so).
+    const int k_whole = a.k / 64 * 64, turns = a.k / 64;
+    const int begin = turns > 0 ? (int)(blockIdx.x * 5u % (unsigned)turns) : 0;
+    auto several = [&](int turn, auto count) {
         constexpr int S = 2 * decltype(count)::value;
         vec wv[S][G], xv[S][NB];
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-            const int at_k = k + s / 2 * stride + s % 2 * 32;
+            int t = turn + s / 2 * waves + begin;
+            t = t >= turns ? t - turns : t;
+            const int k = t * 64 + s % 2 * 32;
 #pragma unroll
-            for (int g = 0; g < G; ++g) wv[s][g] = *(const anywhere *)(w[g] + at_k);
+            for (int g = 0; g < G; ++g) wv[s][g] = *(const anywhere *)(w[g] + k);
 #pragma unroll
-            for (int b = 0; b < NB; ++b) xv[s][b] = *(const anywhere *)(x[b] + at_k);
+            for (int b = 0; b < NB; ++b) xv[s][b] = *(const anywhere *)x_at(b, k);
         }
+        __builtin_amdgcn_sched_barrier(0);              // (all requests go out before the first is used)
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
@@ -219,27 +232,32 @@ __global__ __launch_bounds__(NB == 4 ? 512 : 1024) void gated_few(const FewArgs 
 #pragma unroll
                 for (int b = 0; b < NB; ++b) sum[g][b] = mfma_16x16x32<T>(wv[s][g], xv[s][b], sum[g][b]);
     };
-    int k = wave * 64;
-    for (; k + stride < k_whole; k += 2 * stride) turns(k, std::integral_constant<int, 2>{});
-    if (k < k_whole) turns(k, std::integral_constant<int, 1>{});
-    if (k_whole < a.k && wave == k_whole / 64 % waves) {            // the last values: element by element at the end of a row
-        auto piece = [&](const T *p, int k) {
-            vec v = {};
-            const int left = a.k - k - quarter * 8;
-            if (left >= 8) v = *(const anywhere *)(p + k);
-            else
+    int turn = wave;
+    for (; turn + waves < turns; turn += 2 * waves) several(turn, std::integral_constant<int, 2>{});
+    if (turn < turns) several(turn, std::integral_constant<int, 1>{});
+    if (k_whole < a.k && wave == turns % waves) {                   // the last values: element by element at the end of a row
+        for (int last = k_whole; last < a.k; last += 32) {
+            const int left = a.k - last - quarter * 8;
+            auto piece = [&](const T *p, bool whole) {
+                vec v = {};
+                if (whole && left > 0) {
+                    v = *(const anywhere *)p;
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e < left) v[e] = p[k + e];
-            return v;
-        };
-        for (int last = k_whole; last < a.k; last += 32)
+                    for (int e = 0; e < 8; ++e) v[e] = e < left ? v[e] : (T)0.f;
+                } else if (left >= 8) v = *(const anywhere *)p;
+                else
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e < left) v[e] = p[e];
+                return v;
+            };
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const vec v = piece(w[g], last);
+                const vec v = piece(w[g] + last, false);
 #pragma unroll
-                for (int b = 0; b < NB; ++b) sum[g][b] = mfma_16x16x32<T>(v, piece(x[b], last), sum[g][b]);
+                for (int b = 0; b < NB; ++b) sum[g][b] = mfma_16x16x32<T>(v, piece(x_at(b, last), !UP), sum[g][b]);
             }
+        }
     }
 #pragma unroll
     for (int g = 0; g < G; ++g)
@@ -256,9 +274,8 @@ __global__ __launch_bounds__(NB == 4 ? 512 : 1024) void gated_few(const FewArgs 
     const int rows = UP || a.lo == 0 ? a.rows : a.lo;
     for (int i = threadIdx.x; i < rows * 4; i += blockDim.x) {
         const int r = i >> 2, q = i & 3, c = n0 + 4 * q, left = a.n - c;
-        floatx4 v = total(0, r, q);
         if (left <= 0) continue;
-        T *out = (T *)a.out + (int64_t)r * a.ldo + c;
+        floatx4 v = total(0, r, q);
         if constexpr (UP) {
             const floatx4 u = total(1, r, q);
             if (a.keep) {
@@ -269,7 +286,10 @@ __global__ __launch_bounds__(NB == 4 ? 512 : 1024) void gated_few(const FewArgs 
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = a.act.operator()<false>(v[e], nullptr) * u[e];
-            T *rest = out + (int64_t)a.lo * a.ldo;
+            // (both forms have as many blocks of rows of h: with lo > 0 it has 2 lo rows)
+            const bool wide = a.lo ? 2 * a.lo > 16 : NB > 1;
+            auto place = [&](int row) { return (T *)a.out + (wide ? few_place<2>(row, c) : few_place<1>(row, c)); };
+            T *out = place(r), *rest = place(r + a.lo);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (e < left) {
@@ -279,6 +299,7 @@ __global__ __launch_bounds__(NB == 4 ? 512 : 1024) void gated_few(const FewArgs 
                 }
         } else {
             if (a.lo) v += total(0, a.lo + r, q);
+            T *out = (T *)a.out + (int64_t)r * a.ldo + c;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (e < left) out[e] = (T)v[e];
@@ -298,7 +319,12 @@ fg_matrix rows_of(const void *p, int32_t dtype, int64_t ld, int32_t layout = FG_
 fg_matrix turned(fg_matrix m) { m.layout = FG_COL; return m; }
 bool as_it_is(int64_t cols, const fg_matrix *m) { return cols % 8 == 0 && aligned_to(m->re, 16) && m->ld % 8 == 0 && m->ld < kKContiguousLd; }
 
-constexpr int64_t kFewTokens = 64, kPartsTokens = 32;
+// Whether gated_few takes so many rows.  Up to 16 it is the fastest (one token of 4096 x 10240 52 us, the tiled kernels 68; 16 63 and 61); up to 32 where the
+// weights are small and launches count (32 tokens of 1024 x 2560 20.1 us, by four launches of tiled kernels and sums 22.1; of 2048 x 5120 34.7 and 27.1).
+bool are_few(int64_t rows, int64_t D, int64_t H) { return rows <= 16 || (rows <= 32 && D * H <= (1 << 22)); }
+
+// Rows for each token of H, dG and dU: two where results are few.
+int64_t parts_of(int64_t T, int64_t D, int64_t H) { return T * std::min(D, H) < 16384 ? 2 : 1; }
 
 // Whether a product goes through FP32 sums: the planner splits its K.
 bool by_sums(int64_t M, int64_t N, int64_t K) { return gemm_stored_scratch(M, N, K) > 0; }
@@ -312,22 +338,24 @@ struct Space {
     void partial(int64_t M, int64_t N, int64_t K) { scratch_bytes = std::max(scratch_bytes, gemm_stored_scratch(M, N, K)); }
 };
 struct ForwardSpace : Space {
+    int64_t parts;
     bool few, up_by_sums, down_by_sums;
     int64_t x = 0, w_in = 0, w_out = 0, gu = 0, h, sums = 0;
     ForwardSpace(int64_t T, int64_t D, int64_t H, bool copy_x, bool copy_in, bool copy_out, bool own_gu) {
         const int64_t dp = up(D, 8), hp = up(H, 8);
-        few = T <= kFewTokens;
-        up_by_sums = !few && by_sums(T, 2 * H, dp);
-        down_by_sums = !few && by_sums(T, D, hp);
-        h = take((T <= kPartsTokens ? 2 : 1) * T * hp * 2);
+        parts = parts_of(T, D, H);
+        few = are_few(parts * T, D, H);
+        up_by_sums = !few && (parts == 2 || by_sums(T, 2 * H, dp));
+        down_by_sums = !few && (parts == 2 || by_sums(T, D, hp));
+        h = take((few ? few_values(parts * T, H) : parts * T * hp) * 2);
         if (few) return;
         if (copy_x) x = take(T * dp * 2);
         if (copy_in) w_in = take(2 * up(H, 32) * dp * 2);
         if (copy_out) w_out = take(D * hp * 2);
         if (up_by_sums && own_gu) gu = take(T * up(2 * H, 4) * 4);
-        if (down_by_sums) sums = take(T * up(D, 4) * 4);
+        if (down_by_sums) sums = take(parts * T * up(D, 4) * 4);
         if (up_by_sums) partial(T, 2 * H, dp);
-        if (down_by_sums) partial(T, D, hp);
+        if (down_by_sums) partial(parts * T, D, hp);
         scratch = take(scratch_bytes);
     }
 };
@@ -337,7 +365,7 @@ struct GradSpace : Space {
     int64_t dy = 0, x = 0, w_in = 0, w_out = 0, dh = 0, h, dgu, sums = 0;
     GradSpace(int64_t T, int64_t D, int64_t H, bool copy_dy, bool copy_x, bool copy_in, bool copy_out) {
         const int64_t dp = up(D, 8), hp = up(H, 8), gp = up(2 * H, 8);
-        parts = T <= kPartsTokens ? 2 : 1;
+        parts = parts_of(T, D, H);
         const int64_t tp = up(parts * T, 8);
         down_by_sums = parts == 2 || by_sums(T, H, dp);
         x_by_sums = parts == 2 || by_sums(T, D, gp);
@@ -451,14 +479,14 @@ struct Call {
             using T = decltype(t);
             auto launch = [&](auto nb) {
                 constexpr int NB = decltype(nb)::value;
-                const int tiles = (a.n + 15) / 16, steps = (a.k + 63) / 64, most = std::min(NB == 4 ? 8 : 16, 64 / ((UP ? 2 : 1) * NB));      // (64 KB of LDS)
+                // Waves to fill the GPU (16 a unit), as long as each has eight turns (one token of 1024 x 2560: four waves for G and U 10.9 us, sixteen 11.5).
+                const int tiles = (a.n + 15) / 16, steps = (a.k + 63) / 64;
                 int waves = 1;
-                while (waves < most && tiles * waves < 4096 && steps >= 4 * waves) waves *= 2;
+                while (waves < 16 && tiles * waves < 4096 && steps >= 8 * waves) waves *= 2;
                 enqueue.with_lds(waves * (UP ? 2 : 1) * NB * 1024, gated_few<T, NB, UP>, dim3((unsigned)tiles), dim3(64 * waves), a);
             };
             if (a.rows <= 16) launch(std::integral_constant<int, 1>{});
-            else if (a.rows <= 32) launch(std::integral_constant<int, 2>{});
-            else launch(std::integral_constant<int, 4>{});
+            else launch(std::integral_constant<int, 2>{});
         });
     }
 };
@@ -491,7 +519,7 @@ extern "C" {
 
 int64_t fg_gated_ffn_workspace(int64_t tokens, int64_t dim, int64_t hidden) {
     if (tokens <= 0 || dim <= 0 || hidden <= 0) return 0;
-    return ForwardSpace(tokens, dim, hidden, true, true, true, false).bytes;
+    return ForwardSpace(tokens, dim, hidden, true, true, true, true).bytes;
 }
 
 fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_matrix *X, const fg_matrix *W_in, const fg_matrix *W_out, int32_t act,
@@ -515,7 +543,7 @@ fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_mat
     const int64_t ldkeep = GU ? GU->ld : 0;
     const Activation activation = Activation::of(act);
     if (at.few) {
-        const int32_t lo = tokens <= kPartsTokens ? (int32_t)tokens : 0;
+        const int32_t lo = at.parts == 2 ? (int32_t)tokens : 0;
         call.few<true>({X->re, W_in->re, h.re, keep, X->ld, W_in->ld, hp, ldkeep, (int32_t)tokens, lo, (int32_t)hidden, (int32_t)dim, activation});
         call.few<false>({h.re, W_out->re, Y->re, nullptr, hp, W_out->ld, Y->ld, 0, (int32_t)tokens + lo, lo, (int32_t)dim, (int32_t)hidden, activation});
         return call.enqueue.status("gated_few");
@@ -526,8 +554,12 @@ fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_mat
         if (fg_status st = call.by_sums(at, tokens, 2 * hidden, dp, 0, x, turned(w_in), gu)) return st;
         with_half(X->dtype, [&](auto t) {
             using T = decltype(t);
-            call.enqueue(gated_product<T>, dim3(groups_for(tokens, hidden)), dim3(256), (const float *)gu.re, gu.ld, (T *)h.re, hp, tokens, (int)hidden, activation,
-                         own_gu ? keep : nullptr, ldkeep);
+            auto pass = [&](auto kernel) {
+                call.enqueue(kernel, dim3(groups_for(tokens, hidden)), dim3(256), (const float *)gu.re, gu.ld, (T *)h.re, hp, tokens, (int)hidden, activation,
+                             own_gu ? keep : nullptr, ldkeep);
+            };
+            if (at.parts == 2) pass(gated_product<T, true>);
+            else pass(gated_product<T, false>);
         });
     } else {
         fg_matrix w_in = *W_in;
@@ -549,6 +581,12 @@ fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_mat
                 p.pair = pair; p.pair_step = pair_step;
                 p.hidden = (int32_t)hidden; p.act = activation;
             })) return st;
+    }
+    if (at.parts == 2) {
+        const fg_matrix sums = rows_of(call.space + at.sums, FG_F32, up(dim, 4));
+        if (fg_status st = call.by_sums(at, 2 * tokens, dim, hp, 0, h, turned(w_out), sums)) return st;
+        call.round<true>(sums, Y, tokens, dim);
+        return call.enqueue.status("gated_round");
     }
     return call.rounded(at, at.sums, at.down_by_sums, GATED_ROUND_KK, tokens, dim, hp, 0, h, w_out, Y);
 }

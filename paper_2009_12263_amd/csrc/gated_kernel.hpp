@@ -1,6 +1,5 @@
 // The products of the gated feed-forward block (gated.hip): the matrix kernels of gemm_kernel.hpp with what becomes of a tile of results written
-// here (TileCfg::OWN_STORE).  Rows are tokens (or the rows of a weight, GATED_ROUND); a lane holds a row's results in runs of RUN
-// consecutive columns, so that 16-bit results leave in pieces of 16 bytes (32x32x16 instructions: 8).
+// here (TileCfg::OWN_STORE).  Rows are tokens (or the rows of a weight, GATED_ROUND); 16-bit results leave in pieces of 16 bytes.
 //   GATED_UP     X W_in^T.  Blocks of 32 columns are rows of G and of U in turn (TileCfg::PAIRED), so a lane holds g and u of the same columns: h = act(g) u in
 //                16 bits is stored, and g and u in FP32 if they are wanted.
 //   GATED_DOWN   dY W_out = dh.  With g and u from memory: dg, du and h in 16 bits.
@@ -50,23 +49,59 @@ struct GatedCfg : Base {
     static constexpr bool OWN_STORE = true, PAIRED = KIND == GATED_UP;
     using Params = GatedParams;
     using T = typename std::conditional<Base::BF16, bf16_t, f16_t>::type;
-    static constexpr int RUN = Base::ACC_LH, RUNS = 16 / RUN;           // consecutive columns of a lane; such runs in a block, 2 RUN columns apart
-    static_assert(Base::acc_col(RUN) == 2 * RUN && Base::acc_col(RUN - 1) == RUN - 1, "");
     static_assert(!PAIRED || Base::TJ % 2 == 0, "a wave has blocks of G and U");
-    typedef float floats __attribute__((ext_vector_type(RUN)));
+    // A lane takes a wave's results in units of eight consecutive columns.  From 16x16 results (TileCfg::M16) a unit is ROWS = 16 rows of 32 columns: a load or a store
+    // of 16 bytes a lane covers 64 bytes of each of 16 rows (the epilogues of the other products have 32 bytes of 32 rows at a time; with FP32
+    // operands of the result's shape each line was then asked for four times).
+    static constexpr int ROWS = Base::M16 ? 16 : 32, WIDTH = Base::M16 ? 32 : 16, UI = Base::WTM / ROWS, UJ = Base::WTN / WIDTH;
+    typedef float eight __attribute__((ext_vector_type(8)));
     typedef float four __attribute__((ext_vector_type(4)));
     typedef four four_anywhere __attribute__((aligned(4)));
-    using Vec = typename RowPiece<T, RUN>::vec;
-    typedef __attribute__((address_space(1))) typename RowPiece<T, RUN>::unaligned *Global;
+    using Vec = typename RowPiece<T, 8>::vec;
+    typedef __attribute__((address_space(1))) typename RowPiece<T, 8>::unaligned *Global;
     typedef __attribute__((address_space(1))) four_anywhere *GlobalFloats;
     typedef const __attribute__((address_space(1))) four_anywhere *ConstFloats;
+
+    // Unit (i, j): the lane's row is ROWS i + lane % ROWS, its first column WIDTH j + 8 (lane / ROWS).
+    template <int I, int J, class Blocks>
+    __device__ static __forceinline__ eight unit(const Blocks &blocks) {
+        eight out;
+        if constexpr (Base::M16) {
+            // Quarter q of the wave has columns 4 q .. of both 16x16 results a and b; exchanged between halves and then between quarters it has a's or b's 8 (q % 2) ..
+            const floatx4 a = acc_sum<Base, I, 2 * J>(), b = acc_sum<Base, I, 2 * J + 1>();
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float x = a[r], y = b[r];
+                const auto h = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, y), false, false);
+                const unsigned h0 = h[0], h1 = h[1];
+                const auto q = __builtin_amdgcn_permlane16_swap(h0, h1, false, false);
+                const unsigned q0 = q[0], q1 = q[1];
+                out[r] = __builtin_bit_cast(float, q0);
+                out[4 + r] = __builtin_bit_cast(float, q1);
+            }
+        } else {
+            // Half a wave has columns 8 h .. + 3 and the other + 4 .. + 7: exchanged, each has eight of two such runs.
+            const floatx16 a = blocks(ic<I>{}, ic<J / 2>{});
+            static_assert(Base::M16 || (Base::ACC_LH == 4 && Base::acc_col(4) == 8), "");
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float x = a[8 * (J % 2) + r], y = a[8 * (J % 2) + 4 + r];
+                const auto h = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, y), false, false);
+                const unsigned h0 = h[0], h1 = h[1];
+                out[r] = __builtin_bit_cast(float, h0);
+                out[4 + r] = __builtin_bit_cast(float, h1);
+            }
+        }
+        return out;
+    }
 
     template <class Blocks>
     __device__ static __forceinline__ void store(const Params &p, const Blocks &blocks, int m_base, int n_base, int lane) {
         if constexpr (Base::WIDE) own_acc();
-        if constexpr (KIND == GATED_UP) up(p, blocks, m_base + lane % 32, n_base / 2 + RUN * (lane >> 5), n_base / 2 + Base::WTN / 2 > p.hidden);
-        else if constexpr (KIND == GATED_DOWN) down(p, blocks, m_base + lane % 32, n_base + RUN * (lane >> 5), n_base + Base::WTN > p.hidden);
-        else round(p, blocks, m_base + lane % 32, n_base + RUN * (lane >> 5), n_base + Base::WTN > p.N);
+        const int row0 = m_base + lane % ROWS, shift = 8 * (lane / ROWS);
+        if constexpr (KIND == GATED_UP) up(p, blocks, row0, n_base / 2 + shift, n_base / 2 + Base::WTN / 2 > p.hidden);
+        else if constexpr (KIND == GATED_DOWN) down(p, blocks, row0, n_base + shift, n_base + Base::WTN > p.hidden);
+        else round(p, blocks, row0, n_base + shift, n_base + Base::WTN > p.N);
     }
     __device__ static __forceinline__ void step() {
         if constexpr (Base::WIDE) {
@@ -74,65 +109,59 @@ struct GatedCfg : Base {
             own_acc();
         }
     }
-    // the run's columns that are there, `left` of them; whole runs in one piece
-    __device__ static __forceinline__ void put(T *to, floats v, int left) {
+    // the columns that are there, `left` of them
+    __device__ static __forceinline__ void put(T *to, eight v, int left) {
         const Vec r = __builtin_convertvector(v, Vec);
-        if (left >= RUN) *(Global)to = r;
+        if (left >= 8) *(Global)to = r;
         else {
 #pragma unroll
-            for (int e = 0; e < RUN; ++e)
+            for (int e = 0; e < 8; ++e)
                 if (e < left) to[e] = r[e];
         }
     }
-    __device__ static __forceinline__ void put(float *to, floats v, int left) {
-        if (left >= RUN) {
-#pragma unroll
-            for (int q = 0; q < RUN / 4; ++q) *((GlobalFloats)to + q) = four{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+    __device__ static __forceinline__ void put(float *to, eight v, int left) {
+        if (left >= 8) {
+            *(GlobalFloats)to = four{v[0], v[1], v[2], v[3]};
+            *((GlobalFloats)to + 1) = four{v[4], v[5], v[6], v[7]};
         } else {
 #pragma unroll
-            for (int e = 0; e < RUN; ++e)
+            for (int e = 0; e < 8; ++e)
                 if (e < left) to[e] = v[e];
         }
     }
 
-    // first: the lane's first column of h; the blocks of G and U lie side by side
+    // first: the lane's first column of h; the blocks of G and U, 32 columns each, lie side by side
     template <class Blocks>
     __device__ static __forceinline__ void up(const Params &p, const Blocks &blocks, int row0, int first, bool edge) {
         const Activation act = p.act;
-        static_for<Base::TI>([&](auto i) {
-            const int row = row0 + 32 * (int)decltype(i)::value;
+        constexpr int PER = 32 / WIDTH;                                 // units of a block
+        static_for<UI>([&](auto i) {
+            constexpr int I = decltype(i)::value;
+            const int row = row0 + ROWS * I;
             T *h = (T *)p.D + (int64_t)row * p.ldd + first;
             float *g_out = p.keep + (int64_t)row * p.ldgu + first, *u_out = g_out + p.hidden;
-            static_for<Base::TJ / 2>([&](auto jj) {
-                constexpr int J = decltype(jj)::value;
-                const floatx16 g = blocks(i, ic<2 * J>{}), u = blocks(i, ic<2 * J + 1>{});
+            static_for<UJ / 2>([&](auto jj) {
+                constexpr int JJ = decltype(jj)::value, J = JJ / PER * 2 * PER + JJ % PER, c = WIDTH * JJ;
+                const eight g = unit<I, J>(blocks), u = unit<I, J + PER>(blocks);
+                eight v;
 #pragma unroll
-                for (int r = 0; r < RUNS; ++r) {
-                    const int c = 32 * J + 2 * RUN * r;
-                    floats gv, uv, v;
+                for (int e = 0; e < 8; ++e) v[e] = act.template operator()<false>(g[e], nullptr) * u[e];
+                if (row < p.M) {
+                    if (!edge) {
+                        put(h + c, v, 8);
+                        if (p.keep) {
+                            put(g_out + c, g, 8);
+                            put(u_out + c, u, 8);
+                        }
+                    } else {
+                        // zeros behind the last column, to the end of h's row
+                        const int left = p.hidden - first - c;
 #pragma unroll
-                    for (int e = 0; e < RUN; ++e) {
-                        gv[e] = g[RUN * r + e];
-                        uv[e] = u[RUN * r + e];
-                        v[e] = act.template operator()<false>(gv[e], nullptr) * uv[e];
-                    }
-                    if (row < p.M) {
-                        if (!edge) {
-                            put(h + c, v, RUN);
-                            if (p.keep) {
-                                put(g_out + c, gv, RUN);
-                                put(u_out + c, uv, RUN);
-                            }
-                        } else {
-                            // zeros behind the last column, to the end of h's row
-                            const int left = p.hidden - first - c;
-#pragma unroll
-                            for (int e = 0; e < RUN; ++e) v[e] = e < left ? v[e] : 0.f;
-                            if (first + c < p.ldd) put(h + c, v, RUN);
-                            if (p.keep) {
-                                put(g_out + c, gv, left);
-                                put(u_out + c, uv, left);
-                            }
+                        for (int e = 0; e < 8; ++e) v[e] = e < left ? v[e] : 0.f;
+                        if (first + c < p.ldd) put(h + c, v, 8);
+                        if (p.keep) {
+                            put(g_out + c, g, left);
+                            put(u_out + c, u, left);
                         }
                     }
                 }
@@ -141,91 +170,78 @@ struct GatedCfg : Base {
         });
     }
 
-    // What a lane needs from memory for a block: g and u of its columns.  Blocks are requested AHEAD of their turn: a lone wave waits for each otherwise.
-    static constexpr int AHEAD = Base::WIDE && Base::TI * Base::TJ >= 4 ? 3 : 1;
-    struct Pair { floats g[RUNS], u[RUNS]; };
-    __device__ static __forceinline__ void fetch(const Params &p, const float *gu, int first, int j, bool edge, Pair &out) {
+    // What a lane needs from memory for a unit: g and u of its columns.  Units are requested AHEAD of their turn: a lone wave waits for each otherwise.
+    static constexpr int AHEAD = Base::WIDE ? 6 : 2;
+    struct Pair { eight g, u; };
+    __device__ static __forceinline__ eight eight_of(const float *at, int left, bool edge) {
+        eight out;
+        if (!edge || left >= 8) {
+            const four a = *(ConstFloats)at, b = *((ConstFloats)at + 1);
+            out = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
 #pragma unroll
-        for (int r = 0; r < RUNS; ++r) {
-            const int c = 32 * j + 2 * RUN * r, left = p.hidden - first - c;
-            const float *g = gu + c, *u = g + p.hidden;
-            if (!edge || left >= RUN) {
-#pragma unroll
-                for (int q = 0; q < RUN / 4; ++q) {
-                    const four a = *((ConstFloats)g + q), b = *((ConstFloats)u + q);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) { out.g[r][4 * q + e] = a[e]; out.u[r][4 * q + e] = b[e]; }
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < RUN; ++e) { out.g[r][e] = e < left ? g[e] : 0.f; out.u[r][e] = e < left ? u[e] : 0.f; }
-            }
+            for (int e = 0; e < 8; ++e) out[e] = e < left ? at[e] : 0.f;
         }
+        return out;
     }
     template <class Blocks>
     __device__ static __forceinline__ void down(const Params &p, const Blocks &blocks, int row0, int first, bool edge) {
         const Activation act = p.act;
-        constexpr int COUNT = Base::TI * Base::TJ;
+        constexpr int COUNT = UI * UJ;
         Pair ahead[AHEAD];
-        auto gu_of = [&](int i) { const int row = row0 + 32 * i; return p.gu + (int64_t)(row < p.M ? row : p.M - 1) * p.ldgu + first; };
-        static_for<(AHEAD < COUNT ? AHEAD : COUNT)>([&](auto b) { fetch(p, gu_of(decltype(b)::value / Base::TJ), first, decltype(b)::value % Base::TJ, edge, ahead[decltype(b)::value]); });
+        auto fetch = [&](auto b) {
+            constexpr int B = decltype(b)::value;
+            const int row = row0 + ROWS * (B / UJ), c = WIDTH * (B % UJ);
+            const float *g = p.gu + (int64_t)(row < p.M ? row : p.M - 1) * p.ldgu + first + c;
+            ahead[B % AHEAD] = {eight_of(g, p.hidden - first - c, edge), eight_of(g + p.hidden, p.hidden - first - c, edge)};
+        };
+        static_for<(AHEAD < COUNT ? AHEAD : COUNT)>(fetch);
         static_for<COUNT>([&](auto b) {
-            constexpr int B = decltype(b)::value, I = B / Base::TJ, J = B % Base::TJ;
-            const int row = row0 + 32 * I;
-            const floatx16 dh = blocks(ic<I>{}, ic<J>{});
+            constexpr int B = decltype(b)::value, I = B / UJ, J = B % UJ, c = WIDTH * J;
+            const int row = row0 + ROWS * I;
+            const eight dh = unit<I, J>(blocks);
             const Pair in = ahead[B % AHEAD];
             T *dg = (T *)p.D + (int64_t)row * p.ldd + first, *du = dg + p.hidden, *h = (T *)p.h + (int64_t)row * p.ldh + first;
+            eight vg, vu, vh;
 #pragma unroll
-            for (int r = 0; r < RUNS; ++r) {
-                const int c = 32 * J + 2 * RUN * r;
-                floats vg, vu, vh;
+            for (int e = 0; e < 8; ++e) {
+                float d;
+                const float a = act.template operator()<true>(in.g[e], &d);
+                vg[e] = dh[e] * in.u[e] * d;
+                vu[e] = dh[e] * a;
+                vh[e] = a * in.u[e];
+            }
+            if (row < p.M) {
+                if (!edge) {
+                    put(dg + c, vg, 8);
+                    put(du + c, vu, 8);
+                    put(h + c, vh, 8);
+                } else {
+                    const int left = p.hidden - first - c;
 #pragma unroll
-                for (int e = 0; e < RUN; ++e) {
-                    const float x = dh[RUN * r + e];
-                    float d;
-                    const float a = act.template operator()<true>(in.g[r][e], &d);
-                    vg[e] = x * in.u[r][e] * d;
-                    vu[e] = x * a;
-                    vh[e] = a * in.u[r][e];
-                }
-                if (row < p.M) {
-                    if (!edge) {
-                        put(dg + c, vg, RUN);
-                        put(du + c, vu, RUN);
-                        put(h + c, vh, RUN);
-                    } else {
-                        const int left = p.hidden - first - c;
-#pragma unroll
-                        for (int e = 0; e < RUN; ++e) vh[e] = e < left ? vh[e] : 0.f;
-                        put(dg + c, vg, left);
-                        put(du + c, vu, left);
-                        if (first + c < p.ldh) put(h + c, vh, RUN);
-                        // the run with the last column: zeros behind du, to the end of its row
-                        if (left > 0 && left <= RUN)
-                            for (int z = 2 * p.hidden; z < (int)p.ldd; ++z) ((T *)p.D)[(int64_t)row * p.ldd + z] = (T)0.f;
-                    }
+                    for (int e = 0; e < 8; ++e) vh[e] = e < left ? vh[e] : 0.f;
+                    put(dg + c, vg, left);
+                    put(du + c, vu, left);
+                    if (first + c < p.ldh) put(h + c, vh, 8);
+                    // with the last column: zeros behind du, to the end of its row
+                    if (left > 0 && left <= 8)
+                        for (int z = 2 * p.hidden; z < (int)p.ldd; ++z) ((T *)p.D)[(int64_t)row * p.ldd + z] = (T)0.f;
                 }
             }
-            if constexpr (B + AHEAD < COUNT) fetch(p, gu_of((B + AHEAD) / Base::TJ), first, (B + AHEAD) % Base::TJ, edge, ahead[B % AHEAD]);
+            if constexpr (B + AHEAD < COUNT) fetch(ic<B + AHEAD>{});
             step();
         });
     }
 
     template <class Blocks>
     __device__ static __forceinline__ void round(const Params &p, const Blocks &blocks, int row0, int first, bool edge) {
-        static_for<Base::TI>([&](auto i) {
-            const int row = row0 + 32 * (int)decltype(i)::value;
+        static_for<UI>([&](auto i) {
+            const int row = row0 + ROWS * (int)decltype(i)::value;
             T *out = (T *)p.D + (int64_t)row * p.ldd + first;
-            static_for<Base::TJ>([&](auto j) {
-                const floatx16 a = blocks(i, j);
-#pragma unroll
-                for (int r = 0; r < RUNS; ++r) {
-                    const int c = 32 * (int)decltype(j)::value + 2 * RUN * r;
-                    floats v;
-#pragma unroll
-                    for (int e = 0; e < RUN; ++e) v[e] = a[RUN * r + e];
-                    if (row < p.M) put(out + c, v, edge ? p.N - first - c : RUN);
-                }
+            static_for<UJ>([&](auto j) {
+                constexpr int c = WIDTH * (int)decltype(j)::value;
+                const eight v = unit<decltype(i)::value, decltype(j)::value>(blocks);
+                if (row < p.M) put(out + c, v, edge ? p.N - first - c : 8);
             });
             step();
         });
