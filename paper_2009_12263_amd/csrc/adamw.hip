@@ -27,7 +27,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kStateBlock = 256;            // values that share a scale
 constexpr int kLaneBlock = 16;              // of them in a lane: 16 lanes, a row of the wave, share one
-constexpr int kChunk = 8192;                // values of a workgroup
+// Values of a workgroup.  Small models: those that its threads take at once; four turns one after the other, each waiting for memory, took 10 us a launch of 48 short
+// tensors, one 4.  Large ones: more, for the sake of what a workgroup does once.
+constexpr int kChunk = 8192, kSmallChunk = 2048;
+constexpr int64_t kSmallModel = 4096 * kSmallChunk;
 constexpr float kTop = 448.f, kLeast = 0x1p-9f;         // of e4m3: the largest number, the smallest one above zero
 constexpr float kNothing = 1e-30f;          // a block whose largest value is smaller is zero (its scale's reciprocal would overflow)
 
@@ -50,6 +53,7 @@ struct StepArgs {
     double lr, beta1, beta2, eps, decay;
     const int64_t *step;
     const float *factor, *lr_factor;
+    int32_t chunk;
 };
 // What a step needs of them, in FP32.
 struct Rates {
@@ -190,9 +194,9 @@ __device__ __forceinline__ float relative(float (&x)[kLaneBlock]) {
 // ---- the step -----------------------------------------------------------------------------------------
 // P: parameters, G: gradients, COPY: with an FP32 copy, which is what the step reads.
 template <class P, class G, bool COPY, bool SMALL>
-__device__ __forceinline__ void step_chunk(const TensorArg &t, const Rates &r, int64_t begin) {
+__device__ __forceinline__ void step_chunk(const TensorArg &t, const Rates &r, int64_t begin, int chunk) {
     constexpr int N = SMALL ? kLaneBlock : 8;
-    const int64_t end = begin + kChunk < t.n ? begin + kChunk : t.n;
+    const int64_t end = begin + chunk < t.n ? begin + chunk : t.n;
     // (the lanes of a row are in the same block, and go round together)
     for (int64_t at = begin + threadIdx.x * N; SMALL ? at / kStateBlock * kStateBlock < end : at < end; at += kThreads * N) {
         float p[N], g[N], m[N], v[N], root[N];
@@ -237,17 +241,17 @@ __global__ __launch_bounds__(kThreads) void adamw(const List<TensorArg, CAP> a, 
     Rates r;
     if (!rates_of(s, r)) return;
     const TensorArg t = a.at[which];
-    const int64_t begin = ((int64_t)blockIdx.x - a.first[which]) * kChunk;
+    const int64_t begin = ((int64_t)blockIdx.x - a.first[which]) * s.chunk;
     switch (a.kind[which]) {
-        case FG_F16: return step_chunk<f16_t, f16_t, false, SMALL>(t, r, begin);
-        case FG_BF16: return step_chunk<bf16_t, bf16_t, false, SMALL>(t, r, begin);
-        case FG_F32 + kWideGrad: return step_chunk<float, float, false, SMALL>(t, r, begin);
-        case FG_F16 + kWideGrad: return step_chunk<f16_t, float, false, SMALL>(t, r, begin);
-        case FG_BF16 + kWideGrad: return step_chunk<bf16_t, float, false, SMALL>(t, r, begin);
-        case FG_F16 + kCopy: return step_chunk<f16_t, f16_t, true, SMALL>(t, r, begin);
-        case FG_BF16 + kCopy: return step_chunk<bf16_t, bf16_t, true, SMALL>(t, r, begin);
-        case FG_F16 + kCopy + kWideGrad: return step_chunk<f16_t, float, true, SMALL>(t, r, begin);
-        case FG_BF16 + kCopy + kWideGrad: return step_chunk<bf16_t, float, true, SMALL>(t, r, begin);
+        case FG_F16: return step_chunk<f16_t, f16_t, false, SMALL>(t, r, begin, s.chunk);
+        case FG_BF16: return step_chunk<bf16_t, bf16_t, false, SMALL>(t, r, begin, s.chunk);
+        case FG_F32 + kWideGrad: return step_chunk<float, float, false, SMALL>(t, r, begin, s.chunk);
+        case FG_F16 + kWideGrad: return step_chunk<f16_t, float, false, SMALL>(t, r, begin, s.chunk);
+        case FG_BF16 + kWideGrad: return step_chunk<bf16_t, float, false, SMALL>(t, r, begin, s.chunk);
+        case FG_F16 + kCopy: return step_chunk<f16_t, f16_t, true, SMALL>(t, r, begin, s.chunk);
+        case FG_BF16 + kCopy: return step_chunk<bf16_t, bf16_t, true, SMALL>(t, r, begin, s.chunk);
+        case FG_F16 + kCopy + kWideGrad: return step_chunk<f16_t, float, true, SMALL>(t, r, begin, s.chunk);
+        case FG_BF16 + kCopy + kWideGrad: return step_chunk<bf16_t, float, true, SMALL>(t, r, begin, s.chunk);
     }
 }
 
@@ -315,7 +319,7 @@ __global__ __launch_bounds__(1024) void grad_norm(const double *partial, int64_t
 constexpr int kFewTensors = 6, kMostTensors = 48, kFewGrads = 16, kMostGrads = 64;
 constexpr int64_t kMostChunks = 1 << 23;    // of a launch: fewer than 2^32 threads
 
-int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
+int64_t chunks_of(int64_t n, int chunk) { return (n + chunk - 1) / chunk; }
 
 fg_status check_tensor_count(int64_t count, const void *tensors) {
     if (count < 0) return fail(FG_ERR_SHAPE, "negative number of tensors: %lld", (long long)count);
@@ -375,10 +379,10 @@ fg_status check_apart(int64_t count, const fg_adamw_tensor *tensors) {
 }
 
 // Hands out tensors to launches: f(first tensor, tensors, chunks) with as many as `most` and kMostChunks allow; tensors without values count as well.
-template <class Length, class F> void in_launches(int64_t count, int most, Length &&length, F &&f) {
+template <class Length, class F> void in_launches(int64_t count, int most, int chunk, Length &&length, F &&f) {
     int64_t begin = 0, chunks = 0;
     for (int64_t i = 0; i < count; ++i) {
-        const int64_t c = chunks_of(length(i));
+        const int64_t c = chunks_of(length(i), chunk);
         if (i > begin && (i - begin == most || chunks + c > kMostChunks)) {
             f(begin, (int)(i - begin), chunks);
             begin = i;
@@ -389,13 +393,13 @@ template <class Length, class F> void in_launches(int64_t count, int most, Lengt
     if (count > begin) f(begin, (int)(count - begin), chunks);
 }
 // The list of a launch's n tensors: fill(i, its arguments) gives each one's kind, length(i) its values.
-template <class Arg, int CAP, class Length, class Fill> void make_list(List<Arg, CAP> &list, int n, Length &&length, Fill &&fill) {
+template <class Arg, int CAP, class Length, class Fill> void make_list(List<Arg, CAP> &list, int n, int chunk, Length &&length, Fill &&fill) {
     int64_t first = 0;
     for (int i = 0; i < CAP; ++i) {
         list.first[i] = (int32_t)first;
         if (i >= n) continue;
         list.kind[i] = fill(i, list.at[i]);
-        first += chunks_of(length(i));
+        first += chunks_of(length(i), chunk);
     }
 }
 
@@ -422,27 +426,30 @@ fg_status fg_adamw(int64_t count, const fg_adamw_tensor *tensors, const int64_t 
     if (!aligned_to(step, 8) || !aligned_to(grad_factor, 4) || !aligned_to(lr_factor, 4))
         return fail(FG_ERR_ALIGN, "step, grad_factor and lr_factor must be aligned to an element");
     bool some[2] = {};
+    int64_t values = 0;
     for (int64_t i = 0; i < count; ++i) {
         if (fg_status st = check_adamw_tensor(i, tensors[i])) return st;
+        values = std::min(values + tensors[i].n, kSmallModel);
         if (tensors[i].n > 0) some[tensors[i].avg_scale != nullptr] = true;
     }
     if (some[0] && some[1]) return fail(FG_ERR_UNSUPPORTED, "moments in FP32 and in eight bits need calls of their own");
     if (!some[0] && !some[1]) return FG_OK;
     if (fg_status st = check_apart(count, tensors)) return st;
+    const int chunk = values < kSmallModel ? kSmallChunk : kChunk;
     Launches enqueue(hip_stream);
     auto launch = [&](auto cap, int64_t begin, int n, int64_t chunks) {
         constexpr int CAP = decltype(cap)::value;
         List<TensorArg, CAP> a = {};
-        make_list(a, n, [&](int i) { return tensors[begin + i].n; }, [&](int i, TensorArg &arg) {
+        make_list(a, n, chunk, [&](int i) { return tensors[begin + i].n; }, [&](int i, TensorArg &arg) {
             const fg_adamw_tensor &t = tensors[begin + i];
             arg = {t.param, t.grad, t.master, t.exp_avg, t.exp_avg_sq, t.avg_scale, t.sq_scale, t.n};
             return t.param_dtype + (t.grad_dtype == FG_F32 ? kWideGrad : 0) + (t.master ? kCopy : 0);
         });
-        const StepArgs s = {lr, beta1, beta2, eps, weight_decay, step, grad_factor, lr_factor};
+        const StepArgs s = {lr, beta1, beta2, eps, weight_decay, step, grad_factor, lr_factor, chunk};
         if (some[1]) enqueue(adamw<CAP, true>, dim3((unsigned)chunks), dim3(kThreads), a, s);
         else enqueue(adamw<CAP, false>, dim3((unsigned)chunks), dim3(kThreads), a, s);
     };
-    in_launches(count, kMostTensors, [&](int64_t i) { return tensors[i].n; }, [&](int64_t begin, int n, int64_t chunks) {
+    in_launches(count, kMostTensors, chunk, [&](int64_t i) { return tensors[i].n; }, [&](int64_t begin, int n, int64_t chunks) {
         if (chunks == 0) return;
         if (n <= kFewTensors) launch(std::integral_constant<int, kFewTensors>{}, begin, n, chunks);
         else launch(std::integral_constant<int, kMostTensors>{}, begin, n, chunks);
@@ -465,7 +472,7 @@ fg_status fg_grad_norm(int64_t count, const fg_values *grads, float scale, float
         if (fg_status st = check_values("grad", i, grads[i].values, grads[i].dtype, grads[i].n)) return st;
     }
     int64_t parts = 0;
-    auto launches = [&](auto &&f) { in_launches(count, kMostGrads, [&](int64_t i) { return grads[i].n; }, f); };
+    auto launches = [&](auto &&f) { in_launches(count, kMostGrads, kChunk, [&](int64_t i) { return grads[i].n; }, f); };
     launches([&](int64_t, int, int64_t chunks) { parts += std::min<int64_t>(chunks, kNormGroups); });
     if (fg_status st = check_workspace(workspace, workspace_bytes, parts * 8)) return st;
     Launches enqueue(hip_stream);
@@ -476,7 +483,7 @@ fg_status fg_grad_norm(int64_t count, const fg_values *grads, float scale, float
         auto launch = [&](auto cap) {
             constexpr int CAP = decltype(cap)::value;
             List<GradArg, CAP> a = {};
-            make_list(a, n, [&](int i) { return grads[begin + i].n; }, [&](int i, GradArg &arg) {
+            make_list(a, n, kChunk, [&](int i) { return grads[begin + i].n; }, [&](int i, GradArg &arg) {
                 arg = {grads[begin + i].values, grads[begin + i].n};
                 return grads[begin + i].dtype;
             });

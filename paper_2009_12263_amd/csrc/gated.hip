@@ -23,21 +23,52 @@
 namespace fg {
 namespace {
 
-// Copies rows of `cols` values to rows of ldo (a multiple of 8), with zeros behind them.
+// Copies of a call's operands for the tiled kernels, all in one launch: rows of `cols` values become rows of ldo (a multiple of 8), with zeros behind them.
+// pair > 0 (W_in for GATED_UP): 32 rows of G, the 32 of U that lie `pair` rows on, and so on, zeros behind the last row of either.
+struct PadArg {
+    const void *in;
+    void *out;
+    int64_t ld, ldo, rows, pair;
+    int32_t cols;
+    int32_t first;                          // number of its first workgroup
+};
+constexpr int kMostPads = 6, kPadPieces = 1024;             // pieces of eight values of a workgroup
+struct PadArgs {
+    PadArg at[kMostPads];
+    int32_t count;
+};
 template <class T>
-__global__ __launch_bounds__(256) void gated_pad(const T *in, int64_t ld, T *out, int64_t ldo, int64_t rows, int cols) {
-    const int pieces = (int)(ldo / 8);
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += (int64_t)gridDim.x * 256) {
+__global__ __launch_bounds__(256) void gated_pad(const PadArgs a) {
+    int which = 0;
+#pragma unroll
+    for (int i = 1; i < kMostPads; ++i) which = i < a.count && a.at[i].first <= (int)blockIdx.x ? i : which;
+    const PadArg p = a.at[which];
+    const int pieces = (int)(p.ldo / 8);
+    const int64_t begin = (int64_t)((int)blockIdx.x - p.first) * kPadPieces, all = p.rows * pieces;
+    typename RowPiece<T>::vec v[kPadPieces / 256] = {};
+    T *to[kPadPieces / 256] = {};
+#pragma unroll
+    for (int t = 0; t < kPadPieces / 256; ++t) {
+        const int64_t i = begin + t * 256 + threadIdx.x;
+        if (i >= all) continue;
         const int64_t row = i / pieces;
-        const int p = (int)(i - row * pieces);
-        const T *from = in + row * ld;
-        typename RowPiece<T>::vec v;
-        if ((p + 1) * 8 <= cols) v = load_raw<T, 8>(from, p, cols);
+        const int c = (int)(i - row * pieces) * 8;
+        to[t] = (T *)p.out + row * p.ldo + c;
+        int64_t from = row;
+        if (p.pair) {
+            from = row / 64 * 32 + row % 32;
+            if (from >= p.pair) continue;
+            from += row / 32 % 2 ? p.pair : 0;
+        }
+        const T *in = (const T *)p.in + from * p.ld;
+        if (c + 8 <= p.cols) v[t] = load_raw<T, 8>(in, c / 8, p.cols);
         else
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = p * 8 + e < cols ? from[p * 8 + e] : (T)0.f;
-        *(typename RowPiece<T>::vec *)(out + row * ldo + p * 8) = v;
+            for (int e = 0; e < 8; ++e) v[t][e] = c + e < p.cols ? in[c + e] : (T)0.f;
     }
+#pragma unroll
+    for (int t = 0; t < kPadPieces / 256; ++t)
+        if (to[t]) *(typename RowPiece<T>::vec *)to[t] = v[t];
 }
 
 // Piece p of eight values of FP32 rows; zeros from `cols` on.
@@ -148,23 +179,6 @@ __global__ __launch_bounds__(256) void gated_round(const float *in, int64_t ldi,
         store_eight<T>(out + row * ldo, c, cols, v, nullptr);
     });
 }
-// Copies W_in for GATED_UP: 32 rows of G, 32 of U, and so on, rows of ldo values with zeros behind them and behind the last row.
-template <class T>
-__global__ __launch_bounds__(256) void gated_interleave(const T *in, int64_t ld, T *out, int64_t ldo, int hidden, int cols) {
-    each_piece((int64_t)(hidden + 31) / 32 * 64, (int)ldo, [&](int64_t row, int c) {
-        const int at = (int)(row / 64) * 32 + (int)(row % 32);
-        const T *from = in + (at + ((row / 32) % 2 ? hidden : 0)) * ld;
-        typename RowPiece<T>::vec v = {};
-        if (at < hidden) {
-            if (c + 8 <= cols) v = load_raw<T, 8>(from, c / 8, cols);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? from[c + e] : (T)0.f;
-        }
-        *(typename RowPiece<T>::vec *)(out + row * ldo + c) = v;
-    });
-}
-
 // ---- few tokens -------------------------------------------------------------------------------------------------
 // Sums over k of w[n][k] x[r][k] for up to 16 NB rows r of x: reading w.  A workgroup takes 16 rows of w (UP: and as many of U), its waves 64 k each in
 // turn: a lane reads its row's 16 bytes straight into the operand of a 16x16x32 matrix instruction, a wave two whole lines of each row.  The waves' sums are added
@@ -424,16 +438,25 @@ struct Call {
     Launches enqueue;
     char *space;
     int dtype;
-    // m, or a copy at `at` whose rows are aligned and padded (`times`: so many, one behind the other)
+    PadArgs pads = {};
+    // m, or a copy at `at` whose rows are aligned and padded (`times`: so many, one behind the other), made by copies()
     fg_matrix aligned(const fg_matrix *m, int64_t rows, int64_t cols, bool copy, int64_t at, int64_t times = 1) {
         if (!copy && times == 1) return *m;
         const int64_t ld = fg::up(cols, 8);
-        with_half(dtype, [&](auto t) {
-            using T = decltype(t);
-            for (int64_t k = 0; k < times; ++k)
-                enqueue(gated_pad<T>, dim3(groups_for(rows, ld)), dim3(256), (const T *)m->re, m->ld, (T *)(space + at) + k * rows * ld, ld, rows, (int)cols);
-        });
+        for (int64_t k = 0; k < times; ++k) add({m->re, space + at + k * rows * ld * 2, m->ld, ld, rows, 0, (int32_t)cols, 0});
         return rows_of(space + at, dtype, ld);
+    }
+    int64_t pad_groups = 0;
+    void add(PadArg p) {
+        p.first = (int32_t)pad_groups;
+        pads.at[pads.count++] = p;
+        pad_groups += (p.rows * (p.ldo / 8) + kPadPieces - 1) / kPadPieces;
+    }
+    void copies() {
+        if (pads.count == 0) return;
+        with_half(dtype, [&](auto t) { enqueue(gated_pad<decltype(t)>, dim3((unsigned)pad_groups), dim3(256), pads); });
+        pads.count = 0;
+        pad_groups = 0;
     }
     fg_status by_sums(const Space &s, int64_t M, int64_t N, int64_t K, int64_t k_rows, const fg_matrix &a, const fg_matrix &b, const fg_matrix &d) {
         if (fg_status st = enqueue.status("gated_pad")) return st;
@@ -551,6 +574,7 @@ fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_mat
     const fg_matrix x = call.aligned(X, tokens, dim, copy_x, at.x), w_out = call.aligned(W_out, dim, hidden, copy_out, at.w_out);
     if (at.up_by_sums) {
         const fg_matrix w_in = call.aligned(W_in, 2 * hidden, dim, copy_in, at.w_in), gu = !own_gu ? *GU : rows_of(call.space + at.gu, FG_F32, up(2 * hidden, 4));
+        call.copies();
         if (fg_status st = call.by_sums(at, tokens, 2 * hidden, dp, 0, x, turned(w_in), gu)) return st;
         with_half(X->dtype, [&](auto t) {
             using T = decltype(t);
@@ -568,11 +592,9 @@ fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_mat
             w_in = rows_of(call.space + at.w_in, X->dtype, dp);
             pair = 32;
             pair_step = 64;
-            with_half(X->dtype, [&](auto t) {
-                using T = decltype(t);
-                call.enqueue(gated_interleave<T>, dim3(groups_for(2 * up(hidden, 32), dp)), dim3(256), (const T *)W_in->re, W_in->ld, (T *)w_in.re, dp, (int)hidden, (int)dim);
-            });
+            call.add({W_in->re, w_in.re, W_in->ld, dp, 2 * up(hidden, 32), hidden, (int32_t)dim, 0});
         }
+        call.copies();
         const int64_t columns = 2 * up(hidden, 32);
         if (fg_status st = call.product(GATED_UP, tokens, columns, dp, 0, x, w_in, [&](GatedParams &p) {
                 p.b_span = up(((copy_in ? columns : 2 * hidden) - 1) * w_in.ld + dp, 8);
@@ -619,7 +641,9 @@ fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const f
     const GradSpace at(tokens, dim, hidden, copy_dy, copy_x, copy_in, copy_out);
     if (fg_status st = check_workspace(workspace, workspace_bytes, at.bytes)) return st;
     const int64_t dp = up(dim, 8), hp = up(hidden, 8), gp = up(2 * hidden, 8), rows = at.parts * tokens, tp = up(rows, 8);
-    const fg_matrix dy = call.aligned(dY, tokens, dim, copy_dy, at.dy, at.parts), w_out = call.aligned(W_out, dim, hidden, copy_out, at.w_out);
+    const fg_matrix dy = call.aligned(dY, tokens, dim, copy_dy, at.dy, at.parts), w_out = call.aligned(W_out, dim, hidden, copy_out, at.w_out),
+                    w_in = dX ? call.aligned(W_in, 2 * hidden, dim, copy_in, at.w_in) : *W_in, x = dW_in ? call.aligned(X, tokens, dim, copy_x, at.x, at.parts) : *X;
+    call.copies();
     const fg_matrix h = rows_of(call.space + at.h, X->dtype, hp), dgu = rows_of(call.space + at.dgu, X->dtype, gp);
     const Activation activation = Activation::of(act);
     if (at.down_by_sums) {
@@ -642,17 +666,14 @@ fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const f
                    p.hidden = (int32_t)hidden; p.act = activation;
                })) return st;
     if (dX) {
-        const fg_matrix w_in = call.aligned(W_in, 2 * hidden, dim, copy_in, at.w_in);
         if (at.parts == 2) {
             const fg_matrix sums = rows_of(call.space + at.sums, FG_F32, up(dim, 4));
             if (fg_status st = call.by_sums(at, rows, dim, gp, 2 * hidden, dgu, w_in, sums)) return st;
             call.round<true>(sums, dX, tokens, dim);
         } else if (fg_status st = call.rounded(at, at.sums, at.x_by_sums, GATED_ROUND_KN, tokens, dim, gp, 2 * hidden, dgu, w_in, dX)) return st;
     }
-    if (dW_in) {
-        const fg_matrix x = call.aligned(X, tokens, dim, copy_x, at.x, at.parts);
+    if (dW_in)
         if (fg_status st = call.rounded(at, at.sums, at.in_by_sums, GATED_ROUND_NN, 2 * hidden, dim, at.in_by_sums ? tp : rows, rows, dgu, x, dW_in)) return st;
-    }
     if (dW_out)
         if (fg_status st = call.rounded(at, at.sums, at.out_by_sums, GATED_ROUND_NN, dim, hidden, at.out_by_sums ? tp : rows, rows, dy, h, dW_out)) return st;
     return call.enqueue.status("gated_ffn_grad");
