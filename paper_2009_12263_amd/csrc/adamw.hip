@@ -34,15 +34,15 @@ constexpr int64_t kSmallModel = 4096 * kSmallChunk;
 constexpr float kTop = 448.f, kLeast = 0x1p-9f;         // of e4m3: the largest number, the smallest one above zero
 constexpr float kNothing = 1e-30f;          // a block whose largest value is smaller is zero (its scale's reciprocal would overflow)
 
-struct TensorArg {
+template <bool SMALL> struct TensorArg {
     void *p;
     const void *g;
     float *master;
     void *m, *v;
-    float *m_scale, *v_scale;
     int64_t n;
 };
-// Arguments are copied through the command path: few tensors have a short list of them.  A list has at most as many as a wave has lanes.
+template <> struct TensorArg<true> : TensorArg<false> { float *m_scale, *v_scale; };
+// Arguments are copied through the command path: few tensors have a short list of them.  A list has at most as many as a wave has lanes, and as fit 4 KB.
 template <class Arg, int CAP> struct List {
     int32_t first[CAP];                     // number of a tensor's first chunk in the launch; behind the last tensor the number of all
     int32_t kind[CAP];
@@ -194,9 +194,11 @@ __device__ __forceinline__ float relative(float (&x)[kLaneBlock]) {
 // ---- the step -----------------------------------------------------------------------------------------
 // P: parameters, G: gradients, COPY: with an FP32 copy, which is what the step reads.
 template <class P, class G, bool COPY, bool SMALL>
-__device__ __forceinline__ void step_chunk(const TensorArg &t, const Rates &r, int64_t begin, int chunk) {
+__device__ __forceinline__ void step_chunk(const TensorArg<SMALL> &t, const StepArgs &s, int64_t begin, int chunk) {
     constexpr int N = SMALL ? kLaneBlock : 8;
     const int64_t end = begin + chunk < t.n ? begin + chunk : t.n;
+    Rates r;
+    bool known = false;
     // (the lanes of a row are in the same block, and go round together)
     for (int64_t at = begin + threadIdx.x * N; SMALL ? at / kStateBlock * kStateBlock < end : at < end; at += kThreads * N) {
         float p[N], g[N], m[N], v[N], root[N];
@@ -213,6 +215,9 @@ __device__ __forceinline__ void step_chunk(const TensorArg &t, const Rates &r, i
             load_values<float, N>((const float *)t.m, at, t.n, m);
             load_values<float, N>((const float *)t.v, at, t.n, v);
         }
+        // (the rates wait for memory too, and take their time: behind the first values' requests)
+        if (!known && !rates_of(s, r)) return;
+        known = true;
 #pragma unroll
         for (int e = 0; e < N; ++e) p[e] = stepped(r, p[e], g[e], m[e], v[e], root[e]);
         if constexpr (COPY) store_values<float, N>(t.master, at, t.n, p);
@@ -236,22 +241,20 @@ __device__ __forceinline__ void step_chunk(const TensorArg &t, const Rates &r, i
 constexpr int kWideGrad = 4, kCopy = 8;
 
 template <int CAP, bool SMALL>
-__global__ __launch_bounds__(kThreads) void adamw(const List<TensorArg, CAP> a, const StepArgs s) {
+__global__ __launch_bounds__(kThreads) void adamw(const List<TensorArg<SMALL>, CAP> a, const StepArgs s) {
     const int which = tensor_of(a, (int)blockIdx.x);
-    Rates r;
-    if (!rates_of(s, r)) return;
-    const TensorArg t = a.at[which];
+    const TensorArg<SMALL> t = a.at[which];
     const int64_t begin = ((int64_t)blockIdx.x - a.first[which]) * s.chunk;
     switch (a.kind[which]) {
-        case FG_F16: return step_chunk<f16_t, f16_t, false, SMALL>(t, r, begin, s.chunk);
-        case FG_BF16: return step_chunk<bf16_t, bf16_t, false, SMALL>(t, r, begin, s.chunk);
-        case FG_F32 + kWideGrad: return step_chunk<float, float, false, SMALL>(t, r, begin, s.chunk);
-        case FG_F16 + kWideGrad: return step_chunk<f16_t, float, false, SMALL>(t, r, begin, s.chunk);
-        case FG_BF16 + kWideGrad: return step_chunk<bf16_t, float, false, SMALL>(t, r, begin, s.chunk);
-        case FG_F16 + kCopy: return step_chunk<f16_t, f16_t, true, SMALL>(t, r, begin, s.chunk);
-        case FG_BF16 + kCopy: return step_chunk<bf16_t, bf16_t, true, SMALL>(t, r, begin, s.chunk);
-        case FG_F16 + kCopy + kWideGrad: return step_chunk<f16_t, float, true, SMALL>(t, r, begin, s.chunk);
-        case FG_BF16 + kCopy + kWideGrad: return step_chunk<bf16_t, float, true, SMALL>(t, r, begin, s.chunk);
+        case FG_F16: return step_chunk<f16_t, f16_t, false, SMALL>(t, s, begin, s.chunk);
+        case FG_BF16: return step_chunk<bf16_t, bf16_t, false, SMALL>(t, s, begin, s.chunk);
+        case FG_F32 + kWideGrad: return step_chunk<float, float, false, SMALL>(t, s, begin, s.chunk);
+        case FG_F16 + kWideGrad: return step_chunk<f16_t, float, false, SMALL>(t, s, begin, s.chunk);
+        case FG_BF16 + kWideGrad: return step_chunk<bf16_t, float, false, SMALL>(t, s, begin, s.chunk);
+        case FG_F16 + kCopy: return step_chunk<f16_t, f16_t, true, SMALL>(t, s, begin, s.chunk);
+        case FG_BF16 + kCopy: return step_chunk<bf16_t, bf16_t, true, SMALL>(t, s, begin, s.chunk);
+        case FG_F16 + kCopy + kWideGrad: return step_chunk<f16_t, float, true, SMALL>(t, s, begin, s.chunk);
+        case FG_BF16 + kCopy + kWideGrad: return step_chunk<bf16_t, float, true, SMALL>(t, s, begin, s.chunk);
     }
 }
 
@@ -316,7 +319,8 @@ __global__ __launch_bounds__(1024) void grad_norm(const double *partial, int64_t
 }
 
 // ---- host ------------------------------------------------------------------------------------------------
-constexpr int kFewTensors = 6, kMostTensors = 48, kFewGrads = 16, kMostGrads = 64;
+constexpr int kFewTensors = 6, kFewGrads = 16, kMostGrads = 64;
+template <bool SMALL> constexpr int kMostTensors = SMALL ? 48 : 64;
 constexpr int64_t kMostChunks = 1 << 23;    // of a launch: fewer than 2^32 threads
 
 int64_t chunks_of(int64_t n, int chunk) { return (n + chunk - 1) / chunk; }
@@ -437,23 +441,29 @@ fg_status fg_adamw(int64_t count, const fg_adamw_tensor *tensors, const int64_t 
     if (fg_status st = check_apart(count, tensors)) return st;
     const int chunk = values < kSmallModel ? kSmallChunk : kChunk;
     Launches enqueue(hip_stream);
-    auto launch = [&](auto cap, int64_t begin, int n, int64_t chunks) {
-        constexpr int CAP = decltype(cap)::value;
-        List<TensorArg, CAP> a = {};
-        make_list(a, n, chunk, [&](int i) { return tensors[begin + i].n; }, [&](int i, TensorArg &arg) {
-            const fg_adamw_tensor &t = tensors[begin + i];
-            arg = {t.param, t.grad, t.master, t.exp_avg, t.exp_avg_sq, t.avg_scale, t.sq_scale, t.n};
-            return t.param_dtype + (t.grad_dtype == FG_F32 ? kWideGrad : 0) + (t.master ? kCopy : 0);
+    auto all = [&](auto small) {
+        constexpr bool SMALL = decltype(small)::value;
+        auto launch = [&](auto cap, int64_t begin, int n, int64_t chunks) {
+            constexpr int CAP = decltype(cap)::value;
+            List<TensorArg<SMALL>, CAP> a = {};
+            static_assert(sizeof a + sizeof(StepArgs) <= 4096, "");
+            make_list(a, n, chunk, [&](int i) { return tensors[begin + i].n; }, [&](int i, TensorArg<SMALL> &arg) {
+                const fg_adamw_tensor &t = tensors[begin + i];
+                arg.p = t.param; arg.g = t.grad; arg.master = t.master; arg.m = t.exp_avg; arg.v = t.exp_avg_sq; arg.n = t.n;
+                if constexpr (SMALL) { arg.m_scale = t.avg_scale; arg.v_scale = t.sq_scale; }
+                return t.param_dtype + (t.grad_dtype == FG_F32 ? kWideGrad : 0) + (t.master ? kCopy : 0);
+            });
+            const StepArgs s = {lr, beta1, beta2, eps, weight_decay, step, grad_factor, lr_factor, chunk};
+            enqueue(adamw<CAP, SMALL>, dim3((unsigned)chunks), dim3(kThreads), a, s);
+        };
+        in_launches(count, kMostTensors<SMALL>, chunk, [&](int64_t i) { return tensors[i].n; }, [&](int64_t begin, int n, int64_t chunks) {
+            if (chunks == 0) return;
+            if (n <= kFewTensors) launch(std::integral_constant<int, kFewTensors>{}, begin, n, chunks);
+            else launch(std::integral_constant<int, kMostTensors<SMALL>>{}, begin, n, chunks);
         });
-        const StepArgs s = {lr, beta1, beta2, eps, weight_decay, step, grad_factor, lr_factor, chunk};
-        if (some[1]) enqueue(adamw<CAP, true>, dim3((unsigned)chunks), dim3(kThreads), a, s);
-        else enqueue(adamw<CAP, false>, dim3((unsigned)chunks), dim3(kThreads), a, s);
     };
-    in_launches(count, kMostTensors, chunk, [&](int64_t i) { return tensors[i].n; }, [&](int64_t begin, int n, int64_t chunks) {
-        if (chunks == 0) return;
-        if (n <= kFewTensors) launch(std::integral_constant<int, kFewTensors>{}, begin, n, chunks);
-        else launch(std::integral_constant<int, kMostTensors>{}, begin, n, chunks);
-    });
+    if (some[1]) all(std::true_type{});
+    else all(std::false_type{});
     return enqueue.status("adamw");
 }
 
