@@ -1437,9 +1437,9 @@ static fg_status gemm_impl(int64_t M, int64_t N, int64_t K, float alpha, const f
 }  // extern "C"
 
 int fg::plan_tile(int64_t M, int64_t N, int64_t K) { return plan_product(M, N, K, false, 2, 0, K <= 512 ? kPricesShort : kPrices).tile; }
-fg_status fg::launch_product(const KernelEntry &k, GemmParams &p, hipStream_t stream) {
+fg_status fg::launch_product(const KernelEntry &k, GemmParams &p, hipStream_t stream, int more_tiles) {
     p.tile_begin = 0;
-    p.tile_count = p.tiles_m * p.tiles_n;
+    p.tile_count = p.tiles_m * p.tiles_n + more_tiles;
     p.splits = 1;
     return launch(k, p, stream);
 }

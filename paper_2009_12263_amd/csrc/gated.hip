@@ -433,6 +433,27 @@ int gated_tile(int64_t M, int64_t N, int64_t K) {
     }
 }
 
+// Which tile both weights' gradients share in one launch; -1: they are faster one by one.  A round of tiles takes the time of one, K steps of 1.1, 0.75 or 0.5 us (256x256,
+// 256x128, 128x128; partly filled rounds measured) and 3 us besides; a product that is split along K 0.6 of that and two passes.  (8192 tokens, 5120 x 1024 and
+// 1024 x 2560: 160 and 80 tiles, 104 and 75 us one by one.)
+int tile_of_both(const GradSpace &s, int64_t M1, int64_t N1, int64_t M2, int64_t N2, int64_t K) {
+    const int bm[] = {256, 256, 128}, bn[] = {256, 128, 128};
+    const double step[] = {1.1, 0.75, 0.5}, steps = (double)((K + 63) / 64);
+    auto tiles = [&](int t, int64_t m, int64_t n) { return ((m + bm[t] - 1) / bm[t]) * ((n + bn[t] - 1) / bn[t]); };
+    auto time = [&](int t, int64_t n) { return (double)((n + 255) / 256) * (steps * step[t] + 3); };
+    double one[2] = {1e30, 1e30}, both = 1e30;
+    int best = 0;
+    for (int t = 0; t < 3; ++t) {
+        const int64_t n1 = tiles(t, M1, N1), n2 = tiles(t, M2, N2);
+        one[0] = std::min(one[0], time(t, n1));
+        one[1] = std::min(one[1], time(t, n2));
+        if (time(t, n1 + n2) < both) { both = time(t, n1 + n2); best = t; }
+    }
+    if (s.in_by_sums) one[0] = std::min(one[0], 0.6 * one[0] + 15);
+    if (s.out_by_sums) one[1] = std::min(one[1], 0.6 * one[1] + 15);
+    return both < one[0] + one[1] ? best : -1;
+}
+
 // A call's operands and launches.
 struct Call {
     Launches enqueue;
@@ -467,6 +488,29 @@ struct Call {
             using T = decltype(t);
             enqueue(gated_round<T, PARTS>, dim3(groups_for(rows, cols)), dim3(256), (const float *)in.re, in.ld, (T *)out->re, out->ld, rows, (int)cols);
         });
+    }
+    // The products of both weights' gradients, [dG dU]^T X and dY^T H, which have the same K, in one launch on the same tile.
+    fg_status both_weights(int tile, int64_t K, const fg_matrix &dgu, const fg_matrix &x, const fg_matrix *d_in, int64_t M1, int64_t N1, const fg_matrix &dy, const fg_matrix &h,
+                           const fg_matrix *d_out, int64_t M2, int64_t N2) {
+        const KernelEntry &k = kernel_table_gated(GATED_ROUND_NN, dtype == FG_BF16)[tile];
+        GatedParams p;
+        memset(&p, 0, sizeof p);
+        auto span = [&](int64_t n, int64_t ld) { return fg::up((K - 1) * ld + n, 8); };
+        p.M = (int32_t)M1; p.N = (int32_t)N1; p.K = (int32_t)K;
+        p.tiles_m = (int32_t)((M1 + k.bm - 1) / k.bm); p.tiles_n = (int32_t)((N1 + k.bn - 1) / k.bn);
+        p.A = (const _Float16 *)dgu.re; p.B = (const _Float16 *)x.re; p.D = (float *)d_in->re; p.ldd = d_in->ld;
+        p.a_rs = p.b_rs = 1;
+        p.a_ks = dgu.ld; p.b_ks = x.ld;
+        p.a_span = span(M1, dgu.ld); p.b_span = span(N1, x.ld);
+        p.alpha = 1.f;
+        SecondProduct &q = p.second;
+        q.M = (int32_t)M2; q.N = (int32_t)N2;
+        q.tiles_m = (int32_t)((M2 + k.bm - 1) / k.bm); q.tiles_n = (int32_t)((N2 + k.bn - 1) / k.bn);
+        q.A = (const _Float16 *)dy.re; q.B = (const _Float16 *)h.re; q.D = (float *)d_out->re; q.ldd = d_out->ld;
+        q.a_ks = dy.ld; q.b_ks = h.ld;
+        q.a_span = span(M2, dy.ld); q.b_span = span(N2, h.ld);
+        q.by_group = tile_group(q.tiles_m, q.tiles_n);
+        return launch_product(k, p, enqueue.stream, q.tiles_m * q.tiles_n);
     }
     // A product of the tiled kernels; k_rows: those that an operand has which is not K-contiguous (others count as zero).  f sets the parameters of its epilogue.
     template <class F> fg_status product(int kind, int64_t M, int64_t N, int64_t K, int64_t k_rows, const fg_matrix &a, const fg_matrix &b, F &&f) {
@@ -672,6 +716,8 @@ fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const f
             call.round<true>(sums, dX, tokens, dim);
         } else if (fg_status st = call.rounded(at, at.sums, at.x_by_sums, GATED_ROUND_KN, tokens, dim, gp, 2 * hidden, dgu, w_in, dX)) return st;
     }
+    const int tile = dW_in && dW_out ? tile_of_both(at, 2 * hidden, dim, dim, hidden, rows) : -1;
+    if (tile >= 0) return call.both_weights(tile, rows, dgu, x, dW_in, 2 * hidden, dim, dy, h, dW_out, dim, hidden);
     if (dW_in)
         if (fg_status st = call.rounded(at, at.sums, at.in_by_sums, GATED_ROUND_NN, 2 * hidden, dim, at.in_by_sums ? tp : rows, rows, dgu, x, dW_in)) return st;
     if (dW_out)

@@ -30,6 +30,14 @@ struct Activation {
     }
 };
 
+// A second product of a launch (GATED_ROUND_NN).
+struct SecondProduct {
+    const _Float16 *A, *B;
+    float *D;
+    int64_t a_ks, b_ks, a_span, b_span, ldd;
+    int32_t M, N, tiles_m, tiles_n;
+    Division by_group;
+};
 struct GatedParams : GemmParams {           // D, ldd: h, dgu or the rounded results, rows contiguous
     float *keep;                            // GATED_UP: g and u, rows of 2 hidden, or null
     const float *gu;                        // GATED_DOWN
@@ -40,13 +48,20 @@ struct GatedParams : GemmParams {           // D, ldd: h, dgu or the rounded res
     int64_t pair, pair_step;
     int32_t hidden;
     Activation act;
+    SecondProduct second;
+    __device__ __forceinline__ void to_second() {
+        A = second.A; B = second.B; D = second.D;
+        a_ks = second.a_ks; b_ks = second.b_ks; a_span = second.a_span; b_span = second.b_span; ldd = second.ldd;
+        M = second.M; N = second.N; tiles_m = second.tiles_m; tiles_n = second.tiles_n;
+        by_group = second.by_group;
+    }
 };
 
 enum GatedKind { GATED_UP = 0, GATED_DOWN = 1, GATED_ROUND_KK = 2, GATED_ROUND_KN = 3, GATED_ROUND_NN = 4 };       // (round: A, B contiguous along K or not)
 
 template <class Base, int KIND>
 struct GatedCfg : Base {
-    static constexpr bool OWN_STORE = true, PAIRED = KIND == GATED_UP;
+    static constexpr bool OWN_STORE = true, PAIRED = KIND == GATED_UP, GROUPED = KIND == GATED_ROUND_NN;
     using Params = GatedParams;
     using T = typename std::conditional<Base::BF16, bf16_t, f16_t>::type;
     static_assert(!PAIRED || Base::TJ % 2 == 0, "a wave has blocks of G and U");

@@ -163,6 +163,8 @@ struct TileCfg {
     static constexpr bool OWN_STORE = false;
     // PAIRED (derived configurations with B contiguous along K): blocks of 32 of B's rows come from two places in turn, GatedParams::pair rows apart.
     static constexpr bool PAIRED = false;
+    // GROUPED (derived configurations): tiles behind those of the product are those of another one with the same K (Params::second).
+    static constexpr bool GROUPED = false;
     // 0: real; 1: complex (i^2 = -1), 2: dual (eps^2 = 0) numbers in planar-split storage
     static constexpr int CPLX = CPLX_;
     static constexpr bool SPLITK_KERNEL = !STRIDED_ && DIAG_ == 0 && CPLX_ == 0;
@@ -1190,7 +1192,7 @@ __global__ __launch_bounds__(Cfg::NTHREADS, Cfg::WAVES) void gemm_kernel(const t
     // start the loads of a tile: point the loaders at its panels and fill the ring
     auto start_tile = [&](int tile_id, int &m0, int &n0, int &split) {
         // parameters are re-read here rather than kept in registers across the K loop
-        const Params tp = load_param<Params>(0);
+        Params tp = load_param<Params>(0);
         int tm, tn;
         [[maybe_unused]] const int item = tile_id;
         split = 0;
@@ -1198,6 +1200,13 @@ __global__ __launch_bounds__(Cfg::NTHREADS, Cfg::WAVES) void gemm_kernel(const t
             // which K range of a split product, and which tile of this launch's range
             split = divided(tile_id, tp.by_count);
             tile_id = tp.tile_begin + (tile_id - split * tp.tile_count);
+        }
+        if constexpr (Cfg::GROUPED) {
+            const int first = tp.tiles_m * tp.tiles_n;
+            if (tile_id >= first) {
+                tile_id -= first;
+                tp.to_second();
+            }
         }
         if constexpr (Cfg::STRIDED) {
             // which batch index
@@ -1719,6 +1728,9 @@ __global__ __launch_bounds__(Cfg::NTHREADS, Cfg::WAVES) void gemm_kernel(const t
                     ep.ldd = BM; ep.M = BM; ep.N = BN;
                     mb = wm * Cfg::WTM; nb = wn * Cfg::WTN;
                 }
+            }
+            if constexpr (Cfg::GROUPED) {
+                if (tile >= ep.tiles_m * ep.tiles_n) ep.to_second();
             }
             if constexpr (Cfg::STRIDED) {
                 const int64_t c_off = group_offset(ep.c_b, sp0);

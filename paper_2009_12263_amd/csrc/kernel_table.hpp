@@ -87,9 +87,9 @@ const KernelEntry *kernel_table_dual();
 enum { CTILE_64x64 = 2, CTILE_64x64_KG2 = 3, CTILE_COUNT = 4 };
 
 // The block tile (TileId) that the planner picks for a product of M x N x K that is not split, and the launch of a kernel on all tiles of p (the other
-// parameters of which are set); both for products whose results a kernel does not store as a matrix.
+// parameters of which are set) and on more_tiles behind them (TileCfg::GROUPED); both for products whose results a kernel does not store as a matrix.
 int plan_tile(int64_t M, int64_t N, int64_t K);
-fg_status launch_product(const KernelEntry &k, GemmParams &p, hipStream_t stream);
+fg_status launch_product(const KernelEntry &k, GemmParams &p, hipStream_t stream, int more_tiles = 0);
 
 // The products of the gated feed-forward block (gated_kernel.hpp): index = tile.
 enum { GATED_KINDS = 5, GATED_TILES = 5 };
