@@ -182,7 +182,7 @@ __device__ __forceinline__ float relative(float (&x)[kLaneBlock]) {
 #pragma unroll
     for (int e = 0; e < kLaneBlock; ++e) top = __builtin_fmaxf(top, __builtin_fabsf(x[e]));
     top = row_max(top);
-    const float by = top >= kNothing ? kTop / top : 0.f;
+    const float by = top >= kNothing ? kTop * (1.f / top) : 0.f;
 #pragma unroll
     for (int e = 0; e < kLaneBlock; ++e) {
         x[e] *= by;

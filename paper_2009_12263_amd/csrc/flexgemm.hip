@@ -1340,7 +1340,7 @@ fg_status fg_init(void) {
 // of a K split go to the static scratch array (FG_ERR_UNSUPPORTED if they do not fit), and nothing
 // on this path allocates, frees or creates anything.
 // stored: what gemm_stored adds.
-struct Stored { int64_t k_rows; float *scratch; int64_t scratch_bytes; };
+struct Stored { int64_t k_rows; float *scratch; int64_t scratch_bytes; fg::RoundedResult *rounded; };
 static fg_status gemm_impl(int64_t M, int64_t N, int64_t K, float alpha, const fg_matrix *A, const fg_matrix *B,
                            float beta, const fg_matrix *C, const fg_matrix *D, const fg_epilogue *ep, bool dual,
                            const fg_load_transforms *lt, void *hip_stream, bool static_only = false, const Stored *stored = nullptr) {
@@ -1428,6 +1428,13 @@ static fg_status gemm_impl(int64_t M, int64_t N, int64_t K, float alpha, const f
     part.D = scratch.ptr;
     part.C = nullptr; part.has_c = 0; part.bias = nullptr; part.act = 0; part.c_act = 0; part.alpha = 1.f; part.beta = 0.f;
     if (fg_status st = launch(k, part, stream)) return st;
+    if (stored && stored->rounded && first == 0) {
+        const fg_matrix *to = stored->rounded->D;
+        hipError_t e = fg::launch_splitk_round(scratch.ptr, S, count, k.bm, k.bn, p.tiles_m, p.tiles_n, (int)q.M, (int)q.N, to->re, to->ld, to->dtype == FG_BF16, stream);
+        if (e != hipSuccess) return fail(FG_ERR_LAUNCH, "launch of the split-K reduction failed: %s", hipGetErrorString(e));
+        stored->rounded->done = true;
+        return FG_OK;
+    }
     hipError_t e = fg::launch_splitk_reduce(scratch.ptr, S, first, count, k.bm, k.bn, p.tiles_m, p.tiles_n, (int)q.M, (int)q.N, q.alpha, q.beta,
                                             q.C, q.ldc, q.D, q.ldd, q.bias, q.bias_dim, q.act, q.c_act, stream);
     if (e != hipSuccess) return fail(FG_ERR_LAUNCH, "launch of the split-K reduction failed: %s", hipGetErrorString(e));
@@ -1445,8 +1452,8 @@ fg_status fg::launch_product(const KernelEntry &k, GemmParams &p, hipStream_t st
 }
 
 fg_status fg::gemm_stored(int64_t M, int64_t N, int64_t K, int64_t k_rows, float alpha, const fg_matrix *A, const fg_matrix *B, float beta,
-                          const fg_matrix *C, const fg_matrix *D, float *scratch, int64_t scratch_bytes, void *hip_stream) {
-    const Stored stored = {k_rows, scratch, scratch_bytes};
+                          const fg_matrix *C, const fg_matrix *D, float *scratch, int64_t scratch_bytes, void *hip_stream, RoundedResult *rounded) {
+    const Stored stored = {k_rows, scratch, scratch_bytes, rounded};
     return gemm_impl(M, N, K, alpha, A, B, beta, C, D, nullptr, false, nullptr, hip_stream, false, &stored);
 }
 int64_t fg::gemm_stored_scratch(int64_t M, int64_t N, int64_t K) {

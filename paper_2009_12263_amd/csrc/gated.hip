@@ -479,9 +479,9 @@ struct Call {
         pads.count = 0;
         pad_groups = 0;
     }
-    fg_status by_sums(const Space &s, int64_t M, int64_t N, int64_t K, int64_t k_rows, const fg_matrix &a, const fg_matrix &b, const fg_matrix &d) {
+    fg_status by_sums(const Space &s, int64_t M, int64_t N, int64_t K, int64_t k_rows, const fg_matrix &a, const fg_matrix &b, const fg_matrix &d, RoundedResult *rounded = nullptr) {
         if (fg_status st = enqueue.status("gated_pad")) return st;
-        return gemm_stored(M, N, K, k_rows, 1.f, &a, &b, 0.f, nullptr, &d, (float *)(space + s.scratch), s.scratch_bytes, enqueue.stream);
+        return gemm_stored(M, N, K, k_rows, 1.f, &a, &b, 0.f, nullptr, &d, (float *)(space + s.scratch), s.scratch_bytes, enqueue.stream, rounded);
     }
     template <bool PARTS> void round(const fg_matrix &in, const fg_matrix *out, int64_t rows, int64_t cols) {
         with_half(dtype, [&](auto t) {
@@ -537,8 +537,9 @@ struct Call {
         if (!through_sums)
             return product(kind, M, N, K, k_rows, a, b, [&](GatedParams &p) { p.D = (float *)out->re; p.ldd = out->ld; });
         const fg_matrix d = rows_of(space + sums, FG_F32, fg::up(N, 4));
-        if (fg_status st = by_sums(s, M, N, K, kind == GATED_ROUND_KK ? 0 : k_rows, kind == GATED_ROUND_NN ? turned(a) : a, kind == GATED_ROUND_KK ? turned(b) : b, d)) return st;
-        round<false>(d, out, M, N);
+        RoundedResult rounded = {out, false};
+        if (fg_status st = by_sums(s, M, N, K, kind == GATED_ROUND_KK ? 0 : k_rows, kind == GATED_ROUND_NN ? turned(a) : a, kind == GATED_ROUND_KK ? turned(b) : b, d, &rounded)) return st;
+        if (!rounded.done) round<false>(d, out, M, N);
         return enqueue.status("gated_round");
     }
     template <bool UP> void few(const FewArgs &a) {

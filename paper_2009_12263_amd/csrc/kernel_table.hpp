@@ -107,6 +107,10 @@ hipError_t launch_splitk_reduce(const float *W, int splits, int tile_begin, int 
                                 int tiles_n, int M, int N, float alpha, float beta, const float *C, int64_t ldc, float *D,
                                 int64_t ldd, const float *bias, int bias_dim, int act, int c_act, hipStream_t stream);
 
+// The same for results in 16 bits without C, bias and activation.
+hipError_t launch_splitk_round(const float *W, int splits, int tile_count, int bm, int bn, int tiles_m, int tiles_n, int M, int N, void *D, int64_t ldd, bool bf16,
+                               hipStream_t stream);
+
 // General kernel (general_kernel.hpp): matrices with unaligned operands or a K that is not a multiple
 // of 8 (gemm_general.hip), contractions the tiled kernels cannot take (contract_general.hip).  128x128
 // tiles with eight 32x64 waves; 64x64 tiles whose two groups of four waves take alternate K steps; 64x64 tiles with one

@@ -70,7 +70,49 @@ __global__ __launch_bounds__(256) void splitk_reduce(const float *W, int splits,
             if (q < valid) d[q] = y[q];
 }
 
+// The same sums of one range of tiles, rounded to 16 bits where they are stored (T: binary16 or bfloat16).
+template <class T>
+__global__ __launch_bounds__(256) void splitk_round(const float *W, int splits, int tile_count, int bm, int bn, int tiles_m, int tiles_n, int M, int N, T *D, int64_t ldd) {
+    typedef T four __attribute__((ext_vector_type(4)));
+    typedef four anywhere __attribute__((aligned(2)));
+    const int per_tile = (bm / 4) * bn;
+    const int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (idx >= (int64_t)per_tile * tile_count) return;
+    const int t = (int)(idx / per_tile);
+    const int e = (int)(idx - (int64_t)t * per_tile);
+    const int col = e / (bm / 4), row = (e - col * (bm / 4)) * 4;
+    int tm, tn;
+    block_to_tile(t, tiles_m, tiles_n, tm, tn);
+    const int m = tm * bm + row, n = tn * bn + col;
+    if (m >= M || n >= N) return;
+    const int valid = M - m < 4 ? M - m : 4;
+    const int64_t slot_elems = (int64_t)bm * bn, step = (int64_t)tile_count * slot_elems;
+    const float *w = W + (int64_t)t * slot_elems + row + (int64_t)col * bm;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < splits; s0 += kAhead) {
+        float4 v[kAhead];
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s) v[s] = *(const float4 *)(w + (int64_t)(s0 + s < splits ? s0 + s : splits - 1) * step);
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s)
+            if (s0 + s < splits) { sum[0] += v[s].x; sum[1] += v[s].y; sum[2] += v[s].z; sum[3] += v[s].w; }
+    }
+    T *d = D + m + (int64_t)n * ldd;
+    const four y = {(T)sum[0], (T)sum[1], (T)sum[2], (T)sum[3]};
+    if (valid == 4) *(anywhere *)d = y;
+    else
+        for (int q = 0; q < 4; ++q)
+            if (q < valid) d[q] = y[q];
+}
+
 }  // namespace
+
+hipError_t launch_splitk_round(const float *W, int splits, int tile_count, int bm, int bn, int tiles_m, int tiles_n, int M, int N, void *D, int64_t ldd, bool bf16,
+                               hipStream_t stream) {
+    const dim3 blocks((unsigned)(((int64_t)(bm / 4) * bn * tile_count + 255) / 256));
+    if (bf16) return launch_kernel(splitk_round<__bf16>, blocks, dim3(256), stream, W, splits, tile_count, bm, bn, tiles_m, tiles_n, M, N, (__bf16 *)D, ldd);
+    return launch_kernel(splitk_round<_Float16>, blocks, dim3(256), stream, W, splits, tile_count, bm, bn, tiles_m, tiles_n, M, N, (_Float16 *)D, ldd);
+}
 
 hipError_t launch_splitk_reduce(const float *W, int splits, int tile_begin, int tile_count, int bm, int bn, int tiles_m,
                                 int tiles_n, int M, int N, float alpha, float beta, const float *C, int64_t ldc, float *D,
