@@ -361,7 +361,7 @@ int64_t fg_linear_xent_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim
 /*
  * Gated feed-forward block: with [G U] = X * W_in^T and H = act(G) * U (element by element),   Y = H * W_out^T.
  *   X, Y  : tokens x dim; W_in : 2 hidden x dim, the rows of G and then those of U; W_out : dim x hidden.  All FG_F16 or all FG_BF16,
- *           multiplied exactly and summed in FP32; H is rounded to that type between the products.  Y may not overlap an operand.
+ *           multiplied exactly and summed in FP32; H is rounded to that type between the products (binary16: above 65504 it is infinite).  Y lies in other memory.
  *   act   : FG_ACT_NONE, FG_ACT_RELU, FG_ACT_SILU, FG_ACT_GELU_TANH.
  *   GU    : tokens x 2 hidden, FG_F32: G and U, written for fg_gated_ffn_grad; NULL: not wanted.  (Rounded to 16 bits they would make the errors of
  *           the gradients 1.4 times as large.)
@@ -415,7 +415,7 @@ typedef struct {
  * Nothing is changed where grad_factor is no finite number (gradients that overflowed, see fg_grad_norm) or *step is below 1.
  * Moments in eight bits stand for number * scale, and the second one for (number * scale)^2: its root is kept.  The scale is the largest absolute
  * value of 256 / 448 (0 below 1e-30 / 448), numbers are rounded to nearest even, a root above zero to the smallest number (2^-9) at least.  The step itself uses
- * the moments before they are rounded.
+ * the moments before they are rounded.  (An infinity among 256 values leaves them without a number, a NaN stays one value's.)
  */
 fg_status fg_adamw(int64_t count, const fg_adamw_tensor *tensors, const int64_t *step, double lr, double beta1, double beta2, double eps,
                    double weight_decay, const float *grad_factor, const float *lr_factor, void *hip_stream);

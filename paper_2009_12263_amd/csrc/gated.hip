@@ -420,6 +420,12 @@ fg_status check_like(const char *name, const fg_matrix *m, int64_t rows, int64_t
     return FG_OK;
 }
 
+// Results are written while operands are still to be read.
+fg_status check_elsewhere(const char *name, const fg_matrix *out, const char *operand, const fg_matrix *in) {
+    if (out && out->re && out->re == in->re) return fail(FG_ERR_LAYOUT, "%s must be in other memory than %s", name, operand);
+    return FG_OK;
+}
+
 unsigned groups_for(int64_t rows, int64_t cols) { return (unsigned)std::min<int64_t>((rows * ((cols + 7) / 8) + 255) / 256, 8192); }
 
 // Which tile of kernel_table_gated serves a product.
@@ -596,6 +602,9 @@ fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_mat
     if (fg_status st = check_like("Y", Y, tokens, dim, X->dtype)) return st;
     if (GU) if (fg_status st = check_like("GU", GU, tokens, 2 * hidden, FG_F32)) return st;
     if (tokens == 0 || dim == 0) return FG_OK;
+    if (fg_status st = check_elsewhere("Y", Y, "X", X)) return st;
+    if (fg_status st = check_elsewhere("Y", Y, "W_in", W_in)) return st;
+    if (fg_status st = check_elsewhere("Y", Y, "W_out", W_out)) return st;
     Call call = {Launches(hip_stream), (char *)workspace, X->dtype};
     if (hidden == 0) {
         call.round<false>(rows_of(nullptr, FG_F32, 0), Y, tokens, dim);
@@ -672,8 +681,13 @@ fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const f
     if (dX) if (fg_status st = check_like("dX", dX, tokens, dim, X->dtype)) return st;
     if (dW_in) if (fg_status st = check_like("dW_in", dW_in, 2 * hidden, dim, X->dtype)) return st;
     if (dW_out) if (fg_status st = check_like("dW_out", dW_out, dim, hidden, X->dtype)) return st;
-    Call call = {Launches(hip_stream), (char *)workspace, X->dtype};
     if (dim == 0) return FG_OK;
+    const struct { const char *name; const fg_matrix *m; } operands[] = {{"dY", dY}, {"X", X}, {"W_in", W_in}, {"W_out", W_out}},
+                                                           results[] = {{"dX", dX}, {"dW_in", dW_in}, {"dW_out", dW_out}};
+    for (const auto &out : results)
+        for (const auto &in : operands)
+            if (fg_status st = check_elsewhere(out.name, out.m, in.name, in.m)) return st;
+    Call call = {Launches(hip_stream), (char *)workspace, X->dtype};
     if (tokens == 0 || hidden == 0) {
         const fg_matrix none = rows_of(nullptr, FG_F32, 0);
         if (dX && tokens > 0) call.round<false>(none, dX, tokens, dim);

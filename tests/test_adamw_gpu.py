@@ -140,6 +140,34 @@ def test_many_tensors_of_all_kinds(bits):
         m.check(want)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_what_lies_beside_a_tensor_stays(bits):
+    """Tensors packed into one memory with values between them that are nobody's."""
+    m = Model([1001, 17, 8193], torch.bfloat16, master=True, bits=bits, seed=2)
+
+    def packed(items, dtype, gap):
+        memory = torch.full((sum(len(t) + gap for t in items),), 7.0, device="cuda").to(dtype)
+        inside, views, at = torch.zeros(len(memory), dtype=torch.bool, device="cuda"), [], 0
+        for t in items:
+            views.append(memory[at:at + len(t)])
+            views[-1].copy_(t)
+            inside[at:at + len(t)] = True
+            at += len(t) + gap - (0 if dtype != torch.float8_e4m3fn else (len(t) + gap) % 16)        # (moments in eight bits are aligned)
+        return memory, inside, views
+    memories = []
+    for name, gap in (("params", 3), ("masters", 5), ("avg", 16), ("sq", 16), ("avg_scales", 1), ("sq_scales", 2)):
+        items = getattr(m, name)
+        if items is not None:
+            memory, inside, views = packed(items, items[0].dtype, gap)
+            memories.append((name, memory, inside))
+            setattr(m, name, views)
+    want = m.want()
+    m.call()
+    m.check(want)
+    for name, memory, inside in memories:
+        assert bool((memory[~inside].float() == 7.0).all()), name
+
+
 def test_one_tensor_and_none():
     m = Model([12345])
     want = m.want()

@@ -280,6 +280,55 @@ def test_other_streams_and_captured_calls(tokens):
         torch.cuda.synchronize()
 
 
+def test_weights_whose_halves_lie_far_apart():
+    """U's rows of W_in begin more than 2^31 bytes behind G's: such weights are copied."""
+    T, D, H, ld = 70, 64, 600, 1 << 21
+    g = torch.Generator(device="cuda").manual_seed(0)
+    memory = torch.empty(2 * H * ld, dtype=torch.bfloat16, device="cuda")
+    c = Case(T, D, H, torch.bfloat16, seed=1)
+    w_in = memory.view(2 * H, ld)[:, :D]
+    w_in.copy_(torch.randn(2 * H, D, generator=g, device="cuda") * D ** -0.5)
+    c.w_in = w_in
+    c.forward("silu")
+    c.backward("silu")
+    c.check("silu", ALL)
+    few = Case(3, D, H, torch.bfloat16, seed=2)
+    few.w_in = w_in
+    few.forward("silu")
+    few.check("silu", ("y", "gu"))
+
+
+def test_offsets_beyond_32_bits():
+    """Results and kept values of more than 2^32 bytes: tokens at the end are those of a call on them alone."""
+    T, D, H = 140000, 64, 4100
+    c = Case(T, D, H, torch.bfloat16, seed=3)
+    assert c.r["gu"].numel() * 4 > 1 << 32
+    c.forward("silu")
+    c.backward("silu", ("dx",))
+    last = slice(T - 200, T)
+    want = reference(c.x[last], c.w_in, c.w_out, "silu", c.dtype, c.dy[last])
+    for name in ("y", "gu", "dx"):
+        check(name, c.r[name][last], want[name])
+
+
+def test_long_sums_of_a_weight_gradient():
+    """dW over many tokens, against 64 bits in blocks of tokens."""
+    T, D, H = 40000, 72, 136
+    c = Case(T, D, H, torch.float16, seed=4)
+    c.dy *= 2 ** -6
+    c.forward("gelu")
+    c.backward("gelu", ("dw_in", "dw_out"))
+    want = {}
+    for t in range(0, T, 8000):
+        part = reference(c.x[t:t + 8000], c.w_in, c.w_out, "gelu", c.dtype, c.dy[t:t + 8000])
+        for name in ("dw_in", "dw_out"):
+            v, e = want.get(name, (0.0, 0.0))
+            want[name] = v + part[name][0], e + part[name][1]
+    # (a block's bound holds for its 8000 terms of the FP32 sum; 40000 have five times that, and each block's bound already holds one rounding of its result)
+    for name in want:
+        check(name, c.r[name], (want[name][0], 5 * want[name][1]))
+
+
 def test_refused_tensors():
     c = Case(4, 16, 24, torch.bfloat16)
     for change, word in ((dict(X=c.x.cpu()), "current GPU"), (dict(W_in=c.w_in[:47]), "W_in"), (dict(W_out=c.w_out[:, :23]), "W_out"),

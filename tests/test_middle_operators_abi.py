@@ -15,12 +15,12 @@ def row(dtype=fg.FG_BF16, ld=128, re=PTR, layout=fg.FG_ROW, im=None):
 
 
 def ffn(tokens=4, dim=64, hidden=48, X=None, W_in=None, W_out=None, act=fg.FG_ACT_SILU, Y=None, GU=NULL, ws=PTR, size=1 << 40):
-    X, W_in, W_out, Y = (row() if m is None else m for m in (X, W_in, W_out, Y))
+    X, W_in, W_out, Y = (row(re=PTR * (k + 1)) if m is None else m for k, m in enumerate((X, W_in, W_out, Y)))
     return fg.load_library().fg_gated_ffn(tokens, dim, hidden, X, W_in, W_out, act, Y, GU, ws, size, None)
 
 
 def ffn_grad(tokens=4, dim=64, hidden=48, dY=None, X=None, W_in=None, W_out=None, act=fg.FG_ACT_SILU, GU=None, dX=None, dW_in=None, dW_out=None, ws=PTR, size=1 << 40):
-    dY, X, W_in, W_out, dX, dW_in, dW_out = (row() if m is None else m for m in (dY, X, W_in, W_out, dX, dW_in, dW_out))
+    dY, X, W_in, W_out, dX, dW_in, dW_out = (row(re=PTR * (k + 1)) if m is None else m for k, m in enumerate((dY, X, W_in, W_out, dX, dW_in, dW_out)))
     GU = row(fg.FG_F32) if GU is None else GU
     return fg.load_library().fg_gated_ffn_grad(tokens, dim, hidden, dY, X, W_in, W_out, act, GU, dX, dW_in, dW_out, ws, size, None)
 
@@ -65,6 +65,12 @@ def norm(grads=((PTR, 100, fg.FG_BF16),), count=None, scale=1.0, limit=1.0, out=
     (ffn, dict(dim=1 << 21, X=row(ld=1 << 21), W_in=row(ld=1 << 21), Y=row(ld=1 << 21)), fg.FG_ERR_UNSUPPORTED, "2^21"),
     (ffn, dict(hidden=1 << 20, W_out=row(ld=1 << 20)), fg.FG_ERR_UNSUPPORTED, "2^21"),
     (ffn, dict(tokens=1 << 30, hidden=1 << 10, W_out=row(ld=1 << 10)), fg.FG_ERR_UNSUPPORTED, "tiles"),
+    (ffn, dict(Y=row()), fg.FG_ERR_LAYOUT, "Y must be in other memory than X"),
+    (ffn, dict(Y=row(re=3 * PTR)), fg.FG_ERR_LAYOUT, "Y must be in other memory than W_out"),
+    (ffn_grad, dict(dX=row()), fg.FG_ERR_LAYOUT, "dX must be in other memory than dY"),
+    (ffn_grad, dict(dX=row(re=2 * PTR)), fg.FG_ERR_LAYOUT, "dX must be in other memory than X"),
+    (ffn_grad, dict(dW_in=row(re=3 * PTR)), fg.FG_ERR_LAYOUT, "dW_in must be in other memory than W_in"),
+    (ffn_grad, dict(dW_out=row(re=4 * PTR)), fg.FG_ERR_LAYOUT, "dW_out must be in other memory than W_out"),
     (ffn, dict(ws=None), fg.FG_ERR_NULL, "workspace"),
     (ffn, dict(size=16), fg.FG_ERR_SHAPE, "workspace"),
     (ffn, dict(ws=PTR + 8), fg.FG_ERR_ALIGN, "workspace"),
