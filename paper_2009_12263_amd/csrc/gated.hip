@@ -440,7 +440,7 @@ int gated_tile(int64_t M, int64_t N, int64_t K) {
 }
 
 // Which tile both weights' gradients share in one launch; -1: they are faster one by one.  A round of tiles takes the time of one, K steps of 1.1, 0.75 or 0.5 us (256x256,
-// 256x128, 128x128; partly filled rounds measured) and 3 us besides; a product that is split along K 0.6 of that and two passes.  (8192 tokens, 5120 x 1024 and
+// 256x128, 128x128; partly filled rounds measured) and 3 us besides; a product that is split along K takes its share of the GPU and 12 us for two launches.  (8192 tokens, 5120 x 1024 and
 // 1024 x 2560: 160 and 80 tiles, 104 and 75 us one by one.)
 int tile_of_both(const GradSpace &s, int64_t M1, int64_t N1, int64_t M2, int64_t N2, int64_t K) {
     const int bm[] = {256, 256, 128}, bn[] = {256, 128, 128};
@@ -455,8 +455,9 @@ int tile_of_both(const GradSpace &s, int64_t M1, int64_t N1, int64_t M2, int64_t
         one[1] = std::min(one[1], time(t, n2));
         if (time(t, n1 + n2) < both) { both = time(t, n1 + n2); best = t; }
     }
-    if (s.in_by_sums) one[0] = std::min(one[0], 0.6 * one[0] + 15);
-    if (s.out_by_sums) one[1] = std::min(one[1], 0.6 * one[1] + 15);
+    auto split = [&](int64_t m, int64_t n) { return (double)tiles(2, m, n) * steps * 0.6 / 256 + 12; };
+    if (s.in_by_sums) one[0] = std::min(one[0], split(M1, N1));
+    if (s.out_by_sums) one[1] = std::min(one[1], split(M2, N2));
     return both < one[0] + one[1] ? best : -1;
 }
 
