@@ -4,6 +4,11 @@
 //                16 bits is stored, and g and u in FP32 if they are wanted.
 //   GATED_DOWN   dY W_out = dh.  With g and u from memory: dg, du and h in 16 bits.
 //   GATED_ROUND  results rounded to 16 bits.
+// What the first two cost beside their products is memory: with g and u kept, UP writes 10 bytes for each value of h and DOWN reads 8 and writes 6, and with one wave
+// per SIMD nothing else runs on a unit meanwhile.  8192 tokens of 1024 x 2560, binary16: UP 128 us (its product alone takes 61, its bytes 44), DOWN 130; without the loads
+// of g and u 89, without the stores of dg and du 109, without the activations 120, with none of them 61.  Two workgroups a unit on smaller tiles, of which one
+// could store while the other multiplies: 141 and 150; loads and stores with the streaming policy: 133 and 142; 3 to 10 units ahead in place of 6: within 1 %.
+// As passes over FP32 products of their own they took 26 % longer on 8192 x 4096 x 10240 (UP and DOWN 1720 us now).
 #pragma once
 #include "kernel_table.hpp"
 #include "row_ops.hpp"
