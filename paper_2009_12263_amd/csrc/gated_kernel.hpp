@@ -8,7 +8,7 @@
 // per SIMD nothing else runs on a unit meanwhile.  8192 tokens of 1024 x 2560, binary16: UP 128 us (its product alone takes 61, its bytes 44), DOWN 130; without the loads
 // of g and u 89, without the stores of dg and du 109, without the activations 120, with none of them 61.  Two workgroups a unit on smaller tiles, of which one
 // could store while the other multiplies: 141 and 150; loads and stores with the streaming policy: 133 and 142; 3 to 10 units ahead in place of 6: within 1 %.
-// As passes over FP32 products of their own they took 26 % longer on 8192 x 4096 x 10240 (UP and DOWN 1720 us now).
+// (FP32 products and passes over them in place of all three, 8192 x 4096 x 10240, forward and backward: 5034 us, 4609 so.)
 #pragma once
 #include "kernel_table.hpp"
 #include "row_ops.hpp"
@@ -16,22 +16,32 @@
 namespace fg {
 
 // act(g) = g q(g) with q = 1 / (1 + exp(-g (k0 + k1 g^2))): silu has k0 = 1, k1 = 0; in gelu (1 + tanh v) / 2 = 1 / (1 + exp(-2 v)).  relu and none have q of 0 or 1.
-// One code for all: four copies of an epilogue would leave the instruction cache.
+// KIND: the epilogues of products have code of their own for silu and gelu (FG_ACT_SILU, FG_ACT_GELU_TANH), half as many instructions as one for all (ANY_ACT):
+// with nothing kept 8192 tokens of 1024 x 2560 114 us so, 97 without an activation.
+constexpr int ANY_ACT = -1;
 struct Activation {
-    float k0, k1;
-    int32_t relu, none;
+    float k0, k1;                           // times -log2 e
+    int32_t kind;
     __host__ __device__ static Activation of(int act) {
-        const float c = 2.f * 0.79788456080286535588f;                  // 2 sqrt(2 / pi)
-        return {act == FG_ACT_GELU_TANH ? c : 1.f, act == FG_ACT_GELU_TANH ? 0.044715f * c : 0.f, act == FG_ACT_RELU, act == FG_ACT_NONE};
+        const float c = act == FG_ACT_GELU_TANH ? 2.f * 0.79788456080286535588f : 1.f, minus_log2e = -1.44269504088896340736f;         // (2 sqrt(2 / pi))
+        return {c * minus_log2e, act == FG_ACT_GELU_TANH ? 0.044715f * c * minus_log2e : 0.f, act};
     }
-    // act(g), and its derivative q + g q (1 - q) (k0 + 3 k1 g^2).  (Beyond 1000 q is 0 or 1: the bound keeps g^2 a number.)
-    template <bool D>
+    // act(g), and its derivative q + g q (1 - q) (k0 + 3 k1 g^2).  (Of gelu's g bounded: far out q (1 - q) is zero, and stays zero times a finite slope.)
+    template <bool D, int KIND = ANY_ACT>
     __device__ __forceinline__ float operator()(float g, float *d) const {
-        const float x = __builtin_amdgcn_fmed3f(g, -1000.f, 1000.f), x2 = x * x, slope = __builtin_fmaf(k1, x2, k0);
-        float q = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * (x * slope)));
-        q = relu ? (g > 0.f ? 1.f : 0.f) : none ? 1.f : q;
-        if constexpr (D) *d = __builtin_fmaf(x * q * (1.f - q), __builtin_fmaf(3.f * k1, x2, k0), q);
-        return relu ? (g > 0.f ? g : 0.f) : g * q;
+        constexpr float kMinusLn2 = -0.69314718055994530942f;
+        if constexpr (KIND == FG_ACT_SILU) {
+            const float q = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * g)), a = g * q;
+            if constexpr (D) *d = __builtin_fmaf(a, 1.f - q, q);
+            return a;
+        } else {
+            const float x = D || KIND == ANY_ACT ? __builtin_amdgcn_fmed3f(g, -1000.f, 1000.f) : g, x2 = x * x;
+            float q = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * __builtin_fmaf(k1, x2, k0)));
+            if constexpr (KIND == ANY_ACT) q = kind == FG_ACT_RELU ? (g > 0.f ? 1.f : 0.f) : kind == FG_ACT_NONE ? 1.f : q;
+            if constexpr (D) *d = __builtin_fmaf(x * q * (1.f - q), kMinusLn2 * __builtin_fmaf(3.f * k1, x2, k0), q);
+            if constexpr (KIND == ANY_ACT) return kind == FG_ACT_RELU ? (g > 0.f ? g : 0.f) : g * q;
+            return g * q;
+        }
     }
 };
 
@@ -119,9 +129,16 @@ struct GatedCfg : Base {
     __device__ static __forceinline__ void store(const Params &p, const Blocks &blocks, int m_base, int n_base, int lane) {
         if constexpr (Base::WIDE) own_acc();
         const int row0 = m_base + lane % ROWS, shift = 8 * (lane / ROWS);
-        if constexpr (KIND == GATED_UP) up(p, blocks, row0, n_base / 2 + shift, n_base / 2 + Base::WTN / 2 > p.hidden);
-        else if constexpr (KIND == GATED_DOWN) down(p, blocks, row0, n_base + shift, n_base + Base::WTN > p.hidden);
-        else round(p, blocks, row0, n_base + shift, n_base + Base::WTN > p.N);
+        auto with_act = [&](auto act) {
+            constexpr int ACT = decltype(act)::value;
+            if constexpr (KIND == GATED_UP) up<ACT>(p, blocks, row0, n_base / 2 + shift, n_base / 2 + Base::WTN / 2 > p.hidden);
+            else down<ACT>(p, blocks, row0, n_base + shift, n_base + Base::WTN > p.hidden);
+        };
+        if constexpr (KIND == GATED_UP || KIND == GATED_DOWN) {
+            if (p.act.kind == FG_ACT_SILU) with_act(ic<FG_ACT_SILU>{});
+            else if (p.act.kind == FG_ACT_GELU_TANH) with_act(ic<FG_ACT_GELU_TANH>{});
+            else with_act(ic<ANY_ACT>{});
+        } else round(p, blocks, row0, n_base + shift, n_base + Base::WTN > p.N);
     }
     __device__ static __forceinline__ void step() {
         if constexpr (Base::WIDE) {
@@ -151,7 +168,7 @@ struct GatedCfg : Base {
     }
 
     // first: the lane's first column of h; the blocks of G and U, 32 columns each, lie side by side
-    template <class Blocks>
+    template <int ACT, class Blocks>
     __device__ static __forceinline__ void up(const Params &p, const Blocks &blocks, int row0, int first, bool edge) {
         const Activation act = p.act;
         constexpr int PER = 32 / WIDTH;                                 // units of a block
@@ -165,7 +182,7 @@ struct GatedCfg : Base {
                 const eight g = unit<I, J>(blocks), u = unit<I, J + PER>(blocks);
                 eight v;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = act.template operator()<false>(g[e], nullptr) * u[e];
+                for (int e = 0; e < 8; ++e) v[e] = act.template operator()<false, ACT>(g[e], nullptr) * u[e];
                 if (row < p.M) {
                     if (!edge) {
                         put(h + c, v, 8);
@@ -204,7 +221,7 @@ struct GatedCfg : Base {
         }
         return out;
     }
-    template <class Blocks>
+    template <int ACT, class Blocks>
     __device__ static __forceinline__ void down(const Params &p, const Blocks &blocks, int row0, int first, bool edge) {
         const Activation act = p.act;
         constexpr int COUNT = UI * UJ;
@@ -226,7 +243,7 @@ struct GatedCfg : Base {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float d;
-                const float a = act.template operator()<true>(in.g[e], &d);
+                const float a = act.template operator()<true, ACT>(in.g[e], &d);
                 vg[e] = dh[e] * in.u[e] * d;
                 vu[e] = dh[e] * a;
                 vh[e] = a * in.u[e];
