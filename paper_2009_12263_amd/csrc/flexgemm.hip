@@ -1319,6 +1319,7 @@ fg_status fg_init(void) {
         for (bool bf16 : {false, true})
             for (int i = 0; i < fg::GATED_TILES; ++i) {
                 int per_cu = 0;
+                if (!fg::kernel_table_gated(kind, bf16)[i].fn) continue;
                 if (fg_status st = prepare(fg::kernel_table_gated(kind, bf16)[i], dev, per_cu)) return st;
             }
     for (auto &tb : tables)

@@ -428,8 +428,12 @@ fg_status check_elsewhere(const char *name, const fg_matrix *out, const char *op
 
 unsigned groups_for(int64_t rows, int64_t cols) { return (unsigned)std::min<int64_t>((rows * ((cols + 7) / 8) + 255) / 256, 8192); }
 
-// Which tile of kernel_table_gated serves a product.
-int gated_tile(int64_t M, int64_t N, int64_t K) {
+// Which tile of kernel_table_gated serves a product.  Two workgroups a unit where the epilogue's memory weighs against the sums and the GPU is filled: G and U up to K = 512
+// (3000 tokens of 400 x 1500 37 -> 27 us, 2000 of 128 x 5000 37 -> 31; 4096 of 768 x 2048 40 -> 54), dh up to 1024 (3000 of 400 x 1500 39 -> 30, 8192 of 1024 x 2560 129 -> 125,
+// 1003 of 1001 x 2729 24 -> 23; 1500 of 2048 x 8000 97 -> 94, but the products beside it, at the power limit, lose as much; with K = 4096 671 -> 925; 96 tiles 15.6 -> 17.9).
+int gated_tile(int kind, int64_t M, int64_t N, int64_t K) {
+    const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128);
+    if ((kind == GATED_UP && K <= 512 && tiles >= 256) || (kind == GATED_DOWN && K <= 1024 && tiles >= 150)) return 5;
     switch (plan_tile(M, N, K)) {
         case TILE_256x256: case TILE_256x256_K32: return 0;
         case TILE_256x128: case TILE_256x128_PASS: return 1;
@@ -523,7 +527,7 @@ struct Call {
     template <class F> fg_status product(int kind, int64_t M, int64_t N, int64_t K, int64_t k_rows, const fg_matrix &a, const fg_matrix &b, F &&f) {
         if (fg_status st = enqueue.status("gated_pad")) return st;
         const bool a_kc = kind != GATED_ROUND_NN, b_kc = kind == GATED_UP || kind == GATED_ROUND_KK;
-        const KernelEntry &k = kernel_table_gated(kind, dtype == FG_BF16)[gated_tile(M, N, K)];
+        const KernelEntry &k = kernel_table_gated(kind, dtype == FG_BF16)[gated_tile(kind, M, N, K)];
         GatedParams p;
         memset(&p, 0, sizeof p);
         p.M = (int32_t)M; p.N = (int32_t)N; p.K = (int32_t)K;

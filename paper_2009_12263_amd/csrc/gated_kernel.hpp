@@ -6,8 +6,9 @@
 //   GATED_ROUND  results rounded to 16 bits.
 // What the first two cost beside their products is memory: with g and u kept, UP writes 10 bytes for each value of h and DOWN reads 8 and writes 6, and with one wave
 // per SIMD nothing else runs on a unit meanwhile.  8192 tokens of 1024 x 2560, binary16: UP 128 us (its product alone takes 61, its bytes 44), DOWN 130; without the loads
-// of g and u 89, without the stores of dg and du 109, without the activations 120, with none of them 61.  Two workgroups a unit on smaller tiles, of which one
-// could store while the other multiplies: 141 and 150; loads and stores with the streaming policy: 133 and 142; 3 to 10 units ahead in place of 6: within 1 %.
+// of g and u 89, without the stores of dg and du 109, without the activations 120, with none of them 61.  (Activations of their own code and, for DOWN, two workgroups a
+// unit, see GatedPair: 124 and 120.)  Loads and stores with the streaming policy: 3 % slower; 3 to 10 units ahead in place of 6: within 1 %; workgroups that begin
+// half a tile apart: none the faster.
 // (FP32 products and passes over them in place of all three, 8192 x 4096 x 10240, forward and backward: 5034 us, 4609 so.)
 #pragma once
 #include "kernel_table.hpp"
@@ -127,7 +128,7 @@ struct GatedCfg : Base {
 
     template <class Blocks>
     __device__ static __forceinline__ void store(const Params &p, const Blocks &blocks, int m_base, int n_base, int lane) {
-        if constexpr (Base::WIDE) own_acc();
+        if constexpr (Base::WIDE) own_acc<Base::WAVES>();
         const int row0 = m_base + lane % ROWS, shift = 8 * (lane / ROWS);
         auto with_act = [&](auto act) {
             constexpr int ACT = decltype(act)::value;
@@ -143,7 +144,7 @@ struct GatedCfg : Base {
     __device__ static __forceinline__ void step() {
         if constexpr (Base::WIDE) {
             __builtin_amdgcn_sched_barrier(0);
-            own_acc();
+            own_acc<Base::WAVES>();
         }
     }
     // the columns that are there, `left` of them
@@ -208,7 +209,7 @@ struct GatedCfg : Base {
     }
 
     // What a lane needs from memory for a unit: g and u of its columns.  Units are requested AHEAD of their turn: a lone wave waits for each otherwise.
-    static constexpr int AHEAD = Base::WIDE ? 6 : 2;
+    static constexpr int AHEAD = Base::WIDE && Base::WAVES == 1 ? 6 : 2;
     struct Pair { eight g, u; };
     __device__ static __forceinline__ eight eight_of(const float *at, int left, bool edge) {
         eight out;
@@ -285,10 +286,18 @@ struct GatedCfg : Base {
     }
 };
 
+// Beside the tiles of a plan GATED_UP and GATED_DOWN have one of 128x128 for two workgroups a unit: 80 KB of LDS (rings of three and two buffers) and half of the
+// registers each, so that one stores, or waits for g and u, while the other multiplies.  Its K loop reaches 0.7 of the 256x256 tile's rate, which short sums are
+// worth (gated_tile in gated.hip).
 // The tiles of a plan: 256x256, 256x128, 128x128 with four buffers, 64x64 and 64x128 with two groups of waves.  On the 64x64 tile a wave has one block
 // of columns, not one of G and one of U: GATED_UP has the 64x128 tile in its place.
 template <class Cfg> KernelEntry gated_entry(const char *name, int kg = 0) {
     return {(const void *)gemm_kernel<Cfg>, name, Cfg::BM, Cfg::BN, Cfg::NTHREADS, Cfg::LDS_BYTES, kg};
+}
+template <bool AKC, bool BKC, bool BF> using GatedPair = TileCfg<128, 128, 64, 2, 2, 2, AKC, BKC, false, 0, 0, true, BF, false, false, false, false, true, 1, false, 2, true>;
+template <int KIND, bool AKC, bool BKC, bool BF> KernelEntry pair_entry(const char *name) {
+    if constexpr (KIND == GATED_UP || KIND == GATED_DOWN) return gated_entry<GatedCfg<GatedPair<AKC, BKC, BF>, KIND>>(name);
+    else return FG_EMPTY_ENTRY;
 }
 template <int KIND, bool AKC, bool BKC, bool BF> const KernelEntry *gated_table(const char *const (&names)[GATED_TILES]) {
     using D = typename std::conditional<KIND == GATED_UP, FG_CFG_KG(AKC, BKC, BF, false, false, 128, 3, true), FG_CFG_KG(AKC, BKC, BF, false, false, 64, 4, true)>::type;
@@ -298,13 +307,14 @@ template <int KIND, bool AKC, bool BKC, bool BF> const KernelEntry *gated_table(
         gated_entry<GatedCfg<FG_CFG_K32(128, 128, 64, 4, 2, 2, AKC, BKC, BF, false), KIND>>(names[2]),
         gated_entry<GatedCfg<D, KIND>>(names[3], 2),
         gated_entry<GatedCfg<FG_CFG_KG(AKC, BKC, BF, false, false, 128, 3, true), KIND>>(names[4], 2),
+        pair_entry<KIND, AKC, BKC, BF>(names[5]),
     };
     return t;
 }
 #define FG_GATED_TABLE(FUNC, KIND, AKC, BKC, BF, NAME)                                                                                       \
     const KernelEntry *FUNC() {                                                                                                              \
         static const char *const names[GATED_TILES] = {NAME "_256x256x64", NAME "_256x128x64", NAME "_128x128x64_deep",                      \
-                                                       (KIND) == GATED_UP ? NAME "_64x128x64" : NAME "_64x64x64", NAME "_64x128x64"};        \
+                                                       (KIND) == GATED_UP ? NAME "_64x128x64" : NAME "_64x64x64", NAME "_64x128x64", NAME "_128x128x64_pair"};        \
         return gated_table<KIND, AKC, BKC, BF>(names);                                                                                       \
     }
 

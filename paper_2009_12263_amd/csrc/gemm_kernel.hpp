@@ -144,7 +144,7 @@ struct TileCfg {
     // that what a unit fetches at a time lies side by side (192x2496x5368, A and B row-major: 21.3 -> 18.0 us).
     static constexpr bool KTURNS = KTURNS_;
     static constexpr int WAVES = WAVES_;                            // waves per SIMD that the registers are to leave room for
-    // WIDE: one wave per SIMD, accumulators in the accumulation registers (wide_loop.hpp).  A's ring has RING_A buffers.
+    // WIDE: one wave per SIMD (WAVES: two, of two workgroups), accumulators in the accumulation registers (wide_loop.hpp).  A's ring has RING_A buffers.
     static constexpr bool WIDE = WIDE_;
     static constexpr int RING_A = WIDE_ && STAGES_ == 2 ? 3 : STAGES_;
     static constexpr int KINC = KTURNS_ ? KG_ : 1;
@@ -229,7 +229,7 @@ struct TileCfg {
     static_assert(!XFORM || (DIAG == 0 && CPLX == 0 && !BF16 && !STRIDED), "element-wise addition on A and B: plain real FP16 matrices");
     static_assert(!CSTREAM || STRIDED, "the streaming variant is a contraction kernel");
     static_assert(!CD16 || (CPLX == 0 && DIAG == 0 && !STRIDED && !ILV), "binary16 C and D: plain real matrix kernels");
-    static_assert(!WIDE || (M16 && NWAVES == 4 && KG == 1 && !STRIDED && !XFORM && 4 * FI * FJ * ACC_SETS <= 256), "one wave per SIMD: plain real matrix kernels on 16x16x32 instructions");
+    static_assert(!WIDE || (M16 && NWAVES == 4 && KG == 1 && !STRIDED && !XFORM && WAVES <= 2 && 4 * FI * FJ * ACC_SETS <= 256 / WAVES), "one wave per SIMD: plain real matrix kernels on 16x16x32 instructions");
     static_assert(!ILV || (CPLX == 1 && STAGES == 2 && !SPREAD && !STRIDED && DIAG == 0), "interleaved storage: plain complex products");
 };
 
@@ -1338,7 +1338,7 @@ __global__ __launch_bounds__(Cfg::NTHREADS, Cfg::WAVES) void gemm_kernel(const t
         constexpr int SETS = Cfg::ACC_SETS;         // (one plane only if there are two)
         AccT acc[P * SETS][TI][TJ];
         if constexpr (Cfg::WIDE) {
-            own_acc();
+            own_acc<Cfg::WAVES>();
             static_for<4 * TI * TJ * SETS>([](auto r) { acc_zero<decltype(r)::value>(); });
         }
 #pragma unroll

@@ -91,8 +91,8 @@ enum { CTILE_64x64 = 2, CTILE_64x64_KG2 = 3, CTILE_COUNT = 4 };
 int plan_tile(int64_t M, int64_t N, int64_t K);
 fg_status launch_product(const KernelEntry &k, GemmParams &p, hipStream_t stream, int more_tiles = 0);
 
-// The products of the gated feed-forward block (gated_kernel.hpp): index = tile.
-enum { GATED_KINDS = 5, GATED_TILES = 5 };
+// The products of the gated feed-forward block (gated_kernel.hpp): index = tile; the last one is empty for some kinds.
+enum { GATED_KINDS = 5, GATED_TILES = 6 };
 const KernelEntry *kernel_table_gated(int kind, bool bf16);
 
 // Load the kernels of the operators on rows (each file's are one image), which their first launch would do otherwise.

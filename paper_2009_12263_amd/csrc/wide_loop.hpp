@@ -36,12 +36,20 @@ __device__ __forceinline__ void static_for(F &&f) { static_for_seq(f, std::make_
 // own in one across it.  That leaves what lives between two of them; that nothing but this assembly touches an accumulation register is
 // checked in the compiled kernels (tests/test_compiled_kernels.py).
 #define FG_ACC10(d) "a" #d "0", "a" #d "1", "a" #d "2", "a" #d "3", "a" #d "4", "a" #d "5", "a" #d "6", "a" #d "7", "a" #d "8", "a" #d "9"
+#define FG_ACC_HALF                                                                                                                     \
+    "a0", "a1", "a2", "a3", "a4", "a5", "a6", "a7", "a8", "a9", FG_ACC10(1), FG_ACC10(2), FG_ACC10(3), FG_ACC10(4), FG_ACC10(5),        \
+    FG_ACC10(6), FG_ACC10(7), FG_ACC10(8), FG_ACC10(9), FG_ACC10(10), FG_ACC10(11), "a120", "a121", "a122", "a123", "a124", "a125", "a126", "a127"
 #define FG_ACC_ALL                                                                                                                      \
     "a0", "a1", "a2", "a3", "a4", "a5", "a6", "a7", "a8", "a9", FG_ACC10(1), FG_ACC10(2), FG_ACC10(3), FG_ACC10(4), FG_ACC10(5),        \
     FG_ACC10(6), FG_ACC10(7), FG_ACC10(8), FG_ACC10(9), FG_ACC10(10), FG_ACC10(11), FG_ACC10(12), FG_ACC10(13), FG_ACC10(14),           \
     FG_ACC10(15), FG_ACC10(16), FG_ACC10(17), FG_ACC10(18), FG_ACC10(19), FG_ACC10(20), FG_ACC10(21), FG_ACC10(22), FG_ACC10(23),       \
     FG_ACC10(24), "a250", "a251", "a252", "a253", "a254", "a255"
-__device__ __forceinline__ void own_acc() { asm volatile("" ::: FG_ACC_ALL); }
+template <int WAVES = 1>
+__device__ __forceinline__ void own_acc() {
+    // (two waves per SIMD: half of them)
+    if constexpr (WAVES == 1) asm volatile("" ::: FG_ACC_ALL);
+    else asm volatile("" ::: FG_ACC_HALF);
+}
 // Registers R .. R + 3.  The two wait states are those that a lane exchange of the results needs; the compiler, which does not
 // see vector instructions in the assembly, would not add them.
 template <int R>
@@ -210,7 +218,7 @@ __device__ __forceinline__ void k_loop_wide(LA &la, LB &lb, const FA &fa, const 
         constexpr int ca = a_tag, cb = b_tag;
         FG_LDS const char *ta = lds_a + ca * Cfg::A_TILE_BYTES, *tb = lds_b + cb * Cfg::B_TILE_BYTES;
         FG_LDS const char *na = lds_a + (ca + 1) % RA * Cfg::A_TILE_BYTES, *nb = lds_b + (cb + 1) % RB * Cfg::B_TILE_BYTES;
-        own_acc();
+        own_acc<Cfg::WAVES>();
         __builtin_amdgcn_sched_barrier(0);
         static_for<SLOTS>([&](auto s_tag) {
             constexpr int s = s_tag, i = s / TJ, j = s % TJ, l = (s - 1) / LOAD_A;
@@ -274,7 +282,7 @@ __device__ __forceinline__ void k_loop_wide(LA &la, LB &lb, const FA &fa, const 
     // the last matrix instructions write their results this long after they were issued; no load stays behind
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
-    own_acc();
+    own_acc<Cfg::WAVES>();
     __builtin_amdgcn_sched_barrier(0);
 }
 

@@ -6,7 +6,7 @@ from tests.test_compiled_kernels import _registers, kernels  # noqa: F401
 
 def test_accumulators_belong_to_the_assembly(kernels):  # noqa: F811
     wide = {name: code for name, code in kernels.items() if "11gemm_kernelINS_8GatedCfg" in name and "Lb1EEELi" in name}
-    assert len(wide) == 30                     # three tiles, five kinds of products, two types
+    assert len(wide) == 34                     # three tiles, five kinds of products, two types; and two kinds on the tile for two workgroups a unit
     for name, code in wide.items():
         cleared, read = [], set()
         for op, rest in code:
@@ -23,6 +23,7 @@ def test_accumulators_belong_to_the_assembly(kernels):  # noqa: F811
                 assert op.startswith("v_mfma_f32_16x16x32_") and touched == [operands[0], operands[3]] and operands[0] == operands[3], (name, op, rest)
         assert sorted(cleared) == [("a", i) for i in range(len(cleared))] and len(cleared) in (128, 256), name
         assert read == set(cleared), name
+    assert sum("Li1ELb0ELi2ELb1EEELi" in name for name in wide) == 4
 
 
 def test_nothing_is_spilled(kernels):  # noqa: F811

@@ -124,7 +124,8 @@ class Case:
 
 ALL = ("y", "gu", "dx", "dw_in", "dw_out")
 SIZES = [(1, 8, 8), (1, 1, 1), (1, 64, 128), (2, 1024, 2560), (5, 33, 17), (15, 129, 40), (16, 256, 512), (17, 72, 264), (33, 500, 31), (48, 264, 1000), (64, 512, 136),
-         (65, 100, 36), (65, 520, 264), (96, 1000, 500), (129, 128, 1032), (200, 256, 40), (300, 257, 131), (513, 264, 520), (777, 1024, 768)]
+         (65, 100, 36), (65, 520, 264), (96, 1000, 500), (129, 128, 1032), (200, 256, 40), (300, 257, 131), (513, 264, 520), (777, 1024, 768),
+         (2100, 200, 1104), (2101, 203, 1103), (1290, 1024, 1664)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
