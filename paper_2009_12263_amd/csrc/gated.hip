@@ -18,6 +18,7 @@
 #include <type_traits>
 
 #include "cache_policy.hpp"
+#include "few_tokens.hpp"
 #include "gated_kernel.hpp"
 
 namespace fg {
@@ -196,11 +197,6 @@ struct FewArgs {
     int32_t rows, lo, n, k;             // of x; see above; rows of w (UP: of G), and their values
     Activation act;
 };
-template <class T>
-__device__ __forceinline__ floatx4 mfma_16x16x32(typename RowPiece<T>::vec a, typename RowPiece<T>::vec b, floatx4 c) {
-    if constexpr (std::is_same<T, bf16_t>::value) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
 // Where h's value of row r and column c is, and the values of all of it.
 template <int NB> __host__ __device__ __forceinline__ int64_t few_place(int r, int c) { return ((int64_t)(c >> 5) * NB + (r >> 4)) * 512 + ((c >> 3) & 3) * 128 + (r & 15) * 8 + (c & 7); }
 constexpr int64_t few_values(int64_t rows, int64_t k) { return (k + 31) / 32 * 512 * ((rows + 15) / 16); }
@@ -383,8 +379,8 @@ struct GradSpace : Space {
         const int64_t tp = up(parts * T, 8);
         down_by_sums = parts == 2 || by_sums(T, H, dp);
         x_by_sums = parts == 2 || by_sums(T, D, gp);
-        in_by_sums = by_sums(2 * H, D, tp);
-        out_by_sums = by_sums(D, H, tp);
+        in_by_sums = parts * T > kFewTokens && by_sums(2 * H, D, tp);
+        out_by_sums = parts * T > kFewTokens && by_sums(D, H, tp);
         if (copy_dy || parts == 2) dy = take(parts * T * dp * 2);
         if (copy_x || parts == 2) x = take(parts * T * dp * 2);
         if (copy_in) w_in = take(2 * H * dp * 2);
@@ -735,6 +731,16 @@ fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const f
             if (fg_status st = call.by_sums(at, rows, dim, gp, 2 * hidden, dgu, w_in, sums)) return st;
             call.round<true>(sums, dX, tokens, dim);
         } else if (fg_status st = call.rounded(at, at.sums, at.x_by_sums, GATED_ROUND_KN, tokens, dim, gp, 2 * hidden, dgu, w_in, dX)) return st;
+    }
+    if (rows <= kFewTokens) {
+        with_half(X->dtype, [&](auto t) {
+            using T = decltype(t);
+            DwOfFew<T> in = {(const T *)dgu.re, (const T *)x.re, nullptr, gp, gp, x.ld, 0, 0, dim, 0}, out = {(const T *)dy.re, (const T *)h.re, nullptr, dy.ld, dp, hp, 0, 0, hidden, 0};
+            if (dW_in) { in.out = (T *)dW_in->re; in.ldo = dW_in->ld; in.words = 2 * hidden; }
+            if (dW_out) { out.out = (T *)dW_out->re; out.ldo = dW_out->ld; out.words = dim; }
+            if (dW_in || dW_out) launch_dw_of_few<T>(call.enqueue, in, out, nullptr, rows);
+        });
+        return call.enqueue.status("dw_of_few");
     }
     const int tile = dW_in && dW_out ? tile_of_both(at, 2 * hidden, dim, dim, hidden, rows) : -1;
     if (tile >= 0) return call.both_weights(tile, rows, dgu, x, dW_in, 2 * hidden, dim, dy, h, dW_out, dim, hidden);

@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "cache_policy.hpp"
+#include "few_tokens.hpp"
 #include "xent_kernel.hpp"
 
 namespace fg {
@@ -94,7 +95,7 @@ __global__ __launch_bounds__(1024) void xent_join(const XentStat *stats, int par
 //
 // The others: x's rows for the products, aligned and padded like xent_pad's, with zeros for the tokens that are left out.  Their dz is zero, but a row of a
 // token nobody asks for may hold anything, and in dw = dz^T x zero times infinity or NaN would reach every word.  (Beside the scaling's chain of latencies up
-// to 64 tokens cost nothing, 4.1 us either way; looked up by xent_dw_few instead, the targets took it from 41 to 47 us, with 64 tokens from 56 to 80.)
+// to 64 tokens cost nothing, 4.1 us either way; looked up by dw_of_few instead, the targets took it from 41 to 47 us, with 64 tokens from 56 to 80.)
 template <class T>
 __global__ __launch_bounds__(1024) void xent_prepare(const float *dloss, int64_t dloss_inc, const void *targets, bool wide, int vocab, int64_t tokens, float scale,
                                                      float *factor, const T *x, int64_t ldx, T *out, int64_t ldo, int cols) {
@@ -140,76 +141,10 @@ __global__ __launch_bounds__(256) void xent_round(const float *in, int64_t ld, c
     }
 }
 
-// ---- dw of few tokens ------------------------------------------------------------------------------------------
-// dw = scale dz^T x where the tokens fit KS steps of 32 k of the matrix units: all of it is writing dw.  A wave takes 16 J words and 128 columns
-// with one read of both operands.  A lane reads J words and 8 columns of 8 tokens' rows and turns the values over in registers (one byte permutation each
-// pair): vectors of 8 tokens, of which the j-th of dz and the i-th of x serve the product of words J m + j with columns 8 n + i.  A lane's
-// results of i = 0 .. 7 are then 16 bytes of a row of dw, and those of 16 lanes two lines.  Bound by the writes (65536 words x 2048: 16 tokens 41 us or 6.5 TB/s, 64 tokens
-// 56); the tiled kernels, whose one wave a SIMD does not write while it multiplies, take 84 and 88 (50001 x 1001, 33 tokens: 25 and 81).  With 128 tokens the operands fill
-// the registers: 103 us and 103.
-template <class T>
-__device__ __forceinline__ floatx4 mfma_16x16x32(typename RowPiece<T>::vec a, typename RowPiece<T>::vec b, floatx4 c) {
-    if constexpr (std::is_same<T, bf16_t>::value) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
-
-template <class T, int KS, int J>
-__global__ __launch_bounds__(256, 2) void xent_dw_few(const T *dz, int64_t ld_dz, const T *x, int64_t ldx, const float *factor, T *out, int64_t ldo, int tokens,
-                                                   int words, int dim, int strips) {
-    typedef typename RowPiece<T>::vec vec;
-    const int lane = threadIdx.x & 63, at = lane & 15, quarter = lane >> 4;
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    typedef typename RowPiece<T, J>::vec words_vec;
-    const int64_t word0 = item / strips * (16 * J);
-    if (word0 >= words) return;
-    const int p = (int)(item % strips) * 16 + at, pieces = (dim + 7) / 8, there = min(p, pieces - 1);
-    const bool in = word0 + at * J < ld_dz;
-    vec a[KS][J], b[KS][8];
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        words_vec w[8] = {};
-        vec v[8] = {};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int t = s * 32 + quarter * 8 + e;
-            if (t < tokens) {
-                if (in) w[e] = *(const words_vec *)(dz + t * ld_dz + word0 + at * J);
-                v[e] = load_raw<T, 8>(x + t * ldx, there, dim);
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-#pragma unroll
-            for (int j = 0; j < J; ++j) a[s][j][e] = w[e][j];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) b[s][i][e] = v[e][i];
-        }
-    }
-    const float f = factor[1];
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-        floatx4 sum[8] = {};
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] = mfma_16x16x32<T>(a[s][j], b[s][i], sum[i]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t word = word0 + (quarter * 4 + r) * J + j;
-            if (word >= words || p >= pieces) continue;
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = sum[i][r] * f;
-            store_piece(out + word * ldo, p, dim, v);
-        }
-    }
-}
-
 // ---- host ----------------------------------------------------------------------------------------------------
 constexpr int64_t kPieceBytes = 256ll << 20;        // of dz: what the memory-side cache holds
 constexpr int64_t kCopyBytes = 64ll << 20;          // of a piece of W that is copied
 constexpr int64_t kTokenBlock = 16384;              // tokens whose statistics are kept at a time
-constexpr int64_t kFewTokens = 64;                  // whose dw xent_dw_few writes
 constexpr int64_t kFewestWords = 256;               // of a piece; pieces begin at multiples of it
 constexpr int64_t kMostWords = kKContiguousLd - kFewestWords;          // of a piece of dz, whose rows the product with dX reads along the words
 
@@ -483,23 +418,11 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
         p.D = (float *)dz.re; p.ldd = at.ld_dz;
         if (fg_status st = launch_product(kz, p, stream)) return st;
         if (tokens <= kFewTokens) {
-            const int strips = (int)((dim + 127) / 128);
             with_half(X->dtype, [&](auto t) {
                 using T = decltype(t);
-                auto few = [&](auto steps, auto run) {
-                    constexpr int KS = decltype(steps)::value, J = decltype(run)::value;
-                    const int64_t waves = (n + 16 * J - 1) / (16 * J) * strips;
-                    enqueue(xent_dw_few<T, KS, J>, dim3((unsigned)((waves + 3) / 4)), dim3(256), (const T *)dz.re, at.ld_dz, (const T *)x.re, x.ld, factor,
-                                       (T *)row_at(dW, v0), dW->ld, (int)tokens, (int)n, (int)dim, strips);
-                };
-                using std::integral_constant;
-                // Fewer waves than there are SIMDs: 64 words each instead of 128 (2496 words x 1000: 16 tokens 5.0 us and 6.7, 64 tokens 5.9 and 8.0;
-                // 65536 x 2048: 53 and 41, 73 and 56).
-                const bool small = (n + 127) / 128 * strips < 1024;
-                if (tokens <= 32) small ? few(integral_constant<int, 1>{}, integral_constant<int, 4>{}) : few(integral_constant<int, 1>{}, integral_constant<int, 8>{});
-                else small ? few(integral_constant<int, 2>{}, integral_constant<int, 4>{}) : few(integral_constant<int, 2>{}, integral_constant<int, 8>{});
+                launch_dw_of_few<T>(enqueue, {(const T *)dz.re, (const T *)x.re, (T *)row_at(dW, v0), at.ld_dz, at.ld_dz, x.ld, dW->ld, n, dim, 0}, {}, factor, tokens);
             });
-            if (fg_status st = enqueue.status("xent_dw_few")) return st;
+            if (fg_status st = enqueue.status("dw_of_few")) return st;
         } else {
             // neither operand is K-contiguous: any number of tokens
             const KernelEntry &kw = kernel_table_xent(XENT_ROUND, bf16)[xent_tile(n, dim, tokens)];
