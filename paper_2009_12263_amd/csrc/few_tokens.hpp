@@ -25,6 +25,7 @@ template <class T> struct DwOfFew {
     const T *dz, *x;
     T *out;
     int64_t ld_dz, have, ldx, ldo, words, dim, items;           // items: of the launch, set by it
+    int32_t dz_again, x_again;              // a token from this one on has the row of the one so many before it (0: each has its own)
 };
 // One or two such products of the same tokens in a launch.  factor[1]: what results are multiplied by.
 template <class T> struct DwsOfFew { DwOfFew<T> at[2]; };
@@ -54,8 +55,9 @@ __global__ __launch_bounds__(256, 2) void dw_of_few(const DwsOfFew<T> products, 
         for (int e = 0; e < 8; ++e) {
             const int t = s * 32 + quarter * 8 + e;
             if (t < tokens) {
-                if (in) w[e] = *(const words_vec *)(dz + t * ld_dz + word0 + at * J);
-                v[e] = load_raw<T, 8>(x + t * ldx, there, dim);
+                const int of_dz = q.dz_again && t >= q.dz_again ? t - q.dz_again : t, of_x = q.x_again && t >= q.x_again ? t - q.x_again : t;
+                if (in) w[e] = *(const words_vec *)(dz + of_dz * ld_dz + word0 + at * J);
+                v[e] = load_raw<T, 8>(x + of_x * ldx, there, dim);
             }
         }
 #pragma unroll

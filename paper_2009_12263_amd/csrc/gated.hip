@@ -370,8 +370,8 @@ struct ForwardSpace : Space {
     }
 };
 struct GradSpace : Space {
-    int64_t parts;
-    bool down_by_sums, x_by_sums, in_by_sums, out_by_sums;
+    int64_t parts, times;           // times: how often dY and X are needed, one copy behind the other
+    bool few, down_by_sums, x_by_sums, in_by_sums, out_by_sums;         // few: dw_of_few writes the weights' gradients
     int64_t dy = 0, x = 0, w_in = 0, w_out = 0, dh = 0, h, dgu, sums = 0;
     GradSpace(int64_t T, int64_t D, int64_t H, bool copy_dy, bool copy_x, bool copy_in, bool copy_out) {
         const int64_t dp = up(D, 8), hp = up(H, 8), gp = up(2 * H, 8);
@@ -379,10 +379,12 @@ struct GradSpace : Space {
         const int64_t tp = up(parts * T, 8);
         down_by_sums = parts == 2 || by_sums(T, H, dp);
         x_by_sums = parts == 2 || by_sums(T, D, gp);
-        in_by_sums = parts * T > kFewTokens && by_sums(2 * H, D, tp);
-        out_by_sums = parts * T > kFewTokens && by_sums(D, H, tp);
-        if (copy_dy || parts == 2) dy = take(parts * T * dp * 2);
-        if (copy_x || parts == 2) x = take(parts * T * dp * 2);
+        few = parts * T <= kFewTokens;
+        in_by_sums = !few && by_sums(2 * H, D, tp);
+        out_by_sums = !few && by_sums(D, H, tp);
+        times = few ? 1 : parts;
+        if (copy_dy || times == 2) dy = take(times * T * dp * 2);
+        if ((copy_x || times == 2) && !few) x = take(times * T * dp * 2);
         if (copy_in) w_in = take(2 * H * dp * 2);
         if (copy_out) w_out = take(D * hp * 2);
         h = take(parts * T * hp * 2);
@@ -701,8 +703,8 @@ fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const f
     const GradSpace at(tokens, dim, hidden, copy_dy, copy_x, copy_in, copy_out);
     if (fg_status st = check_workspace(workspace, workspace_bytes, at.bytes)) return st;
     const int64_t dp = up(dim, 8), hp = up(hidden, 8), gp = up(2 * hidden, 8), rows = at.parts * tokens, tp = up(rows, 8);
-    const fg_matrix dy = call.aligned(dY, tokens, dim, copy_dy, at.dy, at.parts), w_out = call.aligned(W_out, dim, hidden, copy_out, at.w_out),
-                    w_in = dX ? call.aligned(W_in, 2 * hidden, dim, copy_in, at.w_in) : *W_in, x = dW_in ? call.aligned(X, tokens, dim, copy_x, at.x, at.parts) : *X;
+    const fg_matrix dy = call.aligned(dY, tokens, dim, copy_dy, at.dy, at.times), w_out = call.aligned(W_out, dim, hidden, copy_out, at.w_out),
+                    w_in = dX ? call.aligned(W_in, 2 * hidden, dim, copy_in, at.w_in) : *W_in, x = dW_in && !at.few ? call.aligned(X, tokens, dim, copy_x, at.x, at.times) : *X;
     call.copies();
     const fg_matrix h = rows_of(call.space + at.h, X->dtype, hp), dgu = rows_of(call.space + at.dgu, X->dtype, gp);
     const Activation activation = Activation::of(act);
@@ -732,10 +734,12 @@ fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const f
             call.round<true>(sums, dX, tokens, dim);
         } else if (fg_status st = call.rounded(at, at.sums, at.x_by_sums, GATED_ROUND_KN, tokens, dim, gp, 2 * hidden, dgu, w_in, dX)) return st;
     }
-    if (rows <= kFewTokens) {
+    if (at.few) {
         with_half(X->dtype, [&](auto t) {
             using T = decltype(t);
-            DwOfFew<T> in = {(const T *)dgu.re, (const T *)x.re, nullptr, gp, gp, x.ld, 0, 0, dim, 0}, out = {(const T *)dy.re, (const T *)h.re, nullptr, dy.ld, dp, hp, 0, 0, hidden, 0};
+            const int32_t again = at.parts == 2 ? (int32_t)tokens : 0;          // (both parts of a token have its row of x and dy)
+            DwOfFew<T> in = {(const T *)dgu.re, (const T *)X->re, nullptr, gp, gp, X->ld, 0, 0, dim, 0, 0, again},
+                       out = {(const T *)dy.re, (const T *)h.re, nullptr, dy.ld, dp, hp, 0, 0, hidden, 0, again, 0};
             if (dW_in) { in.out = (T *)dW_in->re; in.ldo = dW_in->ld; in.words = 2 * hidden; }
             if (dW_out) { out.out = (T *)dW_out->re; out.ldo = dW_out->ld; out.words = dim; }
             if (dW_in || dW_out) launch_dw_of_few<T>(call.enqueue, in, out, nullptr, rows);

@@ -420,7 +420,7 @@ fg_status fg_linear_xent_grad(int64_t tokens, int64_t vocab, int64_t dim, const 
         if (tokens <= kFewTokens) {
             with_half(X->dtype, [&](auto t) {
                 using T = decltype(t);
-                launch_dw_of_few<T>(enqueue, {(const T *)dz.re, (const T *)x.re, (T *)row_at(dW, v0), at.ld_dz, at.ld_dz, x.ld, dW->ld, n, dim, 0}, {}, factor, tokens);
+                launch_dw_of_few<T>(enqueue, {(const T *)dz.re, (const T *)x.re, (T *)row_at(dW, v0), at.ld_dz, at.ld_dz, x.ld, dW->ld, n, dim, 0, 0, 0}, {}, factor, tokens);
             });
             if (fg_status st = enqueue.status("dw_of_few")) return st;
         } else {
