@@ -6,13 +6,13 @@
 //
 // Bound by memory: each value of a tensor is read and written once (28 bytes a 16-bit parameter with an FP32 copy, gradient and FP32 moments,
 // 10 with moments in eight bits and no copy).  A launch covers the tensors that a kernel's arguments hold; each workgroup takes a
-// chunk of one, found by bisection of the chunks' numbers.  Nothing is kept between calls: the tensors' addresses travel with the launch.
+// chunk of one, which its lanes find together.  Nothing is kept between calls: the tensors' addresses travel with the launch.
 //
 // Moments in eight bits (e4m3) have an FP32 scale for each 256 values, the largest of them / 448.  Of v the root is kept: its range
 // of 2^17 is one of 2^34 of v.  A root that is not zero is held at least as the smallest such number: m / (root + eps) of a v that was rounded
 // to zero would be m / eps.  The step itself uses m and v in FP32, as they are before they are rounded.
 //
-// Measured: 386 M values, bfloat16 with FP32 copies 2076 us (5.2 TB/s), in eight bits 762 (5.1), 75 M FP32 values 398 (5.3), 193 tensors of 1.6 M values in four launches 26; the
+// Measured: 386 M values, bfloat16 with FP32 copies 2076 us (5.2 TB/s), in eight bits 762 (5.1), 75 M FP32 values 398 (5.3), 193 tensors of 1.6 M values in two launches 18; the
 // norm of 386 M binary16 values 129 (6.0).
 //
 // The operations are written one by one, without fused ones: what eight bits hold changes by 1/16 where a sum falls on the other side of a border.
@@ -43,12 +43,42 @@ template <bool SMALL> struct TensorArg {
     float *master;
     void *m, *v;
     int64_t n;
+    int32_t kind;
 };
 template <> struct TensorArg<true> : TensorArg<false> { float *m_scale, *v_scale; };
-// Arguments are copied through the command path: few tensors have a short list of them.  A list has at most as many as a wave has lanes, and as fit 4 KB.
+// The same of a short tensor whose memory is near to the others': the arrays' distances from the lowest address, in steps of two bytes, 32 bits each and five more
+// beside n and kind.  Twice as many fit a launch.
+constexpr int kNearStep = 2, kNearBits = 23, kKindBits = 4, kFarBits = 5;          // kNearBits: of n
+constexpr uint64_t kNear = (uint64_t)kNearStep << (32 + kFarBits);
+template <bool SMALL> struct NearArg {
+    static constexpr int kArrays = SMALL ? 7 : 5;           // p, g, master, m, v, m_scale, v_scale
+    uint32_t low[kArrays], more[2];
+    void set(int64_t n, int kind, uint64_t base, const void *const (&arrays)[kArrays]) {
+        uint64_t rest = (uint64_t)n | (uint64_t)kind << kNearBits;
+        for (int i = 0; i < kArrays; ++i) {
+            const uint64_t at = arrays[i] && n > 0 ? ((uint64_t)arrays[i] - base) / kNearStep : 0;
+            low[i] = (uint32_t)at;
+            rest |= at >> 32 << (kNearBits + kKindBits + kFarBits * i);
+        }
+        more[0] = (uint32_t)rest;
+        more[1] = (uint32_t)(rest >> 32);
+    }
+    __device__ __forceinline__ TensorArg<SMALL> whole(char *base) const {
+        const uint64_t rest = more[0] | (uint64_t)more[1] << 32;
+        auto there = [&](int i) { return base + (low[i] | (rest >> (kNearBits + kKindBits + kFarBits * i) & ((1 << kFarBits) - 1)) << 32) * kNearStep; };
+        TensorArg<SMALL> t;
+        t.p = there(0); t.g = there(1); t.master = (float *)there(2); t.m = there(3); t.v = there(4);
+        if constexpr (SMALL) { t.m_scale = (float *)there(5); t.v_scale = (float *)there(6); }
+        t.n = (int64_t)(rest & ((1 << kNearBits) - 1));
+        t.kind = (int32_t)(rest >> kNearBits & ((1 << kKindBits) - 1));
+        return t;
+    }
+};
+static_assert(kNearBits + kKindBits + 7 * kFarBits <= 64 && kSmallModel <= 1 << kNearBits, "");
+
+// Arguments are copied through the command path: few tensors have a short list of them.  A list has at most two for each lane of a wave, and as many as fit 4 KB.
 template <class Arg, int CAP> struct List {
     int32_t first[CAP];                     // number of a tensor's first chunk in the launch; behind the last tensor the number of all
-    int32_t kind[CAP];
     Arg at[CAP];
 };
 
@@ -56,6 +86,7 @@ struct StepArgs {
     double lr, beta1, beta2, eps, decay;
     const int64_t *step;
     const float *factor, *lr_factor;
+    char *base;                             // of NearArg
     int32_t chunk;
 };
 // What a step needs of them, in FP32.
@@ -63,14 +94,18 @@ struct Rates {
     float beta1, other1, beta2, other2, eps, keep, rate, root, factor;
 };
 
-// Which tensor chunk c is in: the last one that does not begin behind it.  Each lane looks at one: a bisection, six reads of the arguments one after the other, took
+// Which tensor chunk c is in: the last one that does not begin behind it.  Each lane looks at one or two: a bisection, six reads of the arguments one after the other, took
 // 8 us of a launch, whose workgroups all wait for them.
 template <class L, int CAP = sizeof(L::first) / 4>
 __device__ __forceinline__ int tensor_of(const L &list, int c) {
-    static_assert(CAP <= 64, "");
+    static_assert(CAP <= 128, "");
     const int lane = threadIdx.x & 63;
-    return __builtin_popcountll(__ballot(lane < CAP && list.first[lane < CAP ? lane : 0] <= c)) - 1;
+    int before = __builtin_popcountll(__ballot(lane < CAP && list.first[lane < CAP ? lane : 0] <= c));
+    if constexpr (CAP > 64) before += __builtin_popcountll(__ballot(64 + lane < CAP && list.first[64 + lane < CAP ? 64 + lane : 0] <= c));
+    return before - 1;
 }
+template <bool SMALL> __device__ __forceinline__ TensorArg<SMALL> whole(const TensorArg<SMALL> &t, char *) { return t; }
+template <bool SMALL> __device__ __forceinline__ TensorArg<SMALL> whole(const NearArg<SMALL> &t, char *base) { return t.whole(base); }
 
 // x^t by squaring; 64-bit, for 1 - x^t of an x near 1.
 __device__ __forceinline__ double power(double x, int64_t t) {
@@ -242,13 +277,15 @@ __device__ __forceinline__ void step_chunk(const TensorArg<SMALL> &t, const Step
 
 // kind: the type of the parameters (FG_F16, FG_BF16, FG_F32), + 4 with FP32 gradients, + 8 with an FP32 copy of the parameters
 constexpr int kWideGrad = 4, kCopy = 8;
+static_assert(FG_F32 < kWideGrad && FG_BF16 < kWideGrad && kWideGrad + kCopy + FG_BF16 < 1 << kKindBits, "");
 
-template <int CAP, bool SMALL>
-__global__ __launch_bounds__(kThreads) void adamw(const List<TensorArg<SMALL>, CAP> a, const StepArgs s) {
+// Arg: TensorArg or NearArg
+template <int CAP, bool SMALL, class Arg>
+__global__ __launch_bounds__(kThreads) void adamw(const List<Arg, CAP> a, const StepArgs s) {
     const int which = tensor_of(a, (int)blockIdx.x);
-    const TensorArg<SMALL> t = a.at[which];
+    const TensorArg<SMALL> t = whole<SMALL>(a.at[which], s.base);
     const int64_t begin = ((int64_t)blockIdx.x - a.first[which]) * s.chunk;
-    switch (a.kind[which]) {
+    switch (t.kind) {
         case FG_F16: return step_chunk<f16_t, f16_t, false, SMALL>(t, s, begin, s.chunk);
         case FG_BF16: return step_chunk<bf16_t, bf16_t, false, SMALL>(t, s, begin, s.chunk);
         case FG_F32 + kWideGrad: return step_chunk<float, float, false, SMALL>(t, s, begin, s.chunk);
@@ -266,6 +303,7 @@ constexpr int kNormGroups = 2048;           // of a launch, at most
 struct GradArg {
     const void *g;
     int64_t n;
+    int32_t dtype;
 };
 
 template <class G>
@@ -300,10 +338,10 @@ __global__ __launch_bounds__(kThreads) void grad_squares(const List<GradArg, CAP
     __shared__ double slots[kThreads];
     double sum = 0.0;
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int which = tensor_of(a, c), dtype = a.kind[which];
+        const int which = tensor_of(a, c);
         const GradArg t = a.at[which];
         const int64_t begin = ((int64_t)c - a.first[which]) * kChunk;
-        sum += dtype == FG_F16 ? squares_of<f16_t>(t, begin) : dtype == FG_BF16 ? squares_of<bf16_t>(t, begin) : squares_of<float>(t, begin);
+        sum += t.dtype == FG_F16 ? squares_of<f16_t>(t, begin) : t.dtype == FG_BF16 ? squares_of<bf16_t>(t, begin) : squares_of<float>(t, begin);
     }
     sum = group_total<kThreads / 64>(sum, slots);
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
@@ -322,8 +360,9 @@ __global__ __launch_bounds__(1024) void grad_norm(const double *partial, int64_t
 }
 
 // ---- host ------------------------------------------------------------------------------------------------
-constexpr int kFewTensors = 6, kFewGrads = 16, kMostGrads = 64;
+constexpr int kFewTensors = 6, kFewGrads = 16, kMoreGrads = 64, kMostGrads = 128;
 template <bool SMALL> constexpr int kMostTensors = SMALL ? 48 : 64;
+template <bool SMALL> constexpr int kMostNear = SMALL ? 100 : 120;
 constexpr int64_t kMostChunks = 1 << 23;    // of a launch: fewer than 2^32 threads
 
 int64_t chunks_of(int64_t n, int chunk) { return (n + chunk - 1) / chunk; }
@@ -385,6 +424,21 @@ fg_status check_apart(int64_t count, const fg_adamw_tensor *tensors) {
     return FG_OK;
 }
 
+// The lowest address of the tensors' memory; 0 where some begins too far from it for NearArg.
+uintptr_t near_base(int64_t count, const fg_adamw_tensor *tensors) {
+    uintptr_t low = UINTPTR_MAX, high = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        const fg_adamw_tensor &t = tensors[i];
+        if (t.n == 0) continue;
+        for (const void *p : {(const void *)t.param, t.grad, (const void *)t.master, (const void *)t.exp_avg, (const void *)t.exp_avg_sq, (const void *)t.avg_scale, (const void *)t.sq_scale}) {
+            if (!p) continue;
+            low = std::min(low, (uintptr_t)p);
+            high = std::max(high, (uintptr_t)p);
+        }
+    }
+    return high - low < kNear ? low : 0;
+}
+
 // Hands out tensors to launches: f(first tensor, tensors, chunks) with as many as `most` and kMostChunks allow; tensors without values count as well.
 template <class Length, class F> void in_launches(int64_t count, int most, int chunk, Length &&length, F &&f) {
     int64_t begin = 0, chunks = 0;
@@ -399,13 +453,13 @@ template <class Length, class F> void in_launches(int64_t count, int most, int c
     }
     if (count > begin) f(begin, (int)(count - begin), chunks);
 }
-// The list of a launch's n tensors: fill(i, its arguments) gives each one's kind, length(i) its values.
+// The list of a launch's n tensors: fill(i, its arguments) sets one's arguments, length(i) its values.
 template <class Arg, int CAP, class Length, class Fill> void make_list(List<Arg, CAP> &list, int n, int chunk, Length &&length, Fill &&fill) {
     int64_t first = 0;
     for (int i = 0; i < CAP; ++i) {
         list.first[i] = (int32_t)first;
         if (i >= n) continue;
-        list.kind[i] = fill(i, list.at[i]);
+        fill(i, list.at[i]);
         first += chunks_of(length(i), chunk);
     }
 }
@@ -446,23 +500,32 @@ fg_status fg_adamw(int64_t count, const fg_adamw_tensor *tensors, const int64_t 
     Launches enqueue(hip_stream);
     auto all = [&](auto small) {
         constexpr bool SMALL = decltype(small)::value;
-        auto launch = [&](auto cap, int64_t begin, int n, int64_t chunks) {
+        // A small model takes as long as its launches; one of more tensors than the long list has is handed over as NearArg where its memory allows it
+        // (193 tensors of 1.6 M values: four launches 24.7 us, two 17.8; with moments in eight bits five 45 and two 19).
+        const uintptr_t base = values < kSmallModel && count > kMostTensors<SMALL> ? near_base(count, tensors) : 0;
+        auto launch = [&](auto cap, auto list_of, int64_t begin, int n, int64_t chunks) {
             constexpr int CAP = decltype(cap)::value;
-            List<TensorArg<SMALL>, CAP> a = {};
+            using Arg = decltype(list_of);
+            List<Arg, CAP> a = {};
             static_assert(sizeof a + sizeof(StepArgs) <= 4096, "");
-            make_list(a, n, chunk, [&](int i) { return tensors[begin + i].n; }, [&](int i, TensorArg<SMALL> &arg) {
+            make_list(a, n, chunk, [&](int i) { return tensors[begin + i].n; }, [&](int i, Arg &arg) {
                 const fg_adamw_tensor &t = tensors[begin + i];
-                arg.p = t.param; arg.g = t.grad; arg.master = t.master; arg.m = t.exp_avg; arg.v = t.exp_avg_sq; arg.n = t.n;
-                if constexpr (SMALL) { arg.m_scale = t.avg_scale; arg.v_scale = t.sq_scale; }
-                return t.param_dtype + (t.grad_dtype == FG_F32 ? kWideGrad : 0) + (t.master ? kCopy : 0);
+                const int kind = t.param_dtype + (t.grad_dtype == FG_F32 ? kWideGrad : 0) + (t.master ? kCopy : 0);
+                if constexpr (!std::is_same<Arg, NearArg<SMALL>>::value) {
+                    arg.p = t.param; arg.g = t.grad; arg.master = t.master; arg.m = t.exp_avg; arg.v = t.exp_avg_sq; arg.n = t.n; arg.kind = kind;
+                    if constexpr (SMALL) { arg.m_scale = t.avg_scale; arg.v_scale = t.sq_scale; }
+                } else if constexpr (SMALL) arg.set(t.n, kind, base, {t.param, t.grad, t.master, t.exp_avg, t.exp_avg_sq, t.avg_scale, t.sq_scale});
+                else arg.set(t.n, kind, base, {t.param, t.grad, t.master, t.exp_avg, t.exp_avg_sq});
             });
-            const StepArgs s = {lr, beta1, beta2, eps, weight_decay, step, grad_factor, lr_factor, chunk};
-            enqueue(adamw<CAP, SMALL>, dim3((unsigned)chunks), dim3(kThreads), a, s);
+            const StepArgs s = {lr, beta1, beta2, eps, weight_decay, step, grad_factor, lr_factor, (char *)base, chunk};
+            enqueue(adamw<CAP, SMALL, Arg>, dim3((unsigned)chunks), dim3(kThreads), a, s);
         };
-        in_launches(count, kMostTensors<SMALL>, chunk, [&](int64_t i) { return tensors[i].n; }, [&](int64_t begin, int n, int64_t chunks) {
+        in_launches(count, base ? kMostNear<SMALL> : kMostTensors<SMALL>, chunk, [&](int64_t i) { return tensors[i].n; }, [&](int64_t begin, int n, int64_t chunks) {
+            using std::integral_constant;
             if (chunks == 0) return;
-            if (n <= kFewTensors) launch(std::integral_constant<int, kFewTensors>{}, begin, n, chunks);
-            else launch(std::integral_constant<int, kMostTensors<SMALL>>{}, begin, n, chunks);
+            if (n <= kFewTensors) launch(integral_constant<int, kFewTensors>{}, TensorArg<SMALL>{}, begin, n, chunks);
+            else if (n <= kMostTensors<SMALL>) launch(integral_constant<int, kMostTensors<SMALL>>{}, TensorArg<SMALL>{}, begin, n, chunks);
+            else launch(integral_constant<int, kMostNear<SMALL>>{}, NearArg<SMALL>{}, begin, n, chunks);
         });
     };
     if (some[1]) all(std::true_type{});
@@ -496,13 +559,14 @@ fg_status fg_grad_norm(int64_t count, const fg_values *grads, float scale, float
         auto launch = [&](auto cap) {
             constexpr int CAP = decltype(cap)::value;
             List<GradArg, CAP> a = {};
+            static_assert(sizeof a <= 4000, "");
             make_list(a, n, kChunk, [&](int i) { return grads[begin + i].n; }, [&](int i, GradArg &arg) {
-                arg = {grads[begin + i].values, grads[begin + i].n};
-                return grads[begin + i].dtype;
+                arg = {grads[begin + i].values, grads[begin + i].n, grads[begin + i].dtype};
             });
             enqueue(grad_squares<CAP>, dim3(groups), dim3(kThreads), a, (int)chunks, partial);
         };
         if (n <= kFewGrads) launch(std::integral_constant<int, kFewGrads>{});
+        else if (n <= kMoreGrads) launch(std::integral_constant<int, kMoreGrads>{});
         else launch(std::integral_constant<int, kMostGrads>{});
         partial += groups;
     });
