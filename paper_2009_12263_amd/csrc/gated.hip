@@ -202,7 +202,33 @@ struct FewArgs {
 template <int NB> __host__ __device__ __forceinline__ int64_t few_place(int r, int c) { return ((int64_t)(c >> 5) * NB + (r >> 4)) * 512 + ((c >> 3) & 3) * 128 + (r & 15) * 8 + (c & 7); }
 constexpr int64_t few_values(int64_t rows, int64_t k) { return (k + 31) / 32 * 512 * ((rows + 15) / 16); }
 
-template <class T, int NB, bool UP>
+// Eight values of 16 bits from memory.  ODD: they may begin between two 32-bit words, where a load of 16 bytes takes several times as long; then the words that they lie in
+// are read, and shifted once they are there (8 tokens of 1023 x 8191: 23 and 30 us the two forms, 15 and 16 so; of 1024 x 8192 9 and 13).
+template <class T, bool ODD> struct FewPiece {
+    typedef typename RowPiece<T>::vec vec;
+    vec v;
+    __device__ __forceinline__ void fetch(const T *p) { v = *(const typename RowPiece<T>::unaligned *)p; }
+    __device__ __forceinline__ vec get(const T *) const { return v; }
+};
+template <class T> struct FewPiece<T, true> {
+    typedef typename RowPiece<T>::vec vec;
+    typedef uint32_t words __attribute__((ext_vector_type(4))), words_anywhere __attribute__((ext_vector_type(4), aligned(4)));
+    words v;
+    uint32_t last;                      // the word of the last value: the one behind v, or its end
+    __device__ __forceinline__ void fetch(const T *p) {
+        v = *(const words_anywhere *)((uintptr_t)p & ~(uintptr_t)3);
+        last = *(const uint32_t *)(((uintptr_t)p + 14) & ~(uintptr_t)3);
+    }
+    __device__ __forceinline__ vec get(const T *row) const {            // row: where p was, but for whole words
+        const uint32_t by = (uint32_t)(uintptr_t)row & 2;
+        words r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_alignbyte(i < 3 ? v[i + 1] : last, v[i], by);
+        return __builtin_bit_cast(vec, r);
+    }
+};
+
+template <class T, int NB, bool UP, bool ODD>
 __global__ __launch_bounds__(1024) void gated_few(const FewArgs a) {
     typedef typename RowPiece<T>::vec vec;
     typedef typename RowPiece<T>::unaligned anywhere;
@@ -224,16 +250,17 @@ __global__ __launch_bounds__(1024) void gated_few(const FewArgs a) {
     const int begin = turns > 0 ? (int)(blockIdx.x * 5u % (unsigned)turns) : 0;
     auto several = [&](int turn, auto count) {
         constexpr int S = 2 * decltype(count)::value;
-        vec wv[S][G], xv[S][NB];
+        FewPiece<T, ODD> wv[S][G];
+        FewPiece<T, ODD && UP> xv[S][NB];
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             int t = turn + s / 2 * waves + begin;
             t = t >= turns ? t - turns : t;
             const int k = t * 64 + s % 2 * 32;
 #pragma unroll
-            for (int g = 0; g < G; ++g) wv[s][g] = *(const anywhere *)(w[g] + k);
+            for (int g = 0; g < G; ++g) wv[s][g].fetch(w[g] + k);
 #pragma unroll
-            for (int b = 0; b < NB; ++b) xv[s][b] = *(const anywhere *)x_at(b, k);
+            for (int b = 0; b < NB; ++b) xv[s][b].fetch(x_at(b, k));
         }
         __builtin_amdgcn_sched_barrier(0);              // (all requests go out before the first is used)
 #pragma unroll
@@ -241,7 +268,7 @@ __global__ __launch_bounds__(1024) void gated_few(const FewArgs a) {
 #pragma unroll
             for (int g = 0; g < G; ++g)
 #pragma unroll
-                for (int b = 0; b < NB; ++b) sum[g][b] = mfma_16x16x32<T>(wv[s][g], xv[s][b], sum[g][b]);
+                for (int b = 0; b < NB; ++b) sum[g][b] = mfma_16x16x32<T>(wv[s][g].get(w[g]), xv[s][b].get(x[b]), sum[g][b]);
     };
     int turn = wave;
     for (; turn + waves < turns; turn += 2 * waves) several(turn, std::integral_constant<int, 2>{});
@@ -556,16 +583,19 @@ struct Call {
     template <bool UP> void few(const FewArgs &a) {
         with_half(dtype, [&](auto t) {
             using T = decltype(t);
-            auto launch = [&](auto nb) {
+            auto launch = [&](auto nb, auto odd) {
                 constexpr int NB = decltype(nb)::value;
+                constexpr bool ODD = decltype(odd)::value;
                 // Waves to fill the GPU (16 a unit), as long as each has eight turns (one token of 1024 x 2560: four waves for G and U 10.9 us, sixteen 11.5).
                 const int tiles = (a.n + 15) / 16, steps = (a.k + 63) / 64;
                 int waves = 1;
                 while (waves < 16 && tiles * waves < 4096 && steps >= 8 * waves) waves *= 2;
-                enqueue.with_lds(waves * (UP ? 2 : 1) * NB * 1024, gated_few<T, NB, UP>, dim3((unsigned)tiles), dim3(64 * waves), a);
+                enqueue.with_lds(waves * (UP ? 2 : 1) * NB * 1024, gated_few<T, NB, UP, ODD>, dim3((unsigned)tiles), dim3(64 * waves), a);
             };
-            if (a.rows <= 16) launch(std::integral_constant<int, 1>{});
-            else launch(std::integral_constant<int, 2>{});
+            const bool odd = !aligned_to(a.w, 4) || a.ldw % 2 != 0 || (UP && (!aligned_to(a.x, 4) || a.ldx % 2 != 0));
+            auto either = [&](auto nb) { odd ? launch(nb, std::true_type{}) : launch(nb, std::false_type{}); };
+            if (a.rows <= 16) either(std::integral_constant<int, 1>{});
+            else either(std::integral_constant<int, 2>{});
         });
     }
 };
