@@ -182,14 +182,14 @@ __global__ __launch_bounds__(256) void gated_round(const float *in, int64_t ldi,
     });
 }
 // ---- few tokens -------------------------------------------------------------------------------------------------
-// Sums over k of w[n][k] x[r][k] for up to 16 NB rows r of x: reading w.  A workgroup takes 16 rows of w (UP: and as many of U), its waves 64 k each in
+// Sums over k of w[n][k] x[r][k] for up to 16 NB rows r of x, NB = 1, 2 or 4: reading w.  A workgroup takes 16 rows of w (UP: and as many of U), its waves 64 k each in
 // turn: a lane reads its row's 16 bytes straight into the operand of a 16x16x32 matrix instruction, a wave two whole lines of each row.  The waves' sums are added
 // up through LDS in their order.
 // UP: h = act(g) u of the sums, in 16 bits, and what its rounding leaves `lo` rows further on (lo > 0); g and u are kept in FP32 where that is wanted.  x is row-major; h
 // is written as the other form reads its x: operands of matrix instructions, those of 32 k and 16 rows one after the other.
 // Otherwise: rounded; with lo > 0 the sums of rows r and lo + r.
 // Bound by reading w with one token (4096 x 10240: 252 MB in 50 us); with more, x costs as well, which each workgroup reads from the L2: every row of it is a
-// line of its own (16 tokens 61 us), and from 17 on the tiled kernels, which share x through LDS, are as fast.
+// line of its own (16 tokens 61 us); of more rows (are_few) the tiled kernels share x through LDS.
 struct FewArgs {
     const void *x, *w;
     void *out;
@@ -199,8 +199,10 @@ struct FewArgs {
     Activation act;
 };
 // Where h's value of row r and column c is, and the values of all of it.
-template <int NB> __host__ __device__ __forceinline__ int64_t few_place(int r, int c) { return ((int64_t)(c >> 5) * NB + (r >> 4)) * 512 + ((c >> 3) & 3) * 128 + (r & 15) * 8 + (c & 7); }
-constexpr int64_t few_values(int64_t rows, int64_t k) { return (k + 31) / 32 * 512 * ((rows + 15) / 16); }
+constexpr int few_blocks(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }          // of 16 rows
+__device__ __forceinline__ int64_t few_place(int blocks, int r, int c) { return ((int64_t)(c >> 5) * blocks + (r >> 4)) * 512 + ((c >> 3) & 3) * 128 + (r & 15) * 8 + (c & 7); }
+constexpr int64_t few_values(int64_t rows, int64_t k) { return (k + 31) / 32 * 512 * few_blocks(rows); }
+constexpr int few_threads(int blocks) { return blocks == 4 ? 512 : 1024; }             // of a workgroup, at most: operands of 64 rows take 142 registers
 
 // Eight values of 16 bits from memory.  ODD: they may begin between two 32-bit words, where a load of 16 bytes takes several times as long; then the words that they lie in
 // are read, and shifted once they are there (8 tokens of 1023 x 8191: 23 and 30 us the two forms, 15 and 16 so; of 1024 x 8192 9 and 13).
@@ -229,7 +231,7 @@ template <class T> struct FewPiece<T, true> {
 };
 
 template <class T, int NB, bool UP, bool ODD>
-__global__ __launch_bounds__(1024) void gated_few(const FewArgs a) {
+__global__ __launch_bounds__(few_threads(NB)) void gated_few(const FewArgs a) {
     typedef typename RowPiece<T>::vec vec;
     typedef typename RowPiece<T>::unaligned anywhere;
     constexpr int G = UP ? 2 : 1;
@@ -325,8 +327,7 @@ __global__ __launch_bounds__(1024) void gated_few(const FewArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = a.act.operator()<false>(v[e], nullptr) * u[e];
             // (both forms have as many blocks of rows of h: with lo > 0 it has 2 lo rows)
-            const bool wide = a.lo ? 2 * a.lo > 16 : NB > 1;
-            auto place = [&](int row) { return (T *)a.out + (wide ? few_place<2>(row, c) : few_place<1>(row, c)); };
+            auto place = [&](int row) { return (T *)a.out + few_place(few_blocks(a.lo ? 2 * a.lo : a.rows), row, c); };
             T *out = place(r), *rest = place(r + a.lo);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -357,9 +358,16 @@ fg_matrix rows_of(const void *p, int32_t dtype, int64_t ld, int32_t layout = FG_
 fg_matrix turned(fg_matrix m) { m.layout = FG_COL; return m; }
 bool as_it_is(int64_t cols, const fg_matrix *m) { return cols % 8 == 0 && aligned_to(m->re, 16) && m->ld % 8 == 0 && m->ld < kKContiguousLd; }
 
-// Whether gated_few takes so many rows.  Up to 16 it is the fastest (one token of 4096 x 10240 52 us, the tiled kernels 68; 16 63 and 61); up to 32 where the
-// weights are small and launches count (32 tokens of 1024 x 2560 20.1 us, by four launches of tiled kernels and sums 22.1; of 2048 x 5120 34.7 and 27.1).
-bool are_few(int64_t rows, int64_t D, int64_t H) { return rows <= 16 || (rows <= 32 && D * H <= (1 << 22)); }
+// Whether gated_few takes so many rows; copies: the tiled kernels would need copies of weights.  Up to 16 rows it is the fastest (one token of 4096 x 10240 52 us, the tiled
+// kernels 68; 16 63 and 61).  Up to 32 where the weights are small and launches count (32 tokens of 1024 x 2560 20.1 us, by four launches of tiled kernels and sums 22.1; of
+// 2048 x 5120 34.7 and 27.1) or would be copied (32 of 2047 x 5119 44 and 50, of 4094 x 10238 113 and 159, 20 of 3754 x 1634 20 and 41).  Up to 64 where neither sum is long,
+// for which its workgroups are too few (48 of 1024 x 2560 17 and 23, 64 of 2048 x 1500 21 and 30, of 512 x 1536 12 and 17, 50 of 999 x 3001 28 and 33; 64 of 768 x 4096 21 and
+// 19, of 512 x 8192 28 and 20, 40 of 4096 x 1000 28 and 23, 64 of 2048 x 5120 39 and 27).
+bool are_few(int64_t rows, int64_t D, int64_t H, bool copies) {
+    if (rows <= 16) return true;
+    if (rows <= 32) return copies || D * H <= (1 << 22);
+    return rows <= 64 && D <= 2048 && H <= 3500 && D * H <= (3 << 20);
+}
 
 // Rows for each token of H, dG and dU: two where results are few.
 int64_t parts_of(int64_t T, int64_t D, int64_t H) { return T * std::min(D, H) < 16384 ? 2 : 1; }
@@ -382,7 +390,7 @@ struct ForwardSpace : Space {
     ForwardSpace(int64_t T, int64_t D, int64_t H, bool copy_x, bool copy_in, bool copy_out, bool own_gu) {
         const int64_t dp = up(D, 8), hp = up(H, 8);
         parts = parts_of(T, D, H);
-        few = are_few(parts * T, D, H);
+        few = are_few(parts * T, D, H, copy_in || copy_out);            // (x is read where it is)
         up_by_sums = !few && (parts == 2 || by_sums(T, 2 * H, dp));
         down_by_sums = !few && (parts == 2 || by_sums(T, D, hp));
         h = take((few ? few_values(parts * T, H) : parts * T * hp) * 2);
@@ -589,13 +597,16 @@ struct Call {
                 // Waves to fill the GPU (16 a unit), as long as each has eight turns (one token of 1024 x 2560: four waves for G and U 10.9 us, sixteen 11.5).
                 const int tiles = (a.n + 15) / 16, steps = (a.k + 63) / 64;
                 int waves = 1;
-                while (waves < 16 && tiles * waves < 4096 && steps >= 8 * waves) waves *= 2;
+                while (waves < few_threads(NB) / 64 && tiles * waves < 4096 && steps >= 8 * waves) waves *= 2;
                 enqueue.with_lds(waves * (UP ? 2 : 1) * NB * 1024, gated_few<T, NB, UP, ODD>, dim3((unsigned)tiles), dim3(64 * waves), a);
             };
             const bool odd = !aligned_to(a.w, 4) || a.ldw % 2 != 0 || (UP && (!aligned_to(a.x, 4) || a.ldx % 2 != 0));
             auto either = [&](auto nb) { odd ? launch(nb, std::true_type{}) : launch(nb, std::false_type{}); };
-            if (a.rows <= 16) either(std::integral_constant<int, 1>{});
-            else either(std::integral_constant<int, 2>{});
+            switch (few_blocks(a.rows)) {
+                case 1: either(std::integral_constant<int, 1>{}); break;
+                case 2: either(std::integral_constant<int, 2>{}); break;
+                default: either(std::integral_constant<int, 4>{});
+            }
         });
     }
 };
@@ -628,7 +639,8 @@ extern "C" {
 
 int64_t fg_gated_ffn_workspace(int64_t tokens, int64_t dim, int64_t hidden) {
     if (tokens <= 0 || dim <= 0 || hidden <= 0) return 0;
-    return ForwardSpace(tokens, dim, hidden, true, true, true, true).bytes;
+    // (the kernel for few tokens makes no copies)
+    return std::max(ForwardSpace(tokens, dim, hidden, true, true, true, true).bytes, ForwardSpace(tokens, dim, hidden, true, false, false, true).bytes);
 }
 
 fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_matrix *X, const fg_matrix *W_in, const fg_matrix *W_out, int32_t act,

@@ -35,3 +35,20 @@ def test_single_operands_between_words(tokens):
         c.forward("gelu")
         check("y", c.r["y"], want["y"])
         check("gu", c.r["gu"], want["gu"])
+
+
+@pytest.mark.parametrize("pad,offset", [(0, 0), (8, 8), (3, 1), (2, 1)])
+@pytest.mark.parametrize("size", [(17, 1000, 2000), (20, 40, 24), (29, 70, 3000), (32, 511, 2000), (33, 600, 1200), (40, 1001, 2729), (47, 400, 3500), (48, 360, 3501), (50, 2048, 1500),
+                                  (63, 2049, 264), (64, 512, 1536), (64, 300, 333), (65, 512, 1536)])
+def test_up_to_64_rows(size, pad, offset):
+    c = Case(*size, torch.bfloat16 if (size[0] + pad) % 2 else torch.float16, seed=size[2], pad=pad, offset=offset)
+    want = reference(c.x, c.w_in, c.w_out, "silu", c.dtype)
+    for keep in (True, False):
+        c.r["y"].fill_(3.0)
+        c.forward("silu", keep)
+        check("y", c.r["y"], want["y"])
+    check("gu", c.r["gu"], want["gu"])
+    for name in ("y", "gu"):                # what lies beside the results stays
+        values, memory = c.results[name]
+        values.fill_(c.SENTINEL)
+        assert bool((memory == c.SENTINEL).all())
