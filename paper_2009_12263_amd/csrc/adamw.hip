@@ -399,28 +399,43 @@ fg_status check_adamw_tensor(int64_t i, const fg_adamw_tensor &t) {
     return FG_OK;
 }
 
-// The same values in two tensors would be updated by two workgroups at once.
-fg_status check_apart(int64_t count, const fg_adamw_tensor *tensors) {
-    auto end_of = [](const fg_adamw_tensor &t) { return (const char *)t.param + t.n * element_bytes(t.param_dtype); };
+// The same values in two tensors would be updated by two workgroups at once.  begin(t), bytes(t): an array of theirs.
+template <class Begin, class Bytes> fg_status check_apart(const char *name, int64_t count, const fg_adamw_tensor *tensors, Begin &&begin, Bytes &&bytes) {
+    auto end = [&](const fg_adamw_tensor &t) { return begin(t) + bytes(t); };
     const char *last = nullptr;
     bool in_order = true;
     for (int64_t i = 0; i < count && in_order; ++i) {
-        if (tensors[i].n == 0) continue;
-        in_order = (const char *)tensors[i].param >= last;
-        last = end_of(tensors[i]);
+        if (tensors[i].n == 0 || !begin(tensors[i])) continue;
+        in_order = begin(tensors[i]) >= last;
+        last = end(tensors[i]);
     }
     if (in_order) return FG_OK;
     try {
         std::vector<int64_t> order;
         for (int64_t i = 0; i < count; ++i)
-            if (tensors[i].n > 0) order.push_back(i);
-        std::sort(order.begin(), order.end(), [&](int64_t a, int64_t b) { return tensors[a].param < tensors[b].param; });
+            if (tensors[i].n > 0 && begin(tensors[i])) order.push_back(i);
+        std::sort(order.begin(), order.end(), [&](int64_t a, int64_t b) { return begin(tensors[a]) < begin(tensors[b]); });
         for (size_t k = 1; k < order.size(); ++k)
-            if (end_of(tensors[order[k - 1]]) > (const char *)tensors[order[k]].param)
-                return fail(FG_ERR_LAYOUT, "tensors %lld and %lld have values of param in common", (long long)order[k - 1], (long long)order[k]);
+            if (end(tensors[order[k - 1]]) > begin(tensors[order[k]]))
+                return fail(FG_ERR_LAYOUT, "tensors %lld and %lld have values of %s in common", (long long)order[k - 1], (long long)order[k], name);
     } catch (const std::bad_alloc &) {
         return fail(FG_ERR_UNSUPPORTED, "no host memory for a list of %lld tensors", (long long)count);
     }
+    return FG_OK;
+}
+fg_status check_apart(int64_t count, const fg_adamw_tensor *tensors) {
+    typedef const fg_adamw_tensor &Tensor;
+    auto moment_bytes = [](Tensor t) { return t.n * (t.avg_scale ? 1 : 4); };
+    auto scale_bytes = [](Tensor t) { return (t.n + kStateBlock - 1) / kStateBlock * 4; };
+    if (fg_status st = check_apart("param", count, tensors, [](Tensor t) { return (const char *)t.param; }, [](Tensor t) { return t.n * element_bytes(t.param_dtype); })) return st;
+    if (fg_status st = check_apart("master", count, tensors, [](Tensor t) { return (const char *)t.master; }, [](Tensor t) { return t.n * 4; })) return st;
+    if (fg_status st = check_apart("exp_avg", count, tensors, [](Tensor t) { return (const char *)t.exp_avg; }, moment_bytes)) return st;
+    if (fg_status st = check_apart("exp_avg_sq", count, tensors, [](Tensor t) { return (const char *)t.exp_avg_sq; }, moment_bytes)) return st;
+    if (fg_status st = check_apart("avg_scale", count, tensors, [](Tensor t) { return (const char *)t.avg_scale; }, scale_bytes)) return st;
+    if (fg_status st = check_apart("sq_scale", count, tensors, [](Tensor t) { return (const char *)t.sq_scale; }, scale_bytes)) return st;
+    for (int64_t i = 0; i < count; ++i)
+        if (tensors[i].n > 0 && (tensors[i].exp_avg == tensors[i].exp_avg_sq || (tensors[i].avg_scale && tensors[i].avg_scale == tensors[i].sq_scale)))
+            return fail(FG_ERR_LAYOUT, "tensor %lld: both moments are in the same memory", (long long)i);
     return FG_OK;
 }
 

@@ -649,14 +649,17 @@ fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_mat
     if (fg_status st = check_like("Y", Y, tokens, dim, X->dtype)) return st;
     if (GU) if (fg_status st = check_like("GU", GU, tokens, 2 * hidden, FG_F32)) return st;
     if (tokens == 0 || dim == 0) return FG_OK;
-    if (fg_status st = check_elsewhere("Y", Y, "X", X)) return st;
-    if (fg_status st = check_elsewhere("Y", Y, "W_in", W_in)) return st;
-    if (fg_status st = check_elsewhere("Y", Y, "W_out", W_out)) return st;
+    const struct { const char *name; const fg_matrix *m; } operands[] = {{"X", X}, {"W_in", W_in}, {"W_out", W_out}};
+    for (const auto &in : operands)
+        if (fg_status st = check_elsewhere("Y", Y, in.name, in.m)) return st;
     Call call = {Launches(hip_stream), (char *)workspace, X->dtype};
     if (hidden == 0) {
         call.round<false>(rows_of(nullptr, FG_F32, 0), Y, tokens, dim);
         return call.enqueue.status("gated_round");
     }
+    for (const auto &in : operands)
+        if (fg_status st = check_elsewhere("GU", GU, in.name, in.m)) return st;
+    if (fg_status st = check_elsewhere("GU", GU, "Y", Y)) return st;
     const bool copy_x = !as_it_is(dim, X), copy_out = !as_it_is(hidden, W_out), copy_in = !as_it_is(dim, W_in) || !in_reach(hidden, W_in);
     const bool own_gu = !GU || !aligned_to(GU->re, 16) || GU->ld % 4 != 0 || GU->ld >= kResultLd;        // (so that results do not depend on where GU is)
     const ForwardSpace at(tokens, dim, hidden, copy_x, copy_in, copy_out, own_gu);
@@ -743,6 +746,11 @@ fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const f
         return call.enqueue.status("gated_round");
     }
     if (!dX && !dW_in && !dW_out) return FG_OK;
+    for (const auto &out : results)
+        if (fg_status st = check_elsewhere(out.name, out.m, "GU", GU)) return st;
+    if (dX && dW_in) if (fg_status st = check_elsewhere("dX", dX, "dW_in", dW_in)) return st;
+    if (dX && dW_out) if (fg_status st = check_elsewhere("dX", dX, "dW_out", dW_out)) return st;
+    if (dW_in && dW_out) if (fg_status st = check_elsewhere("dW_in", dW_in, "dW_out", dW_out)) return st;
     const bool copy_dy = !as_it_is(dim, dY), copy_x = !as_it_is(dim, X), copy_in = !as_it_is(dim, W_in), copy_out = !as_it_is(hidden, W_out);
     const GradSpace at(tokens, dim, hidden, copy_dy, copy_x, copy_in, copy_out);
     if (fg_status st = check_workspace(workspace, workspace_bytes, at.bytes)) return st;

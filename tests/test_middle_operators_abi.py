@@ -30,6 +30,12 @@ def tensor(**change):
     return fg.fg_adamw_tensor(*t.values())
 
 
+def apart(i, **change):
+    """Tensors whose arrays have memory of their own."""
+    at = (1 << 30) + (i << 16)
+    return tensor(**(dict(param=at, grad=at + 4096, exp_avg=at + 8192, exp_avg_sq=at + 16384) | change))
+
+
 def adamw(tensors=None, count=None, step=PTR, lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, decay=0.1, factor=None, lr_factor=None):
     tensors = [tensor()] if tensors is None else tensors
     items = (fg.fg_adamw_tensor * len(tensors))(*tensors) if tensors != "NULL" else None
@@ -67,6 +73,12 @@ def norm(grads=((PTR, 100, fg.FG_BF16),), count=None, scale=1.0, limit=1.0, out=
     (ffn, dict(tokens=1 << 30, hidden=1 << 10, W_out=row(ld=1 << 10)), fg.FG_ERR_UNSUPPORTED, "tiles"),
     (ffn, dict(Y=row()), fg.FG_ERR_LAYOUT, "Y must be in other memory than X"),
     (ffn, dict(Y=row(re=3 * PTR)), fg.FG_ERR_LAYOUT, "Y must be in other memory than W_out"),
+    (ffn, dict(GU=row(fg.FG_F32)), fg.FG_ERR_LAYOUT, "GU must be in other memory than X"),
+    (ffn, dict(GU=row(fg.FG_F32, re=4 * PTR)), fg.FG_ERR_LAYOUT, "GU must be in other memory than Y"),
+    (ffn_grad, dict(GU=row(fg.FG_F32, re=6 * PTR)), fg.FG_ERR_LAYOUT, "dW_in must be in other memory than GU"),
+    (ffn_grad, dict(dX=row(re=6 * PTR)), fg.FG_ERR_LAYOUT, "dX must be in other memory than dW_in"),
+    (ffn_grad, dict(dX=row(re=7 * PTR)), fg.FG_ERR_LAYOUT, "dX must be in other memory than dW_out"),
+    (ffn_grad, dict(dW_out=row(re=6 * PTR)), fg.FG_ERR_LAYOUT, "dW_in must be in other memory than dW_out"),
     (ffn_grad, dict(dX=row()), fg.FG_ERR_LAYOUT, "dX must be in other memory than dY"),
     (ffn_grad, dict(dX=row(re=2 * PTR)), fg.FG_ERR_LAYOUT, "dX must be in other memory than X"),
     (ffn_grad, dict(dW_in=row(re=3 * PTR)), fg.FG_ERR_LAYOUT, "dW_in must be in other memory than W_in"),
@@ -113,6 +125,13 @@ def norm(grads=((PTR, 100, fg.FG_BF16),), count=None, scale=1.0, limit=1.0, out=
     (adamw, dict(tensors=[tensor(), tensor(param=1 << 20, avg_scale=PTR, sq_scale=PTR)]), fg.FG_ERR_UNSUPPORTED, "eight bits"),
     (adamw, dict(tensors=[tensor(), tensor()]), fg.FG_ERR_LAYOUT, "in common"),
     (adamw, dict(tensors=[tensor(param=PTR + 198), tensor(param=1 << 20), tensor(n=100)]), fg.FG_ERR_LAYOUT, "tensors 2 and 0"),
+    (adamw, dict(tensors=[apart(0), apart(1, master=1 << 20), apart(2, master=(1 << 20) + 396)]), fg.FG_ERR_LAYOUT, "tensors 1 and 2 have values of master"),
+    (adamw, dict(tensors=[apart(1), apart(0, exp_avg=apart(1).exp_avg)]), fg.FG_ERR_LAYOUT, "values of exp_avg in"),
+    (adamw, dict(tensors=[apart(0), apart(2), apart(1, exp_avg_sq=apart(0).exp_avg_sq + 4)]), fg.FG_ERR_LAYOUT, "tensors 0 and 2 have values of exp_avg_sq"),
+    (adamw, dict(tensors=[apart(0, avg_scale=1 << 20, sq_scale=1 << 21), apart(1, avg_scale=1 << 20, sq_scale=1 << 22)]), fg.FG_ERR_LAYOUT, "avg_scale in"),
+    (adamw, dict(tensors=[apart(0, avg_scale=1 << 20, sq_scale=1 << 21), apart(1, avg_scale=1 << 22, sq_scale=1 << 21)]), fg.FG_ERR_LAYOUT, "sq_scale in"),
+    (adamw, dict(tensors=[apart(0), tensor(param=1 << 20)]), fg.FG_ERR_LAYOUT, "tensor 1: both moments"),
+    (adamw, dict(tensors=[apart(0, avg_scale=1 << 20, sq_scale=1 << 20)]), fg.FG_ERR_LAYOUT, "tensor 0: both moments"),
     (norm, dict(count=-1), fg.FG_ERR_SHAPE, "negative"),
     (norm, dict(grads="NULL", count=1), fg.FG_ERR_NULL, "list"),
     (norm, dict(out=None), fg.FG_ERR_NULL, "norm"),
