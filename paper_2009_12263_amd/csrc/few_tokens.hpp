@@ -10,6 +10,8 @@
 #include "gemm_kernel.hpp"
 #include "row_ops.hpp"
 
+#include "few_items.hpp"
+
 namespace fg {
 
 constexpr int64_t kFewTokens = 64;          // whose dw is written so
@@ -33,18 +35,17 @@ template <class T, int KS, int J>
 __global__ __launch_bounds__(256, 2) void dw_of_few(const DwsOfFew<T> products, const float *factor, int tokens) {
     typedef typename RowPiece<T>::vec vec;
     const int lane = threadIdx.x & 63, at = lane & 15, quarter = lane >> 4;
-    int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const bool second = item >= products.at[0].items;
-    if (second) item -= products.at[0].items;
-    const DwOfFew<T> q = products.at[second ? 1 : 0];
+    const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    FewItem item;
+    if (!few_item(wave, products.at[0].items, products.at[0].dim, products.at[1].items, products.at[1].dim, 16 * J, item)) return;
+    const DwOfFew<T> q = products.at[item.second ? 1 : 0];
     const T *dz = q.dz, *x = q.x;
     T *out = q.out;
     const int64_t ld_dz = q.ld_dz, have = q.have, ldx = q.ldx, ldo = q.ldo;
-    const int words = (int)q.words, dim = (int)q.dim, strips = (dim + 127) / 128;
+    const int words = (int)q.words, dim = (int)q.dim;
     typedef typename RowPiece<T, J>::vec words_vec;
-    const int64_t word0 = item / strips * (16 * J);
-    if (word0 >= words) return;
-    const int p = (int)(item % strips) * 16 + at, pieces = (dim + 7) / 8, there = min(p, pieces - 1);
+    const int64_t word0 = item.word;
+    const int p = item.strip * 16 + at, pieces = (dim + 7) / 8, there = min(p, pieces - 1);
     const bool in = word0 + at * J < have;
     vec a[KS][J], b[KS][8];
 #pragma unroll
@@ -88,10 +89,10 @@ __global__ __launch_bounds__(256, 2) void dw_of_few(const DwsOfFew<T> products, 
     }
 }
 
-// tokens <= kFewTokens; `second` may have no words
+// tokens <= kFewTokens; either product may have no words
 template <class T>
 void launch_dw_of_few(Launches &enqueue, DwOfFew<T> first, DwOfFew<T> second, const float *factor, int64_t tokens) {
-    auto items = [](const DwOfFew<T> &q, int64_t each) { return (q.words + each - 1) / each * ((q.dim + 127) / 128); };
+    auto items = [](const DwOfFew<T> &q, int64_t each) { return few_items(q.words, q.dim, each); };
     auto few = [&](auto steps, auto run) {
         constexpr int KS = decltype(steps)::value, J = decltype(run)::value;
         first.items = items(first, 16 * J);
