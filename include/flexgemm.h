@@ -362,7 +362,8 @@ int64_t fg_linear_xent_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim
  * Gated feed-forward block: with [G U] = X * W_in^T and H = act(G) * U (element by element),   Y = H * W_out^T.
  *   X, Y  : tokens x dim; W_in : 2 hidden x dim, the rows of G and then those of U; W_out : dim x hidden.  All FG_F16 or all FG_BF16,
  *           multiplied exactly and summed in FP32; H is rounded to that type between the products (binary16: above 65504 it is infinite).  Y and GU lie in other memory.
- *   act   : FG_ACT_NONE, FG_ACT_RELU, FG_ACT_SILU, FG_ACT_GELU_TANH.
+ *   act   : FG_ACT_NONE, FG_ACT_RELU, FG_ACT_SILU, FG_ACT_GELU_TANH.  Of a NaN each is NaN (relu too, which makes 0 of one in a product's epilogue), and its
+ *           derivative but for FG_ACT_NONE's.
  *   GU    : tokens x 2 hidden, FG_F32: G and U, written for fg_gated_ffn_grad; NULL: not wanted.  (Rounded to 16 bits they would make the errors of
  *           the gradients 1.4 times as large.)
  * Rows that are not 16-byte aligned, or not of a multiple of 8 values, are copied into the workspace first.

@@ -126,8 +126,10 @@ __global__ __launch_bounds__(256) void gated_product(const float *gu, int64_t ld
         float g[8], u[8], v[8];
         load_eight(gu + row * ldgu, c, hidden, g);
         load_eight(gu + row * ldgu + hidden, c, hidden, u);
+        act.pick([&](auto kind) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c + e < hidden ? act.operator()<false>(g[e], nullptr) * u[e] : 0.f;
+            for (int e = 0; e < 8; ++e) v[e] = c + e < hidden ? act.template at<false, decltype(kind)::value>(g[e], nullptr) * u[e] : 0.f;
+        });
         store_eight<T>(h + row * ldh, c, (int)ldh, v, PARTS ? h + (rows + row) * ldh : nullptr);
         if (keep) {
 #pragma unroll
@@ -148,14 +150,16 @@ __global__ __launch_bounds__(256) void gated_product_grad(const float *gu, int64
         load_eight(gu + row * ldgu, c, hidden, g);
         load_eight(gu + row * ldgu + hidden, c, hidden, u);
         load_eight(dh + row * lddh, c, hidden, x);
+        act.pick([&](auto kind) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float d;
-            const float a = act.operator()<true>(g[e], &d);
-            vg[e] = x[e] * u[e] * d;
-            vu[e] = x[e] * a;
-            vh[e] = c + e < hidden ? a * u[e] : 0.f;
-        }
+            for (int e = 0; e < 8; ++e) {
+                float d;
+                const float a = act.template at<true, decltype(kind)::value>(g[e], &d);
+                vg[e] = x[e] * u[e] * d;
+                vu[e] = x[e] * a;
+                vh[e] = c + e < hidden ? a * u[e] : 0.f;
+            }
+        });
         T *to = dgu + row * ldd, *rest = PARTS ? to + rows * ldd : nullptr;
         store_eight<T>(to, c, hidden, vg, rest);
         store_eight<T>(to + hidden, c, hidden, vu, PARTS ? rest + hidden : nullptr);
@@ -324,8 +328,10 @@ __global__ __launch_bounds__(few_threads(NB)) void gated_few(const FewArgs a) {
                 for (int e = 0; e < 4; ++e)
                     if (e < left) { g_out[e] = v[e]; u_out[e] = u[e]; }
             }
+            a.act.pick([&](auto kind) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = a.act.operator()<false>(v[e], nullptr) * u[e];
+                for (int e = 0; e < 4; ++e) v[e] = a.act.template at<false, decltype(kind)::value>(v[e], nullptr) * u[e];
+            });
             // (both forms have as many blocks of rows of h: with lo > 0 it has 2 lo rows)
             auto place = [&](int row) { return (T *)a.out + few_place(few_blocks(a.lo ? 2 * a.lo : a.rows), row, c); };
             T *out = place(r), *rest = place(r + a.lo);

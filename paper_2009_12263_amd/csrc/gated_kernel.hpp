@@ -16,32 +16,39 @@
 
 namespace fg {
 
-// act(g) = g q(g) with q = 1 / (1 + exp(-g (k0 + k1 g^2))): silu has k0 = 1, k1 = 0; in gelu (1 + tanh v) / 2 = 1 / (1 + exp(-2 v)).  relu and none have q of 0 or 1.
-// KIND: the epilogues of products have code of their own for silu and gelu (FG_ACT_SILU, FG_ACT_GELU_TANH), half as many instructions as one for all (ANY_ACT):
-// with nothing kept 8192 tokens of 1024 x 2560 114 us so, 97 without an activation.
-constexpr int ANY_ACT = -1;
+// act(g) = g q(g) with q = 1 / (1 + exp(-g (k0 + k1 g^2))): silu has k0 = 1, k1 = 0; in gelu (1 + tanh v) / 2 = 1 / (1 + exp(-2 v)).
+// KIND: each has code of its own, half as many instructions as one for all (with nothing kept 8192 tokens of 1024 x 2560 114 us so, 97 without an activation);
+// FG_ACT_RELU is relu or none.  All kernels share it, so what a NaN or an infinity of g becomes does not depend on which of them a size takes.
 struct Activation {
-    float k0, k1;                           // times -log2 e
+    float k0, k1;                           // of gelu, times -log2 e
     int32_t kind;
     __host__ __device__ static Activation of(int act) {
-        const float c = act == FG_ACT_GELU_TANH ? 2.f * 0.79788456080286535588f : 1.f, minus_log2e = -1.44269504088896340736f;         // (2 sqrt(2 / pi))
-        return {c * minus_log2e, act == FG_ACT_GELU_TANH ? 0.044715f * c * minus_log2e : 0.f, act};
+        const float c = 2.f * 0.79788456080286535588f, minus_log2e = -1.44269504088896340736f;         // (2 sqrt(2 / pi))
+        return {c * minus_log2e, 0.044715f * c * minus_log2e, act};
     }
-    // act(g), and its derivative q + g q (1 - q) (k0 + 3 k1 g^2).  (Of gelu's g bounded: far out q (1 - q) is zero, and stays zero times a finite slope.)
-    template <bool D, int KIND = ANY_ACT>
-    __device__ __forceinline__ float operator()(float g, float *d) const {
+    template <class F> __device__ __forceinline__ void pick(F &&f) const {
+        if (kind == FG_ACT_SILU) f(std::integral_constant<int, FG_ACT_SILU>{});
+        else if (kind == FG_ACT_GELU_TANH) f(std::integral_constant<int, FG_ACT_GELU_TANH>{});
+        else f(std::integral_constant<int, FG_ACT_RELU>{});
+    }
+    // act(g), and its derivative q + g q (1 - q) (k0 + 3 k1 g^2).  (Of gelu's g bounded, by operations that keep a NaN: far out q (1 - q) is zero, and stays zero times a
+    // finite slope.)
+    template <bool D, int KIND>
+    __device__ __forceinline__ float at(float g, float *d) const {
         constexpr float kMinusLn2 = -0.69314718055994530942f;
         if constexpr (KIND == FG_ACT_SILU) {
             const float q = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * g)), a = g * q;
             if constexpr (D) *d = __builtin_fmaf(a, 1.f - q, q);
             return a;
-        } else {
-            const float x = D || KIND == ANY_ACT ? __builtin_amdgcn_fmed3f(g, -1000.f, 1000.f) : g, x2 = x * x;
-            float q = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * __builtin_fmaf(k1, x2, k0)));
-            if constexpr (KIND == ANY_ACT) q = kind == FG_ACT_RELU ? (g > 0.f ? 1.f : 0.f) : kind == FG_ACT_NONE ? 1.f : q;
+        } else if constexpr (KIND == FG_ACT_GELU_TANH) {
+            const float x = D ? __builtin_elementwise_minimum(__builtin_elementwise_maximum(g, -1000.f), 1000.f) : g, x2 = x * x;
+            const float q = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * __builtin_fmaf(k1, x2, k0)));
             if constexpr (D) *d = __builtin_fmaf(x * q * (1.f - q), kMinusLn2 * __builtin_fmaf(3.f * k1, x2, k0), q);
-            if constexpr (KIND == ANY_ACT) return kind == FG_ACT_RELU ? (g > 0.f ? g : 0.f) : g * q;
             return g * q;
+        } else {
+            const bool off = kind == FG_ACT_RELU && g <= 0.f;           // (not of a NaN)
+            if constexpr (D) *d = off ? 0.f : kind == FG_ACT_RELU && g != g ? g : 1.f;
+            return off ? 0.f : g;
         }
     }
 };
@@ -130,16 +137,13 @@ struct GatedCfg : Base {
     __device__ static __forceinline__ void store(const Params &p, const Blocks &blocks, int m_base, int n_base, int lane) {
         if constexpr (Base::WIDE) own_acc<Base::WAVES>();
         const int row0 = m_base + lane % ROWS, shift = 8 * (lane / ROWS);
-        auto with_act = [&](auto act) {
-            constexpr int ACT = decltype(act)::value;
-            if constexpr (KIND == GATED_UP) up<ACT>(p, blocks, row0, n_base / 2 + shift, n_base / 2 + Base::WTN / 2 > p.hidden);
-            else down<ACT>(p, blocks, row0, n_base + shift, n_base + Base::WTN > p.hidden);
-        };
-        if constexpr (KIND == GATED_UP || KIND == GATED_DOWN) {
-            if (p.act.kind == FG_ACT_SILU) with_act(ic<FG_ACT_SILU>{});
-            else if (p.act.kind == FG_ACT_GELU_TANH) with_act(ic<FG_ACT_GELU_TANH>{});
-            else with_act(ic<ANY_ACT>{});
-        } else round(p, blocks, row0, n_base + shift, n_base + Base::WTN > p.N);
+        if constexpr (KIND == GATED_UP || KIND == GATED_DOWN)
+            p.act.pick([&](auto act) {
+                constexpr int ACT = decltype(act)::value;
+                if constexpr (KIND == GATED_UP) up<ACT>(p, blocks, row0, n_base / 2 + shift, n_base / 2 + Base::WTN / 2 > p.hidden);
+                else down<ACT>(p, blocks, row0, n_base + shift, n_base + Base::WTN > p.hidden);
+            });
+        else round(p, blocks, row0, n_base + shift, n_base + Base::WTN > p.N);
     }
     __device__ static __forceinline__ void step() {
         if constexpr (Base::WIDE) {
@@ -183,7 +187,7 @@ struct GatedCfg : Base {
                 const eight g = unit<I, J>(blocks), u = unit<I, J + PER>(blocks);
                 eight v;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = act.template operator()<false, ACT>(g[e], nullptr) * u[e];
+                for (int e = 0; e < 8; ++e) v[e] = act.template at<false, ACT>(g[e], nullptr) * u[e];
                 if (row < p.M) {
                     if (!edge) {
                         put(h + c, v, 8);
@@ -244,7 +248,7 @@ struct GatedCfg : Base {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float d;
-                const float a = act.template operator()<true, ACT>(in.g[e], &d);
+                const float a = act.template at<true, ACT>(in.g[e], &d);
                 vg[e] = dh[e] * in.u[e] * d;
                 vu[e] = dh[e] * a;
                 vh[e] = a * in.u[e];
