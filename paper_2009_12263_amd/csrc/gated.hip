@@ -654,11 +654,16 @@ fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_mat
     if (fg_status st = check_gated(tokens, dim, hidden, X, W_in, W_out, act)) return st;
     if (fg_status st = check_like("Y", Y, tokens, dim, X->dtype)) return st;
     if (GU) if (fg_status st = check_like("GU", GU, tokens, 2 * hidden, FG_F32)) return st;
-    if (tokens == 0 || dim == 0) return FG_OK;
+    if (tokens == 0) return FG_OK;
+    Call call = {Launches(hip_stream), (char *)workspace, X->dtype};
+    if (dim == 0) {                         // G and U are empty sums
+        if (GU && hidden > 0)
+            call.enqueue(gated_round<float, false>, dim3(groups_for(tokens, 2 * hidden)), dim3(256), (const float *)nullptr, (int64_t)0, (float *)GU->re, GU->ld, tokens, (int)(2 * hidden));
+        return call.enqueue.status("gated_round");
+    }
     const struct { const char *name; const fg_matrix *m; } operands[] = {{"X", X}, {"W_in", W_in}, {"W_out", W_out}};
     for (const auto &in : operands)
         if (fg_status st = check_elsewhere("Y", Y, in.name, in.m)) return st;
-    Call call = {Launches(hip_stream), (char *)workspace, X->dtype};
     if (hidden == 0) {
         call.round<false>(rows_of(nullptr, FG_F32, 0), Y, tokens, dim);
         return call.enqueue.status("gated_round");
