@@ -486,13 +486,15 @@ PyObject *gated_ffn_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
-// The items of a list or tuple of tensors; none (and size 0) if it is None.
+// The items of a list or tuple of tensors; given: it is not None (an empty list has no items either).
 struct Items {
     PyObject *const *at = nullptr;
     Py_ssize_t n = 0;
+    bool given = false;
     bool read(PyObject *o) {
         if (o == Py_None) return true;
         if (!PyList_CheckExact(o) && !PyTuple_CheckExact(o)) return false;
+        given = true;
         at = PySequence_Fast_ITEMS(o);
         n = PySequence_Fast_GET_SIZE(o);
         return true;
@@ -504,8 +506,8 @@ PyObject *adamw(PyObject *, PyObject *const *a, Py_ssize_t n) {
         Items params, grads, avg, sq, masters, avg_scales, sq_scales;
         if (!params.read(a[0]) || !grads.read(a[1]) || !avg.read(a[2]) || !sq.read(a[3]) || !masters.read(a[10]) || !avg_scales.read(a[11]) || !sq_scales.read(a[12])) return false;
         const Py_ssize_t count = params.n;
-        if (grads.n != count || avg.n != count || sq.n != count || (masters.at && masters.n != count) || !avg_scales.at != !sq_scales.at) return false;
-        const bool small = avg_scales.at != nullptr;
+        if (!params.given || !grads.given || !avg.given || !sq.given || grads.n != count || avg.n != count || sq.n != count || (masters.given && masters.n != count) || avg_scales.given != sq_scales.given) return false;
+        const bool small = avg_scales.given;
         if (small && (avg_scales.n != count || sq_scales.n != count)) return false;
         double rates[5];
         for (int i = 0; i < 5; ++i) {
@@ -529,7 +531,7 @@ PyObject *adamw(PyObject *, PyObject *const *a, Py_ssize_t n) {
             if (t.param_dtype < 0 || t.param_dtype > FG_F32 || t.grad_dtype < 0 || t.grad_dtype > FG_F32) return false;
             t.param = p->data_ptr(); t.grad = g->data_ptr(); t.exp_avg = m->data_ptr(); t.exp_avg_sq = v->data_ptr();
             t.master = t.avg_scale = t.sq_scale = nullptr;
-            if (masters.at && masters.at[i] != Py_None) {
+            if (masters.given && masters.at[i] != Py_None) {
                 const at::Tensor *w = c.tensor(masters.at[i]);
                 if (!w || !w->is_contiguous() || w->sizes() != p->sizes() || w->scalar_type() != at::kFloat) return false;
                 t.master = (float *)w->data_ptr();
