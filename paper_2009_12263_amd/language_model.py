@@ -130,8 +130,8 @@ class AdamW:
         """One step on the mean loss, its gradients scaled to a norm of MAX_NORM at most; returns the losses before it."""
         loss, grads = self.model.mean_grads(ids, targets)
         grads = [grads[name] for name in self.names]
-        self.count.add_(1)
         fg.fg_grad_norm(grads, 1.0, self.MAX_NORM, self.norm, self.factor, workspace=self.space)
+        self.count.add_(torch.isfinite(self.factor))            # (gradients that overflowed change nothing: no step of the moments' either)
         fg.fg_adamw([self.model.params[name] for name in self.names], grads, self.avg, self.sq, self.count, rate, self.BETA1, self.BETA2, self.EPS, self.DECAY,
                     masters=self.masters, avg_scales=self.avg_scales, sq_scales=self.sq_scales, grad_factor=self.factor)
         return loss
