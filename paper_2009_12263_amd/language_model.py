@@ -53,7 +53,6 @@ class LanguageModel:
         if not hidden:
             self.grads["W"] = new(dim, dim, dtype=f32)
         self.h, self.a, self.u, self.n = (new(tokens, dim) for _ in range(4))
-        self.u32, self.da32 = new(tokens, dim, dtype=f32), new(tokens, dim, dtype=f32)
         self.dn, self.du, self.da, self.dh = (new(tokens, dim) for _ in range(4))
         self.mean1, self.rstd1, self.mean2, self.rstd2, self.loss, self.lse = (new(tokens, dtype=f32) for _ in range(6))
         space = lambda n: torch.empty(n, dtype=torch.uint8, device=device)
@@ -62,6 +61,8 @@ class LanguageModel:
         if hidden:
             self.gu = new(tokens, 2 * hidden, dtype=f32)
             self.spaces.update(ffn=space(fg.fg_gated_ffn_workspace(tokens, dim, hidden)), ffn_grad=space(fg.fg_gated_ffn_grad_workspace(tokens, dim, hidden)))
+        else:
+            self.u32, self.da32 = new(tokens, dim, dtype=f32), new(tokens, dim, dtype=f32)
 
     def forward(self, ids: torch.Tensor, targets: torch.Tensor) -> torch.Tensor:
         """The losses of the tokens (0 where there is no target)."""
