@@ -21,6 +21,7 @@
 #include "cache_policy.hpp"
 #include "few_tokens.hpp"
 #include "gated_kernel.hpp"
+#include "shared_rows.hpp"
 
 namespace fg {
 namespace {
@@ -461,9 +462,16 @@ fg_status check_like(const char *name, const fg_matrix *m, int64_t rows, int64_t
     return FG_OK;
 }
 
+// An operand or a result (null: not wanted) of checked rows.
+struct Rows {
+    const char *name;
+    const fg_matrix *m;
+    int64_t rows, cols;
+    RowSpan span() const { return {(uintptr_t)m->re, rows, m->ld * element_bytes(m->dtype), cols * element_bytes(m->dtype)}; }
+};
 // Results are written while operands are still to be read.
-fg_status check_elsewhere(const char *name, const fg_matrix *out, const char *operand, const fg_matrix *in) {
-    if (out && out->re && out->re == in->re) return fail(FG_ERR_LAYOUT, "%s must be in other memory than %s", name, operand);
+fg_status check_elsewhere(const Rows &out, const Rows &in) {
+    if (out.m && in.m && share_bytes(out.span(), in.span())) return fail(FG_ERR_LAYOUT, "%s must be in other memory than %s", out.name, in.name);
     return FG_OK;
 }
 
@@ -661,16 +669,16 @@ fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_mat
             call.enqueue(gated_round<float, false>, dim3(groups_for(tokens, 2 * hidden)), dim3(256), (const float *)nullptr, (int64_t)0, (float *)GU->re, GU->ld, tokens, (int)(2 * hidden));
         return call.enqueue.status("gated_round");
     }
-    const struct { const char *name; const fg_matrix *m; } operands[] = {{"X", X}, {"W_in", W_in}, {"W_out", W_out}};
-    for (const auto &in : operands)
-        if (fg_status st = check_elsewhere("Y", Y, in.name, in.m)) return st;
+    const Rows operands[] = {{"X", X, tokens, dim}, {"W_in", W_in, 2 * hidden, dim}, {"W_out", W_out, dim, hidden}}, y = {"Y", Y, tokens, dim}, kept = {"GU", GU, tokens, 2 * hidden};
+    for (const Rows &in : operands)
+        if (fg_status st = check_elsewhere(y, in)) return st;
     if (hidden == 0) {
         call.round<false>(rows_of(nullptr, FG_F32, 0), Y, tokens, dim);
         return call.enqueue.status("gated_round");
     }
-    for (const auto &in : operands)
-        if (fg_status st = check_elsewhere("GU", GU, in.name, in.m)) return st;
-    if (fg_status st = check_elsewhere("GU", GU, "Y", Y)) return st;
+    for (const Rows &in : operands)
+        if (fg_status st = check_elsewhere(kept, in)) return st;
+    if (fg_status st = check_elsewhere(kept, y)) return st;
     const bool copy_x = !as_it_is(dim, X), copy_out = !as_it_is(hidden, W_out), copy_in = !as_it_is(dim, W_in) || !in_reach(hidden, W_in);
     const bool own_gu = !GU || !aligned_to(GU->re, 16) || GU->ld % 4 != 0 || GU->ld >= kResultLd;        // (so that results do not depend on where GU is)
     const ForwardSpace at(tokens, dim, hidden, copy_x, copy_in, copy_out, own_gu);
@@ -743,11 +751,11 @@ fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const f
     if (dW_in) if (fg_status st = check_like("dW_in", dW_in, 2 * hidden, dim, X->dtype)) return st;
     if (dW_out) if (fg_status st = check_like("dW_out", dW_out, dim, hidden, X->dtype)) return st;
     if (dim == 0) return FG_OK;
-    const struct { const char *name; const fg_matrix *m; } operands[] = {{"dY", dY}, {"X", X}, {"W_in", W_in}, {"W_out", W_out}},
-                                                           results[] = {{"dX", dX}, {"dW_in", dW_in}, {"dW_out", dW_out}};
-    for (const auto &out : results)
-        for (const auto &in : operands)
-            if (fg_status st = check_elsewhere(out.name, out.m, in.name, in.m)) return st;
+    const Rows operands[] = {{"dY", dY, tokens, dim}, {"X", X, tokens, dim}, {"W_in", W_in, 2 * hidden, dim}, {"W_out", W_out, dim, hidden}},
+               results[] = {{"dX", dX, tokens, dim}, {"dW_in", dW_in, 2 * hidden, dim}, {"dW_out", dW_out, dim, hidden}}, kept = {"GU", GU, tokens, 2 * hidden};
+    for (const Rows &out : results)
+        for (const Rows &in : operands)
+            if (fg_status st = check_elsewhere(out, in)) return st;
     Call call = {Launches(hip_stream), (char *)workspace, X->dtype};
     if (tokens == 0 || hidden == 0) {
         const fg_matrix none = rows_of(nullptr, FG_F32, 0);
@@ -757,11 +765,11 @@ fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const f
         return call.enqueue.status("gated_round");
     }
     if (!dX && !dW_in && !dW_out) return FG_OK;
-    for (const auto &out : results)
-        if (fg_status st = check_elsewhere(out.name, out.m, "GU", GU)) return st;
-    if (dX && dW_in) if (fg_status st = check_elsewhere("dX", dX, "dW_in", dW_in)) return st;
-    if (dX && dW_out) if (fg_status st = check_elsewhere("dX", dX, "dW_out", dW_out)) return st;
-    if (dW_in && dW_out) if (fg_status st = check_elsewhere("dW_in", dW_in, "dW_out", dW_out)) return st;
+    for (const Rows &out : results)
+        if (fg_status st = check_elsewhere(out, kept)) return st;
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 3; ++j)
+            if (fg_status st = check_elsewhere(results[i], results[j])) return st;
     const bool copy_dy = !as_it_is(dim, dY), copy_x = !as_it_is(dim, X), copy_in = !as_it_is(dim, W_in), copy_out = !as_it_is(hidden, W_out);
     const GradSpace at(tokens, dim, hidden, copy_dy, copy_x, copy_in, copy_out);
     if (fg_status st = check_workspace(workspace, workspace_bytes, at.bytes)) return st;
