@@ -443,12 +443,19 @@ struct GradSpace : Space {
     }
 };
 
+// Sizes that are not negative, with fewer than 2^25 tiles of 64 x 64 results in each product.
+constexpr int64_t kMostTokens = 1 << 30;
+bool in_range(int64_t T, int64_t D, int64_t H) { return T <= kMostTokens && D < kLargestWidth && H < (kLargestWidth + 1) / 2; }
+bool few_tiles(int64_t T, int64_t D, int64_t H) {
+    auto tiles = [](int64_t m, int64_t n) { return ((m + 63) / 64) * ((n + 63) / 64); };
+    return tiles(T, std::max(2 * H, D)) < (1ll << 25) && tiles(2 * H, D) < (1ll << 25);
+}
+
 fg_status check_gated(int64_t T, int64_t D, int64_t H, const fg_matrix *X, const fg_matrix *W_in, const fg_matrix *W_out, int32_t act) {
     if (T < 0 || D < 0 || H < 0) return fail(FG_ERR_SHAPE, "negative size: %lld tokens, %lld values, %lld hidden", (long long)T, (long long)D, (long long)H);
-    if (T > (1 << 30) || D >= kLargestWidth || 2 * H >= kLargestWidth)
+    if (!in_range(T, D, H))
         return fail(FG_ERR_UNSUPPORTED, "more than 2^30 tokens, or dim or 2 hidden of 2^21 - 8 and more, are not supported");
-    auto tiles = [](int64_t m, int64_t n) { return ((m + 63) / 64) * ((n + 63) / 64); };
-    if (tiles(T, std::max(2 * H, D)) >= (1ll << 25) || tiles(2 * H, D) >= (1ll << 25)) return fail(FG_ERR_UNSUPPORTED, "products of more than 2^25 tiles are not supported");
+    if (!few_tiles(T, D, H)) return fail(FG_ERR_UNSUPPORTED, "products of more than 2^25 tiles are not supported");
     if (fg_status st = check_rows("X", X, T, D)) return st;
     if (fg_status st = check_rows("W_in", W_in, 2 * H, D)) return st;
     if (fg_status st = check_rows("W_out", W_out, D, H)) return st;
@@ -652,7 +659,7 @@ using namespace fg;
 extern "C" {
 
 int64_t fg_gated_ffn_workspace(int64_t tokens, int64_t dim, int64_t hidden) {
-    if (tokens <= 0 || dim <= 0 || hidden <= 0) return 0;
+    if (tokens <= 0 || dim <= 0 || hidden <= 0 || !in_range(tokens, dim, hidden) || !few_tiles(tokens, dim, hidden)) return 0;
     // (the kernel for few tokens makes no copies)
     return std::max(ForwardSpace(tokens, dim, hidden, true, true, true, true).bytes, ForwardSpace(tokens, dim, hidden, true, false, false, true).bytes);
 }
@@ -737,7 +744,7 @@ fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_mat
 }
 
 int64_t fg_gated_ffn_grad_workspace(int64_t tokens, int64_t dim, int64_t hidden) {
-    if (tokens <= 0 || dim <= 0 || hidden <= 0) return 0;
+    if (tokens <= 0 || dim <= 0 || hidden <= 0 || !in_range(tokens, dim, hidden) || !few_tiles(tokens, dim, hidden)) return 0;
     return GradSpace(tokens, dim, hidden, true, true, true, true).bytes;
 }
 
