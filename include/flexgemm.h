@@ -361,7 +361,7 @@ int64_t fg_linear_xent_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim
 /*
  * Gated feed-forward block: with [G U] = X * W_in^T and H = act(G) * U (element by element),   Y = H * W_out^T.
  *   X, Y  : tokens x dim; W_in : 2 hidden x dim, the rows of G and then those of U; W_out : dim x hidden.  All FG_F16 or all FG_BF16,
- *           multiplied exactly and summed in FP32; H is rounded to that type between the products (binary16: above 65504 it is infinite).  Y and GU lie in other memory.
+ *           multiplied exactly and summed in FP32; H is rounded to that type between the products (binary16: above 65504 it is infinite).  Y and GU lie in other memory (FG_ERR_LAYOUT; rows may lie between each other's).
  *   act   : FG_ACT_NONE, FG_ACT_RELU, FG_ACT_SILU, FG_ACT_GELU_TANH.  Of a NaN each is NaN (relu too, which makes 0 of one in a product's epilogue), and its
  *           derivative but for FG_ACT_NONE's.
  *   GU    : tokens x 2 hidden, FG_F32: G and U, written for fg_gated_ffn_grad; NULL: not wanted.  (Rounded to 16 bits they would make the errors of
@@ -377,7 +377,7 @@ int64_t fg_gated_ffn_workspace(int64_t tokens, int64_t dim, int64_t hidden);
  * Its gradient, from the GU of the forward call: with dH = dY * W_out, dG = dH * U * act'(G), dU = dH * act(G),
  *   dX = [dG dU] * W_in,   dW_in = [dG dU]^T * X,   dW_out = dY^T * H        (zero without tokens; relu'(0) = 0).
  * dG, dU and H are rounded to the type of X between the products (binary16: gradients are kept in range by a scaled loss).
- * dX, dW_in and dW_out are of the type and shape of X, W_in and W_out, each in other memory than the rest; each may be NULL: not wanted.
+ * dX, dW_in and dW_out are of the type and shape of X, W_in and W_out, each in other memory than the rest (FG_ERR_LAYOUT); each may be NULL: not wanted.
  */
 fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const fg_matrix *dY, const fg_matrix *X, const fg_matrix *W_in,
                             const fg_matrix *W_out, int32_t act, const fg_matrix *GU, const fg_matrix *dX, const fg_matrix *dW_in, const fg_matrix *dW_out,
@@ -411,7 +411,8 @@ typedef struct {
  * One step of AdamW on all tensors: with t = *step, counted from 1, g = grad_factor * grad and lr multiplied by lr_factor,
  *   exp_avg = beta1 * exp_avg + (1 - beta1) * g,   exp_avg_sq = beta2 * exp_avg_sq + (1 - beta2) * g^2,
  *   param = (1 - lr * weight_decay) * param - lr / (1 - beta1^t) * exp_avg / (sqrt(exp_avg_sq) / sqrt(1 - beta2^t) + eps).
- *   tensors : `count` descriptions, in host memory, read before the call returns; none of the arrays that are written may be shared.  All with moments in FP32 or all in eight bits.
+ *   tensors : `count` descriptions, in host memory, read before the call returns.  All with moments in FP32 or all in eight bits.  An array that is written may share no memory
+ *             with any other of the call, step and the factors included (FG_ERR_LAYOUT); gradients may with each other.
  *   step, grad_factor, lr_factor : one value each in device memory (a captured step is replayed with others); the factors may be NULL: 1.
  * Nothing is changed where grad_factor is no finite number (gradients that overflowed, see fg_grad_norm) or *step is below 1.
  * Moments in eight bits stand for number * scale, and the second one for (number * scale)^2: its root is kept.  The scale is the largest absolute

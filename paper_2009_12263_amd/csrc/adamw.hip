@@ -17,6 +17,7 @@
 //
 // The operations are written one by one, without fused ones: what eight bits hold changes by 1/16 where a sum falls on the other side of a border.
 #include "row_ops.hpp"
+#include "shared_spans.hpp"
 
 #include <algorithm>
 #include <cmath>
@@ -399,44 +400,85 @@ fg_status check_adamw_tensor(int64_t i, const fg_adamw_tensor &t) {
     return FG_OK;
 }
 
-// The same values in two tensors would be updated by two workgroups at once.  begin(t), bytes(t): an array of theirs.
-template <class Begin, class Bytes> fg_status check_apart(const char *name, int64_t count, const fg_adamw_tensor *tensors, Begin &&begin, Bytes &&bytes) {
-    auto end = [&](const fg_adamw_tensor &t) { return begin(t) + bytes(t); };
-    const char *last = nullptr;
-    bool in_order = true;
-    for (int64_t i = 0; i < count && in_order; ++i) {
-        if (tensors[i].n == 0 || !begin(tensors[i])) continue;
-        in_order = begin(tensors[i]) >= last;
-        last = end(tensors[i]);
+// The arrays of a tensor (end 0: it has none such); all but the first are written.
+constexpr int kArrays = 7;
+constexpr const char *kArrayNames[kArrays] = {"grad", "param", "master", "exp_avg", "exp_avg_sq", "avg_scale", "sq_scale"};
+struct Arrays {
+    uintptr_t begin[kArrays], end[kArrays];
+    explicit Arrays(const fg_adamw_tensor &t) {
+        const int64_t moment = t.n * (t.avg_scale ? 1 : 4), scales = (t.n + kStateBlock - 1) / kStateBlock * 4;
+        const struct { const void *at; int64_t bytes; } arrays[kArrays] = {{t.grad, t.n * element_bytes(t.grad_dtype)}, {t.param, t.n * element_bytes(t.param_dtype)}, {t.master, t.n * 4},
+                                                                           {t.exp_avg, moment}, {t.exp_avg_sq, moment}, {t.avg_scale, scales}, {t.sq_scale, scales}};
+        for (int k = 0; k < kArrays; ++k) {
+            begin[k] = (uintptr_t)arrays[k].at;
+            end[k] = arrays[k].at && t.n > 0 ? begin[k] + (uintptr_t)arrays[k].bytes : 0;
+        }
     }
-    if (in_order) return FG_OK;
+};
+
+// What one workgroup writes another would read or write at the same time.
+fg_status check_apart(int64_t count, const fg_adamw_tensor *tensors, const int64_t *step, const float *grad_factor, const float *lr_factor) {
+    const struct { const char *name; uintptr_t at, bytes; } values[] = {{"step", (uintptr_t)step, 8}, {"grad_factor", (uintptr_t)grad_factor, 4}, {"lr_factor", (uintptr_t)lr_factor, 4}};
+    constexpr int kValues = 3;
+    // Each kind of array in the order of the tensors and away from the other kinds: nothing more to look at.
+    uintptr_t begin[kArrays], end[kArrays] = {}, last = 0;
+    for (uintptr_t &b : begin) b = UINTPTR_MAX;
+    bool apart = true;
+    int64_t falls = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        const Arrays a(tensors[i]);
+        if (tensors[i].n == 0) continue;
+        falls += a.begin[1] < last;
+        last = a.begin[1];
+        for (int k = 0; k < kArrays; ++k) {
+            if (!a.end[k]) continue;
+            apart &= k == 0 || a.begin[k] >= end[k];
+            begin[k] = std::min(begin[k], a.begin[k]);
+            end[k] = std::max(end[k], a.end[k]);
+        }
+    }
+    for (int k = 1; k < kArrays; ++k) {
+        for (int j = 0; j < k; ++j) apart &= end[j] <= begin[k] || end[k] <= begin[j];
+        for (const auto &v : values) apart &= !v.at || v.at + v.bytes <= begin[k] || end[k] <= v.at;
+    }
+    if (apart) return FG_OK;
     try {
-        std::vector<int64_t> order;
+        // Lists whose tensors are in another order than their memory are mostly all in the same one: that of the parameters.
+        std::vector<std::pair<uintptr_t, int64_t>> order;
+        if (falls > count / 8 && falls < count - count / 8) {
+            for (int64_t i = 0; i < count; ++i) order.push_back({(uintptr_t)tensors[i].param, i});
+            std::sort(order.begin(), order.end());
+        }
+        // of: kArrays i + k, array k of tensor i; -1 - j, a value
+        std::vector<Arrays> arrays;
+        arrays.reserve((size_t)count);
+        for (int64_t i = 0; i < count; ++i) arrays.emplace_back(tensors[order.empty() ? i : order[(size_t)i].second]);
+        auto array = [&](int k, int64_t i) {
+            const Arrays &a = arrays[(size_t)i];
+            return Span{a.begin[k], a.end[k], kArrays * (order.empty() ? i : order[(size_t)i].second) + k, k > 0};
+        };
+        auto any = [&](int k, int64_t i) {
+            if (k < kArrays) return array(k, i);
+            const auto &v = values[k - kArrays];
+            return Span{v.at, i == 0 && v.at ? v.at + v.bytes : 0, kArrays - 1 - k, false};
+        };
+        Span x, y, first, second;
+        if (!shared_spans(kArrays + kValues, count, any, x, y)) return FG_OK;
+        for (int k = 1; k < kArrays; ++k)               // (the plainest words for it)
+            if (shared_spans(1, count, [&](int, int64_t i) { return array(k, i); }, first, second))
+                return fail(FG_ERR_LAYOUT, "tensors %lld and %lld have values of %s in common", (long long)(first.of / kArrays), (long long)(second.of / kArrays), kArrayNames[k]);
         for (int64_t i = 0; i < count; ++i)
-            if (tensors[i].n > 0 && begin(tensors[i])) order.push_back(i);
-        std::sort(order.begin(), order.end(), [&](int64_t a, int64_t b) { return begin(tensors[a]) < begin(tensors[b]); });
-        for (size_t k = 1; k < order.size(); ++k)
-            if (end(tensors[order[k - 1]]) > begin(tensors[order[k]]))
-                return fail(FG_ERR_LAYOUT, "tensors %lld and %lld have values of %s in common", (long long)order[k - 1], (long long)order[k], name);
+            if (tensors[i].n > 0 && (tensors[i].exp_avg == tensors[i].exp_avg_sq || (tensors[i].avg_scale && tensors[i].avg_scale == tensors[i].sq_scale)))
+                return fail(FG_ERR_LAYOUT, "tensor %lld: both moments are in the same memory", (long long)i);
+        if (x.of < 0 || y.of < 0) {
+            const Span &in = x.of < 0 ? y : x, &value = x.of < 0 ? x : y;
+            return fail(FG_ERR_LAYOUT, "%s is in %s of tensor %lld", values[-1 - value.of].name, kArrayNames[in.of % kArrays], (long long)(in.of / kArrays));
+        }
+        return fail(FG_ERR_LAYOUT, "%s of tensor %lld and %s of tensor %lld have memory in common", kArrayNames[x.of % kArrays], (long long)(x.of / kArrays), kArrayNames[y.of % kArrays],
+                    (long long)(y.of / kArrays));
     } catch (const std::bad_alloc &) {
         return fail(FG_ERR_UNSUPPORTED, "no host memory for a list of %lld tensors", (long long)count);
     }
-    return FG_OK;
-}
-fg_status check_apart(int64_t count, const fg_adamw_tensor *tensors) {
-    typedef const fg_adamw_tensor &Tensor;
-    auto moment_bytes = [](Tensor t) { return t.n * (t.avg_scale ? 1 : 4); };
-    auto scale_bytes = [](Tensor t) { return (t.n + kStateBlock - 1) / kStateBlock * 4; };
-    if (fg_status st = check_apart("param", count, tensors, [](Tensor t) { return (const char *)t.param; }, [](Tensor t) { return t.n * element_bytes(t.param_dtype); })) return st;
-    if (fg_status st = check_apart("master", count, tensors, [](Tensor t) { return (const char *)t.master; }, [](Tensor t) { return t.n * 4; })) return st;
-    if (fg_status st = check_apart("exp_avg", count, tensors, [](Tensor t) { return (const char *)t.exp_avg; }, moment_bytes)) return st;
-    if (fg_status st = check_apart("exp_avg_sq", count, tensors, [](Tensor t) { return (const char *)t.exp_avg_sq; }, moment_bytes)) return st;
-    if (fg_status st = check_apart("avg_scale", count, tensors, [](Tensor t) { return (const char *)t.avg_scale; }, scale_bytes)) return st;
-    if (fg_status st = check_apart("sq_scale", count, tensors, [](Tensor t) { return (const char *)t.sq_scale; }, scale_bytes)) return st;
-    for (int64_t i = 0; i < count; ++i)
-        if (tensors[i].n > 0 && (tensors[i].exp_avg == tensors[i].exp_avg_sq || (tensors[i].avg_scale && tensors[i].avg_scale == tensors[i].sq_scale)))
-            return fail(FG_ERR_LAYOUT, "tensor %lld: both moments are in the same memory", (long long)i);
-    return FG_OK;
 }
 
 // The lowest address of the tensors' memory; 0 where some begins too far from it for NearArg.
@@ -510,7 +552,7 @@ fg_status fg_adamw(int64_t count, const fg_adamw_tensor *tensors, const int64_t 
     }
     if (some[0] && some[1]) return fail(FG_ERR_UNSUPPORTED, "moments in FP32 and in eight bits need calls of their own");
     if (!some[0] && !some[1]) return FG_OK;
-    if (fg_status st = check_apart(count, tensors)) return st;
+    if (fg_status st = check_apart(count, tensors, step, grad_factor, lr_factor)) return st;
     const int chunk = values < kSmallModel ? kSmallChunk : kChunk;
     Launches enqueue(hip_stream);
     auto all = [&](auto small) {
