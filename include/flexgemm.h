@@ -390,7 +390,7 @@ typedef struct { const void *values; int64_t n; int32_t dtype; } fg_values;
 /*
  * Norm of many gradients: norm = scale * sqrt(sum of the squares of all values of all tensors), in 64 bits, and the factor that brings them to
  * max_norm at most: factor = scale * min(1, max_norm / norm); NaN if the norm is no finite number.  (scale: one over a scaled loss's scale.)
- *   grads  : `count` descriptions, in host memory, read before the call returns; norm, factor : one FP32 value each, factor may be NULL.
+ *   grads  : `count` descriptions, in host memory, read before the call returns; norm, factor : one FP32 value each, in memory of its own, factor may be NULL.
  */
 fg_status fg_grad_norm(int64_t count, const fg_values *grads, float scale, float max_norm, float *norm, float *factor, void *workspace,
                        int64_t workspace_bytes, void *hip_stream);

@@ -608,6 +608,12 @@ fg_status fg_grad_norm(int64_t count, const fg_values *grads, float scale, float
     auto launches = [&](auto &&f) { in_launches(count, kMostGrads, kChunk, [&](int64_t i) { return grads[i].n; }, f); };
     launches([&](int64_t, int, int64_t chunks) { parts += std::min<int64_t>(chunks, kNormGroups); });
     if (fg_status st = check_workspace(workspace, workspace_bytes, parts * 8)) return st;
+    for (int64_t i = 0; i < count; ++i) {
+        const uintptr_t begin = (uintptr_t)grads[i].values, end = begin + (uintptr_t)(grads[i].n * element_bytes(grads[i].dtype));
+        for (const float *out : {norm, factor})
+            if (out && (uintptr_t)out < end && begin < (uintptr_t)out + 4) return fail(FG_ERR_LAYOUT, "%s is in gradient %lld", out == norm ? "norm" : "factor", (long long)i);
+    }
+    if (norm == factor) return fail(FG_ERR_LAYOUT, "norm and factor are in the same memory");
     Launches enqueue(hip_stream);
     double *partial = (double *)workspace;
     launches([&](int64_t begin, int n, int64_t chunks) {
