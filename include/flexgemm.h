@@ -361,12 +361,15 @@ int64_t fg_linear_xent_grad_workspace(int64_t tokens, int64_t vocab, int64_t dim
 /*
  * Gated feed-forward block: with [G U] = X * W_in^T and H = act(G) * U (element by element),   Y = H * W_out^T.
  *   X, Y  : tokens x dim; W_in : 2 hidden x dim, the rows of G and then those of U; W_out : dim x hidden.  All FG_F16 or all FG_BF16,
- *           multiplied exactly and summed in FP32; H is rounded to that type between the products (binary16: above 65504 it is infinite).  Y and GU lie in other memory (FG_ERR_LAYOUT; rows may lie between each other's).
+ *           multiplied exactly and summed in FP32; H is rounded to that type between the products (binary16: above 65504 it is infinite), which makes the error of Y
+ *           1.4 times that of its own rounding.  With tokens * min(dim, hidden) below 16384 what the rounding of H left is multiplied as well, and Y is as exact as its
+ *           rounding.  Y and GU lie in other memory (FG_ERR_LAYOUT; rows may lie between each other's).
  *   act   : FG_ACT_NONE, FG_ACT_RELU, FG_ACT_SILU, FG_ACT_GELU_TANH.  Of a NaN each is NaN (relu too, which makes 0 of one in a product's epilogue), and its
  *           derivative but for FG_ACT_NONE's.
  *   GU    : tokens x 2 hidden, FG_F32: G and U, written for fg_gated_ffn_grad; NULL: not wanted.  (Rounded to 16 bits they would make the errors of
  *           the gradients 1.4 times as large.)
- * Rows that are not 16-byte aligned, or not of a multiple of 8 values, are copied into the workspace first.
+ * Rows that are not 16-byte aligned, or not of a multiple of 8 values, are copied into the workspace first; of few tokens (up to 8, of some
+ * sizes up to 64) they are read where they are.
  * FG_ERR_UNSUPPORTED for dim or 2 hidden of 2^21 - 8 and more, and for products of more than 2^25 tiles of 64 x 64 results.
  */
 fg_status fg_gated_ffn(int64_t tokens, int64_t dim, int64_t hidden, const fg_matrix *X, const fg_matrix *W_in, const fg_matrix *W_out, int32_t act,
@@ -376,7 +379,7 @@ int64_t fg_gated_ffn_workspace(int64_t tokens, int64_t dim, int64_t hidden);
 /*
  * Its gradient, from the GU of the forward call: with dH = dY * W_out, dG = dH * U * act'(G), dU = dH * act(G),
  *   dX = [dG dU] * W_in,   dW_in = [dG dU]^T * X,   dW_out = dY^T * H        (zero without tokens; relu'(0) = 0).
- * dG, dU and H are rounded to the type of X between the products (binary16: gradients are kept in range by a scaled loss).
+ * dG, dU and H are rounded to the type of X between the products, or kept in two parts, as H is there (binary16: gradients are kept in range by a scaled loss).
  * dX, dW_in and dW_out are of the type and shape of X, W_in and W_out, each in other memory than the rest (FG_ERR_LAYOUT); each may be NULL: not wanted.
  */
 fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const fg_matrix *dY, const fg_matrix *X, const fg_matrix *W_in,

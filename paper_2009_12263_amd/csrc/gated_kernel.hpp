@@ -5,9 +5,9 @@
 //   GATED_DOWN   dY W_out = dh.  With g and u from memory: dg, du and h in 16 bits.
 //   GATED_ROUND  results rounded to 16 bits.
 // What the first two cost beside their products is memory: with g and u kept, UP writes 10 bytes for each value of h and DOWN reads 8 and writes 6, and with one wave
-// per SIMD nothing else runs on a unit meanwhile.  8192 tokens of 1024 x 2560, binary16: UP 128 us (its product alone takes 61, its bytes 44), DOWN 130; without the loads
+// per SIMD nothing else runs on a unit meanwhile.  8192 tokens of 1024 x 2560, binary16, with one code for all activations: UP 128 us (its product alone takes 61, its bytes 44), DOWN 130; without the loads
 // of g and u 89, without the stores of dg and du 109, without the activations 120, with none of them 61.  (Activations of their own code and, for DOWN, two workgroups a
-// unit, see GatedPair: 124 and 120.)  Loads and stores with the streaming policy: 3 % slower; 3 to 10 units ahead in place of 6: within 1 %; workgroups that begin
+// unit, see GatedPair: 126 and 123.)  Loads and stores with the streaming policy: 3 % slower; 3 to 10 units ahead in place of 6: within 1 %; workgroups that begin
 // half a tile apart: none the faster.
 // (FP32 products and passes over them in place of all three, 8192 x 4096 x 10240, forward and backward: 5034 us, 4609 so.)
 #pragma once
