@@ -12,7 +12,7 @@
 // of 2^17 is one of 2^34 of v.  A root that is not zero is held at least as the smallest such number: m / (root + eps) of a v that was rounded
 // to zero would be m / eps.  The step itself uses m and v in FP32, as they are before they are rounded.
 //
-// Measured: 386 M values, bfloat16 with FP32 copies 2076 us (5.2 TB/s), in eight bits 764 to 772 (5.05), 75 M FP32 values 398 (5.3), 193 tensors of 1.6 M values in two launches 18 to 22; the
+// Measured: 386 M values, bfloat16 with FP32 copies 2076 us (5.2 TB/s), in eight bits 764 to 781 (5.0), 75 M FP32 values 398 (5.3), 193 tensors of 1.6 M values in two launches 18 to 22; the
 // norm of 386 M binary16 values 129 (6.0).
 //
 // The operations are written one by one, without fused ones: what eight bits hold changes by 1/16 where a sum falls on the other side of a border.
