@@ -379,7 +379,8 @@ int64_t fg_gated_ffn_workspace(int64_t tokens, int64_t dim, int64_t hidden);
 /*
  * Its gradient, from the GU of the forward call: with dH = dY * W_out, dG = dH * U * act'(G), dU = dH * act(G),
  *   dX = [dG dU] * W_in,   dW_in = [dG dU]^T * X,   dW_out = dY^T * H        (zero without tokens; relu'(0) = 0).
- * dG, dU and H are rounded to the type of X between the products, or kept in two parts, as H is there (binary16: gradients are kept in range by a scaled loss).
+ * dG, dU and H are rounded to the type of X between the products, or kept in two parts, as H is there (binary16: gradients are kept in range by a scaled loss).  An infinity
+ * of X or dY leaves the gradients of weights that it reaches infinite or, of two parts, NaN.
  * dX, dW_in and dW_out are of the type and shape of X, W_in and W_out, each in other memory than the rest (FG_ERR_LAYOUT); each may be NULL: not wanted.
  */
 fg_status fg_gated_ffn_grad(int64_t tokens, int64_t dim, int64_t hidden, const fg_matrix *dY, const fg_matrix *X, const fg_matrix *W_in,

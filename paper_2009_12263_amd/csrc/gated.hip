@@ -111,6 +111,8 @@ __device__ __forceinline__ void store_eight(T *row, int c0, int cols, const floa
             }
     }
 }
+// The sums of values and of what their rounding left.  (Of an infinite weight the first is infinite, and the second, of zeros and of either sign, must not make a NaN of it.)
+__device__ __forceinline__ float both_parts(float sum, float rest) { return __builtin_fabsf(sum) < __builtin_inff() ? sum + rest : sum; }
 // f(row, first column) for pieces of eight columns
 template <class F> __device__ __forceinline__ void each_piece(int64_t rows, int cols, F &&f) {
     const int pieces = (cols + 7) / 8;
@@ -181,7 +183,7 @@ __global__ __launch_bounds__(256) void gated_round(const float *in, int64_t ldi,
         if constexpr (PARTS) {
             load_eight(in + (rows + row) * ldi, c, cols, w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += w[e];
+            for (int e = 0; e < 8; ++e) v[e] = both_parts(v[e], w[e]);
         }
         store_eight<T>(out + row * ldo, c, cols, v, nullptr);
     });
@@ -344,7 +346,11 @@ __global__ __launch_bounds__(few_threads(NB)) void gated_few(const FewArgs a) {
                     if (a.lo) rest[e] = __builtin_fabsf(off) < __builtin_inff() ? (T)off : (T)0.f;
                 }
         } else {
-            if (a.lo) v += total(0, a.lo + r, q);
+            if (a.lo) {
+                const floatx4 rest = total(0, a.lo + r, q);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = both_parts(v[e], rest[e]);
+            }
             T *out = (T *)a.out + (int64_t)r * a.ldo + c;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
